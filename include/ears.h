@@ -421,6 +421,131 @@ int ears_describe_plan(int dtype, int B, int K, int V, char* out, size_t out_byt
 int ears_profile_begin(int max_calls);
 int ears_profile_end(float* kernel_ms, int capacity, int* n_calls);
 
+/*
+ * ---- Operators on rows of logits ----------------------------------------------------------------
+ *
+ * What a program that verifies drafts does with the same rows next to the verification: take the
+ * target's top logits as a teacher for the draft (ears_top_logits), train the draft towards them
+ * (ears_distill_*), score the emitted tokens (ears_token_logprobs*), and train a policy on sampled
+ * tokens (ears_policy_*; with beta > 0 the emitted tokens follow a wider law than P_t, so their
+ * log probability at sampling time enters as `old`).
+ *
+ * Common arguments:
+ *   logits        [B, R, V], entries of a row contiguous; row (b, k) starts at logits + b stride_b +
+ *                 k stride_r (strides in entries, >= 0), so that the first K rows of a target
+ *                 [B, K+1, V], or rows padded to a longer pitch, are used in place.  Any alignment of at
+ *                 least the element size and any V serve; rows that share their alignment with the
+ *                 gradient's rows run at full speed.  Per-row arrays are contiguous, row b R + k.
+ *   temperature   l / temperature enters every softmax; seq_temperature [B] replaces it where not NULL.
+ *   status        optional DEVICE word into which EARS_DEV_INVALID_INPUT is OR-ed when a row could not be
+ *                 used; the caller clears it.
+ *   out_grad      [B, R, V] in the logits' type, with strides of its own; rows must not overlap.  It may be
+ *                 the logits themselves (same pointer, same strides): the gradient then replaces them.
+ *                 Any other overlap with the logits is refused.
+ *   out_saved     optional, 4 floats per row, 16-byte aligned: what the backward call of the same
+ *                 operator needs (`saved`); logits and the other inputs must be unchanged until then.
+ * -inf logits (masked vocabulary) are legal, and so are masks of the type's lowest value.  A row left out
+ * (see each operator) is not read: its outputs are 0 and its gradient row is zeros.  A row that cannot be
+ * used (NaN or +inf logit, no finite logit, index outside [0, V), unusable temperature) gives NaN outputs
+ * and a gradient row of zeros, and sets the status bit.  Other rows are unaffected.
+ * Sums and row scalars are kept in 32 bits and 64 bits; a gradient entry is rounded once, to its type.
+ * The calls use no workspace, allocate nothing and may be recorded into CUDA graphs and run side by side
+ * on any streams.  Results do not depend on anything but the inputs and the launch's CTAs per row.
+ */
+#define EARS_MAX_TOP 128
+#define EARS_MAX_DISTILL_V (1 << 20)
+enum { EARS_DISTILL_FORWARD_KL = 0, EARS_DISTILL_REVERSE_KL = 1, EARS_DISTILL_JSD = 2 };
+
+/*
+ * The k largest logits of every row (1 <= k <= EARS_MAX_TOP) in descending order, equal ones by ascending
+ * index: out_values, out_ids [B R, k]; and out_lse [B R] = ln sum_v exp(l_v / temperature).  Entries of
+ * -inf are never listed: where fewer than k are finite the rest is id -1, value -inf.
+ * accept_len [B], optional: the lengths a verification call reported.  Rows k > accept_len[b], which lie
+ * behind the first rejection (all rows of an invalid sequence, -1), are left out: ids -1, values and lse -inf.
+ * A row that cannot be used has ids -1, values -inf and a NaN lse.
+ */
+int ears_top_logits(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                    float temperature, const float* seq_temperature, const int32_t* accept_len, int k,
+                    float* out_values, int32_t* out_ids, float* out_lse, int32_t* status, void* stream);
+
+/*
+ * Log probability of one token per row, and optionally the row's entropy (nats):
+ *   out_logp = l_x / T - ln sum exp(l / T),   out_entropy = -sum q ln q.
+ * tokens [B R] int32; -1 leaves the row out (out_tokens of a verification call serves as it is).
+ * The backward call adds d_logp[r] (1[v = x] - q_v) / T - d_entropy[r] q_v (ln q_v + H) / T; d_entropy is
+ * optional, and needs `saved` of a call that returned the entropy.  The step call does both at once for
+ * upstream gradients that are known beforehand (d_logp = -weight is the cross entropy).
+ */
+int ears_token_logprobs(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                        float temperature, const float* seq_temperature, const int32_t* tokens,
+                        float* out_logp, float* out_entropy, float* out_saved, int32_t* status, void* stream);
+int ears_token_logprobs_backward(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                                 float temperature, const float* seq_temperature, const int32_t* tokens, const float* saved,
+                                 const float* d_logp, const float* d_entropy, void* out_grad, int64_t grad_stride_b,
+                                 int64_t grad_stride_r, int32_t* status, void* stream);
+int ears_token_logprobs_step(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                             float temperature, const float* seq_temperature, const int32_t* tokens, const float* d_logp,
+                             const float* d_entropy, float* out_logp, float* out_entropy, void* out_grad,
+                             int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream);
+
+/*
+ * Clipped policy loss per token, with rho = exp(logp - old_logp), logp as above:
+ *   loss = -min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A) + kl_coef kl - entropy_coef H,
+ *   kl   = exp(ref_logp - logp) - (ref_logp - logp) - 1     (0 without ref_logp; kl_coef > 0 needs it).
+ * tokens, old_logp, ref_logp, advantage [B R]; token -1 leaves the row out.  out_logp, out_kl and out_entropy
+ * are optional (not differentiated).  Where the clipped branch is taken the ratio's gradient is 0; on a tie
+ * it is the unclipped branch's.  The gradient is that of sum_r w_r loss_r with w = d_loss (backward) or
+ * row_weight (step; NULL: 1).  A row whose loss or gradient is not finite counts as unusable.
+ */
+int ears_policy_loss(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                     float temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
+                     const float* ref_logp, const float* advantage, double clip_low, double clip_high, double kl_coef,
+                     double entropy_coef, float* out_loss, float* out_logp, float* out_kl, float* out_entropy,
+                     float* out_saved, int32_t* status, void* stream);
+int ears_policy_backward(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                         float temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
+                         const float* ref_logp, const float* advantage, double clip_low, double clip_high, double kl_coef,
+                         double entropy_coef, const float* saved, const float* d_loss, void* out_grad,
+                         int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream);
+int ears_policy_step(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                     float temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
+                     const float* ref_logp, const float* advantage, double clip_low, double clip_high, double kl_coef,
+                     double entropy_coef, const float* row_weight, float* out_loss, float* out_logp, float* out_kl,
+                     float* out_entropy, void* out_grad, int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status,
+                     void* stream);
+
+/*
+ * Divergence of a draft row's distribution q (at `temperature`) from a teacher given by its top logits:
+ * values, ids [B R, k] and, optionally, lse [B R] (its log normaliser at the same temperature), as
+ * ears_top_logits writes them.  With lse, p_j = exp(value_j / T - lse) for the listed entries and everything
+ * else is one outcome of mass max(1 - sum p_j, 2^-20) (2^-20: what a 32-bit lse resolves; 0 if the draft has
+ * no mass outside the list either); without it the listed entries are renormalised and the rest has mass 0.
+ *   EARS_DISTILL_FORWARD_KL   sum p ln(p / q)
+ *   EARS_DISTILL_REVERSE_KL   sum q ln(q / p)                     (needs lse: infinite otherwise)
+ *   EARS_DISTILL_JSD          mix sum p ln(p / m) + (1 - mix) sum q ln(q / m), m = mix p + (1 - mix) q, 0 < mix < 1
+ * over the k + 1 outcomes.  An entry is absent when its id is -1 or its value -inf; a row without any is left
+ * out.  A list that names an id twice, an id outside [0, V), or a value of NaN or +inf make the row unusable.
+ * V <= EARS_MAX_DISTILL_V.  The gradient is that of sum_r w_r loss_r with w = d_loss (backward) or row_weight
+ * (step; NULL: 1); rows of weight 0 get zeros.
+ */
+int ears_distill_loss(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                      float temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
+                      const float* lse, int kind, double mix, float* out_loss, float* out_saved, int32_t* status, void* stream);
+int ears_distill_backward(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                          float temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
+                          const float* lse, int kind, double mix, const float* saved, const float* d_loss, void* out_grad,
+                          int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream);
+int ears_distill_step(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                      float temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
+                      const float* lse, int kind, double mix, const float* row_weight, float* out_loss, void* out_grad,
+                      int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream);
+
+/*
+ * CTAs per row of the operators above, for tests and measurements: 1, 2, 4, 8 or 16; 0 = automatic.
+ * Results differ only through floating-point summation order.
+ */
+int ears_set_row_cluster(int cluster);
+
 const char* ears_status_string(int status);
 const char* ears_last_cuda_error(void); /* text of the last failing CUDA call on this thread, or "" */
 int ears_version(void);

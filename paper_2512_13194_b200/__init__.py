@@ -33,3 +33,15 @@ from .binding import (  # noqa: F401
     workspace_bytes,
     workspace_device_status,
 )
+from .rows import (  # noqa: F401,E402
+    PolicyTerms,
+    TopLogits,
+    distill_loss,
+    distill_step,
+    policy_loss,
+    policy_step,
+    set_row_cluster,
+    token_logprobs,
+    token_logprobs_step,
+    top_logits,
+)

@@ -94,6 +94,24 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.ears_profile_begin.restype = c.c_int
     lib.ears_profile_end.argtypes = [c.c_void_p, c.c_int, c.POINTER(c.c_int)]
     lib.ears_profile_end.restype = c.c_int
+    rows = [c.c_int, c.c_void_p, c.c_int, c.c_int, c.c_int, c.c_int64, c.c_int64, c.c_float, c.c_void_p]
+    place, ptrs = [c.c_void_p, c.c_int64, c.c_int64], lambda n: [c.c_void_p] * n
+    policy = ptrs(4) + [c.c_double] * 4
+    distill = [c.c_int] + ptrs(3) + [c.c_int, c.c_double]
+    for name, args in (("ears_top_logits", ptrs(1) + [c.c_int] + ptrs(3)),
+                       ("ears_token_logprobs", ptrs(4)),
+                       ("ears_token_logprobs_backward", ptrs(4) + place),
+                       ("ears_token_logprobs_step", ptrs(5) + place),
+                       ("ears_policy_loss", policy + ptrs(5)),
+                       ("ears_policy_backward", policy + ptrs(2) + place),
+                       ("ears_policy_step", policy + ptrs(5) + place),
+                       ("ears_distill_loss", distill + ptrs(2)),
+                       ("ears_distill_backward", distill + ptrs(2) + place),
+                       ("ears_distill_step", distill + ptrs(2) + place)):
+        getattr(lib, name).argtypes = rows + args + ptrs(2)     # ..., status, stream
+        getattr(lib, name).restype = c.c_int
+    lib.ears_set_row_cluster.argtypes = [c.c_int]
+    lib.ears_set_row_cluster.restype = c.c_int
     lib.ears_status_string.argtypes = [c.c_int]
     lib.ears_status_string.restype = c.c_char_p
     lib.ears_last_cuda_error.argtypes = []

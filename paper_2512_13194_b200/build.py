@@ -5,12 +5,14 @@ import glob
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libears.so")
+UNITS = ("ears_api.cu", "ears_rows_api.cu")      # translation units, compiled side by side
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC"]
 
 
 def _nvcc() -> str:
@@ -21,7 +23,7 @@ def _nvcc() -> str:
 
 
 def sources():
-    return sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "*.cuh"))
+    return sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h"))
                   + [os.path.join(os.path.dirname(HERE), "include", "ears.h")])
 
 
@@ -41,13 +43,15 @@ def build(force: bool = False, verbose: bool = False, trace: bool = False) -> st
     out = TRACE_LIB if trace else LIB
     if not force and os.path.exists(out) and all(os.path.getmtime(s) <= os.path.getmtime(out) for s in sources()):
         return out
-    cmd = [_nvcc()] + NVCC_FLAGS
-    if verbose:
-        cmd += ["-Xptxas", "-v"]
-    if trace:
-        cmd += ["-DEARS_TRACE"]
-    cmd += ["-o", out, os.path.join(CSRC, "ears_api.cu")]
-    subprocess.run(cmd, check=True)
+    flags = NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + (["-DEARS_TRACE"] if trace else [])
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, u[:-3] + ".o") for u in UNITS]
+        jobs = [subprocess.Popen([_nvcc()] + flags + ["-c", "-o", o, os.path.join(CSRC, u)]) for u, o in zip(UNITS, objects)]
+        codes = [j.wait() for j in jobs]
+        for u, code in zip(UNITS, codes):
+            if code:
+                raise subprocess.CalledProcessError(code, f"nvcc -c {u}")
+        subprocess.run([_nvcc()] + NVCC_FLAGS + ["-shared", "-o", out] + objects, check=True)
     return out
 
 

@@ -13,6 +13,7 @@
 #include <utility>
 #include <vector>
 
+#include "ears_host.h"
 #include "ears_common.cuh"
 #include "ears_kernel.cuh"
 #include "ears_resident.cuh"
@@ -976,6 +977,17 @@ int shard_common(int dtype, const void* t, const void* d, const int32_t* x, int 
 }
 
 }  // namespace
+
+int ears::host_cuda_fail(cudaError_t e, const char* what) { return cuda_fail(e, what); }
+
+int ears::host_device_sms(int* sms) {
+    int dev = 0;
+    EARS_CUDA(cudaGetDevice(&dev));
+    DeviceInfo* di = nullptr;
+    const int rc = device_info(dev, &di);
+    if (rc == EARS_OK) *sms = di->sms;
+    return rc;
+}
 
 extern "C" {
 

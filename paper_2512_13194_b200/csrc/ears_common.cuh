@@ -135,7 +135,7 @@ template <class P> __device__ __forceinline__ double seq_beta(const P& p, int b)
 }
 // (kept out of line: the fp64 division would otherwise sit in every role's hot loop, and the
 // streaming kernel is sensitive to the size of those loops)
-__device__ __noinline__ float seq_c_from_array(const float* seq_T, int b) {
+static __device__ __noinline__ float seq_c_from_array(const float* seq_T, int b) {
     return (float)(1.4426950408889634 / (double)__ldg(seq_T + b));
 }
 template <class P> __device__ __forceinline__ float seq_c(const P& p, int b) {

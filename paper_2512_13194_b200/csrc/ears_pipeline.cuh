@@ -29,8 +29,8 @@ __device__ __forceinline__ unsigned long long global_timer_ns() {
 // Without the macro the marks compile to nothing.
 #ifdef EARS_TRACE
 constexpr int kTraceCtas = 96, kTraceEvents = 192;
-__device__ unsigned long long g_trace[kTraceCtas][kTraceEvents][2];
-__device__ int g_trace_n[kTraceCtas];
+static __device__ unsigned long long g_trace[kTraceCtas][kTraceEvents][2];
+static __device__ int g_trace_n[kTraceCtas];
 // called by one thread of the CTA
 __device__ __forceinline__ void trace_mark(int tag, int arg) {
     if (blockIdx.x < kTraceCtas) {

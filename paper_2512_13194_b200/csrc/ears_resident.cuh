@@ -21,6 +21,7 @@
 // No CTA ever waits for work another cluster has yet to start; the only waits are on copies
 // into the CTA's own memory and on the C peers of its own cluster, all bounded in time.
 #pragma once
+#include "ears_cluster.cuh"
 #include "ears_common.cuh"
 #include "ears_math.cuh"
 #include "ears_philox.cuh"
@@ -95,76 +96,12 @@ struct RSmem {
     int abort_flag;
 };
 
-// ---- cluster primitives (sm_90+) ------------------------------------------------
-__device__ __forceinline__ uint32_t cluster_ctarank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t map_to_peer(uint32_t local_smem_addr, uint32_t rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local_smem_addr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void peer_store(uint32_t addr, float4 v) {
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
-                 : "memory");
-}
-__device__ __forceinline__ void peer_store(uint32_t addr, double v) {
-    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory");
-}
-__device__ __forceinline__ void peer_store(uint32_t addr, int v) {
-    asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
-}
-// Arrival on a peer's barrier; what this thread stored before is visible to whoever then
-// observes the phase with cluster-scope acquire.
-__device__ __forceinline__ void peer_arrive(uint32_t bar_addr) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_addr) : "memory");
-}
-// A waiter suspended on a barrier that peers complete by remote arrivals was seen to sleep out
-// its whole time hint, so the hint is kept short here and the wait polls.
-constexpr unsigned kPeerWaitHintNs = 200;
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity), "r"(kPeerWaitHintNs)
-        : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-    unsigned long long t0 = 0;
-    for (uint32_t spin = 0;; ++spin) {
-        if (mbar_try_wait_cluster(bar, parity)) return true;
-        if ((spin & 63u) == 63u) {
-            if (*abort_flag) return false;
-            unsigned long long now = global_timer_ns();
-            if (t0 == 0) t0 = now;
-            else if (now - t0 > kWaitLimitNs) { *abort_flag = 1; return false; }
-        }
-    }
-}
-// All threads of all CTAs of the cluster.  Used at the start (barriers initialised before any
-// peer arrives on them) and at the end (no CTA leaves while a peer may still store into it);
-// every path to it is bounded in time.
-__device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
 // Sub-chunk q of a slice of n valid entries: every thread takes two 16-byte vectors.
 template <typename E, bool ENT>
 __device__ __forceinline__ void stats_sub(const unsigned char* buf, int q, int n, int tid, float c, RowAccT<ENT>& a) {
     constexpr int SUB_VECS = kRSubBytes / 16;
     const int v0 = q * SUB_VECS + tid, v1 = v0 + kRThreads;
     stats_two_vectors<E, ENT>(buf, v0, v1, (q + 1) * SUB_VECS * Vec<E>::N <= n, n, c, a);
-}
-
-__device__ __forceinline__ void peer_store(uint32_t addr, float v) {
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 
 // Warp 0 of every CTA after the exchange: the C x 8 partial results -> the rows' (max, Z) and, ENT, the

@@ -1,0 +1,362 @@
+// C ABI of the operators on rows of logits (see include/ears.h): argument checks, the number of CTAs
+// per row and the kernel launch.  These calls need no workspace: everything a row's CTAs exchange goes
+// through their cluster's shared memory.
+#include "../../include/ears.h"
+
+#include <atomic>
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "ears_host.h"
+#include "ears_distill.cuh"
+#include "ears_rows.cuh"
+#include "ears_token.cuh"
+#include "ears_top.cuh"
+
+namespace {
+
+using namespace ears;
+
+std::atomic<int> g_row_cluster{0};   // ears_set_row_cluster
+
+int esize_of(int dtype) { return dtype == EARS_DTYPE_F32 ? 4 : 2; }
+bool misaligned(const void* p, size_t a) { return ((uintptr_t)p % a) != 0; }
+
+struct RowCall {   // what every entry point is given about its rows
+    int dtype; const void* x; int B, R, V; int64_t sb, sr; float T; const float* seq_T;
+};
+
+int check_rows(const RowCall& c) {
+    if (!c.x) return EARS_ERR_NULL;
+    if (c.dtype != EARS_DTYPE_F32 && c.dtype != EARS_DTYPE_BF16 && c.dtype != EARS_DTYPE_F16) return EARS_ERR_PARAM;
+    if (c.B < 1 || c.R < 1 || c.V < 1 || c.V > (1 << 30)) return EARS_ERR_SHAPE;
+    if ((long long)c.B * c.R > (1ll << 31) / kLMaxCluster - 1) return EARS_ERR_SHAPE;   // CTAs of a launch
+    if (c.sb < 0 || c.sr < 0) return EARS_ERR_SHAPE;
+    const long double span = (long double)(c.B - 1) * c.sb + (long double)(c.R - 1) * c.sr + c.V;
+    if (span * 4 > 4.0e18L) return EARS_ERR_SHAPE;
+    if (!c.seq_T) {
+        if (!(c.T > 0.0f) || !std::isfinite(c.T) || !std::isfinite((float)(kLog2e / (double)c.T))) return EARS_ERR_PARAM;
+    }
+    if (misaligned(c.x, esize_of(c.dtype)) || misaligned(c.seq_T, 4)) return EARS_ERR_ALIGN;
+    return EARS_OK;
+}
+
+// The gradient's rows must not share memory with each other, nor with the logits' unless they are the same
+// rows (a gradient may be written over its logits).
+int check_grad(const RowCall& c, const void* grad, int64_t gsb, int64_t gsr) {
+    if (!grad) return EARS_ERR_NULL;
+    if (misaligned(grad, esize_of(c.dtype))) return EARS_ERR_ALIGN;
+    if (gsb < 0 || gsr < 0) return EARS_ERR_SHAPE;
+    const long double last_b = (long double)(c.B - 1) * gsb, last_r = (long double)(c.R - 1) * gsr;
+    if ((last_b + last_r + c.V) * 4 > 4.0e18L) return EARS_ERR_SHAPE;
+    const bool rows_inside = (c.R == 1 || gsr >= c.V) && (c.B == 1 || gsb >= last_r + c.V);
+    const bool batch_inside = (c.B == 1 || gsb >= c.V) && (c.R == 1 || gsr >= last_b + c.V);
+    if (!rows_inside && !batch_inside) return EARS_ERR_SHAPE;
+    const bool same = grad == c.x && (c.B == 1 || gsb == c.sb) && (c.R == 1 || gsr == c.sr);
+    if (!same) {
+        const size_t es = (size_t)esize_of(c.dtype);
+        const uintptr_t x0 = (uintptr_t)c.x, g0 = (uintptr_t)grad;
+        const uintptr_t x1 = x0 + ((size_t)(c.B - 1) * c.sb + (size_t)(c.R - 1) * c.sr + c.V) * es;
+        const uintptr_t g1 = g0 + ((size_t)(c.B - 1) * gsb + (size_t)(c.R - 1) * gsr + c.V) * es;
+        if (x0 < g1 && g0 < x1) return EARS_ERR_PARAM;
+    }
+    return EARS_OK;
+}
+
+// CTAs per row: enough of them to fill the device when there are few rows, and for calls that read a
+// slice twice so many that the rows in flight stay in L2.
+int choose_cluster(long long rows, size_t row_bytes, bool twice, int sms) {
+    const int forced = g_row_cluster.load(std::memory_order_relaxed);
+    if (forced) return forced;
+    int C = 1;
+    while (C < kLMaxCluster && rows * C < 2ll * sms && row_bytes / (size_t)C > 8192) C *= 2;
+    if (twice)
+        while (C < 8 && (size_t)(4 * sms / C) * row_bytes > (40u << 20)) C *= 2;
+    return C;
+}
+
+int make_span(const RowCall& c, bool twice, RowSpan* out) {
+    int sms = 0;
+    const int rc = host_device_sms(&sms);
+    if (rc) return rc;
+    RowSpan s;
+    s.x = c.x; s.stride_b = c.sb; s.stride_r = c.sr;
+    s.rows = (long long)c.B * c.R;
+    s.R = c.R; s.V = c.V; s.T = c.T; s.seq_T = c.seq_T;
+    s.C = choose_cluster(s.rows, (size_t)c.V * esize_of(c.dtype), twice, sms);
+    const int n = 16 / esize_of(c.dtype);
+    const long long vectors = ((long long)c.V + 2 * n - 2) / n;   // a row that starts anywhere covers at most this many
+    const long long per = (vectors + s.C - 1) / s.C;
+    s.slice = (int)((per + kSliceAlign - 1) / kSliceAlign * kSliceAlign);
+    *out = s;
+    return EARS_OK;
+}
+
+template <typename P>
+int launch_rows(void (*kernel)(P), const P& p, size_t smem, cudaStream_t stream, const char* what) {
+    const RowSpan& r = p.rows;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(r.rows * r.C), 1, 1);
+    cfg.blockDim = dim3(kLThreads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    if (r.C > 1) {
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)r.C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+    }
+    if (r.C > 8) {
+        const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return host_cuda_fail(e, what);
+    }
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();
+        return host_cuda_fail(e, what);
+    }
+    return EARS_OK;
+}
+
+template <typename F>
+int with_type(int dtype, F&& f) {
+    if (dtype == EARS_DTYPE_F32) return f((float*)nullptr);
+    if (dtype == EARS_DTYPE_F16) return f((f16_t*)nullptr);
+    return f((uint16_t*)nullptr);
+}
+
+template <int MODE>
+int launch_token(int dtype, const TokenParams& p, bool ent, void* stream) {
+    return with_type(dtype, [&](auto* e) {
+        typedef std::remove_pointer_t<decltype(e)> E;
+        return launch_rows(ent ? ears_token_kernel<E, true, MODE> : ears_token_kernel<E, false, MODE>, p, 0, (cudaStream_t)stream,
+                           "ears_token_kernel launch");
+    });
+}
+
+template <int MODE>
+int launch_distill(int dtype, const DistillParams& p, void* stream) {
+    const size_t smem = MODE == kBackward ? 0 : (size_t)((p.rows.slice + kLRound - 1) / kLRound) * kLThreads;
+    return with_type(dtype, [&](auto* e) {
+        typedef std::remove_pointer_t<decltype(e)> E;
+        return launch_rows(ears_distill_kernel<E, MODE>, p, smem, (cudaStream_t)stream, "ears_distill_kernel launch");
+    });
+}
+
+int check_words(std::initializer_list<const void*> needed, std::initializer_list<const void*> optional) {
+    for (const void* q : needed)
+        if (!q) return EARS_ERR_NULL;
+    for (auto* list : {&needed, &optional})
+        for (const void* q : *list)
+            if (misaligned(q, 4)) return EARS_ERR_ALIGN;
+    return EARS_OK;
+}
+
+int check_policy(double clip_low, double clip_high, double kl_coef, double entropy_coef, const float* ref) {
+    if (!(clip_low >= 0.0 && clip_low <= 1.0) || !(clip_high >= 0.0) || !std::isfinite(clip_high)) return EARS_ERR_PARAM;
+    if (!(kl_coef >= 0.0) || !std::isfinite(kl_coef) || !std::isfinite(entropy_coef)) return EARS_ERR_PARAM;
+    if (kl_coef > 0.0 && !ref) return EARS_ERR_PARAM;
+    return EARS_OK;
+}
+
+int check_distill(int V, int k, int kind, double mix, const float* lse) {
+    if (k < 1 || k > EARS_MAX_TOP || V > EARS_MAX_DISTILL_V) return EARS_ERR_SHAPE;
+    if (kind != EARS_DISTILL_FORWARD_KL && kind != EARS_DISTILL_REVERSE_KL && kind != EARS_DISTILL_JSD) return EARS_ERR_PARAM;
+    if (kind == EARS_DISTILL_JSD && !(mix > 0.0 && mix < 1.0)) return EARS_ERR_PARAM;
+    if (kind == EARS_DISTILL_REVERSE_KL && !lse) return EARS_ERR_PARAM;   // infinite: the teacher has nothing outside the list
+    return EARS_OK;
+}
+
+static_assert(kMaxTop == EARS_MAX_TOP, "list length");
+
+}  // namespace
+
+#define EARS_TRY(call)         \
+    do {                       \
+        const int rc_ = (call); \
+        if (rc_) return rc_;   \
+    } while (0)
+
+extern "C" {
+
+int ears_set_row_cluster(int cluster) {
+    if (cluster != 0 && cluster != 1 && cluster != 2 && cluster != 4 && cluster != 8 && cluster != 16) return EARS_ERR_PARAM;
+    g_row_cluster.store(cluster, std::memory_order_relaxed);
+    return EARS_OK;
+}
+
+int ears_top_logits(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                    float temperature, const float* seq_temperature, const int32_t* accept_len, int k,
+                    float* out_values, int32_t* out_ids, float* out_lse, int32_t* status, void* stream) {
+    const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
+    EARS_TRY(check_words({out_values, out_ids, out_lse}, {accept_len, status}));
+    EARS_TRY(check_rows(c));
+    if (k < 1 || k > EARS_MAX_TOP) return EARS_ERR_SHAPE;
+    TopParams p{};
+    EARS_TRY(make_span(c, false, &p.rows));
+    p.k = k; p.accept_len = accept_len;
+    p.out_values = out_values; p.out_ids = out_ids; p.out_lse = out_lse; p.status = status;
+    return with_type(dtype, [&](auto* e) {
+        return launch_rows(ears_top_kernel<std::remove_pointer_t<decltype(e)>>, p, 0, (cudaStream_t)stream, "ears_top_kernel launch");
+    });
+}
+
+int ears_token_logprobs(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                        float temperature, const float* seq_temperature, const int32_t* tokens,
+                        float* out_logp, float* out_entropy, float* out_saved, int32_t* status, void* stream) {
+    const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
+    EARS_TRY(check_words({tokens, out_logp}, {out_entropy, status}));
+    EARS_TRY(check_rows(c));
+    if (misaligned(out_saved, 16)) return EARS_ERR_ALIGN;
+    TokenParams p{};
+    EARS_TRY(make_span(c, false, &p.rows));
+    p.tokens = tokens; p.out_logp = out_logp; p.out_entropy = out_entropy; p.stats = (float4*)out_saved; p.status = status;
+    return launch_token<kForward>(dtype, p, out_entropy != nullptr, stream);
+}
+
+int ears_token_logprobs_backward(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                                 float temperature, const float* seq_temperature, const int32_t* tokens, const float* saved,
+                                 const float* d_logp, const float* d_entropy, void* out_grad, int64_t grad_stride_b,
+                                 int64_t grad_stride_r, int32_t* status, void* stream) {
+    const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
+    EARS_TRY(check_words({tokens, saved, d_logp}, {d_entropy, status}));
+    EARS_TRY(check_rows(c));
+    EARS_TRY(check_grad(c, out_grad, grad_stride_b, grad_stride_r));
+    if (misaligned(saved, 16)) return EARS_ERR_ALIGN;
+    TokenParams p{};
+    EARS_TRY(make_span(c, false, &p.rows));
+    p.tokens = tokens; p.stats = (float4*)const_cast<float*>(saved); p.d_logp = d_logp; p.d_entropy = d_entropy; p.status = status;
+    p.grad = out_grad; p.gsb = grad_stride_b; p.gsr = grad_stride_r;
+    return launch_token<kBackward>(dtype, p, d_entropy != nullptr, stream);
+}
+
+int ears_token_logprobs_step(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                             float temperature, const float* seq_temperature, const int32_t* tokens, const float* d_logp,
+                             const float* d_entropy, float* out_logp, float* out_entropy, void* out_grad,
+                             int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream) {
+    const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
+    EARS_TRY(check_words({tokens, d_logp, out_logp}, {d_entropy, out_entropy, status}));
+    EARS_TRY(check_rows(c));
+    EARS_TRY(check_grad(c, out_grad, grad_stride_b, grad_stride_r));
+    TokenParams p{};
+    EARS_TRY(make_span(c, true, &p.rows));
+    p.tokens = tokens; p.d_logp = d_logp; p.d_entropy = d_entropy; p.out_logp = out_logp; p.out_entropy = out_entropy;
+    p.grad = out_grad; p.gsb = grad_stride_b; p.gsr = grad_stride_r; p.status = status;
+    return launch_token<kStep>(dtype, p, d_entropy != nullptr || out_entropy != nullptr, stream);
+}
+
+int ears_policy_loss(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                     float temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
+                     const float* ref_logp, const float* advantage, double clip_low, double clip_high, double kl_coef,
+                     double entropy_coef, float* out_loss, float* out_logp, float* out_kl, float* out_entropy,
+                     float* out_saved, int32_t* status, void* stream) {
+    const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
+    EARS_TRY(check_words({tokens, old_logp, advantage, out_loss}, {ref_logp, out_logp, out_kl, out_entropy, status}));
+    EARS_TRY(check_rows(c));
+    EARS_TRY(check_policy(clip_low, clip_high, kl_coef, entropy_coef, ref_logp));
+    if (misaligned(out_saved, 16)) return EARS_ERR_ALIGN;
+    TokenParams p{};
+    EARS_TRY(make_span(c, false, &p.rows));
+    p.policy = 1;
+    p.tokens = tokens; p.old_logp = old_logp; p.ref_logp = ref_logp; p.advantage = advantage;
+    p.clip_low = clip_low; p.clip_high = clip_high; p.kl_coef = kl_coef; p.entropy_coef = entropy_coef;
+    p.out_loss = out_loss; p.out_logp = out_logp; p.out_kl = out_kl; p.out_entropy = out_entropy;
+    p.stats = (float4*)out_saved; p.status = status;
+    return launch_token<kForward>(dtype, p, entropy_coef != 0.0 || out_entropy != nullptr, stream);
+}
+
+int ears_policy_backward(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                         float temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
+                         const float* ref_logp, const float* advantage, double clip_low, double clip_high, double kl_coef,
+                         double entropy_coef, const float* saved, const float* d_loss, void* out_grad,
+                         int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream) {
+    const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
+    EARS_TRY(check_words({tokens, old_logp, advantage, saved, d_loss}, {ref_logp, status}));
+    EARS_TRY(check_rows(c));
+    EARS_TRY(check_policy(clip_low, clip_high, kl_coef, entropy_coef, ref_logp));
+    EARS_TRY(check_grad(c, out_grad, grad_stride_b, grad_stride_r));
+    if (misaligned(saved, 16)) return EARS_ERR_ALIGN;
+    TokenParams p{};
+    EARS_TRY(make_span(c, false, &p.rows));
+    p.policy = 1;
+    p.tokens = tokens; p.old_logp = old_logp; p.ref_logp = ref_logp; p.advantage = advantage; p.weight = d_loss;
+    p.clip_low = clip_low; p.clip_high = clip_high; p.kl_coef = kl_coef; p.entropy_coef = entropy_coef;
+    p.stats = (float4*)const_cast<float*>(saved); p.status = status;
+    p.grad = out_grad; p.gsb = grad_stride_b; p.gsr = grad_stride_r;
+    return launch_token<kBackward>(dtype, p, entropy_coef != 0.0, stream);
+}
+
+int ears_policy_step(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                     float temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
+                     const float* ref_logp, const float* advantage, double clip_low, double clip_high, double kl_coef,
+                     double entropy_coef, const float* row_weight, float* out_loss, float* out_logp, float* out_kl,
+                     float* out_entropy, void* out_grad, int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status,
+                     void* stream) {
+    const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
+    EARS_TRY(check_words({tokens, old_logp, advantage, out_loss}, {ref_logp, row_weight, out_logp, out_kl, out_entropy, status}));
+    EARS_TRY(check_rows(c));
+    EARS_TRY(check_policy(clip_low, clip_high, kl_coef, entropy_coef, ref_logp));
+    EARS_TRY(check_grad(c, out_grad, grad_stride_b, grad_stride_r));
+    TokenParams p{};
+    EARS_TRY(make_span(c, true, &p.rows));
+    p.policy = 1;
+    p.tokens = tokens; p.old_logp = old_logp; p.ref_logp = ref_logp; p.advantage = advantage; p.weight = row_weight;
+    p.clip_low = clip_low; p.clip_high = clip_high; p.kl_coef = kl_coef; p.entropy_coef = entropy_coef;
+    p.out_loss = out_loss; p.out_logp = out_logp; p.out_kl = out_kl; p.out_entropy = out_entropy; p.status = status;
+    p.grad = out_grad; p.gsb = grad_stride_b; p.gsr = grad_stride_r;
+    return launch_token<kStep>(dtype, p, entropy_coef != 0.0 || out_entropy != nullptr, stream);
+}
+
+int ears_distill_loss(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                      float temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
+                      const float* lse, int kind, double mix, float* out_loss, float* out_saved, int32_t* status, void* stream) {
+    const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
+    EARS_TRY(check_words({values, ids, out_loss}, {lse, status}));
+    EARS_TRY(check_rows(c));
+    EARS_TRY(check_distill(V, k, kind, mix, lse));
+    if (misaligned(out_saved, 16)) return EARS_ERR_ALIGN;
+    DistillParams p{};
+    EARS_TRY(make_span(c, false, &p.rows));
+    p.k = k; p.kind = kind; p.mix = mix; p.values = values; p.ids = ids; p.lse = lse;
+    p.out_loss = out_loss; p.stats = (float4*)out_saved; p.status = status;
+    return launch_distill<kForward>(dtype, p, stream);
+}
+
+int ears_distill_backward(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                          float temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
+                          const float* lse, int kind, double mix, const float* saved, const float* d_loss, void* out_grad,
+                          int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream) {
+    const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
+    EARS_TRY(check_words({values, ids, saved, d_loss}, {lse, status}));
+    EARS_TRY(check_rows(c));
+    EARS_TRY(check_distill(V, k, kind, mix, lse));
+    EARS_TRY(check_grad(c, out_grad, grad_stride_b, grad_stride_r));
+    if (misaligned(saved, 16)) return EARS_ERR_ALIGN;
+    DistillParams p{};
+    EARS_TRY(make_span(c, false, &p.rows));
+    p.k = k; p.kind = kind; p.mix = mix; p.values = values; p.ids = ids; p.lse = lse; p.weight = d_loss;
+    p.stats = (float4*)const_cast<float*>(saved); p.status = status;
+    p.grad = out_grad; p.gsb = grad_stride_b; p.gsr = grad_stride_r;
+    return launch_distill<kBackward>(dtype, p, stream);
+}
+
+int ears_distill_step(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
+                      float temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
+                      const float* lse, int kind, double mix, const float* row_weight, float* out_loss, void* out_grad,
+                      int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream) {
+    const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
+    EARS_TRY(check_words({values, ids, out_loss}, {lse, row_weight, status}));
+    EARS_TRY(check_rows(c));
+    EARS_TRY(check_distill(V, k, kind, mix, lse));
+    EARS_TRY(check_grad(c, out_grad, grad_stride_b, grad_stride_r));
+    DistillParams p{};
+    EARS_TRY(make_span(c, true, &p.rows));
+    p.k = k; p.kind = kind; p.mix = mix; p.values = values; p.ids = ids; p.lse = lse; p.weight = row_weight;
+    p.out_loss = out_loss; p.status = status;
+    p.grad = out_grad; p.gsb = grad_stride_b; p.gsr = grad_stride_r;
+    return launch_distill<kStep>(dtype, p, stream);
+}
+
+}  // extern "C"

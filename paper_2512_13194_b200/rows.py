@@ -1,0 +1,335 @@
+"""Operators on rows of logits beside the verification step (include/ears.h, "Operators on rows of
+logits"): a teacher's top logits, token log probabilities, distillation from top logits and the clipped
+policy loss.  Argument marshalling only; every computation runs in the CUDA library.
+
+Logits are CUDA tensors [B, R, V] or [R, V] (float32, bfloat16, float16); rows are used where they
+lie as long as the entries of a row are contiguous (a slice ``target[:, :K]`` is not copied).  Per-row tensors
+have the logits' shape without V and are converted to contiguous float32 / int32 where they are not.
+``*_loss`` and ``token_logprobs`` can be differentiated by autograd; ``*_step`` return the gradient at once,
+reading the logits from memory a single time, and are what a step recorded into a CUDA graph uses.
+``status``: optional int32 CUDA tensor of one element that gets EARS_DEV_INVALID_INPUT OR-ed in.
+"""
+from __future__ import annotations
+
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import binding
+from .binding import EarsError, _check, _stream_ptr, load_library
+
+MAX_TOP = 128
+DISTILL_KINDS = {"forward_kl": 0, "reverse_kl": 1, "jsd": 2}
+_DTYPES = {torch.float32: binding.EARS_DTYPE_F32, torch.bfloat16: binding.EARS_DTYPE_BF16, torch.float16: binding.EARS_DTYPE_F16}
+
+
+class TopLogits(NamedTuple):
+    values: torch.Tensor                 # [..., k] float32, descending; -inf where absent
+    ids: torch.Tensor                    # [..., k] int32, -1 where absent
+    lse: Optional[torch.Tensor]          # [...] float32 log normaliser at the call's temperature, or None
+
+
+class PolicyTerms(NamedTuple):
+    loss: torch.Tensor
+    logp: torch.Tensor
+    kl: Optional[torch.Tensor]
+    entropy: Optional[torch.Tensor]
+
+
+class _Rows:
+    """The common head of a call: dtype, pointer, sizes, strides, temperature."""
+
+    def __init__(self, logits: torch.Tensor, temperature, seq_temperature, status):
+        if logits.dtype not in _DTYPES:
+            raise TypeError(f"logits must be float32, bfloat16 or float16, got {logits.dtype}")
+        if logits.dim() not in (2, 3):
+            raise ValueError("expected logits [B,R,V] or [R,V]")
+        if not logits.is_cuda:
+            raise ValueError("logits must be a CUDA tensor")
+        if 0 in logits.shape:
+            raise ValueError("logits must not be empty")
+        if logits.shape[-1] > 1 and logits.stride(-1) != 1 or min(logits.stride()) < 0:
+            logits = logits.contiguous()
+        self.logits, self.lead = logits, tuple(logits.shape[:-1])
+        self.device = logits.device
+        if logits.dim() == 3:
+            (self.B, self.R, self.V), (sb, sr, _) = logits.shape, logits.stride()
+        else:
+            (self.R, self.V), (sr, _) = logits.shape, logits.stride()
+            self.B, sb = 1, 0
+        self.T = float(temperature)
+        self.seq_T = self.per(seq_temperature, torch.float32, (self.B,), "seq_temperature")
+        if status is not None and (status.device != self.device or status.dtype != torch.int32 or status.numel() != 1):
+            raise ValueError("status must be an int32 CUDA tensor of one element on the logits' device")
+        self.status = status
+        self.args = (_DTYPES[logits.dtype], logits.data_ptr(), self.B, self.R, self.V, sb, sr, self.T, _ptr(self.seq_T))
+
+    def per(self, t, dtype, shape, name, extra=()):
+        if t is None:
+            return None
+        if t.device != self.device:
+            raise ValueError(f"{name} must live on the logits' device")
+        if tuple(t.shape) != tuple(shape) + tuple(extra):
+            raise ValueError(f"{name} must have shape {list(shape) + list(extra)}, got {list(t.shape)}")
+        if dtype == torch.int32 and (t.dtype.is_floating_point or t.dtype == torch.bool):
+            raise TypeError(f"{name} must hold integers")
+        return t.detach().to(dtype).contiguous()
+
+    def row(self, t, name, dtype=torch.float32):
+        return self.per(t, dtype, self.lead, name)
+
+    def out(self, extra=(), dtype=torch.float32):
+        return torch.empty(self.lead + tuple(extra), dtype=dtype, device=self.device)
+
+    def grad(self, out_grad):
+        if out_grad is None:
+            out_grad = torch.empty(self.logits.shape, dtype=self.logits.dtype, device=self.device)
+        elif out_grad.shape != self.logits.shape or out_grad.dtype != self.logits.dtype or out_grad.device != self.device:
+            raise ValueError("out_grad must have the logits' shape, type and device")
+        elif out_grad.shape[-1] > 1 and out_grad.stride(-1) != 1:
+            raise ValueError("the entries of out_grad's rows must be contiguous")
+        st = out_grad.stride()
+        return out_grad, (out_grad.data_ptr(), st[0] if len(st) == 3 else 0, st[-2])
+
+    def call(self, fn, *tail, stream=None):
+        """fn(*head, *tail, status, stream) with the logits' device current."""
+        if torch.cuda.current_device() == self.device.index:
+            _check(fn(*self.args, *tail, _ptr(self.status), _stream_ptr(stream)))
+        else:
+            with torch.cuda.device(self.device):
+                _check(fn(*self.args, *tail, _ptr(self.status), _stream_ptr(stream)))
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _refuse_capture():
+    # a backward pass recorded into a CUDA graph meets the gradient accumulators of whatever eager graph
+    # of the same leaves is alive; the step calls need no autograd graph
+    if torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("autograd through this operator cannot be recorded into a CUDA graph; record the *_step call")
+
+
+def _wants_grad(logits) -> bool:
+    return logits.requires_grad and torch.is_grad_enabled()
+
+
+# ---- top logits ------------------------------------------------------------------------------
+
+def top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0, *, accept_len: Optional[torch.Tensor] = None,
+               seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None) -> TopLogits:
+    """The k largest logits of every row (1 <= k <= 128), equal values by ascending index, and the row's log
+    normaliser at ``temperature`` (ears_top_logits).  Entries of -inf are not listed (id -1, value -inf).
+    ``accept_len`` [B] int32, as a verification call returns it: rows behind a sequence's first rejection
+    are left out."""
+    rows = _Rows(logits, temperature, seq_temperature, status)
+    acc = rows.per(accept_len, torch.int32, (rows.B,), "accept_len")
+    k = int(k)
+    if not 1 <= k <= MAX_TOP:
+        raise ValueError(f"k must lie in 1..{MAX_TOP}")
+    values, ids, lse = rows.out((k,)), rows.out((k,), torch.int32), rows.out()
+    rows.call(load_library().ears_top_logits, _ptr(acc), k, values.data_ptr(), ids.data_ptr(), lse.data_ptr(), stream=stream)
+    return TopLogits(values, ids, lse)
+
+
+# ---- token log probabilities --------------------------------------------------------------------
+
+def _token_forward(rows, tokens, entropy, saved, stream):
+    logp, H = rows.out(), rows.out() if entropy else None
+    rows.call(load_library().ears_token_logprobs, tokens.data_ptr(), logp.data_ptr(), _ptr(H), _ptr(saved), stream=stream)
+    return logp, H
+
+
+class _TokenLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, tokens, temperature, seq_temperature, entropy, status, stream):
+        _refuse_capture()
+        rows = _Rows(logits.detach(), temperature, seq_temperature, status)
+        saved = rows.out((4,))
+        ctx.rows, ctx.tokens, ctx.saved = rows, rows.row(tokens, "tokens", torch.int32), saved
+        ctx.save_for_backward(logits)          # notices a change of the logits before the backward pass
+        logp, H = _token_forward(rows, ctx.tokens, entropy, saved, stream)
+        ctx.with_entropy = entropy
+        return (logp, H) if entropy else logp
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_logp, d_entropy=None):
+        _refuse_capture()
+        ctx.saved_tensors
+        rows = ctx.rows
+        g, place = rows.grad(None)
+        dl = rows.row(d_logp, "d_logp")
+        dh = rows.row(d_entropy, "d_entropy")
+        rows.call(load_library().ears_token_logprobs_backward, ctx.tokens.data_ptr(), ctx.saved.data_ptr(), dl.data_ptr(),
+                  _ptr(dh), *place)
+        return (g,) + (None,) * 6
+
+
+def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, temperature: float = 1.0, *, entropy: bool = False,
+                   seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+    """Log probability of ``tokens`` (one per row, int; -1 leaves the row out: 0) at ``temperature``; with
+    ``entropy=True`` the pair (logp, entropy in nats).  Differentiable (ears_token_logprobs, _backward)."""
+    if _wants_grad(logits):
+        return _TokenLogprobs.apply(logits, tokens, temperature, seq_temperature, bool(entropy), status, stream)
+    rows = _Rows(logits, temperature, seq_temperature, status)
+    logp, H = _token_forward(rows, rows.row(tokens, "tokens", torch.int32), entropy, None, stream)
+    return (logp, H) if entropy else logp
+
+
+def token_logprobs_step(logits: torch.Tensor, tokens: torch.Tensor, d_logp: torch.Tensor, d_entropy: Optional[torch.Tensor] = None,
+                        temperature: float = 1.0, *, out_grad: Optional[torch.Tensor] = None,
+                        seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+    """(logp, entropy or None, gradient) for upstream gradients known beforehand (ears_token_logprobs_step):
+    ``d_logp`` and, optionally, ``d_entropy`` per row.  ``out_grad=logits`` writes the gradient over them."""
+    rows = _Rows(logits.detach(), temperature, seq_temperature, status)
+    tok, dl, dh = rows.row(tokens, "tokens", torch.int32), rows.row(d_logp, "d_logp"), rows.row(d_entropy, "d_entropy")
+    logp, H = rows.out(), rows.out() if dh is not None else None
+    g, place = rows.grad(out_grad)
+    rows.call(load_library().ears_token_logprobs_step, tok.data_ptr(), dl.data_ptr(), _ptr(dh), logp.data_ptr(), _ptr(H),
+              *place, stream=stream)
+    return logp, H, g
+
+
+# ---- clipped policy loss ---------------------------------------------------------------------------
+
+def _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, clip_low, clip_high, kl_coef, entropy_coef):
+    held = (rows.row(tokens, "tokens", torch.int32), rows.row(old_logp, "old_logp"), rows.row(ref_logp, "ref_logp"),
+            rows.row(advantage, "advantage"))
+    return held, tuple(_ptr(t) for t in held) + (float(clip_low), float(clip_high), float(kl_coef), float(entropy_coef))
+
+
+def _policy_outputs(rows, ref, entropy):
+    return PolicyTerms(rows.out(), rows.out(), rows.out() if ref is not None else None, rows.out() if entropy else None)
+
+
+class _PolicyLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, tokens, old_logp, advantage, ref_logp, temperature, coefs, seq_temperature, entropy, status, stream):
+        _refuse_capture()
+        rows = _Rows(logits.detach(), temperature, seq_temperature, status)
+        ctx.held, ctx.args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, *coefs)
+        ctx.rows, ctx.saved = rows, rows.out((4,))
+        ctx.save_for_backward(logits)
+        t = _policy_outputs(rows, ref_logp, entropy)
+        rows.call(load_library().ears_policy_loss, *ctx.args, *(_ptr(o) for o in t), ctx.saved.data_ptr(), stream=stream)
+        ctx.mark_non_differentiable(*(o for o in t[1:] if o is not None))
+        return tuple(t)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_loss, *_):
+        _refuse_capture()
+        ctx.saved_tensors
+        rows = ctx.rows
+        g, place = rows.grad(None)
+        dl = rows.row(d_loss, "d_loss")
+        rows.call(load_library().ears_policy_backward, *ctx.args, ctx.saved.data_ptr(), dl.data_ptr(), *place)
+        return (g,) + (None,) * 10
+
+
+def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tensor, advantage: torch.Tensor,
+                temperature: float = 1.0, *, ref_logp: Optional[torch.Tensor] = None, clip_low: float = 0.2,
+                clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0, entropy: bool = False,
+                seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None) -> PolicyTerms:
+    """Clipped policy loss per row with a KL term and an entropy bonus (ears_policy_loss), differentiable in the
+    logits through ``loss``; the other terms (kl with ``ref_logp``, entropy when its coefficient is not 0 or
+    ``entropy=True``) come without gradients.  Token -1 leaves a row out."""
+    with_entropy = bool(entropy) or entropy_coef != 0.0
+    coefs = (clip_low, clip_high, kl_coef, entropy_coef)
+    if _wants_grad(logits):
+        return PolicyTerms(*_PolicyLoss.apply(logits, tokens, old_logp, advantage, ref_logp, temperature, coefs, seq_temperature,
+                                              with_entropy, status, stream))
+    rows = _Rows(logits, temperature, seq_temperature, status)
+    held, args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, *coefs)
+    t = _policy_outputs(rows, ref_logp, with_entropy)
+    rows.call(load_library().ears_policy_loss, *args, *(_ptr(o) for o in t), None, stream=stream)
+    return t
+
+
+def policy_step(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tensor, advantage: torch.Tensor,
+                temperature: float = 1.0, *, ref_logp: Optional[torch.Tensor] = None, clip_low: float = 0.2,
+                clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0, entropy: bool = False,
+                row_weight: Optional[torch.Tensor] = None, out_grad: Optional[torch.Tensor] = None,
+                seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+    """(PolicyTerms, gradient of sum row_weight * loss) in one call (ears_policy_step)."""
+    rows = _Rows(logits.detach(), temperature, seq_temperature, status)
+    held, args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, clip_low, clip_high, kl_coef, entropy_coef)
+    w = rows.row(row_weight, "row_weight")
+    t = _policy_outputs(rows, ref_logp, bool(entropy) or entropy_coef != 0.0)
+    g, place = rows.grad(out_grad)
+    rows.call(load_library().ears_policy_step, *args, _ptr(w), *(_ptr(o) for o in t), *place, stream=stream)
+    return t, g
+
+
+# ---- distillation from top logits ----------------------------------------------------------------------
+
+def _distill_inputs(rows, teacher, kind, mix):
+    if kind not in DISTILL_KINDS:
+        raise ValueError(f"kind must be one of {sorted(DISTILL_KINDS)}")
+    values, ids, lse = teacher
+    k = int(ids.shape[-1]) if ids.dim() else 0
+    if not 1 <= k <= MAX_TOP:
+        raise ValueError(f"the teacher's lists must have 1..{MAX_TOP} entries")
+    held = (rows.per(values, torch.float32, rows.lead, "teacher values", (k,)),
+            rows.per(ids, torch.int32, rows.lead, "teacher ids", (k,)), rows.row(lse, "teacher lse"))
+    return held, (k,) + tuple(_ptr(t) for t in held) + (DISTILL_KINDS[kind], float(mix))
+
+
+class _DistillLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, teacher, temperature, kind, mix, seq_temperature, status, stream):
+        _refuse_capture()
+        rows = _Rows(logits.detach(), temperature, seq_temperature, status)
+        ctx.held, ctx.args = _distill_inputs(rows, teacher, kind, mix)
+        ctx.rows, ctx.saved = rows, rows.out((4,))
+        ctx.save_for_backward(logits)
+        loss = rows.out()
+        rows.call(load_library().ears_distill_loss, *ctx.args, loss.data_ptr(), ctx.saved.data_ptr(), stream=stream)
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_loss):
+        _refuse_capture()
+        ctx.saved_tensors
+        rows = ctx.rows
+        g, place = rows.grad(None)
+        dl = rows.row(d_loss, "d_loss")
+        rows.call(load_library().ears_distill_backward, *ctx.args, ctx.saved.data_ptr(), dl.data_ptr(), *place)
+        return (g,) + (None,) * 7
+
+
+def distill_loss(logits: torch.Tensor, teacher: TopLogits, temperature: float = 1.0, *, kind: str = "forward_kl",
+                 mix: float = 0.5, seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                 stream=None) -> torch.Tensor:
+    """Divergence of the draft rows from a teacher's top logits, per row (ears_distill_loss), differentiable in
+    the draft's logits.  ``teacher``: what ``top_logits`` returned for the matching rows at the same temperature;
+    with ``lse=None`` its entries are renormalised, else the rest of the vocabulary is one more outcome.
+    kind: "forward_kl", "reverse_kl" (needs lse) or "jsd" with weight ``mix``.  Rows without entries are left out."""
+    if _wants_grad(logits):
+        return _DistillLoss.apply(logits, teacher, temperature, kind, mix, seq_temperature, status, stream)
+    rows = _Rows(logits, temperature, seq_temperature, status)
+    held, args = _distill_inputs(rows, teacher, kind, mix)
+    loss = rows.out()
+    rows.call(load_library().ears_distill_loss, *args, loss.data_ptr(), None, stream=stream)
+    return loss
+
+
+def distill_step(logits: torch.Tensor, teacher: TopLogits, temperature: float = 1.0, *, kind: str = "forward_kl",
+                 mix: float = 0.5, row_weight: Optional[torch.Tensor] = None, out_grad: Optional[torch.Tensor] = None,
+                 seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+    """(loss per row, gradient of sum row_weight * loss) in one call (ears_distill_step)."""
+    rows = _Rows(logits.detach(), temperature, seq_temperature, status)
+    held, args = _distill_inputs(rows, teacher, kind, mix)
+    w = rows.row(row_weight, "row_weight")
+    loss = rows.out()
+    g, place = rows.grad(out_grad)
+    rows.call(load_library().ears_distill_step, *args, _ptr(w), loss.data_ptr(), *place, stream=stream)
+    return loss, g
+
+
+def set_row_cluster(cluster: int = 0) -> None:
+    """CTAs per row of these operators (1, 2, 4, 8, 16; 0 = automatic), for tests and measurements."""
+    _check(load_library().ears_set_row_cluster(int(cluster)))

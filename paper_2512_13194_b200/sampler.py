@@ -14,7 +14,7 @@ from typing import Optional
 
 import torch
 
-from . import binding
+from . import binding, rows
 
 
 @dataclass
@@ -23,6 +23,8 @@ class StepResult:
     tokens: torch.Tensor          # [B,K+1] int32: accepted prefix, then the resampled or bonus token, then -1
     offset: int                   # the random stream's offset this step used
     entropy: Optional[torch.Tensor] = None   # [B,K] float64 H(P_t) per position, when asked for
+    logprobs: Optional[torch.Tensor] = None  # [B,K+1] float32 ln P_t of the emitted tokens (0 behind the last), when asked for
+    teacher: Optional[rows.TopLogits] = None # top logits of the target rows 0..K-1 up to the first rejection, when asked for
 
     def emitted(self):
         """Per sequence the tokens this step adds to its text (accepted drafts + the final token)."""
@@ -40,15 +42,20 @@ class EarsSampler:
     (H(P_t) / ln V, Sec. 5 item 1).  seed: the random stream of this sampler; the offset starts at
     ``first_offset`` and goes up by one per step, so that a run can be replayed from (seed, offset).
     b_first: global index of this rank's first sequence when a batch is sharded across GPUs.
+    report_logprobs: every step also scores the tokens it emits under the target rows (the log probability a
+    later policy loss needs as ``old_logp``).  teacher_k: every step also keeps the ``teacher_k`` largest logits of
+    the target rows that a draft row stands beside, positions behind the first rejection left out: the
+    ``teacher`` of ``distill_step`` on the step's draft logits.
     """
 
     def __init__(self, temperature=1.0, beta=0.1, *, seed: int = 0, first_offset: int = 0,
                  uncertainty: str = "maxprob", stop_at_first_reject: bool = False, b_first: int = 0,
-                 report_entropy: bool = False):
+                 report_entropy: bool = False, report_logprobs: bool = False, teacher_k: int = 0):
         self.temperature, self.beta = temperature, beta
         self.seed, self.offset = int(seed), int(first_offset)
         self.uncertainty, self.stop_at_first_reject = uncertainty, bool(stop_at_first_reject)
         self.b_first, self.report_entropy = int(b_first), bool(report_entropy)
+        self.report_logprobs, self.teacher_k = bool(report_logprobs), int(teacher_k)
         self.steps = 0
         self.accepted = 0          # draft tokens accepted so far (read from the outputs on request only)
         self._pending = []         # accept_len tensors not yet folded into `accepted`
@@ -72,6 +79,11 @@ class EarsSampler:
                              stop_at_first_reject=self.stop_at_first_reject, uncertainty=self.uncertainty,
                              entropy=self.report_entropy)
         res = StepResult(out[0], out[1], self.offset, out[2]["entropy"] if self.report_entropy else None)
+        if self.report_logprobs:
+            res.logprobs = rows.token_logprobs(target_logits.detach(), res.tokens, T, seq_temperature=seq_T, stream=stream)
+        if self.teacher_k:
+            res.teacher = rows.top_logits(target_logits[:, :-1], self.teacher_k, T, accept_len=res.accept_len,
+                                          seq_temperature=seq_T, stream=stream)
         self.offset += 1
         self.steps += 1
         self._pending.append(res.accept_len)
