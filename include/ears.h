@@ -436,7 +436,8 @@ int ears_profile_end(float* kernel_ms, int capacity, int* n_calls);
  *                 [B, K+1, V], or rows padded to a longer pitch, are used in place.  Any alignment of at
  *                 least the element size and any V serve; rows that share their alignment with the
  *                 gradient's rows run at full speed.  Per-row arrays are contiguous, row b R + k.
- *   temperature   l / temperature enters every softmax; seq_temperature [B] replaces it where not NULL.
+ *   temperature   l / temperature enters every softmax; seq_temperature [B] replaces it where not NULL.  It is
+ *                 taken in 64 bits: rounding it to 32 would move logits of 20 by 1e-6.
  *   status        optional DEVICE word into which EARS_DEV_INVALID_INPUT is OR-ed when a row could not be
  *                 used; the caller clears it.
  *   out_grad      [B, R, V] in the logits' type, with strides of its own; rows must not overlap.  It may be
@@ -465,7 +466,7 @@ enum { EARS_DISTILL_FORWARD_KL = 0, EARS_DISTILL_REVERSE_KL = 1, EARS_DISTILL_JS
  * A row that cannot be used has ids -1, values -inf and a NaN lse.
  */
 int ears_top_logits(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                    float temperature, const float* seq_temperature, const int32_t* accept_len, int k,
+                    double temperature, const float* seq_temperature, const int32_t* accept_len, int k,
                     float* out_values, int32_t* out_ids, float* out_lse, int32_t* status, void* stream);
 
 /*
@@ -477,14 +478,14 @@ int ears_top_logits(int dtype, const void* logits, int B, int R, int V, int64_t 
  * upstream gradients that are known beforehand (d_logp = -weight is the cross entropy).
  */
 int ears_token_logprobs(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                        float temperature, const float* seq_temperature, const int32_t* tokens,
+                        double temperature, const float* seq_temperature, const int32_t* tokens,
                         float* out_logp, float* out_entropy, float* out_saved, int32_t* status, void* stream);
 int ears_token_logprobs_backward(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                                 float temperature, const float* seq_temperature, const int32_t* tokens, const float* saved,
+                                 double temperature, const float* seq_temperature, const int32_t* tokens, const float* saved,
                                  const float* d_logp, const float* d_entropy, void* out_grad, int64_t grad_stride_b,
                                  int64_t grad_stride_r, int32_t* status, void* stream);
 int ears_token_logprobs_step(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                             float temperature, const float* seq_temperature, const int32_t* tokens, const float* d_logp,
+                             double temperature, const float* seq_temperature, const int32_t* tokens, const float* d_logp,
                              const float* d_entropy, float* out_logp, float* out_entropy, void* out_grad,
                              int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream);
 
@@ -498,17 +499,17 @@ int ears_token_logprobs_step(int dtype, const void* logits, int B, int R, int V,
  * row_weight (step; NULL: 1).  A row whose loss or gradient is not finite counts as unusable.
  */
 int ears_policy_loss(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                     float temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
+                     double temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
                      const float* ref_logp, const float* advantage, double clip_low, double clip_high, double kl_coef,
                      double entropy_coef, float* out_loss, float* out_logp, float* out_kl, float* out_entropy,
                      float* out_saved, int32_t* status, void* stream);
 int ears_policy_backward(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                         float temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
+                         double temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
                          const float* ref_logp, const float* advantage, double clip_low, double clip_high, double kl_coef,
                          double entropy_coef, const float* saved, const float* d_loss, void* out_grad,
                          int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream);
 int ears_policy_step(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                     float temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
+                     double temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
                      const float* ref_logp, const float* advantage, double clip_low, double clip_high, double kl_coef,
                      double entropy_coef, const float* row_weight, float* out_loss, float* out_logp, float* out_kl,
                      float* out_entropy, void* out_grad, int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status,
@@ -529,14 +530,14 @@ int ears_policy_step(int dtype, const void* logits, int B, int R, int V, int64_t
  * (step; NULL: 1); rows of weight 0 get zeros.
  */
 int ears_distill_loss(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                      float temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
+                      double temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
                       const float* lse, int kind, double mix, float* out_loss, float* out_saved, int32_t* status, void* stream);
 int ears_distill_backward(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                          float temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
+                          double temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
                           const float* lse, int kind, double mix, const float* saved, const float* d_loss, void* out_grad,
                           int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream);
 int ears_distill_step(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                      float temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
+                      double temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
                       const float* lse, int kind, double mix, const float* row_weight, float* out_loss, void* out_grad,
                       int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream);
 

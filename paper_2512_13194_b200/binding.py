@@ -94,7 +94,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.ears_profile_begin.restype = c.c_int
     lib.ears_profile_end.argtypes = [c.c_void_p, c.c_int, c.POINTER(c.c_int)]
     lib.ears_profile_end.restype = c.c_int
-    rows = [c.c_int, c.c_void_p, c.c_int, c.c_int, c.c_int, c.c_int64, c.c_int64, c.c_float, c.c_void_p]
+    rows = [c.c_int, c.c_void_p, c.c_int, c.c_int, c.c_int, c.c_int64, c.c_int64, c.c_double, c.c_void_p]
     place, ptrs = [c.c_void_p, c.c_int64, c.c_int64], lambda n: [c.c_void_p] * n
     policy = ptrs(4) + [c.c_double] * 4
     distill = [c.c_int] + ptrs(3) + [c.c_int, c.c_double]

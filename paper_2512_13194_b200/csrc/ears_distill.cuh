@@ -65,10 +65,10 @@ __device__ __forceinline__ double warp_max(double v) {
 }
 
 template <int MODE>
-__device__ void distill_scalars(const DistillParams& p, DistillSmem& sm, long long row, int rank, float T, bool ok, Part tail) {
+__device__ void distill_scalars(const DistillParams& p, DistillSmem& sm, long long row, int rank, double T, bool ok, Part tail) {
     constexpr int PER = kMaxTop / 32;
     const int lane = threadIdx.x & 31;
-    const double invT = 1.0 / (double)T;
+    const double invT = 1.0 / T;
     bool on[PER];
     double lp[PER], lq[PER], pr[PER], qr[PER];
     double xm = -INFINITY, tm = -INFINITY;

@@ -32,7 +32,7 @@ struct RowSpan {           // rows r = b R + k of [B, R, V] with strides in entr
     long long stride_b, stride_r;
     long long rows;
     int R, V;
-    float T;
+    double T;
     const float* seq_T;    // [B] temperature per sequence, or NULL
     int C;                 // CTAs per row
     int slice;             // vectors per CTA (a multiple of kSliceAlign)
@@ -342,15 +342,15 @@ __device__ __forceinline__ bool in_slice(const Slice<E>& s, int col) {
 }
 
 // ---- what every kernel does first ---------------------------------------------------------------
-struct RowSetup { long long row; int rank; float T, c; bool T_ok; };
+struct RowSetup { long long row; int rank; double T; float c; bool T_ok; };
 
 __device__ __forceinline__ RowSetup row_setup(const RowSpan& p) {
     RowSetup r;
     r.row = blockIdx.x / (unsigned)p.C;
     r.rank = (int)(blockIdx.x % (unsigned)p.C);
-    r.T = p.seq_T ? __ldg(p.seq_T + r.row / p.R) : p.T;
-    r.c = (float)(kLog2e / (double)r.T);
-    r.T_ok = r.T > 0.f && r.T < INFINITY && r.c < INFINITY;
+    r.T = p.seq_T ? (double)__ldg(p.seq_T + r.row / p.R) : p.T;
+    r.c = (float)(kLog2e / r.T);
+    r.T_ok = r.T > 0.0 && r.T < (double)INFINITY && r.c < INFINITY;
     if (p.C > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     return r;
 }

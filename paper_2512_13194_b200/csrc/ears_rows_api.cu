@@ -24,7 +24,7 @@ int esize_of(int dtype) { return dtype == EARS_DTYPE_F32 ? 4 : 2; }
 bool misaligned(const void* p, size_t a) { return ((uintptr_t)p % a) != 0; }
 
 struct RowCall {   // what every entry point is given about its rows
-    int dtype; const void* x; int B, R, V; int64_t sb, sr; float T; const float* seq_T;
+    int dtype; const void* x; int B, R, V; int64_t sb, sr; double T; const float* seq_T;
 };
 
 int check_rows(const RowCall& c) {
@@ -36,7 +36,7 @@ int check_rows(const RowCall& c) {
     const long double span = (long double)(c.B - 1) * c.sb + (long double)(c.R - 1) * c.sr + c.V;
     if (span * 4 > 4.0e18L) return EARS_ERR_SHAPE;
     if (!c.seq_T) {
-        if (!(c.T > 0.0f) || !std::isfinite(c.T) || !std::isfinite((float)(kLog2e / (double)c.T))) return EARS_ERR_PARAM;
+        if (!(c.T > 0.0) || !std::isfinite(c.T) || !std::isfinite((float)(kLog2e / c.T))) return EARS_ERR_PARAM;
     }
     if (misaligned(c.x, esize_of(c.dtype)) || misaligned(c.seq_T, 4)) return EARS_ERR_ALIGN;
     return EARS_OK;
@@ -188,7 +188,7 @@ int ears_set_row_cluster(int cluster) {
 }
 
 int ears_top_logits(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                    float temperature, const float* seq_temperature, const int32_t* accept_len, int k,
+                    double temperature, const float* seq_temperature, const int32_t* accept_len, int k,
                     float* out_values, int32_t* out_ids, float* out_lse, int32_t* status, void* stream) {
     const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
     EARS_TRY(check_words({out_values, out_ids, out_lse}, {accept_len, status}));
@@ -204,7 +204,7 @@ int ears_top_logits(int dtype, const void* logits, int B, int R, int V, int64_t 
 }
 
 int ears_token_logprobs(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                        float temperature, const float* seq_temperature, const int32_t* tokens,
+                        double temperature, const float* seq_temperature, const int32_t* tokens,
                         float* out_logp, float* out_entropy, float* out_saved, int32_t* status, void* stream) {
     const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
     EARS_TRY(check_words({tokens, out_logp}, {out_entropy, status}));
@@ -217,7 +217,7 @@ int ears_token_logprobs(int dtype, const void* logits, int B, int R, int V, int6
 }
 
 int ears_token_logprobs_backward(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                                 float temperature, const float* seq_temperature, const int32_t* tokens, const float* saved,
+                                 double temperature, const float* seq_temperature, const int32_t* tokens, const float* saved,
                                  const float* d_logp, const float* d_entropy, void* out_grad, int64_t grad_stride_b,
                                  int64_t grad_stride_r, int32_t* status, void* stream) {
     const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
@@ -233,7 +233,7 @@ int ears_token_logprobs_backward(int dtype, const void* logits, int B, int R, in
 }
 
 int ears_token_logprobs_step(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                             float temperature, const float* seq_temperature, const int32_t* tokens, const float* d_logp,
+                             double temperature, const float* seq_temperature, const int32_t* tokens, const float* d_logp,
                              const float* d_entropy, float* out_logp, float* out_entropy, void* out_grad,
                              int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream) {
     const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
@@ -248,7 +248,7 @@ int ears_token_logprobs_step(int dtype, const void* logits, int B, int R, int V,
 }
 
 int ears_policy_loss(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                     float temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
+                     double temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
                      const float* ref_logp, const float* advantage, double clip_low, double clip_high, double kl_coef,
                      double entropy_coef, float* out_loss, float* out_logp, float* out_kl, float* out_entropy,
                      float* out_saved, int32_t* status, void* stream) {
@@ -268,7 +268,7 @@ int ears_policy_loss(int dtype, const void* logits, int B, int R, int V, int64_t
 }
 
 int ears_policy_backward(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                         float temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
+                         double temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
                          const float* ref_logp, const float* advantage, double clip_low, double clip_high, double kl_coef,
                          double entropy_coef, const float* saved, const float* d_loss, void* out_grad,
                          int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream) {
@@ -289,7 +289,7 @@ int ears_policy_backward(int dtype, const void* logits, int B, int R, int V, int
 }
 
 int ears_policy_step(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                     float temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
+                     double temperature, const float* seq_temperature, const int32_t* tokens, const float* old_logp,
                      const float* ref_logp, const float* advantage, double clip_low, double clip_high, double kl_coef,
                      double entropy_coef, const float* row_weight, float* out_loss, float* out_logp, float* out_kl,
                      float* out_entropy, void* out_grad, int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status,
@@ -310,7 +310,7 @@ int ears_policy_step(int dtype, const void* logits, int B, int R, int V, int64_t
 }
 
 int ears_distill_loss(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                      float temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
+                      double temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
                       const float* lse, int kind, double mix, float* out_loss, float* out_saved, int32_t* status, void* stream) {
     const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
     EARS_TRY(check_words({values, ids, out_loss}, {lse, status}));
@@ -325,7 +325,7 @@ int ears_distill_loss(int dtype, const void* logits, int B, int R, int V, int64_
 }
 
 int ears_distill_backward(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                          float temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
+                          double temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
                           const float* lse, int kind, double mix, const float* saved, const float* d_loss, void* out_grad,
                           int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream) {
     const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};
@@ -343,7 +343,7 @@ int ears_distill_backward(int dtype, const void* logits, int B, int R, int V, in
 }
 
 int ears_distill_step(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
-                      float temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
+                      double temperature, const float* seq_temperature, int k, const float* values, const int32_t* ids,
                       const float* lse, int kind, double mix, const float* row_weight, float* out_loss, void* out_grad,
                       int64_t grad_stride_b, int64_t grad_stride_r, int32_t* status, void* stream) {
     const RowCall c{dtype, logits, B, R, V, stride_b, stride_r, temperature, seq_temperature};

@@ -49,9 +49,9 @@ struct TokenParams {
 struct TokenScalars { float A, Bt, entry; int zero; };
 
 template <bool ENT, int MODE>
-__device__ __forceinline__ TokenScalars token_scalars(const TokenParams& p, long long row, int rank, float T, bool T_ok, float lt, Part st) {
+__device__ __forceinline__ TokenScalars token_scalars(const TokenParams& p, long long row, int rank, double T, bool T_ok, float lt, Part st) {
     const bool ok = T_ok && rowstat_ok(st.m, st.s) && (!ENT || st.w == st.w);
-    const double Z = st.s, lnZ = log(Z), invT = 1.0 / (double)T;
+    const double Z = st.s, lnZ = log(Z), invT = 1.0 / T;
     double logp = ((double)lt - (double)st.m) * invT - lnZ;
     double H = ENT ? lnZ - kLn2 * (double)st.w / Z : 0.0;
     double loss = 0.0, kl = 0.0, g = 0.0, h = 0.0;

@@ -50,7 +50,7 @@ def test_rows_are_checked_by_every_entry_point(name):
     assert call(rows(B=2**20, R=2**10)) == -2                    # more CTAs than a launch can hold
     assert call(rows(sb=-1)) == -2 and call(rows(sr=-8)) == -2
     assert call(rows(sb=2**62)) == -2
-    for T in (0.0, -1.0, float("nan"), float("inf"), 1e-45):
+    for T in (0.0, -1.0, float("nan"), float("inf"), 1e-39):
         assert call(rows(T=T)) == -3
     assert call(rows(x=P + 2)) == -4 and call(rows(dtype=1, x=P + 1)) == -4
     assert call(rows(seq=P + 2)) == -4
