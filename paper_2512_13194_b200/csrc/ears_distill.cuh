@@ -15,6 +15,7 @@
 // 1e-4 and less, of which the difference would keep no digits): the sweep skips the listed entries.  One
 // byte of shared memory per thread and round says which of its eight vectors hold any.
 #pragma once
+#include "ears_ring.cuh"
 #include "ears_rows.cuh"
 #include "ears_token.cuh"   // LossMode
 
@@ -39,20 +40,22 @@ struct DistillParams {
     int32_t* status;
 };
 
+constexpr int kListSlots = 256;
+
 struct DistillSmem {
     float4 xs[kLMaxCluster * kLWarps];
+    alignas(16) int col[kMaxTop];   // listed ids, -1: absent
     int vec[kMaxTop];            // vector that holds the listed entry, -1: absent
-    int col[kMaxTop];
     float x[kMaxTop];            // draft logit of the listed entry
     float t[kMaxTop];            // teacher logit
     float entry[kMaxTop];        // gradient of the listed entry
+    int head[kListSlots];        // first of the listed entries whose vector falls into the slot, -1: none
+    int next[kMaxTop];
     float factor;
     int zero;
     int seen;                    // bit 0: an entry is present, bit 1: something is wrong
 };
 
-// Warp 0 of every CTA: loss, the factor of the entries outside the list, the listed entries' gradients.
-// Lane i has the entries i, i + 32, ..; sums over lanes in one fixed order, identical in every CTA.
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
@@ -64,112 +67,133 @@ __device__ __forceinline__ double warp_max(double v) {
     return v;
 }
 
-template <int MODE>
-__device__ void distill_scalars(const DistillParams& p, DistillSmem& sm, long long row, int rank, double T, bool ok, Part tail) {
-    constexpr int PER = kMaxTop / 32;
+// One warp of every CTA works out the row's scalars in 64 bits: lane i has the entries i, i + 32, .., sums over
+// lanes in one fixed order, identical in every CTA.  The teacher's part first: it needs nothing of the draft.
+constexpr int kTopPer = kMaxTop / 32;
+struct TeacherPart { double lp[kTopPer], pr[kTopPer], ps, L; };
+
+__device__ __forceinline__ bool listed(const DistillParams& p, const DistillSmem& sm, int i) {
+    const int j = (threadIdx.x & 31) + 32 * i;
+    return j < p.k && sm.col[j] >= 0;
+}
+
+__device__ __forceinline__ TeacherPart teacher_part(const DistillParams& p, const DistillSmem& sm, long long row, double invT) {
     const int lane = threadIdx.x & 31;
-    const double invT = 1.0 / T;
-    bool on[PER];
-    double lp[PER], lq[PER], pr[PER], qr[PER];
-    double xm = -INFINITY, tm = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int j = lane + 32 * i;
-        on[i] = j < p.k && sm.vec[j] >= 0;
-        lq[i] = on[i] ? (double)sm.x[j] : -INFINITY;
-        lp[i] = on[i] ? (double)sm.t[j] : -INFINITY;
-        xm = fmax(xm, lq[i]);
-        tm = fmax(tm, lp[i]);
-    }
-    const bool has_tail = tail.m > -INFINITY;
-    const double M = fmax(warp_max(xm), (double)tail.m);
-    tm = warp_max(tm);
-    // draft: Z relative to M
-    double zs = 0.0, ps = 0.0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        lq[i] = (lq[i] - M) * invT;
-        qr[i] = on[i] ? exp(lq[i]) : 0.0;
-        zs += qr[i];
-    }
-    const double zt = has_tail ? exp(((double)tail.m - M) * invT) * (double)tail.s : 0.0;
-    const double Z = warp_sum(zs) + zt, lnZ = log(Z);
-    const double rho = zt / Z;
-    const double ln_rho = has_tail ? ((double)tail.m - M) * invT + log((double)tail.s) - lnZ : -INFINITY;
-    // teacher
-    double L;
+    TeacherPart t;
     if (p.lse) {
-        L = (double)__ldg(p.lse + row);
+        t.L = (double)__ldg(p.lse + row);
     } else {
-        double ts = 0.0;
+        double tm = -INFINITY, ts = 0.0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) ts += on[i] ? exp((lp[i] - tm) * invT) : 0.0;
-        L = tm * invT + log(warp_sum(ts));
+        for (int i = 0; i < kTopPer; ++i)
+            if (listed(p, sm, i)) tm = fmax(tm, (double)sm.t[lane + 32 * i]);
+        tm = warp_max(tm);
+#pragma unroll
+        for (int i = 0; i < kTopPer; ++i)
+            if (listed(p, sm, i)) ts += exp(((double)sm.t[lane + 32 * i] - tm) * invT);
+        t.L = tm * invT + log(warp_sum(ts));
     }
+    t.ps = 0.0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
+    for (int i = 0; i < kTopPer; ++i) {
+        t.lp[i] = t.pr[i] = 0.0;
+        if (listed(p, sm, i)) {
+            t.lp[i] = (double)sm.t[lane + 32 * i] * invT - t.L;
+            t.pr[i] = exp(t.lp[i]);
+            t.ps += t.pr[i];
+        }
+    }
+    t.ps = warp_sum(t.ps);
+    return t;
+}
+
+template <int MODE>
+__device__ __forceinline__ void distill_scalars(const DistillParams& p, DistillSmem& sm, long long row, int rank, double invT, bool ok,
+                                                const TeacherPart& te, float weight, Part tail) {
+    const int lane = threadIdx.x & 31;
+    double lq[kTopPer], qr[kTopPer], gs[kTopPer];
+    double xm = (double)tail.m;
+#pragma unroll
+    for (int i = 0; i < kTopPer; ++i)
+        if (listed(p, sm, i)) xm = fmax(xm, (double)sm.x[lane + 32 * i]);
+    const bool has_tail = tail.m > -INFINITY;
+    const double M = warp_max(xm);
+    // draft: Z relative to M
+    double zs = 0.0;
+#pragma unroll
+    for (int i = 0; i < kTopPer; ++i) {
+        lq[i] = qr[i] = gs[i] = 0.0;
+        if (listed(p, sm, i)) {
+            lq[i] = ((double)sm.x[lane + 32 * i] - M) * invT;
+            qr[i] = exp(lq[i]);
+            zs += qr[i];
+        }
+    }
+    const double tt = has_tail ? ((double)tail.m - M) * invT : 0.0;
+    const double zt = has_tail ? exp(tt) * (double)tail.s : 0.0;
+    const double Z = warp_sum(zs) + zt, lnZ = log(Z), invZ = 1.0 / Z;
+    const double rho = zt * invZ;
+    const double ln_rho = has_tail ? tt + log((double)tail.s) - lnZ : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kTopPer; ++i) {
         lq[i] -= lnZ;
-        qr[i] /= Z;
-        lp[i] = lp[i] * invT - L;
-        pr[i] = on[i] ? exp(lp[i]) : 0.0;
-        ps += pr[i];
+        qr[i] *= invZ;
     }
-    ps = warp_sum(ps);
     double rt = 0.0;
     if (p.lse) {
-        rt = 1.0 - ps;
+        rt = 1.0 - te.ps;
         if (rt < kTailFloor) rt = rho > 0.0 ? kTailFloor : 0.0;
     }
     const double ln_rt = log(rt);
-    // loss; q (g - cbar) of every outcome
+    // loss; q (g - cbar) of every outcome.  Entries that are not listed have p = q = 0 and stay out of every sum.
     const double a = p.mix;
-    double part = 0.0, loss, gt, gs[PER];
+    double part = 0.0, loss, gt;
     if (p.kind == kForwardKl) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            part += pr[i] > 0.0 ? pr[i] * (lp[i] - lq[i]) : 0.0;
-            gs[i] = qr[i] * (ps + rt) - pr[i];
+        for (int i = 0; i < kTopPer; ++i) {
+            part += te.pr[i] > 0.0 ? te.pr[i] * (te.lp[i] - lq[i]) : 0.0;
+            gs[i] = qr[i] * (te.ps + rt) - te.pr[i];
         }
         loss = warp_sum(part) + (rt > 0.0 ? rt * (ln_rt - ln_rho) : 0.0);
-        gt = rho * (ps + rt) - rt;
+        gt = rho * (te.ps + rt) - rt;
     } else if (p.kind == kReverseKl) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            gs[i] = qr[i] > 0.0 ? lq[i] - lp[i] : 0.0;
+        for (int i = 0; i < kTopPer; ++i) {
+            gs[i] = qr[i] > 0.0 ? lq[i] - te.lp[i] : 0.0;
             part += qr[i] * gs[i];
         }
         gt = rho > 0.0 ? ln_rho - ln_rt : 0.0;
         loss = warp_sum(part) + rho * gt;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) gs[i] = qr[i] * (gs[i] - loss);
+        for (int i = 0; i < kTopPer; ++i) gs[i] = qr[i] * (gs[i] - loss);
         gt = rho * (gt - loss);
     } else {
         double cq = 0.0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const double lm = log(a * pr[i] + (1.0 - a) * qr[i]);
-            gs[i] = qr[i] > 0.0 ? lq[i] - lm : 0.0;
-            part += pr[i] > 0.0 ? pr[i] * (lp[i] - lm) : 0.0;
-            cq += qr[i] * gs[i];
+        for (int i = 0; i < kTopPer; ++i) {
+            if (listed(p, sm, i)) {
+                const double lm = log(a * te.pr[i] + (1.0 - a) * qr[i]);
+                gs[i] = qr[i] > 0.0 ? lq[i] - lm : 0.0;
+                part += te.pr[i] > 0.0 ? te.pr[i] * (te.lp[i] - lm) : 0.0;
+                cq += qr[i] * gs[i];
+            }
         }
         const double lmt = log(a * rt + (1.0 - a) * rho);
         const double kt = rho > 0.0 ? ln_rho - lmt : 0.0;
         cq = (1.0 - a) * (warp_sum(cq) + rho * kt);
         loss = a * (warp_sum(part) + (rt > 0.0 ? rt * (ln_rt - lmt) : 0.0)) + cq;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) gs[i] = qr[i] * ((1.0 - a) * gs[i] - cq);
+        for (int i = 0; i < kTopPer; ++i) gs[i] = qr[i] * ((1.0 - a) * gs[i] - cq);
         gt = rho * ((1.0 - a) * kt - cq);
     }
-    ok = ok && M > -INFINITY && M < INFINITY && isfinite(L) && loss == loss;
+    ok = ok && M > -INFINITY && M < INFINITY && isfinite(te.L) && loss == loss;
     if (MODE != kForward) {
-        const double w = (p.weight ? (double)__ldg(p.weight + row) : 1.0) * invT;
+        const double w = (double)weight * invT;
         bool finite = true;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int j = lane + 32 * i;
-            const float e = (float)(w * gs[i]);
-            if (on[i]) {
-                sm.entry[j] = e;
+        for (int i = 0; i < kTopPer; ++i) {
+            if (listed(p, sm, i)) {
+                sm.entry[lane + 32 * i] = (float)(w * gs[i]);
                 finite = finite && isfinite(gs[i]);
             }
         }
@@ -190,31 +214,26 @@ __device__ void distill_scalars(const DistillParams& p, DistillSmem& sm, long lo
     }
 }
 
-template <typename E, int MODE>
-__global__ void __launch_bounds__(kLThreads) ears_distill_kernel(const DistillParams p) {
+// The row's list, by all threads of the CTA (THREADS >= kMaxTop of them, in whole warps): into sm, with a flag for
+// every vector among [base, base + count) that holds a listed entry -- byte (i / (PER kLThreads)) kLThreads + i % kLThreads,
+// bit i / kLThreads % PER, for vector base + i: what the thread that folds the vector looks at.  -> sm.seen.
+template <typename E, int PER, int THREADS>
+__device__ __forceinline__ int distill_list(const DistillParams& p, DistillSmem& sm, uint32_t* flags, long long row_index, const E* row,
+                                            int lead, int base, int count) {
     constexpr int N = Words<E>::N;
-    extern __shared__ __align__(16) unsigned char smem_raw[];
-    __shared__ DistillSmem sm;
-    uint32_t* flags = reinterpret_cast<uint32_t*>(smem_raw);   // byte (round * kLThreads + thread): bit j = vector j of the round
     const int tid = threadIdx.x, k = p.k;
-    const RowSetup r = row_setup(p.rows);
-    const E* row = row_ptr<E>(p.rows, r.row);
-    const Slice<E> s = make_slice<E>(row, p.rows.V, p.rows.slice, r.rank);
-    E* grad = MODE == kForward ? nullptr : grad_ptr<E>(p.grad, p.rows, p.gsb, p.gsr, r.row) - s.lead;
-    // the list
     int id = -1;
     float tv = -INFINITY;
     if (tid < k) {
-        id = __ldg(p.ids + r.row * k + tid);
-        tv = __ldg(p.values + r.row * k + tid);
+        id = __ldg(p.ids + row_index * k + tid);
+        tv = __ldg(p.values + row_index * k + tid);
     }
     bool wrong = id < -1 || id >= p.rows.V || (id >= 0 && !(tv < INFINITY));   // NaN and +inf
     const bool present = !wrong && id >= 0 && tv > -INFINITY;
     if (tid == 0) sm.seen = 0;
-    if (MODE != kBackward) {
-        const int rounds = (s.n + kLRound - 1) / kLRound;
-        for (int i = tid; i < rounds * (kLThreads / 4); i += kLThreads) flags[i] = 0;
-    }
+    const int words = (count + PER * kLThreads - 1) / (PER * kLThreads) * (kLThreads / 4);
+    for (int i = tid; i < words; i += THREADS) flags[i] = 0;
+    if (tid < kListSlots) sm.head[tid] = -1;
     if (tid < kMaxTop) {
         float x = -INFINITY;
         if (present) {
@@ -222,32 +241,69 @@ __global__ void __launch_bounds__(kLThreads) ears_distill_kernel(const DistillPa
             Words<E>::unpack(make_uint4(raw_bits(row + id), 0, 0, 0), xx);
             x = xx[0];
         }
-        sm.vec[tid] = present ? (s.lead + id) / N : -1;
+        sm.vec[tid] = present ? (lead + id) / N : -1;
         sm.col[tid] = present ? id : -1;
         sm.x[tid] = x;
         sm.t[tid] = tv;
     }
     __syncthreads();
-    if (tid < k && present) {
-        for (int j = 0; j < tid; ++j) wrong = wrong || sm.col[j] == id;   // an id listed twice
-        const int i = sm.vec[tid] - s.v0;
-        if (MODE != kBackward && i >= 0 && i < s.n) {
-            const int byte = (i / kLRound) * kLThreads + i % kLThreads, bit = (i / kLThreads) % kLUnroll;
-            atomicOr(&flags[byte >> 2], 1u << ((byte & 3) * 8 + bit));
-        }
-    }
     if (tid < kMaxTop) {
+        if (present) {
+            // an id listed twice
+            const int4* c4 = reinterpret_cast<const int4*>(sm.col);
+            int same = 0;
+#pragma unroll 4
+            for (int j = 0; j < (k + 3) / 4; ++j) {
+                const int4 c = c4[j];
+                same += (c.x == id) + (c.y == id) + (c.z == id) + (c.w == id);
+            }
+            wrong = same > 1;
+            sm.next[tid] = atomicExch(&sm.head[sm.vec[tid] % kListSlots], tid);
+            const int i = sm.vec[tid] - base;
+            if (i >= 0 && i < count) {
+                const int byte = (i / (PER * kLThreads)) * kLThreads + i % kLThreads, bit = (i / kLThreads) % PER;
+                atomicOr(&flags[byte >> 2], 1u << ((byte & 3) * 8 + bit));
+            }
+        }
         const unsigned any = __ballot_sync(0xffffffffu, present), bad = __ballot_sync(0xffffffffu, wrong);
         if ((tid & 31) == 0 && (any | bad)) atomicOr(&sm.seen, (any ? 1 : 0) | (bad ? 2 : 0));
     }
     __syncthreads();
-    if (sm.seen != 1) {   // nothing listed, or a list that cannot be used: the same in every CTA of the cluster
-        const bool bad = (sm.seen & 2) != 0;
-        if (tid == 0 && r.rank == 0) {
-            if (MODE != kBackward) p.out_loss[r.row] = bad ? __int_as_float(0x7fc00000) : 0.f;
-            if (MODE == kForward && p.stats) p.stats[r.row] = make_float4(0.f, __int_as_float(0x7fc00000), 0.f, 0.f);
-            if (bad && p.status) atomicOr(p.status, kDevInvalidInput);
-        }
+    return sm.seen;
+}
+
+// Vector v with the entries that are listed taken out: the entries of its slot, a few at most.
+template <typename E>
+__device__ __forceinline__ void mask_listed(const DistillSmem& sm, int lead, int v, uint4& w) {
+    for (int q = sm.head[v % kListSlots]; q >= 0; q = sm.next[q])
+        if (sm.vec[q] == v) put_entry(w, (lead + sm.col[q]) % Words<E>::N, minus_inf_bits<E>(), E{});
+}
+
+// Nothing listed, or a list that cannot be used.
+template <int MODE>
+__device__ __forceinline__ void distill_unused(const DistillParams& p, long long row, bool bad) {
+    if (MODE != kBackward) p.out_loss[row] = bad ? __int_as_float(0x7fc00000) : 0.f;
+    if (MODE == kForward && p.stats) p.stats[row] = make_float4(0.f, __int_as_float(0x7fc00000), 0.f, 0.f);
+    if (bad && p.status) atomicOr(p.status, kDevInvalidInput);
+}
+
+// The tail's statistics are usable, or there is no tail (no entry outside the list is finite).
+__device__ __forceinline__ bool tail_empty(Part st) { return st.m == -INFINITY && st.s == 0.f; }
+
+// Forward and backward calls: one sweep, straight from memory.
+template <typename E, int MODE>
+__global__ void __launch_bounds__(kLThreads) ears_distill_kernel(const DistillParams p) {
+    extern __shared__ __align__(16) unsigned char smem_raw[];
+    __shared__ DistillSmem sm;
+    uint32_t* flags = reinterpret_cast<uint32_t*>(smem_raw);
+    const int tid = threadIdx.x, k = p.k;
+    const RowSetup r = row_setup(p.rows);
+    const E* row = row_ptr<E>(p.rows, r);
+    const Slice<E> s = make_slice<E>(row, p.rows.V, p.rows.slice, r.rank);
+    E* grad = MODE == kForward ? nullptr : grad_ptr<E>(p.grad, p.gsb, p.gsr, r) - s.lead;
+    const int seen = distill_list<E, kLUnroll, kLThreads>(p, sm, flags, r.row, row, s.lead, s.v0, MODE == kBackward ? 0 : s.n);
+    if (seen != 1) {   // the same in every CTA of the cluster
+        if (tid == 0 && r.rank == 0) distill_unused<MODE>(p, r.row, (seen & 2) != 0);
         if (MODE != kForward) dense_pass<E, false>(s, grad, true, 0.f, 0.f, 0.f, 0.f);
         return;
     }
@@ -263,36 +319,116 @@ __global__ void __launch_bounds__(kLThreads) ears_distill_kernel(const DistillPa
     } else {
         Stat<false> a;
         stat_open(a);
+        const uint64_t pol = l2_policy_evict_first();
         const unsigned char* flag_bytes = reinterpret_cast<const unsigned char*>(flags);
         for (int i0 = tid, round = 0; i0 < s.n; i0 += kLRound, ++round) {
             uint4 w[kLUnroll];
-            load_round(s, i0, w);
+            load_round(s, i0, w, pol);
             const unsigned f = flag_bytes[round * kLThreads + tid];
             if (f) {
 #pragma unroll
-                for (int j = 0; j < kLUnroll; ++j) {
-                    if (f >> j & 1u) {
-                        const int v = s.v0 + i0 + j * kLThreads;
-                        for (int q = 0; q < k; ++q)
-                            if (sm.vec[q] == v) put_entry(w[j], (s.lead + sm.col[q]) % N, minus_inf_bits<E>(), E{});
-                    }
-                }
+                for (int j = 0; j < kLUnroll; ++j)
+                    if (f >> j & 1u) mask_listed<E>(sm, s.lead, s.v0 + i0 + j * kLThreads, w[j]);
             }
             stat_fold<E, kLUnroll, false>(w, r.c, a);
         }
         st = exchange_parts<false>(a, sm.xs, p.rows.C, r.rank, r.c);
     }
-    // no entry outside the list is finite: the tail is empty
-    const bool empty = st.m == -INFINITY && st.s == 0.f;
-    const bool ok = r.T_ok && (empty || rowstat_ok(st.m, st.s));
-    if (tid < 32) distill_scalars<MODE>(p, sm, r.row, r.rank, r.T, ok, st);
+    const bool empty = tail_empty(st);
+    if (tid < 32) {
+        const double invT = 1.0 / r.T;
+        const float weight = MODE != kForward && p.weight ? __ldg(p.weight + r.row) : 1.f;
+        distill_scalars<MODE>(p, sm, r.row, r.rank, invT, r.T_ok && (empty || rowstat_ok(st.m, st.s)),
+                              teacher_part(p, sm, r.row, invT), weight, st);
+    }
     if (MODE == kForward) return;
     __syncthreads();
     const bool zero = sm.zero != 0;
     dense_pass<E, false>(s, grad, zero, empty ? 0.f : st.m, r.c, sm.factor, 0.f);
     if (zero) return;
     __syncthreads();   // the dense values of the listed entries have been written
-    if (tid < k && present && in_slice(s, id)) store_entry(grad + s.lead + id, sm.entry[tid]);
+    if (tid < k && sm.col[tid] >= 0 && in_slice(s, sm.col[tid])) store_entry(grad + s.lead + sm.col[tid], sm.entry[tid]);
+}
+
+// Loss and gradient in one call: the slice through the ring of ears_ring.cuh, with one more warp for the
+// scalars, which has the teacher's part done while the others sweep.
+constexpr int kDistillThreads = kRingThreads + 32;
+
+template <typename E>
+__global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(const DistillParams p, int stages) {
+    extern __shared__ __align__(128) unsigned char ring_buf[];
+    __shared__ DistillSmem sm;
+    __shared__ RingBars bars;
+    uint32_t* flags = reinterpret_cast<uint32_t*>(ring_buf + (size_t)stages * kRingChunk);
+    const int tid = threadIdx.x, k = p.k, C = p.rows.C;
+    const RowSetup r = row_setup(p.rows);
+    const E* row = row_ptr<E>(p.rows, r);
+    const Slice<E> s = make_slice<E>(row, p.rows.V, p.rows.slice, r.rank);
+    E* grad = grad_ptr<E>(p.grad, p.gsb, p.gsr, r) - s.lead;
+    const Ring<E> ring = make_ring(s, ring_buf, &bars, stages);
+    const uint64_t keep = l2_policy_evict_last(), drop = l2_policy_evict_first();
+    int issued = 0;
+    if (tid >= kRingConsumers && tid < kRingThreads) {
+        // loads begin as soon as the list is known not to be empty
+        bool any = false;
+        for (int j = tid - kRingConsumers; j < k; j += 32)
+            any = any || (__ldg(p.ids + r.row * k + j) >= 0 && __ldg(p.values + r.row * k + j) > -INFINITY);
+        if (__any_sync(0xffffffffu, any) && tid == kRingConsumers) {
+            ring_init(&bars, stages);
+            issued = ring_load(ring, 0, ring.H, keep, drop);
+        }
+    }
+    const int seen = distill_list<E, kRingPer, kDistillThreads>(p, sm, flags, r.row, row, s.lead, ring.v0, ring.vecs);
+    if (seen != 1) {   // the same in every CTA of the cluster
+        if (tid == 0 && r.rank == 0) distill_unused<kStep>(p, r.row, (seen & 2) != 0);
+        if (tid < kLThreads) dense_pass<E, false>(s, grad, true, 0.f, 0.f, 0.f, 0.f);
+        if (tid == kRingConsumers) ring_drain(ring, issued);
+        return;
+    }
+    if (tid >= kRingThreads) {   // scalars
+        const double invT = 1.0 / r.T;
+        const float weight = p.weight ? __ldg(p.weight + r.row) : 1.f;
+        const TeacherPart te = teacher_part(p, sm, r.row, invT);
+        exchange_join(C);
+        const Part st = merge_parts<false>(sm.xs, C * kRingWarps, r.c);
+        distill_scalars<kStep>(p, sm, r.row, r.rank, invT, r.T_ok && (tail_empty(st) || rowstat_ok(st.m, st.s)), te, weight, st);
+        __syncwarp();
+        asm volatile("bar.arrive 1, %0;" ::"n"(kRingConsumers + 32) : "memory");
+        return;
+    }
+    if (tid >= kRingConsumers) {
+        ring_loader_warp(ring, issued, C, keep, drop);
+        return;
+    }
+    Stat<false> a;
+    stat_open(a);
+    const unsigned char* flag_bytes = reinterpret_cast<const unsigned char*>(flags) + tid;
+    const bool swept = ring_stats(ring, [&](uint4 (&w)[kRingPer], int chunk) {
+        const unsigned f = flag_bytes[chunk * kLThreads];
+        if (f) {
+#pragma unroll
+            for (int j = 0; j < kRingPer; ++j)
+                if (f >> j & 1u) mask_listed<E>(sm, s.lead, ring.v0 + chunk * kRingVecs + tid + j * kRingConsumers, w[j]);
+        }
+        stat_fold<E, kRingPer, false>(w, r.c, a);
+    });
+    if (!swept) {
+        a.s[0] = pack2(__int_as_float(0x7fc00000), 0.f);   // the row counts as unusable in every CTA
+        if (p.status) atomicOr(p.status, kDevTimeout);
+    }
+    const int v = edge_vector(ring, s);
+    if (v >= 0) {
+        uint4 w[1] = {load_partial(s.base, v, s.lead, s.end)};
+        mask_listed<E>(sm, s.lead, v, w[0]);
+        stat_fold<E, 1, false>(w, r.c, a);
+    }
+    const Part st = exchange_parts<false, kRingWarps>(a, sm.xs, C, r.rank, r.c);
+    asm volatile("bar.sync 1, %0;" ::"n"(kRingConsumers + 32) : "memory");   // the scalars
+    const bool zero = sm.zero != 0;
+    ring_gradient<E, false>(ring, s, grad, zero, tail_empty(st) ? 0.f : st.m, r.c, sm.factor, 0.f, drop, p.status);
+    if (zero) return;
+    asm volatile("bar.sync 2, %0;" ::"n"(kRingConsumers) : "memory");   // the dense values of the listed entries have been written
+    if (tid < k && sm.col[tid] >= 0 && in_slice(s, sm.col[tid])) store_entry(grad + s.lead + sm.col[tid], sm.entry[tid]);
 }
 
 }  // namespace ears

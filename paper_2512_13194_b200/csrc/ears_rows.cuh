@@ -70,6 +70,16 @@ __device__ __forceinline__ uint4 ld_row16(const void* p) {
                  : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p) : "memory");
     return r;
 }
+__device__ __forceinline__ uint4 ld_row16_hint(const void* p, uint64_t pol) {
+    uint4 r;
+    asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+                 : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p), "l"(pol) : "memory");
+    return r;
+}
+__device__ __forceinline__ void st_row16_hint(void* p, uint4 r, uint64_t pol) {
+    asm volatile("st.global.L1::no_allocate.L2::cache_hint.v4.u32 [%0], {%1, %2, %3, %4}, %5;"
+                 :: "l"(p), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w), "l"(pol) : "memory");
+}
 __device__ __forceinline__ uint32_t raw_bits(const float* p) { return __float_as_uint(*p); }
 __device__ __forceinline__ uint32_t raw_bits(const uint16_t* p) { return *p; }
 __device__ __forceinline__ uint32_t raw_bits(const f16_t* p) { return p->bits; }
@@ -102,11 +112,11 @@ __device__ __noinline__ uint4 load_partial(const E* base, int v, int lead, int e
 
 // The vectors of one round of one thread: slice-local indices i0 + j kLThreads.
 template <typename E>
-__device__ __forceinline__ void load_round(const Slice<E>& s, int i0, uint4 (&w)[kLUnroll]) {
+__device__ __forceinline__ void load_round(const Slice<E>& s, int i0, uint4 (&w)[kLUnroll], uint64_t pol) {
     const uint4* p = reinterpret_cast<const uint4*>(s.base) + s.v0;
     if (i0 + (kLUnroll - 1) * kLThreads < s.n && s.whole(s.v0 + i0) && s.whole(s.v0 + i0 + (kLUnroll - 1) * kLThreads)) {
 #pragma unroll
-        for (int j = 0; j < kLUnroll; ++j) w[j] = ld_row16(p + i0 + j * kLThreads);
+        for (int j = 0; j < kLUnroll; ++j) w[j] = ld_row16_hint(p + i0 + j * kLThreads, pol);
     } else {
 #pragma unroll
         for (int j = 0; j < kLUnroll; ++j) {
@@ -196,27 +206,11 @@ __device__ __forceinline__ void cluster_wait_peers() {
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Every warp's part goes to every CTA of the cluster through distributed shared memory; after one
-// barrier every warp merges the same C x 8 parts in the same order, so all CTAs hold identical bits.
+// One warp: the n parts that the exchange left in xs -> the row's; the same in every warp and CTA.
 template <bool ENT>
-__device__ __forceinline__ Part exchange_parts(const Stat<ENT>& a, float4* xs /* [kLMaxCluster * kLWarps] */, int C, int rank, float c) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float s0, s1, w0 = 0.f, w1 = 0.f;
-    unpack2(add2(a.s[0], a.s[1]), s0, s1);
-    if (ENT) unpack2(add2(a.w[0], a.w[ENT ? 1 : 0]), w0, w1);
-    Part p = merge_lanes(Part{a.m, s0 + s1, w0 + w1}, c, ENT);
-    const float4 v = make_float4(p.m, p.s, p.w, 0.f);
-    if (C == 1) {
-        if (lane == 0) xs[warp] = v;
-        __syncthreads();
-    } else {
-        cluster_wait_peers();
-        if (lane < C) peer_store(map_to_peer(smem_u32(xs + rank * kLWarps + warp), (uint32_t)lane), v);
-        __syncwarp();
-        cluster_sync_all();
-    }
+__device__ __forceinline__ Part merge_parts(const float4* xs, int n, float c) {
+    const int lane = threadIdx.x & 31;
     Part q{-INFINITY, 0.f, 0.f};
-    const int n = C * kLWarps;
     if (n <= 32) {
         if (lane < n) q = Part{xs[lane].x, xs[lane].y, xs[lane].z};
     } else {
@@ -230,6 +224,39 @@ __device__ __forceinline__ Part exchange_parts(const Stat<ENT>& a, float4* xs /*
         }
     }
     return merge_lanes(q, c, ENT);
+}
+
+// Every warp's part goes to every CTA of the cluster through distributed shared memory; after one
+// barrier every warp merges the same C x WARPS parts in the same order, so all CTAs hold identical bits.
+template <bool ENT, int WARPS = kLWarps>
+__device__ __forceinline__ Part exchange_parts(const Stat<ENT>& a, float4* xs /* [kLMaxCluster * WARPS] */, int C, int rank, float c) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float s0, s1, w0 = 0.f, w1 = 0.f;
+    unpack2(add2(a.s[0], a.s[1]), s0, s1);
+    if (ENT) unpack2(add2(a.w[0], a.w[ENT ? 1 : 0]), w0, w1);
+    Part p = merge_lanes(Part{a.m, s0 + s1, w0 + w1}, c, ENT);
+    const float4 v = make_float4(p.m, p.s, p.w, 0.f);
+    if (C == 1) {
+        if (lane == 0) xs[warp] = v;
+        __syncthreads();
+    } else {
+        cluster_wait_peers();
+        if (lane < C) peer_store(map_to_peer(smem_u32(xs + rank * WARPS + warp), (uint32_t)lane), v);
+        __syncwarp();
+        cluster_sync_all();
+    }
+    return merge_parts<ENT>(xs, C * WARPS, c);
+}
+
+// The same barriers for a warp that has no part to hand on.
+__device__ __forceinline__ void exchange_join(int C) {
+    __syncwarp();
+    if (C == 1) {
+        __syncthreads();
+    } else {
+        cluster_wait_peers();
+        cluster_sync_all();
+    }
 }
 
 // ---- dense gradient ------------------------------------------------------------------------
@@ -313,10 +340,11 @@ template <typename E, bool ENT>
 __device__ __forceinline__ void dense_pass(const Slice<E>& s, E* g, bool zero, float ref, float c, float A, float Bt) {
     const bool aligned = ((uintptr_t)g & 15) == 0;
     uint4* out = reinterpret_cast<uint4*>(g) + s.v0;
+    const uint64_t pol = l2_policy_evict_first();
     for (int i0 = threadIdx.x; i0 < s.n; i0 += kLRound) {
         uint4 w[kLUnroll];
         if (!zero) {
-            load_round(s, i0, w);
+            load_round(s, i0, w, pol);
 #pragma unroll
             for (int j = 0; j < kLUnroll; ++j) w[j] = dense_words<E, ENT>(w[j], ref, c, A, Bt);
         } else {
@@ -327,7 +355,7 @@ __device__ __forceinline__ void dense_pass(const Slice<E>& s, E* g, bool zero, f
         for (int j = 0; j < kLUnroll; ++j) {
             const int i = i0 + j * kLThreads;
             if (i < s.n) {
-                if (aligned && s.whole(s.v0 + i)) out[i] = w[j];
+                if (aligned && s.whole(s.v0 + i)) st_row16_hint(out + i, w[j], pol);
                 else store_partial(g, s.v0 + i, w[j], s.lead, s.end);
             }
         }
@@ -342,25 +370,28 @@ __device__ __forceinline__ bool in_slice(const Slice<E>& s, int col) {
 }
 
 // ---- what every kernel does first ---------------------------------------------------------------
-struct RowSetup { long long row; int rank; double T; float c; bool T_ok; };
+struct RowSetup { long long row; unsigned b, k; int rank; double T; float c; bool T_ok; };
 
 __device__ __forceinline__ RowSetup row_setup(const RowSpan& p) {
     RowSetup r;
-    r.row = blockIdx.x / (unsigned)p.C;
-    r.rank = (int)(blockIdx.x % (unsigned)p.C);
-    r.T = p.seq_T ? (double)__ldg(p.seq_T + r.row / p.R) : p.T;
+    const unsigned row = blockIdx.x / (unsigned)p.C;   // rows fit 32 bits
+    r.rank = (int)(blockIdx.x - row * (unsigned)p.C);
+    r.row = row;
+    r.b = row / (unsigned)p.R;
+    r.k = row - r.b * (unsigned)p.R;
+    r.T = p.seq_T ? (double)__ldg(p.seq_T + r.b) : p.T;
     r.c = (float)(kLog2e / r.T);
     r.T_ok = r.T > 0.0 && r.T < (double)INFINITY && r.c < INFINITY;
     if (p.C > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     return r;
 }
 template <typename E>
-__device__ __forceinline__ const E* row_ptr(const RowSpan& p, long long row) {
-    return reinterpret_cast<const E*>(p.x) + (row / p.R) * p.stride_b + (row % p.R) * p.stride_r;
+__device__ __forceinline__ const E* row_ptr(const RowSpan& p, const RowSetup& r) {
+    return reinterpret_cast<const E*>(p.x) + r.b * p.stride_b + r.k * p.stride_r;
 }
 template <typename E>
-__device__ __forceinline__ E* grad_ptr(void* g, const RowSpan& p, long long gsb, long long gsr, long long row) {
-    return reinterpret_cast<E*>(g) + (row / p.R) * gsb + (row % p.R) * gsr;
+__device__ __forceinline__ E* grad_ptr(void* g, long long gsb, long long gsr, const RowSetup& r) {
+    return reinterpret_cast<E*>(g) + r.b * gsb + r.k * gsr;
 }
 
 }  // namespace ears

@@ -6,6 +6,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstdint>
+#include <cstdlib>
 #include <type_traits>
 
 #include "ears_host.h"
@@ -18,6 +19,7 @@ namespace {
 
 using namespace ears;
 
+const int g_ring_stages = getenv("RING_S") ? atoi(getenv("RING_S")) : 6;
 std::atomic<int> g_row_cluster{0};   // ears_set_row_cluster
 
 int esize_of(int dtype) { return dtype == EARS_DTYPE_F32 ? 4 : 2; }
@@ -93,12 +95,12 @@ int make_span(const RowCall& c, bool twice, RowSpan* out) {
     return EARS_OK;
 }
 
-template <typename P>
-int launch_rows(void (*kernel)(P), const P& p, size_t smem, cudaStream_t stream, const char* what) {
+template <typename P, typename... Extra>
+int launch_rows(void (*kernel)(P, Extra...), const P& p, int threads, size_t smem, cudaStream_t stream, const char* what, Extra... extra) {
     const RowSpan& r = p.rows;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(r.rows * r.C), 1, 1);
-    cfg.blockDim = dim3(kLThreads, 1, 1);
+    cfg.blockDim = dim3((unsigned)threads, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -108,11 +110,15 @@ int launch_rows(void (*kernel)(P), const P& p, size_t smem, cudaStream_t stream,
         cfg.attrs = attr;
         cfg.numAttrs = 1;
     }
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return host_cuda_fail(e, what);
+    }
     if (r.C > 8) {
         const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return host_cuda_fail(e, what);
     }
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p, extra...);
     if (e != cudaSuccess) {
         (void)cudaGetLastError();
         return host_cuda_fail(e, what);
@@ -131,8 +137,33 @@ template <int MODE>
 int launch_token(int dtype, const TokenParams& p, bool ent, void* stream) {
     return with_type(dtype, [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
-        return launch_rows(ent ? ears_token_kernel<E, true, MODE> : ears_token_kernel<E, false, MODE>, p, 0, (cudaStream_t)stream,
-                           "ears_token_kernel launch");
+        return launch_rows(ent ? ears_token_kernel<E, true, MODE> : ears_token_kernel<E, false, MODE>, p, kLThreads, 0,
+                           (cudaStream_t)stream, "ears_token_kernel launch");
+    });
+}
+
+int ring_stages(int slice) {
+    const int chunks = (slice + kRingVecs - 1) / kRingVecs;
+    const int most = g_ring_stages;
+    return chunks < most ? chunks : most;
+}
+
+int launch_token_step(int dtype, const TokenParams& p, bool ent, void* stream) {
+    const int stages = ring_stages(p.rows.slice);
+    return with_type(dtype, [&](auto* e) {
+        typedef std::remove_pointer_t<decltype(e)> E;
+        return launch_rows(ent ? ears_token_step_kernel<E, true> : ears_token_step_kernel<E, false>, p, kRingThreads,
+                           (size_t)stages * kRingChunk, (cudaStream_t)stream, "ears_token_step_kernel launch", stages);
+    });
+}
+
+int launch_distill_step(int dtype, const DistillParams& p, void* stream) {
+    const int stages = ring_stages(p.rows.slice);
+    const size_t flags = (size_t)((p.rows.slice + kRingVecs - 1) / kRingVecs) * kLThreads;
+    return with_type(dtype, [&](auto* e) {
+        typedef std::remove_pointer_t<decltype(e)> E;
+        return launch_rows(ears_distill_step_kernel<E>, p, kDistillThreads, (size_t)stages * kRingChunk + flags, (cudaStream_t)stream,
+                           "ears_distill_step_kernel launch", stages);
     });
 }
 
@@ -141,7 +172,7 @@ int launch_distill(int dtype, const DistillParams& p, void* stream) {
     const size_t smem = MODE == kBackward ? 0 : (size_t)((p.rows.slice + kLRound - 1) / kLRound) * kLThreads;
     return with_type(dtype, [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
-        return launch_rows(ears_distill_kernel<E, MODE>, p, smem, (cudaStream_t)stream, "ears_distill_kernel launch");
+        return launch_rows(ears_distill_kernel<E, MODE>, p, kLThreads, smem, (cudaStream_t)stream, "ears_distill_kernel launch");
     });
 }
 
@@ -199,7 +230,7 @@ int ears_top_logits(int dtype, const void* logits, int B, int R, int V, int64_t 
     p.k = k; p.accept_len = accept_len;
     p.out_values = out_values; p.out_ids = out_ids; p.out_lse = out_lse; p.status = status;
     return with_type(dtype, [&](auto* e) {
-        return launch_rows(ears_top_kernel<std::remove_pointer_t<decltype(e)>>, p, 0, (cudaStream_t)stream, "ears_top_kernel launch");
+        return launch_rows(ears_top_kernel<std::remove_pointer_t<decltype(e)>>, p, kLThreads, 0, (cudaStream_t)stream, "ears_top_kernel launch");
     });
 }
 
@@ -244,7 +275,7 @@ int ears_token_logprobs_step(int dtype, const void* logits, int B, int R, int V,
     EARS_TRY(make_span(c, true, &p.rows));
     p.tokens = tokens; p.d_logp = d_logp; p.d_entropy = d_entropy; p.out_logp = out_logp; p.out_entropy = out_entropy;
     p.grad = out_grad; p.gsb = grad_stride_b; p.gsr = grad_stride_r; p.status = status;
-    return launch_token<kStep>(dtype, p, d_entropy != nullptr || out_entropy != nullptr, stream);
+    return launch_token_step(dtype, p, d_entropy != nullptr || out_entropy != nullptr, stream);
 }
 
 int ears_policy_loss(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
@@ -306,7 +337,7 @@ int ears_policy_step(int dtype, const void* logits, int B, int R, int V, int64_t
     p.clip_low = clip_low; p.clip_high = clip_high; p.kl_coef = kl_coef; p.entropy_coef = entropy_coef;
     p.out_loss = out_loss; p.out_logp = out_logp; p.out_kl = out_kl; p.out_entropy = out_entropy; p.status = status;
     p.grad = out_grad; p.gsb = grad_stride_b; p.gsr = grad_stride_r;
-    return launch_token<kStep>(dtype, p, entropy_coef != 0.0 || out_entropy != nullptr, stream);
+    return launch_token_step(dtype, p, entropy_coef != 0.0 || out_entropy != nullptr, stream);
 }
 
 int ears_distill_loss(int dtype, const void* logits, int B, int R, int V, int64_t stride_b, int64_t stride_r,
@@ -356,7 +387,7 @@ int ears_distill_step(int dtype, const void* logits, int B, int R, int V, int64_
     p.k = k; p.kind = kind; p.mix = mix; p.values = values; p.ids = ids; p.lse = lse; p.weight = row_weight;
     p.out_loss = out_loss; p.status = status;
     p.grad = out_grad; p.gsb = grad_stride_b; p.gsr = grad_stride_r;
-    return launch_distill<kStep>(dtype, p, stream);
+    return launch_distill_step(dtype, p, stream);
 }
 
 }  // extern "C"

@@ -16,6 +16,7 @@
 // (loss and gradient together) sweeps the slice twice, the second time out of L2: the rows in
 // flight (CTAs on the device / C of them) are far smaller than L2.
 #pragma once
+#include "ears_ring.cuh"
 #include "ears_rows.cuh"
 
 namespace ears {
@@ -45,11 +46,30 @@ struct TokenParams {
     int32_t* status;
 };
 
+// The row's own inputs: asked for at the start, used after the sweep.
+struct TokenInputs { float lt, old_logp, ref_logp, advantage, weight, d_logp, d_entropy; };
+
+template <typename E, bool ENT, int MODE>
+__device__ __forceinline__ TokenInputs token_inputs(const TokenParams& p, const E* row, long long r, int tok) {
+    TokenInputs in;
+    float x[Words<E>::N];
+    Words<E>::unpack(make_uint4(raw_bits(row + tok), 0, 0, 0), x);
+    in.lt = x[0];
+    in.old_logp = p.policy ? __ldg(p.old_logp + r) : 0.f;
+    in.advantage = p.policy ? __ldg(p.advantage + r) : 0.f;
+    in.ref_logp = p.policy && p.ref_logp ? __ldg(p.ref_logp + r) : 0.f;
+    in.weight = MODE != kForward && p.weight ? __ldg(p.weight + r) : 1.f;
+    in.d_logp = MODE != kForward && !p.policy ? __ldg(p.d_logp + r) : 0.f;
+    in.d_entropy = MODE != kForward && ENT && !p.policy && p.d_entropy ? __ldg(p.d_entropy + r) : 0.f;
+    return in;
+}
+
 // What the row's scalars come to, in 64 bits: one lane of one warp per CTA, identical in all of them.
 struct TokenScalars { float A, Bt, entry; int zero; };
 
 template <bool ENT, int MODE>
-__device__ __forceinline__ TokenScalars token_scalars(const TokenParams& p, long long row, int rank, double T, bool T_ok, float lt, Part st) {
+__device__ __forceinline__ TokenScalars token_scalars(const TokenParams& p, long long row, int rank, double T, bool T_ok, const TokenInputs& in, Part st) {
+    const float lt = in.lt;
     const bool ok = T_ok && rowstat_ok(st.m, st.s) && (!ENT || st.w == st.w);
     const double Z = st.s, lnZ = log(Z), invT = 1.0 / T;
     double logp = ((double)lt - (double)st.m) * invT - lnZ;
@@ -57,13 +77,13 @@ __device__ __forceinline__ TokenScalars token_scalars(const TokenParams& p, long
     double loss = 0.0, kl = 0.0, g = 0.0, h = 0.0;
     bool fine = ok;
     if (p.policy) {
-        const double old = __ldg(p.old_logp + row), A = __ldg(p.advantage + row);
+        const double old = in.old_logp, A = in.advantage;
         const double rho = exp(logp - old);
         const double plain = rho * A, clipped = fmin(fmax(rho, 1.0 - p.clip_low), 1.0 + p.clip_high) * A;
         loss = -fmin(plain, clipped);
         g = plain <= clipped ? -plain : 0.0;
         if (p.ref_logp) {
-            const double d = (double)__ldg(p.ref_logp + row) - logp, ed = exp(d);
+            const double d = (double)in.ref_logp - logp, ed = exp(d);
             kl = ed - d - 1.0;
             loss += p.kl_coef * kl;
             g += p.kl_coef * (1.0 - ed);
@@ -71,13 +91,13 @@ __device__ __forceinline__ TokenScalars token_scalars(const TokenParams& p, long
         if (ENT) loss -= p.entropy_coef * H;
         fine = fine && isfinite(old) && isfinite(A) && isfinite(loss) && isfinite(g);
         if (MODE != kForward) {
-            const double w = p.weight ? (double)__ldg(p.weight + row) : 1.0;
+            const double w = in.weight;
             g *= w;
             h = -w * p.entropy_coef;
         }
     } else if (MODE != kForward) {
-        g = __ldg(p.d_logp + row);
-        if (ENT && p.d_entropy) h = __ldg(p.d_entropy + row);
+        g = in.d_logp;
+        h = in.d_entropy;
     }
     TokenScalars r{0.f, 0.f, 0.f, 1};
     if (MODE != kForward) {
@@ -105,38 +125,38 @@ __device__ __forceinline__ TokenScalars token_scalars(const TokenParams& p, long
     return r;
 }
 
+// A row that is left out, or whose token is no index: outputs of 0 or NaN.
+template <int MODE>
+__device__ __forceinline__ void token_unused(const TokenParams& p, long long row, bool bad) {
+    const float v = bad ? __int_as_float(0x7fc00000) : 0.f;
+    if (MODE != kBackward) {
+        if (p.out_logp) p.out_logp[row] = v;
+        if (p.out_loss) p.out_loss[row] = v;
+        if (p.out_kl) p.out_kl[row] = v;
+        if (p.out_entropy) p.out_entropy[row] = v;
+        if (MODE == kForward && p.stats) p.stats[row] = make_float4(0.f, __int_as_float(0x7fc00000), 0.f, 0.f);
+    }
+    if (bad && p.status) atomicOr(p.status, kDevInvalidInput);
+}
+
+// Forward and backward calls: one sweep, straight from memory.
 template <typename E, bool ENT, int MODE>
 __global__ void __launch_bounds__(kLThreads) ears_token_kernel(const TokenParams p) {
     __shared__ float4 xs[kLMaxCluster * kLWarps];
     __shared__ TokenScalars sc;
     const RowSetup r = row_setup(p.rows);
-    const E* row = row_ptr<E>(p.rows, r.row);
+    const E* row = row_ptr<E>(p.rows, r);
     const Slice<E> s = make_slice<E>(row, p.rows.V, p.rows.slice, r.rank);
-    E* grad = MODE == kForward ? nullptr : grad_ptr<E>(p.grad, p.rows, p.gsb, p.gsr, r.row) - s.lead;
+    E* grad = MODE == kForward ? nullptr : grad_ptr<E>(p.grad, p.gsb, p.gsr, r) - s.lead;
     const int tok = __ldg(p.tokens + r.row);
     const bool absent = tok == -1, bad = tok < -1 || tok >= p.rows.V;
     if (absent || bad) {   // the same in every CTA of the cluster
-        if (threadIdx.x == 0 && r.rank == 0) {
-            const float v = bad ? __int_as_float(0x7fc00000) : 0.f;
-            if (MODE != kBackward) {
-                if (p.out_logp) p.out_logp[r.row] = v;
-                if (p.out_loss) p.out_loss[r.row] = v;
-                if (p.out_kl) p.out_kl[r.row] = v;
-                if (p.out_entropy) p.out_entropy[r.row] = v;
-                if (MODE == kForward && p.stats) p.stats[r.row] = make_float4(0.f, __int_as_float(0x7fc00000), 0.f, 0.f);
-            }
-            if (bad && p.status) atomicOr(p.status, kDevInvalidInput);
-        }
+        if (threadIdx.x == 0 && r.rank == 0) token_unused<MODE>(p, r.row, bad);
         if (MODE != kForward) dense_pass<E, ENT>(s, grad, true, 0.f, 0.f, 0.f, 0.f);
         return;
     }
-    // asked for now, used after the sweep
-    float lt = 0.f;
-    if (threadIdx.x == 0) {
-        float x[Words<E>::N];
-        Words<E>::unpack(make_uint4(raw_bits(row + tok), 0, 0, 0), x);
-        lt = x[0];
-    }
+    TokenInputs in{};
+    if (threadIdx.x == 0) in = token_inputs<E, ENT, MODE>(p, row, r.row, tok);
     Part st;
     if (MODE == kBackward) {
         const float4 q = p.stats[r.row];
@@ -145,14 +165,15 @@ __global__ void __launch_bounds__(kLThreads) ears_token_kernel(const TokenParams
     } else {
         Stat<ENT> a;
         stat_open(a);
+    const uint64_t pol = l2_policy_evict_first();
         for (int i0 = threadIdx.x; i0 < s.n; i0 += kLRound) {
             uint4 w[kLUnroll];
-            load_round(s, i0, w);
+            load_round(s, i0, w, pol);
             stat_fold<E, kLUnroll, ENT>(w, r.c, a);
         }
         st = exchange_parts<ENT>(a, xs, p.rows.C, r.rank, r.c);
     }
-    if (threadIdx.x == 0) sc = token_scalars<ENT, MODE>(p, r.row, r.rank, r.T, r.T_ok, lt, st);
+    if (threadIdx.x == 0) sc = token_scalars<ENT, MODE>(p, r.row, r.rank, r.T, r.T_ok, in, st);
     if (MODE == kForward) return;
     if (MODE == kBackward && p.rows.C > 1) {
         // the gradient may overwrite the logits: no slice is written before every CTA has its token logit
@@ -165,6 +186,60 @@ __global__ void __launch_bounds__(kLThreads) ears_token_kernel(const TokenParams
     if (!t.zero && in_slice(s, tok)) {
         __syncthreads();   // the dense value of this entry has been written
         if (threadIdx.x == 0) store_entry(grad + s.lead + tok, t.entry);
+    }
+}
+
+// Loss and gradient in one call: the slice through the ring of ears_ring.cuh.
+template <typename E, bool ENT>
+__global__ void __launch_bounds__(kRingThreads, 2) ears_token_step_kernel(const TokenParams p, int stages) {
+    extern __shared__ __align__(128) unsigned char ring_buf[];
+    __shared__ float4 xs[kLMaxCluster * kRingWarps];
+    __shared__ TokenScalars sc;
+    __shared__ RingBars bars;
+    const RowSetup r = row_setup(p.rows);
+    const E* row = row_ptr<E>(p.rows, r);
+    const Slice<E> s = make_slice<E>(row, p.rows.V, p.rows.slice, r.rank);
+    E* grad = grad_ptr<E>(p.grad, p.gsb, p.gsr, r) - s.lead;
+    const int tid = threadIdx.x;
+    const int tok = __ldg(p.tokens + r.row);
+    const bool absent = tok == -1, bad = tok < -1 || tok >= p.rows.V;
+    if (absent || bad) {   // the same in every CTA of the cluster
+        if (tid == 0 && r.rank == 0) token_unused<kStep>(p, r.row, bad);
+        if (tid < kLThreads) dense_pass<E, ENT>(s, grad, true, 0.f, 0.f, 0.f, 0.f);
+        return;
+    }
+    const Ring<E> ring = make_ring(s, ring_buf, &bars, stages);
+    const uint64_t keep = l2_policy_evict_last(), drop = l2_policy_evict_first();
+    if (tid == kRingConsumers) {
+        ring_init(&bars, stages);
+        ring_load(ring, 0, ring.H, keep, drop);
+    }
+    TokenInputs in{};
+    if (tid == 0) in = token_inputs<E, ENT, kStep>(p, row, r.row, tok);
+    __syncthreads();
+    if (tid >= kRingConsumers) {
+        ring_loader_warp(ring, ring.H, p.rows.C, keep, drop);
+        return;
+    }
+    Stat<ENT> a;
+    stat_open(a);
+    if (!ring_stats(ring, [&](uint4 (&w)[kRingPer], int) { stat_fold<E, kRingPer, ENT>(w, r.c, a); })) {
+        a.s[0] = pack2(__int_as_float(0x7fc00000), 0.f);   // the row counts as unusable in every CTA
+        if (p.status) atomicOr(p.status, kDevTimeout);
+    }
+    const int v = edge_vector(ring, s);
+    if (v >= 0) {
+        const uint4 w[1] = {load_partial(s.base, v, s.lead, s.end)};
+        stat_fold<E, 1, ENT>(w, r.c, a);
+    }
+    const Part st = exchange_parts<ENT, kRingWarps>(a, xs, p.rows.C, r.rank, r.c);
+    if (tid == 0) sc = token_scalars<ENT, kStep>(p, r.row, r.rank, r.T, r.T_ok, in, st);
+    ring_sync_consumers();
+    const TokenScalars t = sc;
+    ring_gradient<E, ENT>(ring, s, grad, t.zero != 0, st.m, r.c, t.A, t.Bt, drop, p.status);
+    if (!t.zero && in_slice(s, tok)) {
+        ring_sync_consumers();   // the dense value of this entry has been written
+        if (tid == 0) store_entry(grad + s.lead + tok, t.entry);
     }
 }
 

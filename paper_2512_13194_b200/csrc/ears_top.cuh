@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kLThreads) ears_top_kernel(const TopParams p) 
     __shared__ TopSmem sm;
     const int tid = threadIdx.x, k = p.k;
     const RowSetup r = row_setup(p.rows);
-    if (p.accept_len && (int)(r.row % p.rows.R) > __ldg(p.accept_len + r.row / p.rows.R)) {   // the same in the whole cluster
+    if (p.accept_len && (int)r.k > __ldg(p.accept_len + r.b)) {   // the same in the whole cluster
         if (r.rank == 0) {
             if (tid < k) {
                 p.out_values[r.row * k + tid] = -INFINITY;
@@ -139,10 +139,11 @@ __global__ void __launch_bounds__(kLThreads) ears_top_kernel(const TopParams p) 
         }
         return;
     }
-    const Slice<E> s = make_slice<E>(row_ptr<E>(p.rows, r.row), p.rows.V, p.rows.slice, r.rank);
+    const Slice<E> s = make_slice<E>(row_ptr<E>(p.rows, r), p.rows.V, p.rows.slice, r.rank);
     if (tid == 0) { sm.total = 0; sm.overflow[0] = sm.overflow[1] = 0; sm.threshold = 0ull; }
     Stat<false> a;
     stat_open(a);
+    const uint64_t pol = l2_policy_evict_first();
     float floor = -INFINITY;
     top_key threshold = 0;
     int offers = 0;
@@ -150,7 +151,7 @@ __global__ void __launch_bounds__(kLThreads) ears_top_kernel(const TopParams p) 
     for (int round = 0; round < rounds; ++round) {
         const int i0 = round * kLRound + tid;
         uint4 w[kLUnroll];
-        load_round(s, i0, w);   // beyond the slice: -inf
+        load_round(s, i0, w, pol);   // beyond the slice: -inf
         stat_fold<E, kLUnroll, false>(w, r.c, a);
         float top = Words<E>::template vmax_all<kLUnroll>(w);
         if (!(top > -INFINITY)) top = -INFINITY;   // nothing but NaN
