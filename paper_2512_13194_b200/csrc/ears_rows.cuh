@@ -148,8 +148,9 @@ __device__ __forceinline__ f32x2 clamp_masked(f32x2 t) {
 
 // G vectors: the maximum first, one rescale of the sums if it grew, then per entry a subtraction,
 // a multiplication, an exp2 and an addition, all but the exp2 on pairs.
+// -> the vectors' maximum.
 template <typename E, int G, bool ENT>
-__device__ __forceinline__ void stat_fold(const uint4 (&w)[G], float c, Stat<ENT>& a) {
+__device__ __forceinline__ float stat_fold(const uint4 (&w)[G], float c, Stat<ENT>& a) {
     constexpr int PN = Words<E>::N / 2;
     const float cm = Words<E>::template vmax_all<G>(w);
     if (cm > a.m) {
@@ -177,6 +178,7 @@ __device__ __forceinline__ void stat_fold(const uint4 (&w)[G], float c, Stat<ENT
             if (ENT) a.w[i & 1] = fma2(e, clamp_masked(t), a.w[i & 1]);
         }
     }
+    return cm;
 }
 
 // The statistics of a part: what one warp hands on, and what the whole row ends with.

@@ -4,20 +4,21 @@
 // row was split: an entry's key is its value as an order-preserving 32-bit integer followed by the
 // complement of its index, all keys of a row are distinct, and the k largest keys are unique.
 //
-// One sweep of the slice, with the statistics of the row's softmax on the way.  A CTA keeps a buffer of
-// candidates and a threshold below which nothing can be among the slice's k largest:
-//   * first round: the k-th largest of the threads' maxima (k entries are at least that large).  For
-//     rows in no particular order a slice then yields about 256 ln(256 / (256 - k)) candidates a round,
-//     falling with the rounds behind it;
-//   * candidates are appended to the buffer.  When it cannot take them all, its k largest are
-//     sorted to its front, the threshold rises to the k-th and what is still pending is offered again:
-//     rows in ascending order or with most entries equal run slower, never wrong.
-// The rank of a candidate is the number of larger keys: one comparison with every other, read from
-// shared memory two to a load, without a barrier.  The C sorted lists of a cluster are handed to every
-// CTA, and each CTA finds the final ranks of its own entries by binary search in the others.
-//
-// Bound by HBM for long rows, by latency for few: a row of 256 KB in one CTA takes 18 us at a CTA's
-// share of the bandwidth, its ranks about 1.
+// One sweep of the slice yields the statistics of the row's softmax and, as a by-product, the maximum of
+// every group of entries that one thread held in registers together (64 of them; at most kTopRounds groups
+// per thread).  The k-th largest of the group maxima is a threshold: at least k entries reach it.  For rows in
+// no particular order few others do (of G groups about G ln(G / (G - k)) entries: 133 for k = 128 and
+// 2048 groups), so only the groups that reach it are fetched again, and their entries are candidates.
+//   * thresholds and group maxima are compared by the upper 16 bits of their ordered pattern, which is
+//     exact for bf16 and a threshold a little lower for the others; the k-th largest is found two bits at a time by
+//     counting;
+//   * the rank of a candidate is the number of larger keys: one comparison with every other, read from
+//     shared memory two to a load, without a barrier;
+//   * when too many entries reach the threshold (rows with most entries equal), they are offered to the buffer
+//     round by round instead, and whenever it is full its k largest stay and the threshold rises to the k-th:
+//     slower, never wrong.
+// The C sorted lists of a cluster are handed to every CTA, and each CTA finds the final ranks of its own
+// entries by binary search in the others.
 #pragma once
 #include "ears_distill.cuh"   // kMaxTop
 #include "ears_rows.cuh"
@@ -26,6 +27,8 @@ namespace ears {
 
 typedef unsigned long long top_key;
 constexpr int kTopBuf = 2048;                // candidates a CTA holds: 128 + 64 < 2048, so each offer takes one thread's at least
+constexpr int kTopRounds = 16;               // groups per thread: round r of the sweep counts to group r % kTopRounds
+constexpr int kTopGroups = 1024;             // groups fetched again
 
 struct TopParams {
     RowSpan rows;
@@ -40,12 +43,16 @@ struct TopParams {
 struct TopSmem {
     float4 xs[kLMaxCluster * kLWarps];
     alignas(16) top_key buf[kTopBuf];
-    top_key list[kLMaxCluster][kMaxTop];     // sorted lists of the cluster's CTAs
+    union {
+        top_key list[kLMaxCluster][kMaxTop];          // sorted lists of the cluster's CTAs
+        uint16_t group[kTopRounds][kLThreads];        // before them: 16-bit prefixes of the group maxima
+    };
     int count[kLMaxCluster];
-    alignas(16) float tmax[kLThreads];
+    uint16_t reach[kTopGroups];              // groups that reach the threshold
+    uint2 tally[2][kLWarps];
     int total;                               // places of buf given out
+    int groups;                              // places of reach given out
     int overflow[2];                         // alternating by offer
-    top_key threshold;
 };
 
 // larger float -> larger integer; -0 and 0 are one value
@@ -58,41 +65,78 @@ __device__ __forceinline__ float unorder_bits(uint32_t u) {
 }
 __device__ __forceinline__ top_key make_key(float x, int col) { return ((top_key)order_bits(x) << 32) | (uint32_t)~col; }
 
+constexpr uint32_t kLowestPrefix = 0x0080u;   // of the lowest finite value; -inf lies below it
+
+// The largest 16-bit t >= kLowestPrefix that at least k of the threads' values v reach (kLowestPrefix if fewer do).
+// All threads; values below kLowestPrefix stand for nothing.
+template <int PER>
+__device__ __forceinline__ uint32_t kth_prefix(const uint32_t (&v)[PER], int per, int k, TopSmem& sm) {
+    uint32_t t = 0;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll 1
+    for (int s = 14; s >= 0; s -= 2) {
+        const uint32_t t1 = t | 1u << s, t2 = t | 2u << s, t3 = t | 3u << s;
+        uint32_t a = 0, b = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (i >= per) break;
+            a += (v[i] >= t1 ? 1u : 0u) + (v[i] >= t2 ? 1u << 16 : 0u);
+            b += v[i] >= t3 ? 1u : 0u;
+        }
+        a = __reduce_add_sync(0xffffffffu, a);
+        b = __reduce_add_sync(0xffffffffu, b);
+        uint2* tally = sm.tally[(s >> 1) & 1];
+        if (lane == 0) tally[warp] = make_uint2(a, b);
+        __syncthreads();
+        a = b = 0;
+#pragma unroll
+        for (int w = 0; w < kLWarps; ++w) { a += tally[w].x; b += tally[w].y; }
+        if ((int)b >= k) t = t3;
+        else if ((int)(a >> 16) >= k) t = t2;
+        else if ((int)(a & 0xffffu) >= k) t = t1;
+    }
+    return max(t, kLowestPrefix);
+}
+
 // The k largest of buf[0 .. n) sorted to its front.  All threads; buf is final when it returns.
 __device__ __forceinline__ int compact_candidates(TopSmem& sm, int n, int k) {
     constexpr int PER = kTopBuf / kLThreads;
     const int tid = threadIdx.x;
+    if (n > kLThreads && n > k) {
+        // drop what the k-th largest prefix leaves behind, so that the ranking has little more than k to compare
+        top_key mine[PER];
+        uint32_t v[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = tid + i * kLThreads;
+            mine[i] = at < n ? sm.buf[at] : 0ull;
+            v[i] = (uint32_t)(mine[i] >> 48);
+        }
+        if (tid == 0) sm.total = 0;
+        const uint32_t t = kth_prefix(v, (n + kLThreads - 1) / kLThreads, k, sm);   // its barriers part the reads from the writes
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (v[i] >= t) sm.buf[atomicAdd(&sm.total, 1)] = mine[i];
+        __syncthreads();
+        n = sm.total;
+    }
     if (tid == 0 && (n & 1)) sm.buf[n] = 0ull;   // kTopBuf is even
     __syncthreads();
+    const ulonglong2* pairs = reinterpret_cast<const ulonglong2*>(sm.buf);
+    const int n2 = (n + 1) / 2;
     top_key mine[PER];
     int rank[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int at = tid + i * kLThreads;
-        mine[i] = at < n ? sm.buf[at] : 0ull;
+        mine[i] = 0ull;
+        if (at >= n) continue;
+        mine[i] = sm.buf[at];
         rank[i] = 0;
-    }
-    const ulonglong2* pairs = reinterpret_cast<const ulonglong2*>(sm.buf);
-    const int n2 = (n + 1) / 2;
-    // as many of a thread's candidates as there are (n is the same for all threads)
-    if (n <= kLThreads) {
 #pragma unroll 4
         for (int j = 0; j < n2; ++j) {
             const ulonglong2 q = pairs[j];
-            rank[0] += (q.x > mine[0]) + (q.y > mine[0]);
-        }
-    } else if (n <= 2 * kLThreads) {
-#pragma unroll 4
-        for (int j = 0; j < n2; ++j) {
-            const ulonglong2 q = pairs[j];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) rank[i] += (q.x > mine[i]) + (q.y > mine[i]);
-        }
-    } else {
-        for (int j = 0; j < n2; ++j) {
-            const ulonglong2 q = pairs[j];
-#pragma unroll
-            for (int i = 0; i < PER; ++i) rank[i] += (q.x > mine[i]) + (q.y > mine[i]);
+            rank[i] += (q.x > mine[i]) + (q.y > mine[i]);
         }
     }
     __syncthreads();
@@ -103,24 +147,62 @@ __device__ __forceinline__ int compact_candidates(TopSmem& sm, int n, int k) {
     return min(n, k);
 }
 
-// Calls f(value, column) for every entry of the thread's round whose value is at least `floor`.  The vectors
-// are fetched again (from L2, and seldom): keeping all eight for this path would cost the sweep its registers.
+// Calls f(value, column) for every finite entry of vector i of the slice whose prefix is at least t16.
 template <typename E, class F>
-__device__ __forceinline__ void each_candidate(const Slice<E>& s, int i0, float floor, F f) {
+__device__ __forceinline__ void each_candidate(const Slice<E>& s, int i, uint32_t t16, F f) {
     constexpr int N = Words<E>::N;
-#pragma unroll 1
-    for (int i = i0; i < s.n && i < i0 + kLRound; i += kLThreads) {
-        const int v = s.v0 + i;
-        const uint4 w = s.whole(v) ? ld_row16(reinterpret_cast<const uint4*>(s.base) + v) : load_partial(s.base, v, s.lead, s.end);
-        const uint4 one[1] = {w};
-        if (Words<E>::template vmax_all<1>(one) >= floor) {
-            float x[N];
-            Words<E>::unpack(w, x);
-            const int col = v * N - s.lead;
+    const int v = s.v0 + i;
+    const uint4 w = s.whole(v) ? ld_row16(reinterpret_cast<const uint4*>(s.base) + v) : load_partial(s.base, v, s.lead, s.end);
+    float x[N];
+    Words<E>::unpack(w, x);
+    const int col = v * N - s.lead;
 #pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (x[j] >= floor && x[j] > -INFINITY) f(x[j], col + j);
+    for (int j = 0; j < N; ++j)
+        if ((order_bits(x[j]) >> 16) >= t16) f(x[j], col + j);
+}
+
+// Too many entries reach the threshold: every thread offers its entries round by round, and when the buffer cannot take
+// them all, its k largest stay, the threshold rises to the k-th and what is still pending is offered again.
+template <typename E>
+__device__ __noinline__ void offer_rounds(const Slice<E>& s, TopSmem& sm, int rounds, uint32_t t16, int k) {
+    const int tid = threadIdx.x;
+    top_key threshold = (top_key)t16 << 48;
+    int offers = 0;
+    __syncthreads();
+    if (tid == 0) sm.total = 0;
+    __syncthreads();
+    for (int round = 0; round < rounds; ++round) {
+        const int i0 = round * kLRound + tid;
+        bool pending = true;
+        for (;; ++offers) {
+            if (pending) {
+                int n = 0;
+                for (int i = i0; i < s.n && i < i0 + kLRound; i += kLThreads)
+                    each_candidate(s, i, t16, [&](float x, int col) { n += make_key(x, col) >= threshold; });
+                const int at = n ? atomicAdd(&sm.total, n) : 0;
+                if (at + n <= kTopBuf) {
+                    int o = at;
+                    for (int i = i0; i < s.n && i < i0 + kLRound; i += kLThreads)
+                        each_candidate(s, i, t16, [&](float x, int col) {
+                            const top_key key = make_key(x, col);
+                            if (key >= threshold) sm.buf[o++] = key;
+                        });
+                    pending = false;
+                } else {
+                    for (int o = at; o < kTopBuf; ++o) sm.buf[o] = 0ull;   // places given out and not used
+                    sm.overflow[offers & 1] = 1;
+                }
+            }
+            __syncthreads();
+            if (!sm.overflow[offers & 1]) break;
+            const int held = min(sm.total, kTopBuf);
+            __syncthreads();
+            const int n = compact_candidates(sm, held, k);
+            threshold = n == k ? sm.buf[k - 1] : threshold;
+            if (tid == 0) { sm.total = n; sm.overflow[offers & 1] = 0; }
+            __syncthreads();
         }
+        ++offers;
     }
 }
 
@@ -140,71 +222,52 @@ __global__ void __launch_bounds__(kLThreads) ears_top_kernel(const TopParams p) 
         return;
     }
     const Slice<E> s = make_slice<E>(row_ptr<E>(p.rows, r), p.rows.V, p.rows.slice, r.rank);
-    if (tid == 0) { sm.total = 0; sm.overflow[0] = sm.overflow[1] = 0; sm.threshold = 0ull; }
+    if (tid == 0) { sm.total = sm.groups = 0; sm.overflow[0] = sm.overflow[1] = 0; }
     Stat<false> a;
     stat_open(a);
     const uint64_t pol = l2_policy_evict_first();
-    float floor = -INFINITY;
-    top_key threshold = 0;
-    int offers = 0;
-    const int rounds = (s.n + kLRound - 1) / kLRound;
+    const int rounds = (s.n + kLRound - 1) / kLRound, groups = min(rounds, kTopRounds);
     for (int round = 0; round < rounds; ++round) {
-        const int i0 = round * kLRound + tid;
         uint4 w[kLUnroll];
-        load_round(s, i0, w, pol);   // beyond the slice: -inf
-        stat_fold<E, kLUnroll, false>(w, r.c, a);
-        float top = Words<E>::template vmax_all<kLUnroll>(w);
-        if (!(top > -INFINITY)) top = -INFINITY;   // nothing but NaN
-        if (round == 0) {
-            // the k-th largest of the threads' maxima
-            sm.tmax[tid] = top;
-            __syncthreads();
-            int larger = 0;
-            const float4* q4 = reinterpret_cast<const float4*>(sm.tmax);
-#pragma unroll 4
-            for (int q = 0; q < kLThreads / 4; ++q) {
-                const float4 v = q4[q];
-                // equal maxima in thread order: the ranks are a permutation
-                larger += (v.x > top || (v.x == top && 4 * q < tid)) + (v.y > top || (v.y == top && 4 * q + 1 < tid))
-                        + (v.z > top || (v.z == top && 4 * q + 2 < tid)) + (v.w > top || (v.w == top && 4 * q + 3 < tid));
-            }
-            if (larger == k - 1) sm.threshold = top > -INFINITY ? ((top_key)order_bits(top) << 32) : 0ull;
-            __syncthreads();
-            threshold = sm.threshold;
-            floor = threshold ? unorder_bits((uint32_t)(threshold >> 32)) : -INFINITY;
-        }
-        bool pending = top >= floor && top > -INFINITY;
-        for (;; ++offers) {
-            if (pending) {
-                int n = 0;
-                each_candidate(s, i0, floor, [&](float x, int col) { n += make_key(x, col) >= threshold; });
-                const int at = n ? atomicAdd(&sm.total, n) : 0;
-                if (at + n <= kTopBuf) {
-                    int o = at;
-                    each_candidate(s, i0, floor, [&](float x, int col) {
-                        const top_key key = make_key(x, col);
-                        if (key >= threshold) sm.buf[o++] = key;
-                    });
-                    pending = false;
-                } else {
-                    for (int o = at; o < kTopBuf; ++o) sm.buf[o] = 0ull;   // places given out and not used
-                    sm.overflow[offers & 1] = 1;
-                }
-            }
-            __syncthreads();
-            if (!sm.overflow[offers & 1]) break;
-            const int n = compact_candidates(sm, min(sm.total, kTopBuf), k);
-            if (tid == 0) { sm.total = n; sm.overflow[offers & 1] = 0; }
-            threshold = sm.buf[n - 1];
-            if (n == k) floor = unorder_bits((uint32_t)(threshold >> 32));
-            else threshold = 0;
-            __syncthreads();
-        }
-        ++offers;
+        load_round(s, round * kLRound + tid, w, pol);   // beyond the slice: -inf
+        const float top = stat_fold<E, kLUnroll, false>(w, r.c, a);
+        uint16_t* g = &sm.group[round % kTopRounds][tid];
+        const uint16_t prefix = top > -INFINITY ? (uint16_t)(order_bits(top) >> 16) : (uint16_t)0;   // NaN: the row is unusable anyway
+        *g = round < kTopRounds ? prefix : max(*g, prefix);
     }
-    // the slice's k largest, sorted
+    uint32_t v[kTopRounds];
+#pragma unroll
+    for (int i = 0; i < kTopRounds; ++i) v[i] = i < groups ? sm.group[i][tid] : 0u;   // the thread's own
+    const uint32_t t16 = kth_prefix(v, groups, k, sm);
+#pragma unroll
+    for (int i = 0; i < kTopRounds; ++i) {
+        if (v[i] >= t16) {
+            const int at = atomicAdd(&sm.groups, 1);
+            if (at < kTopGroups) sm.reach[at] = (uint16_t)(i * kLThreads + tid);
+        }
+    }
     __syncthreads();
-    const int got = compact_candidates(sm, min(sm.total, kTopBuf), k);
+    const int reached = sm.groups;
+    if (reached <= kTopGroups) {
+        // eight threads to a group, one vector each
+        for (int q = tid / kLUnroll; q < reached; q += kLThreads / kLUnroll) {
+            const int g = sm.reach[q];
+            for (int round = g / kLThreads; round < rounds; round += kTopRounds) {
+                const int i = round * kLRound + (tid % kLUnroll) * kLThreads + g % kLThreads;
+                if (i < s.n)
+                    each_candidate(s, i, t16, [&](float x, int col) {
+                        const int at = atomicAdd(&sm.total, 1);
+                        if (at < kTopBuf) sm.buf[at] = make_key(x, col);
+                    });
+            }
+        }
+    }
+    __syncthreads();
+    if (reached > kTopGroups || sm.total > kTopBuf) offer_rounds(s, sm, rounds, t16, k);
+    // the slice's k largest, sorted
+    const int found = sm.total;
+    __syncthreads();
+    const int got = compact_candidates(sm, found, k);
     const Part st = exchange_parts<false>(a, sm.xs, p.rows.C, r.rank, r.c);
     const bool ok = r.T_ok && rowstat_ok(st.m, st.s);
     if (r.rank == 0 && tid == 0) {
