@@ -42,8 +42,7 @@ struct DistillParams {
 
 constexpr int kListSlots = 256;
 
-struct DistillSmem {
-    float4 xs[kLMaxCluster * kLWarps];
+struct ListSmem {
     alignas(16) int col[kMaxTop];   // listed ids, -1: absent
     int vec[kMaxTop];            // vector that holds the listed entry, -1: absent
     float x[kMaxTop];            // draft logit of the listed entry
@@ -72,12 +71,12 @@ __device__ __forceinline__ double warp_max(double v) {
 constexpr int kTopPer = kMaxTop / 32;
 struct TeacherPart { double lp[kTopPer], pr[kTopPer], ps, L; };
 
-__device__ __forceinline__ bool listed(const DistillParams& p, const DistillSmem& sm, int i) {
+__device__ __forceinline__ bool listed(const DistillParams& p, const ListSmem& sm, int i) {
     const int j = (threadIdx.x & 31) + 32 * i;
     return j < p.k && sm.col[j] >= 0;
 }
 
-__device__ __forceinline__ TeacherPart teacher_part(const DistillParams& p, const DistillSmem& sm, long long row, double invT) {
+__device__ __forceinline__ TeacherPart teacher_part(const DistillParams& p, const ListSmem& sm, long long row, double invT) {
     const int lane = threadIdx.x & 31;
     TeacherPart t;
     if (p.lse) {
@@ -108,7 +107,7 @@ __device__ __forceinline__ TeacherPart teacher_part(const DistillParams& p, cons
 }
 
 template <int MODE>
-__device__ __forceinline__ void distill_scalars(const DistillParams& p, DistillSmem& sm, long long row, int rank, double invT, bool ok,
+__device__ __forceinline__ void distill_scalars(const DistillParams& p, ListSmem& sm, long long row, int rank, double invT, bool ok,
                                                 const TeacherPart& te, float weight, Part tail) {
     const int lane = threadIdx.x & 31;
     double lq[kTopPer], qr[kTopPer], gs[kTopPer];
@@ -214,67 +213,92 @@ __device__ __forceinline__ void distill_scalars(const DistillParams& p, DistillS
     }
 }
 
-// The row's list, by all threads of the CTA (THREADS >= kMaxTop of them, in whole warps): into sm, with a flag for
-// every vector among [base, base + count) that holds a listed entry -- byte (i / (PER kLThreads)) kLThreads + i % kLThreads,
-// bit i / kLThreads % PER, for vector base + i: what the thread that folds the vector looks at.  -> sm.seen.
-template <typename E, int PER, int THREADS>
-__device__ __forceinline__ int distill_list(const DistillParams& p, DistillSmem& sm, uint32_t* flags, long long row_index, const E* row,
+// The threads that share a row: a warp, or all threads of the CTA.
+template <int THREADS>
+__device__ __forceinline__ void row_sync() {
+    if (THREADS == 32) __syncwarp();
+    else __syncthreads();
+}
+
+// The row's list, by the THREADS threads that share the row (tid among them): into sm, with a flag for every vector
+// among [base, base + count) that holds a listed entry -- byte (i / (PER SWEEP)) SWEEP + i % SWEEP, bit i / SWEEP % PER, for
+// vector base + i: what the thread that folds the vector, one of SWEEP, looks at.  -> sm.seen.
+template <typename E, int PER, int SWEEP, int THREADS>
+__device__ __forceinline__ int distill_list(const DistillParams& p, ListSmem& sm, uint32_t* flags, int tid, long long row_index, const E* row,
                                             int lead, int base, int count) {
     constexpr int N = Words<E>::N;
-    const int tid = threadIdx.x, k = p.k;
-    int id = -1;
-    float tv = -INFINITY;
-    if (tid < k) {
-        id = __ldg(p.ids + row_index * k + tid);
-        tv = __ldg(p.values + row_index * k + tid);
-    }
-    bool wrong = id < -1 || id >= p.rows.V || (id >= 0 && !(tv < INFINITY));   // NaN and +inf
-    const bool present = !wrong && id >= 0 && tv > -INFINITY;
-    if (tid == 0) sm.seen = 0;
-    const int words = (count + PER * kLThreads - 1) / (PER * kLThreads) * (kLThreads / 4);
-    for (int i = tid; i < words; i += THREADS) flags[i] = 0;
-    if (tid < kListSlots) sm.head[tid] = -1;
-    if (tid < kMaxTop) {
-        float x = -INFINITY;
-        if (present) {
-            float xx[N];
-            Words<E>::unpack(make_uint4(raw_bits(row + id), 0, 0, 0), xx);
-            x = xx[0];
+    constexpr int HAND = THREADS < kMaxTop ? kMaxTop / THREADS : 1;   // entries per thread
+    const int k = p.k;
+    int id[HAND];
+    float tv[HAND];
+#pragma unroll
+    for (int h = 0; h < HAND; ++h) {
+        const int j = tid + h * THREADS;
+        id[h] = -1;
+        tv[h] = -INFINITY;
+        if (j < k) {
+            id[h] = __ldg(p.ids + row_index * k + j);
+            tv[h] = __ldg(p.values + row_index * k + j);
         }
-        sm.vec[tid] = present ? (lead + id) / N : -1;
-        sm.col[tid] = present ? id : -1;
-        sm.x[tid] = x;
-        sm.t[tid] = tv;
     }
-    __syncthreads();
-    if (tid < kMaxTop) {
-        if (present) {
+    if (tid == 0) sm.seen = 0;
+    const int words = (count + PER * SWEEP - 1) / (PER * SWEEP) * (SWEEP / 4);
+    for (int i = tid; i < words; i += THREADS) flags[i] = 0;
+    for (int i = tid; i < kListSlots; i += THREADS) sm.head[i] = -1;
+    bool wrong = false, present[HAND];
+#pragma unroll
+    for (int h = 0; h < HAND; ++h) {
+        const int j = tid + h * THREADS;
+        const bool off = id[h] < -1 || id[h] >= p.rows.V || (id[h] >= 0 && !(tv[h] < INFINITY));   // NaN and +inf
+        wrong = wrong || off;
+        present[h] = !off && id[h] >= 0 && tv[h] > -INFINITY;
+        if (j < kMaxTop) {
+            float x = -INFINITY;
+            if (present[h]) {
+                float xx[N];
+                Words<E>::unpack(make_uint4(raw_bits(row + id[h]), 0, 0, 0), xx);
+                x = xx[0];
+            }
+            sm.vec[j] = present[h] ? (lead + id[h]) / N : -1;
+            sm.col[j] = present[h] ? id[h] : -1;
+            sm.x[j] = x;
+            sm.t[j] = tv[h];
+        }
+    }
+    row_sync<THREADS>();
+    if (tid < kMaxTop) {   // whole warps
+        bool any = false;
+#pragma unroll
+        for (int h = 0; h < HAND; ++h) {
+            if (!present[h]) continue;
+            any = true;
             // an id listed twice
             const int4* c4 = reinterpret_cast<const int4*>(sm.col);
             int same = 0;
 #pragma unroll 4
             for (int j = 0; j < (k + 3) / 4; ++j) {
                 const int4 c = c4[j];
-                same += (c.x == id) + (c.y == id) + (c.z == id) + (c.w == id);
+                same += (c.x == id[h]) + (c.y == id[h]) + (c.z == id[h]) + (c.w == id[h]);
             }
-            wrong = same > 1;
-            sm.next[tid] = atomicExch(&sm.head[sm.vec[tid] % kListSlots], tid);
-            const int i = sm.vec[tid] - base;
+            wrong = wrong || same > 1;
+            const int j = tid + h * THREADS;
+            sm.next[j] = atomicExch(&sm.head[sm.vec[j] % kListSlots], j);
+            const int i = sm.vec[j] - base;
             if (i >= 0 && i < count) {
-                const int byte = (i / (PER * kLThreads)) * kLThreads + i % kLThreads, bit = (i / kLThreads) % PER;
+                const int byte = (i / (PER * SWEEP)) * SWEEP + i % SWEEP, bit = (i / SWEEP) % PER;
                 atomicOr(&flags[byte >> 2], 1u << ((byte & 3) * 8 + bit));
             }
         }
-        const unsigned any = __ballot_sync(0xffffffffu, present), bad = __ballot_sync(0xffffffffu, wrong);
-        if ((tid & 31) == 0 && (any | bad)) atomicOr(&sm.seen, (any ? 1 : 0) | (bad ? 2 : 0));
+        const unsigned some = __ballot_sync(0xffffffffu, any), bad = __ballot_sync(0xffffffffu, wrong);
+        if ((tid & 31) == 0 && (some | bad)) atomicOr(&sm.seen, (some ? 1 : 0) | (bad ? 2 : 0));
     }
-    __syncthreads();
+    row_sync<THREADS>();
     return sm.seen;
 }
 
 // Vector v with the entries that are listed taken out: the entries of its slot, a few at most.
 template <typename E>
-__device__ __forceinline__ void mask_listed(const DistillSmem& sm, int lead, int v, uint4& w) {
+__device__ __forceinline__ void mask_listed(const ListSmem& sm, int lead, int v, uint4& w) {
     for (int q = sm.head[v % kListSlots]; q >= 0; q = sm.next[q])
         if (sm.vec[q] == v) put_entry(w, (lead + sm.col[q]) % Words<E>::N, minus_inf_bits<E>(), E{});
 }
@@ -294,14 +318,15 @@ __device__ __forceinline__ bool tail_empty(Part st) { return st.m == -INFINITY &
 template <typename E, int MODE>
 __global__ void __launch_bounds__(kLThreads) ears_distill_kernel(const DistillParams p) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    __shared__ DistillSmem sm;
+    __shared__ ListSmem sm;
+    __shared__ float4 xs[kLMaxCluster * kLWarps];
     uint32_t* flags = reinterpret_cast<uint32_t*>(smem_raw);
     const int tid = threadIdx.x, k = p.k;
     const RowSetup r = row_setup(p.rows);
     const E* row = row_ptr<E>(p.rows, r);
     const Slice<E> s = make_slice<E>(row, p.rows.V, p.rows.slice, r.rank);
     E* grad = MODE == kForward ? nullptr : grad_ptr<E>(p.grad, p.gsb, p.gsr, r) - s.lead;
-    const int seen = distill_list<E, kLUnroll, kLThreads>(p, sm, flags, r.row, row, s.lead, s.v0, MODE == kBackward ? 0 : s.n);
+    const int seen = distill_list<E, kLUnroll, kLThreads, kLThreads>(p, sm, flags, tid, r.row, row, s.lead, s.v0, MODE == kBackward ? 0 : s.n);
     if (seen != 1) {   // the same in every CTA of the cluster
         if (tid == 0 && r.rank == 0) distill_unused<MODE>(p, r.row, (seen & 2) != 0);
         if (MODE != kForward) dense_pass<E, false>(s, grad, true, 0.f, 0.f, 0.f, 0.f);
@@ -332,7 +357,7 @@ __global__ void __launch_bounds__(kLThreads) ears_distill_kernel(const DistillPa
             }
             stat_fold<E, kLUnroll, false>(w, r.c, a);
         }
-        st = exchange_parts<false>(a, sm.xs, p.rows.C, r.rank, r.c);
+        st = exchange_parts<false>(a, xs, p.rows.C, r.rank, r.c);
     }
     const bool empty = tail_empty(st);
     if (tid < 32) {
@@ -357,7 +382,8 @@ constexpr int kDistillThreads = kRingThreads + 32;
 template <typename E>
 __global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(const DistillParams p, int stages) {
     extern __shared__ __align__(128) unsigned char ring_buf[];
-    __shared__ DistillSmem sm;
+    __shared__ ListSmem sm;
+    __shared__ float4 xs[kLMaxCluster * kRingWarps];
     __shared__ RingBars bars;
     uint32_t* flags = reinterpret_cast<uint32_t*>(ring_buf + (size_t)stages * kRingChunk);
     const int tid = threadIdx.x, k = p.k, C = p.rows.C;
@@ -378,7 +404,7 @@ __global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(c
             issued = ring_load(ring, 0, ring.H, keep, drop);
         }
     }
-    const int seen = distill_list<E, kRingPer, kDistillThreads>(p, sm, flags, r.row, row, s.lead, ring.v0, ring.vecs);
+    const int seen = distill_list<E, kRingPer, kRingConsumers, kDistillThreads>(p, sm, flags, tid, r.row, row, s.lead, ring.v0, ring.vecs);
     if (seen != 1) {   // the same in every CTA of the cluster
         if (tid == 0 && r.rank == 0) distill_unused<kStep>(p, r.row, (seen & 2) != 0);
         if (tid < kLThreads) dense_pass<E, false>(s, grad, true, 0.f, 0.f, 0.f, 0.f);
@@ -390,7 +416,7 @@ __global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(c
         const float weight = p.weight ? __ldg(p.weight + r.row) : 1.f;
         const TeacherPart te = teacher_part(p, sm, r.row, invT);
         exchange_join(C);
-        const Part st = merge_parts<false>(sm.xs, C * kRingWarps, r.c);
+        const Part st = merge_parts<false>(xs, C * kRingWarps, r.c);
         distill_scalars<kStep>(p, sm, r.row, r.rank, invT, r.T_ok && (tail_empty(st) || rowstat_ok(st.m, st.s)), te, weight, st);
         __syncwarp();
         asm volatile("bar.arrive 1, %0;" ::"n"(kRingConsumers + 32) : "memory");
@@ -422,7 +448,7 @@ __global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(c
         mask_listed<E>(sm, s.lead, v, w[0]);
         stat_fold<E, 1, false>(w, r.c, a);
     }
-    const Part st = exchange_parts<false, kRingWarps>(a, sm.xs, C, r.rank, r.c);
+    const Part st = exchange_parts<false, kRingWarps>(a, xs, C, r.rank, r.c);
     asm volatile("bar.sync 1, %0;" ::"n"(kRingConsumers + 32) : "memory");   // the scalars
     const bool zero = sm.zero != 0;
     ring_gradient<E, false>(ring, s, grad, zero, tail_empty(st) ? 0.f : st.m, r.c, sm.factor, 0.f, drop, p.status);

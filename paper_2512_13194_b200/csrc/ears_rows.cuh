@@ -34,6 +34,7 @@ struct RowSpan {           // rows r = b R + k of [B, R, V] with strides in entr
     int R, V;
     double T;
     const float* seq_T;    // [B] temperature per sequence, or NULL
+    int vectors;           // 16-byte vectors that a row, starting anywhere, covers at most
     int C;                 // CTAs per row
     int slice;             // vectors per CTA (a multiple of kSliceAlign)
 };
@@ -374,16 +375,22 @@ __device__ __forceinline__ bool in_slice(const Slice<E>& s, int col) {
 // ---- what every kernel does first ---------------------------------------------------------------
 struct RowSetup { long long row; unsigned b, k; int rank; double T; float c; bool T_ok; };
 
-__device__ __forceinline__ RowSetup row_setup(const RowSpan& p) {
+__device__ __forceinline__ RowSetup row_setup_at(const RowSpan& p, unsigned row) {   // rows fit 32 bits
     RowSetup r;
-    const unsigned row = blockIdx.x / (unsigned)p.C;   // rows fit 32 bits
-    r.rank = (int)(blockIdx.x - row * (unsigned)p.C);
+    r.rank = 0;
     r.row = row;
     r.b = row / (unsigned)p.R;
     r.k = row - r.b * (unsigned)p.R;
     r.T = p.seq_T ? (double)__ldg(p.seq_T + r.b) : p.T;
     r.c = (float)(kLog2e / r.T);
     r.T_ok = r.T > 0.0 && r.T < (double)INFINITY && r.c < INFINITY;
+    return r;
+}
+
+__device__ __forceinline__ RowSetup row_setup(const RowSpan& p) {
+    const unsigned row = blockIdx.x / (unsigned)p.C;
+    RowSetup r = row_setup_at(p, row);
+    r.rank = (int)(blockIdx.x - row * (unsigned)p.C);
     if (p.C > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     return r;
 }

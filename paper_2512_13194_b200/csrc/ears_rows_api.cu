@@ -12,6 +12,7 @@
 #include "ears_host.h"
 #include "ears_distill.cuh"
 #include "ears_rows.cuh"
+#include "ears_short.cuh"
 #include "ears_token.cuh"
 #include "ears_top.cuh"
 
@@ -66,15 +67,17 @@ int check_grad(const RowCall& c, const void* grad, int64_t gsb, int64_t gsr) {
     return EARS_OK;
 }
 
-// CTAs per row: enough of them to fill the device when there are few rows, and for calls that read a
-// slice twice so many that the rows in flight stay in L2.
+// CTAs per row.  Few rows are split until their CTAs cover half the SMs (slices of 16 KB and more), or one and a half per
+// SM where the slices stay above 64 KB; a call that fetches a slice twice splits rows so long that the ones in flight (two
+// CTAs per SM) would not stay in L2.  More CTAs per row than that cost: the CTAs of a cluster start and end together
+// (scoring 256 rows of 256 KB takes 18 us with one, 20 with two, 31 with eight; 64 rows 10, 7.2, 6.4 with four, 9.5).
 int choose_cluster(long long rows, size_t row_bytes, bool twice, int sms) {
     const int forced = g_row_cluster.load(std::memory_order_relaxed);
     if (forced) return forced;
     int C = 1;
-    while (C < kLMaxCluster && rows * C < 2ll * sms && row_bytes / (size_t)C > 8192) C *= 2;
+    while (C < 8 && ((rows * C * 2 <= sms && row_bytes / C > (16u << 10)) || (rows * C <= sms && row_bytes / C > (64u << 10)))) C *= 2;
     if (twice)
-        while (C < 8 && (size_t)(4 * sms / C) * row_bytes > (40u << 20)) C *= 2;
+        while (C < 8 && (size_t)(2 * sms / C) * row_bytes > (100u << 20)) C *= 2;
     return C;
 }
 
@@ -88,9 +91,9 @@ int make_span(const RowCall& c, bool twice, RowSpan* out) {
     s.R = c.R; s.V = c.V; s.T = c.T; s.seq_T = c.seq_T;
     s.C = choose_cluster(s.rows, (size_t)c.V * esize_of(c.dtype), twice, sms);
     const int n = 16 / esize_of(c.dtype);
-    const long long vectors = ((long long)c.V + 2 * n - 2) / n;   // a row that starts anywhere covers at most this many
-    const long long per = (vectors + s.C - 1) / s.C;
-    s.slice = (int)((per + kSliceAlign - 1) / kSliceAlign * kSliceAlign);
+    s.vectors = (int)(((long long)c.V + 2 * n - 2) / n);
+    const int per = (s.vectors + s.C - 1) / s.C;
+    s.slice = (per + kSliceAlign - 1) / kSliceAlign * kSliceAlign;
     *out = s;
     return EARS_OK;
 }
@@ -133,8 +136,59 @@ int with_type(int dtype, F&& f) {
     return f((uint16_t*)nullptr);
 }
 
+// Threads that hold a row in registers (ears_short.cuh), 0 where the row is too long for that or a number of CTAs per
+// row is asked for.
+int short_threads(const RowSpan& r) {
+    if (g_row_cluster.load(std::memory_order_relaxed)) return 0;
+    for (int g : {32, 128, 256})
+        if (r.vectors <= g * kShortSlots) return g;
+    return 0;
+}
+
+// Calls f with the number of threads as a constant.
+template <typename F>
+int with_short(int g, F&& f) {
+    if (g == 32) return f(std::integral_constant<int, 32>());
+    if (g == 128) return f(std::integral_constant<int, 128>());
+    return f(std::integral_constant<int, 256>());
+}
+
+template <typename P>
+int launch_short(void (*kernel)(P), P p, int threads_per_row, cudaStream_t stream, const char* what) {
+    const int rows = threads_per_row == 32 ? kShortWarpRows : 1;   // per CTA
+    p.rows.slice = p.rows.vectors;
+    p.rows.C = 1;
+    kernel<<<(unsigned)((p.rows.rows + rows - 1) / rows), threads_per_row * rows, 0, stream>>>(p);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? EARS_OK : host_cuda_fail(e, what);
+}
+
+template <int MODE>
+int launch_token_short(int dtype, const TokenParams& p, bool ent, int g, void* stream) {
+    return with_type(dtype, [&](auto* e) {
+        typedef std::remove_pointer_t<decltype(e)> E;
+        return with_short(g, [&](auto threads) {
+            constexpr int G = decltype(threads)::value;
+            return launch_short(ent ? ears_token_short_kernel<E, G, true, MODE> : ears_token_short_kernel<E, G, false, MODE>, p, G,
+                                (cudaStream_t)stream, "ears_token_short_kernel launch");
+        });
+    });
+}
+
+template <int MODE>
+int launch_distill_short(int dtype, const DistillParams& p, int g, void* stream) {
+    return with_type(dtype, [&](auto* e) {
+        typedef std::remove_pointer_t<decltype(e)> E;
+        return with_short(g, [&](auto threads) {
+            constexpr int G = decltype(threads)::value;
+            return launch_short(ears_distill_short_kernel<E, G, MODE>, p, G, (cudaStream_t)stream, "ears_distill_short_kernel launch");
+        });
+    });
+}
+
 template <int MODE>
 int launch_token(int dtype, const TokenParams& p, bool ent, void* stream) {
+    if (const int g = short_threads(p.rows)) return launch_token_short<MODE>(dtype, p, ent, g, stream);
     return with_type(dtype, [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
         return launch_rows(ent ? ears_token_kernel<E, true, MODE> : ears_token_kernel<E, false, MODE>, p, kLThreads, 0,
@@ -149,6 +203,7 @@ int ring_stages(int slice) {
 }
 
 int launch_token_step(int dtype, const TokenParams& p, bool ent, void* stream) {
+    if (const int g = short_threads(p.rows)) return launch_token_short<kStep>(dtype, p, ent, g, stream);
     const int stages = ring_stages(p.rows.slice);
     return with_type(dtype, [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
@@ -158,6 +213,7 @@ int launch_token_step(int dtype, const TokenParams& p, bool ent, void* stream) {
 }
 
 int launch_distill_step(int dtype, const DistillParams& p, void* stream) {
+    if (const int g = short_threads(p.rows)) return launch_distill_short<kStep>(dtype, p, g, stream);
     const int stages = ring_stages(p.rows.slice);
     const size_t flags = (size_t)((p.rows.slice + kRingVecs - 1) / kRingVecs) * kLThreads;
     return with_type(dtype, [&](auto* e) {
@@ -169,6 +225,7 @@ int launch_distill_step(int dtype, const DistillParams& p, void* stream) {
 
 template <int MODE>
 int launch_distill(int dtype, const DistillParams& p, void* stream) {
+    if (const int g = short_threads(p.rows)) return launch_distill_short<MODE>(dtype, p, g, stream);
     const size_t smem = MODE == kBackward ? 0 : (size_t)((p.rows.slice + kLRound - 1) / kLRound) * kLThreads;
     return with_type(dtype, [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
@@ -229,6 +286,11 @@ int ears_top_logits(int dtype, const void* logits, int B, int R, int V, int64_t 
     EARS_TRY(make_span(c, false, &p.rows));
     p.k = k; p.accept_len = accept_len;
     p.out_values = out_values; p.out_ids = out_ids; p.out_lse = out_lse; p.status = status;
+    if (short_threads(p.rows) == 32)
+        return with_type(dtype, [&](auto* e) {
+            return launch_short(ears_top_short_kernel<std::remove_pointer_t<decltype(e)>>, p, 32, (cudaStream_t)stream,
+                                "ears_top_short_kernel launch");
+        });
     return with_type(dtype, [&](auto* e) {
         return launch_rows(ears_top_kernel<std::remove_pointer_t<decltype(e)>>, p, kLThreads, 0, (cudaStream_t)stream, "ears_top_kernel launch");
     });

@@ -125,6 +125,11 @@ __device__ __forceinline__ TokenScalars token_scalars(const TokenParams& p, long
     return r;
 }
 
+// What a forward call left for the backward call; an entropy gradient needs the sum that only a forward call with
+// the entropy leaves.
+template <bool ENT>
+__device__ __forceinline__ Part token_saved(float4 q) { return Part{q.x, !ENT || q.w == 1.f ? q.y : __int_as_float(0x7fc00000), q.z}; }
+
 // A row that is left out, or whose token is no index: outputs of 0 or NaN.
 template <int MODE>
 __device__ __forceinline__ void token_unused(const TokenParams& p, long long row, bool bad) {
@@ -160,8 +165,7 @@ __global__ void __launch_bounds__(kLThreads) ears_token_kernel(const TokenParams
     Part st;
     if (MODE == kBackward) {
         const float4 q = p.stats[r.row];
-        // an entropy gradient needs the sum that only a forward call with the entropy leaves
-        st = Part{q.x, !ENT || q.w == 1.f ? q.y : __int_as_float(0x7fc00000), q.z};
+        st = token_saved<ENT>(q);
     } else {
         Stat<ENT> a;
         stat_open(a);

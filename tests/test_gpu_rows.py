@@ -110,6 +110,52 @@ def test_top_logits_orders_that_are_hard(ears, dtype, name, cluster):
     close(top.lse, lse, LOG_TOL * 2)
 
 
+@pytest.mark.parametrize("V", [300, 1501, 2043])
+@pytest.mark.parametrize("name", sorted(PATTERNS))
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_top_logits_of_short_rows_in_hard_orders(ears, dtype, name, V):
+    x = PATTERNS[name](V)
+    if dtype == "fp16":
+        x = x.clamp(-65504.0, 65504.0) if name != "three_finite" else x
+    x = torch.stack([x, x.flip(0), x.roll(7)]).to(DT[dtype])
+    for k in (1, 100, 128):
+        top = ears.top_logits(x.to(DEV), k, 1.0)
+        v, i, lse = R.top_logits(x, k, 1.0)
+        assert torch.equal(top.ids.cpu().long(), i)
+        assert torch.equal(top.values.cpu().double(), v)
+        close(top.lse, lse, LOG_TOL * 2)
+
+
+def test_many_short_rows_and_rows_that_start_anywhere(ears):
+    for dtype in ("fp32", "bf16"):
+        for V in (3, 17, 700, 2030, 6001, 12001):
+            n = 37 if V > 1000 else 203
+            x, g = logits(n, V + 8, dtype, 60 + V, mask=False)
+            for off in (0, 1, 3, 8):
+                rows = x[:, off:off + V]
+                dev = x.to(DEV)[:, off:off + V]
+                tok = torch.randint(0, V, (n,), generator=g, dtype=torch.int32)
+                dl = torch.randn(n, generator=g)
+                o = R.token_logprobs(rows, tok, 0.9, dl)
+                logp, _, grad = ears.token_logprobs_step(dev, tok.to(DEV), dl.to(DEV), None, 0.9)
+                close(logp, o.logp, LOG_TOL)
+                close_grad(grad, o.grad, o.scale, G_TOL, dtype)
+                k = min(V, 5)
+                top = ears.top_logits(dev, k)
+                v, i, lse = R.top_logits(rows, k, 1.0)
+                assert torch.equal(top.ids.cpu().long(), i)
+                teacher = ears.TopLogits(v.float().to(DEV), i.to(torch.int32).to(DEV), lse.float().to(DEV))
+                y = (rows.float() * 0.7).to(DT[dtype])
+                wide = torch.zeros(n, V + 8, dtype=DT[dtype], device=DEV)
+                wide[:, off:off + V] = y.to(DEV)
+                od = R.distill(y, 1.0, v.float(), i.to(torch.int32), lse=lse.float(), kind="jsd", weight=dl.abs())
+                loss, grad = ears.distill_step(wide[:, off:off + V], teacher, kind="jsd", row_weight=dl.abs().to(DEV),
+                                               out_grad=wide[:, off:off + V])
+                close(loss, od.loss, od.loss_scale * (3 * LOG_TOL))
+                close_grad(wide[:, off:off + V], od.grad, od.scale, G_TOL, dtype)
+                assert not wide[:, :off].any() and not wide[:, off + V:].any()
+
+
 def test_top_logits_takes_strided_rows_and_leaves_out_what_lies_behind_a_rejection(ears):
     B, K, V, k = 6, 3, 5003, 9
     x, g = logits(B * (K + 1), V, "bf16", 3)
