@@ -19,44 +19,73 @@ constexpr int kShortWarpRows = 4;            // rows per CTA where a warp has a 
 template <int G> struct ShortShape {
     static constexpr int kRows = G == 32 ? kShortWarpRows : 1;   // rows per CTA
     static constexpr int kThreads = G * kRows;
+    static constexpr int kCtas = G == 256 ? 3 : 6;              // per SM: leaves 80 registers a thread
 };
 
-// The thread's vectors of a row: vector tid + j G; -inf beyond the row.
+// A row's whole vectors, tid + j G of them in w[j], and the one vector at an end that the row covers in part which falls to
+// this thread: thread 0 has the first, thread 1 the last (index `edge`, -1: none).  Beyond the row: -inf.
+template <typename E>
+struct ShortRow {
+    uint4 w[kShortSlots], we;
+    int v0, vecs, edge;
+};
+
 template <typename E, int G>
-__device__ __forceinline__ void short_load(const Slice<E>& s, int tid, uint4 (&w)[kShortSlots]) {
-    const uint4* p = reinterpret_cast<const uint4*>(s.base);
+__device__ __forceinline__ void short_load(const Slice<E>& s, int tid, ShortRow<E>& x) {
+    constexpr int N = Words<E>::N;
+    x.v0 = s.lead > 0 ? 1 : 0;
+    x.vecs = max(0, s.end / N - x.v0);
+    x.edge = -1;
+    if (tid == 0 && x.v0 > 0) x.edge = 0;
+    if (tid == 1 && s.n > x.v0 + x.vecs) x.edge = s.n - 1;
+    const uint4* p = reinterpret_cast<const uint4*>(s.base) + x.v0 + tid;
 #pragma unroll
     for (int j = 0; j < kShortSlots; ++j) {
-        const int v = tid + j * G;
-        w[j] = Words<E>::minus_inf();
-        if (v < s.n) {
-            if (s.whole(v)) w[j] = ld_row16(p + v);
-            else w[j] = load_partial(s.base, v, s.lead, s.end);
-        }
+        x.w[j] = Words<E>::minus_inf();
+        if (tid + j * G < x.vecs) x.w[j] = ld_row16(p + j * G);
     }
-}
-
-template <typename E, int G>
-__device__ __forceinline__ void short_store(const Slice<E>& s, int tid, E* g, int j, uint4 d) {
-    const int v = tid + j * G;
-    if (v < s.n) {
-        if (((uintptr_t)g & 15) == 0 && s.whole(v)) reinterpret_cast<uint4*>(g)[v] = d;
-        else store_partial(g, v, d, s.lead, s.end);
-    }
-}
-
-template <typename E, int G>
-__device__ __forceinline__ void short_zero(const Slice<E>& s, int tid, E* g) {
-#pragma unroll
-    for (int j = 0; j < kShortSlots; ++j) short_store<E, G>(s, tid, g, j, make_uint4(0, 0, 0, 0));
+    x.we = Words<E>::minus_inf();
+    if (x.edge >= 0) x.we = load_partial(s.base, x.edge, s.lead, s.end);
 }
 
 template <typename E, int G, bool ENT>
-__device__ __forceinline__ void short_gradient(const Slice<E>& s, int tid, E* g, const uint4 (&w)[kShortSlots], float ref, float c, float A, float Bt) {
+__device__ __forceinline__ Stat<ENT> short_stats(const ShortRow<E>& x, float c) {
+    Stat<ENT> a;
+    stat_open(a);
+    stat_fold<E, kShortSlots, ENT>(x.w, c, a);
+    if (x.edge >= 0) {
+        const uint4 one[1] = {x.we};
+        stat_fold<E, 1, ENT>(one, c, a);
+    }
+    return a;
+}
+
+// The gradient row, 2^t (A + Bt t) or zeros.
+template <typename E, int G, bool ENT>
+__device__ __forceinline__ void short_gradient(const Slice<E>& s, int tid, E* g, const ShortRow<E>& x, bool zero, float ref, float c, float A, float Bt) {
+    const bool aligned = ((uintptr_t)g & 15) == 0;
+    uint4* out = reinterpret_cast<uint4*>(g) + x.v0 + tid;
 #pragma unroll
     for (int j = 0; j < kShortSlots; ++j) {
-        if (j * G >= s.n) break;
-        short_store<E, G>(s, tid, g, j, dense_words<E, ENT>(w[j], ref, c, A, Bt));
+        if (j * G >= x.vecs) break;
+        const uint4 d = zero ? make_uint4(0, 0, 0, 0) : dense_words<E, ENT>(x.w[j], ref, c, A, Bt);
+        if (tid + j * G < x.vecs) {
+            if (aligned) out[j * G] = d;
+            else store_partial(g, x.v0 + tid + j * G, d, s.lead, s.end);
+        }
+    }
+    if (x.edge >= 0)
+        store_partial(g, x.edge, zero ? make_uint4(0, 0, 0, 0) : dense_words<E, ENT>(x.we, ref, c, A, Bt), s.lead, s.end);
+}
+
+// A gradient row of zeros of which nothing was read.
+template <typename E, int G>
+__device__ __forceinline__ void short_zero(const Slice<E>& s, int tid, E* g) {
+    const bool aligned = ((uintptr_t)g & 15) == 0;
+#pragma unroll 1
+    for (int v = tid; v < s.n; v += G) {
+        if (aligned && s.whole(v)) reinterpret_cast<uint4*>(g)[v] = make_uint4(0, 0, 0, 0);
+        else store_partial(g, v, make_uint4(0, 0, 0, 0), s.lead, s.end);
     }
 }
 
@@ -83,7 +112,7 @@ __device__ __forceinline__ bool short_setup(const RowSpan& p, RowSetup* r) {
 }
 
 template <typename E, int G, bool ENT, int MODE>
-__global__ void __launch_bounds__(ShortShape<G>::kThreads) ears_token_short_kernel(const TokenParams p) {
+__global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas) ears_token_short_kernel(const TokenParams p) {
     __shared__ float4 xs[G / 32];
     __shared__ TokenScalars scalars[ShortShape<G>::kRows];
     RowSetup r;
@@ -102,33 +131,23 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads) ears_token_short_kern
     }
     TokenInputs in{};
     if (tid == 0) in = token_inputs<E, ENT, MODE>(p, row, r.row, tok);
-    uint4 w[kShortSlots];
-    short_load<E, G>(s, tid, w);
+    ShortRow<E> x;
+    short_load<E, G>(s, tid, x);
     Part st;
-    if (MODE == kBackward) {
-        const float4 q = p.stats[r.row];
-        st = token_saved<ENT>(q);
-    } else {
-        Stat<ENT> a;
-        stat_open(a);
-        stat_fold<E, kShortSlots, ENT>(w, r.c, a);
-        st = short_merge<G, ENT>(a, xs, r.c);
-    }
+    if (MODE == kBackward) st = token_saved<ENT>(p.stats[r.row]);
+    else st = short_merge<G, ENT>(short_stats<E, G, ENT>(x, r.c), xs, r.c);
     if (tid == 0) sc = token_scalars<ENT, MODE>(p, r.row, 0, r.T, r.T_ok, in, st);
     if (MODE == kForward) return;
     row_sync<G>();
     const TokenScalars t = sc;
-    if (t.zero) {
-        short_zero<E, G>(s, tid, grad);
-        return;
-    }
-    short_gradient<E, G, ENT>(s, tid, grad, w, st.m, r.c, t.A, t.Bt);
+    short_gradient<E, G, ENT>(s, tid, grad, x, t.zero != 0, st.m, r.c, t.A, t.Bt);
+    if (t.zero) return;
     row_sync<G>();   // the dense value of the token's entry has been written
     if (tid == 0) store_entry(grad + s.lead + tok, t.entry);
 }
 
 template <typename E, int G, int MODE>
-__global__ void __launch_bounds__(ShortShape<G>::kThreads) ears_distill_short_kernel(const DistillParams p) {
+__global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas) ears_distill_short_kernel(const DistillParams p) {
     __shared__ float4 xs[G / 32];
     __shared__ ListSmem lists[ShortShape<G>::kRows];
     __shared__ uint32_t all_flags[ShortShape<G>::kThreads / 4];
@@ -140,14 +159,15 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads) ears_distill_short_ke
     const E* row = row_ptr<E>(p.rows, r);
     const Slice<E> s = make_slice<E>(row, p.rows.V, p.rows.slice, 0);
     E* grad = MODE == kForward ? nullptr : grad_ptr<E>(p.grad, p.gsb, p.gsr, r) - s.lead;
-    const int seen = distill_list<E, kShortSlots, G, G>(p, sm, flags, tid, r.row, row, s.lead, 0, s.n);
+    const int v0 = s.lead > 0 ? 1 : 0;   // the first whole vector
+    const int seen = distill_list<E, kShortSlots, G, G>(p, sm, flags, tid, r.row, row, s.lead, v0, max(0, s.end / Words<E>::N - v0));
     if (seen != 1) {
         if (tid == 0) distill_unused<MODE>(p, r.row, (seen & 2) != 0);
         if (MODE != kForward) short_zero<E, G>(s, tid, grad);
         return;
     }
-    uint4 w[kShortSlots];
-    short_load<E, G>(s, tid, w);
+    ShortRow<E> x;
+    short_load<E, G>(s, tid, x);
     Part st;
     if (MODE == kBackward) {
         const float4 q = p.stats[r.row];
@@ -158,12 +178,10 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads) ears_distill_short_ke
         if (f) {
 #pragma unroll
             for (int j = 0; j < kShortSlots; ++j)
-                if (f >> j & 1u) mask_listed<E>(sm, s.lead, tid + j * G, w[j]);
+                if (f >> j & 1u) mask_listed<E>(sm, s.lead, v0 + tid + j * G, x.w[j]);
         }
-        Stat<false> a;
-        stat_open(a);
-        stat_fold<E, kShortSlots, false>(w, r.c, a);
-        st = short_merge<G, false>(a, xs, r.c);
+        if (x.edge >= 0) mask_listed<E>(sm, s.lead, x.edge, x.we);
+        st = short_merge<G, false>(short_stats<E, G, false>(x, r.c), xs, r.c);
     }
     const bool empty = tail_empty(st);
     if (tid < 32) {
@@ -174,11 +192,9 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads) ears_distill_short_ke
     }
     if (MODE == kForward) return;
     row_sync<G>();
-    if (sm.zero) {
-        short_zero<E, G>(s, tid, grad);
-        return;
-    }
-    short_gradient<E, G, false>(s, tid, grad, w, empty ? 0.f : st.m, r.c, sm.factor, 0.f);
+    const bool zero = sm.zero != 0;
+    short_gradient<E, G, false>(s, tid, grad, x, zero, empty ? 0.f : st.m, r.c, sm.factor, 0.f);
+    if (zero) return;
     row_sync<G>();   // the dense values of the listed entries have been written
     for (int j = tid; j < k; j += G)
         if (sm.col[j] >= 0) store_entry(grad + s.lead + sm.col[j], sm.entry[j]);
@@ -213,7 +229,7 @@ __device__ __forceinline__ uint32_t warp_kth(const uint32_t (&v)[PER], int per, 
 }
 
 template <typename E>
-__global__ void __launch_bounds__(ShortShape<32>::kThreads) ears_top_short_kernel(const TopParams p) {
+__global__ void __launch_bounds__(ShortShape<32>::kThreads, ShortShape<32>::kCtas) ears_top_short_kernel(const TopParams p) {
     constexpr int N = Words<E>::N;
     __shared__ ShortTopSmem rows[ShortShape<32>::kRows];
     RowSetup r;
@@ -225,13 +241,10 @@ __global__ void __launch_bounds__(ShortShape<32>::kThreads) ears_top_short_kerne
     const bool live = !p.accept_len || (int)r.k <= __ldg(p.accept_len + r.b);
     const Slice<E> s = make_slice<E>(row_ptr<E>(p.rows, r), p.rows.V, p.rows.slice, 0);
     Part st{-INFINITY, 0.f, 0.f};
-    uint4 w[kShortSlots];
+    ShortRow<E> row;
     if (live) {
-        short_load<E, 32>(s, lane, w);
-        Stat<false> a;
-        stat_open(a);
-        stat_fold<E, kShortSlots, false>(w, r.c, a);
-        st = short_merge<32, false>(a, nullptr, r.c);
+        short_load<E, 32>(s, lane, row);
+        st = short_merge<32, false>(short_stats<E, 32, false>(row, r.c), nullptr, r.c);
     }
     const bool ok = live && r.T_ok && rowstat_ok(st.m, st.s);
     if (lane == 0) {
@@ -244,25 +257,26 @@ __global__ void __launch_bounds__(ShortShape<32>::kThreads) ears_top_short_kerne
         for (int j = lane; j < k; j += 32) { values[j] = -INFINITY; ids[j] = -1; }
         return;
     }
-    // threshold from the vectors' maxima
-    const int per = (s.n + 31) / 32;
-    uint32_t v[kShortSlots];
+    // threshold from the vectors' maxima; the vector at an end is the first of nine
+    const auto vec = [&](int j) { return j == 0 ? row.we : row.w[j == 0 ? 0 : j - 1]; };
+    const auto col = [&](int j) { return (j == 0 ? row.edge : row.v0 + lane + 32 * (j - 1)) * N - s.lead; };
+    uint32_t v[kShortSlots + 1];
 #pragma unroll
-    for (int j = 0; j < kShortSlots; ++j) {
-        const uint4 one[1] = {w[j]};
+    for (int j = 0; j <= kShortSlots; ++j) {
+        const uint4 one[1] = {vec(j)};
         v[j] = order_bits(Words<E>::template vmax_all<1>(one)) >> 16;
     }
-    const uint32_t t16 = warp_kth(v, per, k);
+    const uint32_t t16 = warp_kth(v, 1 + (row.vecs + 31) / 32, k);
 #pragma unroll
-    for (int j = 0; j < kShortSlots; ++j) {
+    for (int j = 0; j <= kShortSlots; ++j) {
         if (v[j] < t16) continue;
         float x[N];
-        Words<E>::unpack(w[j], x);
+        Words<E>::unpack(vec(j), x);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if ((order_bits(x[i]) >> 16) < t16) continue;
             const int at = atomicAdd(&sm.total, 1);
-            if (at < kShortTopBuf) sm.buf[at] = make_key(x[i], (lane + 32 * j) * N + i - s.lead);
+            if (at < kShortTopBuf) sm.buf[at] = make_key(x[i], col(j) + i);
         }
     }
     __syncwarp();
@@ -275,31 +289,43 @@ __global__ void __launch_bounds__(ShortShape<32>::kThreads) ears_top_short_kerne
             const uint32_t t = u | 1u << b;
             int c = 0;
 #pragma unroll
-            for (int j = 0; j < kShortSlots; ++j) {
+            for (int j = 0; j <= kShortSlots; ++j) {
                 float x[N];
-                Words<E>::unpack(w[j], x);
+                Words<E>::unpack(vec(j), x);
 #pragma unroll
                 for (int i = 0; i < N; ++i) c += order_bits(x[i]) >= t ? 1 : 0;
             }
             if (__reduce_add_sync(0xffffffffu, c) >= k) u = t;
         }
-        int above = 0;
-#pragma unroll
-        for (int j = 0; j < kShortSlots; ++j) {
-            float x[N];
-            Words<E>::unpack(w[j], x);
-#pragma unroll
-            for (int i = 0; i < N; ++i) above += order_bits(x[i]) > u ? 1 : 0;
-        }
-        above = __reduce_add_sync(0xffffffffu, above);
         __syncwarp();
         if (lane == 0) sm.total = 0;
         __syncwarp();
-        int equal = 0;   // equal entries before slot j
+        // the greater ones, fewer than k
 #pragma unroll
-        for (int j = 0; j < kShortSlots; ++j) {
+        for (int j = 0; j <= kShortSlots; ++j) {
             float x[N];
-            Words<E>::unpack(w[j], x);
+            Words<E>::unpack(vec(j), x);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (order_bits(x[i]) > u) sm.buf[atomicAdd(&sm.total, 1)] = make_key(x[i], col(j) + i);
+        }
+        __syncwarp();
+        // equal ones in the order of their columns: the first vector (lane 0 has it), the whole ones, the last (lane 1)
+        int above = sm.total;   // places taken
+#pragma unroll 1
+        for (int q = 0; q < kShortSlots + 2 && above < k; ++q) {
+            uint4 one = Words<E>::minus_inf();
+            int first = 0;
+            if (q == 0) { if (lane == 0) one = row.we; first = -s.lead; }
+            else if (q == kShortSlots + 1) { if (lane == 1) one = row.we; first = row.edge * N - s.lead; }
+            else {
+#pragma unroll
+                for (int j = 0; j < kShortSlots; ++j)
+                    if (j == q - 1) one = row.w[j];
+                first = (row.v0 + lane + 32 * (q - 1)) * N - s.lead;
+            }
+            float x[N];
+            Words<E>::unpack(one, x);
             int mine = 0;
 #pragma unroll
             for (int i = 0; i < N; ++i) mine += order_bits(x[i]) == u ? 1 : 0;
@@ -310,19 +336,18 @@ __global__ void __launch_bounds__(ShortShape<32>::kThreads) ears_top_short_kerne
                 if (lane >= off) before += o;
             }
             const int all = __shfl_sync(0xffffffffu, before, 31);
-            before += equal - mine;
+            before += above - mine;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const uint32_t o = order_bits(x[i]);
-                if (o > u || (o == u && above + before++ < k)) {
-                    const int at = atomicAdd(&sm.total, 1);
-                    if (at < kShortTopBuf) sm.buf[at] = make_key(x[i], (lane + 32 * j) * N + i - s.lead);
+                if (order_bits(x[i]) == u) {
+                    if (before < k) sm.buf[before] = make_key(x[i], first + i);
+                    ++before;
                 }
             }
-            equal += all;
+            above += all;
         }
         __syncwarp();
-        n = min(sm.total, kShortTopBuf);
+        n = min(above, k);
     }
     if (lane == 0 && (n & 1)) sm.buf[n] = 0ull;   // kShortTopBuf is even
     __syncwarp();
