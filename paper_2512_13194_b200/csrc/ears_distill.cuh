@@ -346,17 +346,15 @@ __global__ void __launch_bounds__(kLThreads) ears_distill_kernel(const DistillPa
         stat_open(a);
         const uint64_t pol = l2_policy_evict_first();
         const unsigned char* flag_bytes = reinterpret_cast<const unsigned char*>(flags);
-        for (int i0 = tid, round = 0; i0 < s.n; i0 += kLRound, ++round) {
-            uint4 w[kLUnroll];
-            load_round(s, i0, w, pol);
+        sweep_rounds(s, pol, [&](uint4 (&w)[kLUnroll], int round) {
             const unsigned f = flag_bytes[round * kLThreads + tid];
             if (f) {
 #pragma unroll
                 for (int j = 0; j < kLUnroll; ++j)
-                    if (f >> j & 1u) mask_listed<E>(sm, s.lead, s.v0 + i0 + j * kLThreads, w[j]);
+                    if (f >> j & 1u) mask_listed<E>(sm, s.lead, s.v0 + round * kLRound + tid + j * kLThreads, w[j]);
             }
             stat_fold<E, kLUnroll, false>(w, r.c, a);
-        }
+        });
         st = exchange_parts<false>(a, xs, p.rows.C, r.rank, r.c);
     }
     const bool empty = tail_empty(st);

@@ -170,11 +170,7 @@ __global__ void __launch_bounds__(kLThreads) ears_token_kernel(const TokenParams
         Stat<ENT> a;
         stat_open(a);
     const uint64_t pol = l2_policy_evict_first();
-        for (int i0 = threadIdx.x; i0 < s.n; i0 += kLRound) {
-            uint4 w[kLUnroll];
-            load_round(s, i0, w, pol);
-            stat_fold<E, kLUnroll, ENT>(w, r.c, a);
-        }
+        sweep_rounds(s, pol, [&](uint4 (&w)[kLUnroll], int) { stat_fold<E, kLUnroll, ENT>(w, r.c, a); });
         st = exchange_parts<ENT>(a, xs, p.rows.C, r.rank, r.c);
     }
     if (threadIdx.x == 0) sc = token_scalars<ENT, MODE>(p, r.row, r.rank, r.T, r.T_ok, in, st);

@@ -6,9 +6,10 @@
 //
 // One sweep of the slice yields the statistics of the row's softmax and, as a by-product, the maximum of
 // every group of entries that one thread held in registers together (64 of them; at most kTopRounds groups
-// per thread).  The k-th largest of the group maxima is a threshold: at least k entries reach it.  For rows in
-// no particular order few others do (of G groups about G ln(G / (G - k)) entries: 133 for k = 128 and
-// 2048 groups), so only the groups that reach it are fetched again, and their entries are candidates.
+// per thread).  Of these maxima, folded to kTopBest per thread, the k-th largest is a threshold: at least k
+// entries reach it.  For rows in no particular order few others do (of G folded groups about G ln(G / (G - k))
+// entries: 137 for k = 128 and G = 1024, 177 had each thread one), so only the groups that reach it are
+// fetched again, and their entries are candidates.
 //   * thresholds and group maxima are compared by the upper 16 bits of their ordered pattern, which is
 //     exact for bf16 and a threshold a little lower for the others; the k-th largest is found two bits at a time by
 //     counting;
@@ -29,6 +30,7 @@ typedef unsigned long long top_key;
 constexpr int kTopBuf = 2048;                // candidates a CTA holds: 128 + 64 < 2048, so each offer takes one thread's at least
 constexpr int kTopRounds = 16;               // groups per thread: round r of the sweep counts to group r % kTopRounds
 constexpr int kTopGroups = 1024;             // groups fetched again
+constexpr int kTopBest = 4;                  // maxima per thread that the threshold is taken from
 
 struct TopParams {
     RowSpan rows;
@@ -227,21 +229,21 @@ __global__ void __launch_bounds__(kLThreads) ears_top_kernel(const TopParams p) 
     stat_open(a);
     const uint64_t pol = l2_policy_evict_first();
     const int rounds = (s.n + kLRound - 1) / kLRound, groups = min(rounds, kTopRounds);
-    for (int round = 0; round < rounds; ++round) {
-        uint4 w[kLUnroll];
-        load_round(s, round * kLRound + tid, w, pol);   // beyond the slice: -inf
+    uint32_t best[kTopBest];   // the thread's group maxima, folded
+#pragma unroll
+    for (int i = 0; i < kTopBest; ++i) best[i] = 0u;
+    sweep_rounds(s, pol, [&](uint4 (&w)[kLUnroll], int round) {
         const float top = stat_fold<E, kLUnroll, false>(w, r.c, a);
+        const uint32_t prefix = top > -INFINITY ? order_bits(top) >> 16 : 0u;   // NaN: the row is unusable anyway
         uint16_t* g = &sm.group[round % kTopRounds][tid];
-        const uint16_t prefix = top > -INFINITY ? (uint16_t)(order_bits(top) >> 16) : (uint16_t)0;   // NaN: the row is unusable anyway
-        *g = round < kTopRounds ? prefix : max(*g, prefix);
-    }
-    uint32_t v[kTopRounds];
+        *g = (uint16_t)(round < kTopRounds ? prefix : max((uint32_t)*g, prefix));
 #pragma unroll
-    for (int i = 0; i < kTopRounds; ++i) v[i] = i < groups ? sm.group[i][tid] : 0u;   // the thread's own
-    const uint32_t t16 = kth_prefix(v, groups, k, sm);
-#pragma unroll
-    for (int i = 0; i < kTopRounds; ++i) {
-        if (v[i] >= t16) {
+        for (int i = 0; i < kTopBest; ++i)
+            if (round % kTopBest == i) best[i] = max(best[i], prefix);
+    });
+    const uint32_t t16 = kth_prefix(best, min(rounds, kTopBest), k, sm);
+    for (int i = 0; i < groups; ++i) {
+        if (sm.group[i][tid] >= t16) {   // the thread's own
             const int at = atomicAdd(&sm.groups, 1);
             if (at < kTopGroups) sm.reach[at] = (uint16_t)(i * kLThreads + tid);
         }
