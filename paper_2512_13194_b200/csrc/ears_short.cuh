@@ -205,29 +205,6 @@ constexpr int kShortTopBuf = 256;            // candidates per row; kMaxTop and 
 
 struct ShortTopSmem { alignas(16) top_key buf[kShortTopBuf]; int total; };
 
-// kth_prefix for one warp: the largest 16-bit t (from the bits given) that at least k of the warp's values reach.
-template <int PER>
-__device__ __forceinline__ uint32_t warp_kth(const uint32_t (&v)[PER], int per, int k) {
-    uint32_t t = 0;
-#pragma unroll 1
-    for (int s = 14; s >= 0; s -= 2) {
-        const uint32_t t1 = t | 1u << s, t2 = t | 2u << s, t3 = t | 3u << s;
-        uint32_t a = 0, b = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            if (i >= per) break;
-            a += (v[i] >= t1 ? 1u : 0u) + (v[i] >= t2 ? 1u << 16 : 0u);
-            b += v[i] >= t3 ? 1u : 0u;
-        }
-        a = __reduce_add_sync(0xffffffffu, a);
-        b = __reduce_add_sync(0xffffffffu, b);
-        if ((int)b >= k) t = t3;
-        else if ((int)(a >> 16) >= k) t = t2;
-        else if ((int)(a & 0xffffu) >= k) t = t1;
-    }
-    return max(t, kLowestPrefix);
-}
-
 template <typename E>
 __global__ void __launch_bounds__(ShortShape<32>::kThreads, ShortShape<32>::kCtas) ears_top_short_kernel(const TopParams p) {
     constexpr int N = Words<E>::N;

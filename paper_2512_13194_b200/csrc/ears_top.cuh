@@ -6,13 +6,13 @@
 //
 // One sweep of the slice yields the statistics of the row's softmax and, as a by-product, the maximum of
 // every group of entries that one thread held in registers together (64 of them; at most kTopRounds groups
-// per thread).  Of these maxima, folded to kTopBest per thread, the k-th largest is a threshold: at least k
+// per thread).  Of these maxima, folded to two per thread, the k-th largest is a threshold: at least k
 // entries reach it.  For rows in no particular order few others do (of G folded groups about G ln(G / (G - k))
-// entries: 137 for k = 128 and G = 1024, 177 had each thread one), so only the groups that reach it are
+// entries: 147 for k = 128 and G = 512, 177 had each thread one, 137 four), so only the groups that reach it are
 // fetched again, and their entries are candidates.
-//   * thresholds and group maxima are compared by the upper 16 bits of their ordered pattern, which is
-//     exact for bf16 and a threshold a little lower for the others; the k-th largest is found two bits at a time by
-//     counting;
+//   * the threshold is kept as the upper 16 bits of an ordered pattern, which is exact for bf16 and a little lower
+//     for the others; the k-th largest is found two bits at a time by counting, by one warp: what follows the
+//     sweep is bound by the number of instructions, since the CTAs of a launch reach it together;
 //   * the rank of a candidate is the number of larger keys: one comparison with every other, read from
 //     shared memory two to a load, without a barrier;
 //   * when too many entries reach the threshold (rows with most entries equal), they are offered to the buffer
@@ -30,7 +30,7 @@ typedef unsigned long long top_key;
 constexpr int kTopBuf = 2048;                // candidates a CTA holds: 128 + 64 < 2048, so each offer takes one thread's at least
 constexpr int kTopRounds = 16;               // groups per thread: round r of the sweep counts to group r % kTopRounds
 constexpr int kTopGroups = 1024;             // groups fetched again
-constexpr int kTopBest = 4;                  // maxima per thread that the threshold is taken from
+constexpr int kTopBatch = 10;                // groups fetched at a time by a warp
 
 struct TopParams {
     RowSpan rows;
@@ -47,14 +47,16 @@ struct TopSmem {
     alignas(16) top_key buf[kTopBuf];
     union {
         top_key list[kLMaxCluster][kMaxTop];          // sorted lists of the cluster's CTAs
-        uint16_t group[kTopRounds][kLThreads];        // before them: 16-bit prefixes of the group maxima
+        float group[kTopRounds][kLThreads];           // before them: the group maxima
     };
+    float best[2 * kLThreads];
     int count[kLMaxCluster];
     uint16_t reach[kTopGroups];              // groups that reach the threshold
     uint2 tally[2][kLWarps];
     int total;                               // places of buf given out
     int groups;                              // places of reach given out
     int overflow[2];                         // alternating by offer
+    uint32_t t16;
 };
 
 // larger float -> larger integer; -0 and 0 are one value
@@ -69,8 +71,57 @@ __device__ __forceinline__ top_key make_key(float x, int col) { return ((top_key
 
 constexpr uint32_t kLowestPrefix = 0x0080u;   // of the lowest finite value; -inf lies below it
 
-// The largest 16-bit t >= kLowestPrefix that at least k of the threads' values v reach (kLowestPrefix if fewer do).
-// All threads; values below kLowestPrefix stand for nothing.
+// The largest 16-bit t >= kLowestPrefix that at least k of one warp's values v reach (kLowestPrefix if fewer do); values
+// below kLowestPrefix stand for nothing.
+template <int PER>
+__device__ __forceinline__ uint32_t warp_kth(const uint32_t (&v)[PER], int per, int k) {
+    // the leading bits that the largest and the smallest share are the threshold's as well
+    uint32_t hi = 0, lo = 0xffffu;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (i >= per) break;
+        hi = max(hi, v[i]);
+        lo = min(lo, v[i]);
+    }
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    if (hi == lo || per * 32 < k) return max(lo, kLowestPrefix);
+    const int top = (31 - __clz(hi ^ lo)) & ~1;   // of the two bits tried first
+    uint32_t t = hi >> (top + 2) << (top + 2);
+#pragma unroll 1
+    for (int s = top; s >= 0; s -= 2) {
+        const uint32_t t1 = t | 1u << s, t2 = t | 2u << s, t3 = t | 3u << s;
+        uint32_t a = 0, b = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (i >= per) break;
+            a += (v[i] >= t1 ? 1u : 0u) + (v[i] >= t2 ? 1u << 16 : 0u);
+            b += v[i] >= t3 ? 1u : 0u;
+        }
+        a = __reduce_add_sync(0xffffffffu, a);
+        b = __reduce_add_sync(0xffffffffu, b);
+        if ((int)b >= k) t = t3;
+        else if ((int)(a >> 16) >= k) t = t2;
+        else if ((int)(a & 0xffffu) >= k) t = t1;
+    }
+    return max(t, kLowestPrefix);
+}
+
+// Places for n entries of every lane, one atomic for the warp.  -> the lane's first place.
+__device__ __forceinline__ int warp_reserve(int n, int* counter) {
+    const int lane = threadIdx.x & 31;
+    int sum = n;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, sum, off);
+        if (lane >= off) sum += o;
+    }
+    int base = 0;
+    if (lane == 31 && sum > 0) base = atomicAdd(counter, sum);
+    return __shfl_sync(0xffffffffu, base, 31) + sum - n;
+}
+
+// warp_kth over the values of all threads of the CTA.
 template <int PER>
 __device__ __forceinline__ uint32_t kth_prefix(const uint32_t (&v)[PER], int per, int k, TopSmem& sm) {
     uint32_t t = 0;
@@ -149,15 +200,39 @@ __device__ __forceinline__ int compact_candidates(TopSmem& sm, int n, int k) {
     return min(n, k);
 }
 
-// Calls f(value, column) for every finite entry of vector i of the slice whose prefix is at least t16.
-template <typename E, class F>
-__device__ __forceinline__ void each_candidate(const Slice<E>& s, int i, uint32_t t16, F f) {
-    constexpr int N = Words<E>::N;
+// One 32-bit word of the row's vector run: entry e and what shares its word, -inf beyond the row.
+template <typename E> constexpr int kTopWord = 4 / (int)sizeof(E);   // entries in it
+template <typename E>
+__device__ __forceinline__ uint32_t load_word(const Slice<E>& s, int e) {
+    constexpr int W = kTopWord<E>;
+    if (e >= s.lead && e + W <= s.end) return *reinterpret_cast<const uint32_t*>(s.base + e);
+    uint32_t w = Words<E>::minus_inf().x;
+    if (W == 2) {
+        if (e >= s.lead && e < s.end) put_half(w, 0, raw_bits(s.base + e));
+        if (e + 1 >= s.lead && e + 1 < s.end) put_half(w, 1, raw_bits(s.base + e + 1));
+    }
+    return w;
+}
+__device__ __forceinline__ void unpack_word(uint32_t w, float (&x)[1], float) { x[0] = __uint_as_float(w); }
+__device__ __forceinline__ void unpack_word(uint32_t w, float (&x)[2], uint16_t) { x[0] = __uint_as_float(w << 16); x[1] = __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ void unpack_word(uint32_t w, float (&x)[2], f16_t) { const float2 v = f16x2_to_float2(w); x[0] = v.x; x[1] = v.y; }
+
+template <typename E>
+__device__ __forceinline__ uint4 slice_vector(const Slice<E>& s, int i) {
     const int v = s.v0 + i;
-    const uint4 w = s.whole(v) ? ld_row16(reinterpret_cast<const uint4*>(s.base) + v) : load_partial(s.base, v, s.lead, s.end);
+    return s.whole(v) ? ld_row16(reinterpret_cast<const uint4*>(s.base) + v) : load_partial(s.base, v, s.lead, s.end);
+}
+
+// Calls f(value, column) for every finite entry of w, vector i of the slice, whose prefix is at least t16.
+template <typename E, class F>
+__device__ __forceinline__ void each_candidate(const Slice<E>& s, uint4 w, int i, uint32_t t16, F f) {
+    constexpr int N = Words<E>::N;
+    const uint4 one[1] = {w};
+    const float top = Words<E>::template vmax_all<1>(one);
+    if ((order_bits(top) >> 16) < t16) return;   // false for NaN: the row is unusable anyway
     float x[N];
     Words<E>::unpack(w, x);
-    const int col = v * N - s.lead;
+    const int col = (s.v0 + i) * N - s.lead;
 #pragma unroll
     for (int j = 0; j < N; ++j)
         if ((order_bits(x[j]) >> 16) >= t16) f(x[j], col + j);
@@ -180,12 +255,12 @@ __device__ __noinline__ void offer_rounds(const Slice<E>& s, TopSmem& sm, int ro
             if (pending) {
                 int n = 0;
                 for (int i = i0; i < s.n && i < i0 + kLRound; i += kLThreads)
-                    each_candidate(s, i, t16, [&](float x, int col) { n += make_key(x, col) >= threshold; });
+                    each_candidate(s, slice_vector(s, i), i, t16, [&](float x, int col) { n += make_key(x, col) >= threshold; });
                 const int at = n ? atomicAdd(&sm.total, n) : 0;
                 if (at + n <= kTopBuf) {
                     int o = at;
                     for (int i = i0; i < s.n && i < i0 + kLRound; i += kLThreads)
-                        each_candidate(s, i, t16, [&](float x, int col) {
+                        each_candidate(s, slice_vector(s, i), i, t16, [&](float x, int col) {
                             const top_key key = make_key(x, col);
                             if (key >= threshold) sm.buf[o++] = key;
                         });
@@ -209,7 +284,7 @@ __device__ __noinline__ void offer_rounds(const Slice<E>& s, TopSmem& sm, int ro
 }
 
 template <typename E>
-__global__ void __launch_bounds__(kLThreads) ears_top_kernel(const TopParams p) {
+__global__ void __launch_bounds__(kLThreads, 4) ears_top_kernel(const TopParams p) {
     __shared__ TopSmem sm;
     const int tid = threadIdx.x, k = p.k;
     const RowSetup r = row_setup(p.rows);
@@ -227,40 +302,73 @@ __global__ void __launch_bounds__(kLThreads) ears_top_kernel(const TopParams p) 
     if (tid == 0) { sm.total = sm.groups = 0; sm.overflow[0] = sm.overflow[1] = 0; }
     Stat<false> a;
     stat_open(a);
-    const uint64_t pol = l2_policy_evict_first();
+    const uint64_t pol = l2_policy_normal();   // some of it is fetched again
     const int rounds = (s.n + kLRound - 1) / kLRound, groups = min(rounds, kTopRounds);
-    uint32_t best[kTopBest];   // the thread's group maxima, folded
-#pragma unroll
-    for (int i = 0; i < kTopBest; ++i) best[i] = 0u;
+    float best[2] = {-INFINITY, -INFINITY};   // the thread's group maxima, folded to those of even and of odd rounds
     sweep_rounds(s, pol, [&](uint4 (&w)[kLUnroll], int round) {
         const float top = stat_fold<E, kLUnroll, false>(w, r.c, a);
-        const uint32_t prefix = top > -INFINITY ? order_bits(top) >> 16 : 0u;   // NaN: the row is unusable anyway
-        uint16_t* g = &sm.group[round % kTopRounds][tid];
-        *g = (uint16_t)(round < kTopRounds ? prefix : max((uint32_t)*g, prefix));
-#pragma unroll
-        for (int i = 0; i < kTopBest; ++i)
-            if (round % kTopBest == i) best[i] = max(best[i], prefix);
+        float* g = &sm.group[round % kTopRounds][tid];
+        *g = round < kTopRounds ? top : fmaxf(*g, top);
+        best[round & 1] = fmaxf(best[round & 1], top);
     });
-    const uint32_t t16 = kth_prefix(best, min(rounds, kTopBest), k, sm);
-    for (int i = 0; i < groups; ++i) {
-        if (sm.group[i][tid] >= t16) {   // the thread's own
-            const int at = atomicAdd(&sm.groups, 1);
-            if (at < kTopGroups) sm.reach[at] = (uint16_t)(i * kLThreads + tid);
-        }
+    sm.best[tid] = best[0];
+    sm.best[kLThreads + tid] = best[1];
+    __syncthreads();
+    if (tid < 32) {
+        uint32_t v[2 * kLWarps];
+#pragma unroll
+        for (int i = 0; i < 2 * kLWarps; ++i) v[i] = order_bits(sm.best[tid + 32 * i]) >> 16;
+        const uint32_t t = warp_kth(v, rounds > 1 ? 2 * kLWarps : kLWarps, k);
+        if (tid == 0) sm.t16 = t;
     }
+    __syncthreads();
+    const uint32_t t16 = sm.t16;
+    const float reach = unorder_bits(t16 << 16);
+    // the thread's own groups; false for NaN: the row is unusable anyway
+    int mine = 0;
+    for (int i = 0; i < groups; ++i) mine += sm.group[i][tid] >= reach ? 1 : 0;
+    int place = warp_reserve(mine, &sm.groups);
+    if (mine > 0 && place + mine <= kTopGroups)
+        for (int i = 0; i < groups; ++i)
+            if (sm.group[i][tid] >= reach) sm.reach[place++] = (uint16_t)(i * kLThreads + tid);
     __syncthreads();
     const int reached = sm.groups;
     if (reached <= kTopGroups) {
-        // eight threads to a group, one vector each
-        for (int q = tid / kLUnroll; q < reached; q += kLThreads / kLUnroll) {
-            const int g = sm.reach[q];
-            for (int round = g / kLThreads; round < rounds; round += kTopRounds) {
-                const int i = round * kLRound + (tid % kLUnroll) * kLThreads + g % kLThreads;
-                if (i < s.n)
-                    each_candidate(s, i, t16, [&](float x, int col) {
-                        const int at = atomicAdd(&sm.total, 1);
-                        if (at < kTopBuf) sm.buf[at] = make_key(x, col);
-                    });
+        // a warp to a group, 32 lanes to its eight vectors, kTopBatch groups in flight
+        for (int q0 = tid / 32; q0 < reached; q0 += kTopBatch * kLWarps) {
+            for (int turn = 0; turn < rounds; turn += kTopRounds) {   // once, unless a slice has more rounds than groups
+                uint32_t w[kTopBatch];
+                const auto entry = [&](int j) {   // of the run: vector, word lane % 4
+                    const int q = q0 + j * kLWarps, lane = tid & 31, g = q < reached ? sm.reach[q] : 0;
+                    return ((s.v0 + (turn + g / kLThreads) * kLRound + (lane / 4) * kLThreads + g % kLThreads) * 4 + lane % 4) * kTopWord<E>;
+                };
+#pragma unroll
+                for (int j = 0; j < kTopBatch; ++j) {
+                    w[j] = Words<E>::minus_inf().x;
+                    if (q0 + j * kLWarps < reached) {
+                        const int e = entry(j);
+                        if (e < (s.v0 + s.n) * Words<E>::N) w[j] = load_word(s, e);
+                    }
+                }
+                int hits = 0;
+#pragma unroll
+                for (int j = 0; j < kTopBatch; ++j) {
+                    float x[kTopWord<E>];
+                    unpack_word(w[j], x, E{});
+#pragma unroll
+                    for (int i = 0; i < kTopWord<E>; ++i) hits += x[i] >= reach ? 1 : 0;
+                }
+                int at = warp_reserve(hits, &sm.total);
+                if (hits > 0 && at + hits <= kTopBuf) {
+#pragma unroll
+                    for (int j = 0; j < kTopBatch; ++j) {
+                        float x[kTopWord<E>];
+                        unpack_word(w[j], x, E{});
+#pragma unroll
+                        for (int i = 0; i < kTopWord<E>; ++i)
+                            if (x[i] >= reach) sm.buf[at++] = make_key(x[i], entry(j) + i - s.lead);
+                    }
+                }
             }
         }
     }
