@@ -7,7 +7,11 @@
 #include <cmath>
 #include <cstdint>
 #include <cstdlib>
+#include <initializer_list>
+#include <map>
+#include <mutex>
 #include <type_traits>
+#include <utility>
 
 #include "ears_host.h"
 #include "ears_distill.cuh"
@@ -67,21 +71,21 @@ int check_grad(const RowCall& c, const void* grad, int64_t gsb, int64_t gsr) {
     return EARS_OK;
 }
 
-// CTAs per row.  Few rows are split until their CTAs cover half the SMs (slices of 16 KB and more), or one and a half per
+// CTAs per row.  Few rows are split until their CTAs cover half the SMs (slices of min_slice and more), or one and a half per
 // SM where the slices stay above 64 KB; a call that fetches a slice twice splits rows so long that the ones in flight (two
 // CTAs per SM) would not stay in L2.  More CTAs per row than that cost: the CTAs of a cluster start and end together
 // (scoring 256 rows of 256 KB takes 18 us with one, 20 with two, 31 with eight; 64 rows 10, 7.2, 6.4 with four, 9.5).
-int choose_cluster(long long rows, size_t row_bytes, bool twice, int sms) {
+int choose_cluster(long long rows, size_t row_bytes, bool twice, size_t min_slice, int sms) {
     const int forced = g_row_cluster.load(std::memory_order_relaxed);
     if (forced) return forced;
     int C = 1;
-    while (C < 8 && ((rows * C * 2 <= sms && row_bytes / C > (16u << 10)) || (rows * C <= sms && row_bytes / C > (64u << 10)))) C *= 2;
+    while (C < 8 && ((rows * C * 2 <= sms && row_bytes / C > min_slice) || (rows * C <= sms && row_bytes / C > (64u << 10)))) C *= 2;
     if (twice)
         while (C < 8 && (size_t)(2 * sms / C) * row_bytes > (100u << 20)) C *= 2;
     return C;
 }
 
-int make_span(const RowCall& c, bool twice, RowSpan* out) {
+int make_span(const RowCall& c, bool twice, RowSpan* out, size_t min_slice = 16u << 10) {
     int sms = 0;
     const int rc = host_device_sms(&sms);
     if (rc) return rc;
@@ -89,13 +93,35 @@ int make_span(const RowCall& c, bool twice, RowSpan* out) {
     s.x = c.x; s.stride_b = c.sb; s.stride_r = c.sr;
     s.rows = (long long)c.B * c.R;
     s.R = c.R; s.V = c.V; s.T = c.T; s.seq_T = c.seq_T;
-    s.C = choose_cluster(s.rows, (size_t)c.V * esize_of(c.dtype), twice, sms);
+    s.C = choose_cluster(s.rows, (size_t)c.V * esize_of(c.dtype), twice, min_slice, sms);
     const int n = 16 / esize_of(c.dtype);
     s.vectors = (int)(((long long)c.V + 2 * n - 2) / n);
     const int per = (s.vectors + s.C - 1) / s.C;
     s.slice = (per + kSliceAlign - 1) / kSliceAlign * kSliceAlign;
     *out = s;
     return EARS_OK;
+}
+
+// Opts a kernel in to shared memory above 48 KB and to clusters of 16, once per kernel and device.
+cudaError_t allow_launch(const void* kernel, size_t smem, int C) {
+    static std::mutex mutex;
+    static std::map<std::pair<const void*, int>, std::pair<size_t, bool>> allowed;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    std::lock_guard<std::mutex> lock(mutex);
+    auto& have = allowed[{kernel, dev}];
+    if (smem > 48 * 1024 && smem > have.first) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        have.first = smem;
+    }
+    if (C > 8 && !have.second) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+        have.second = true;
+    }
+    return cudaSuccess;
 }
 
 template <typename P, typename... Extra>
@@ -113,12 +139,8 @@ int launch_rows(void (*kernel)(P, Extra...), const P& p, int threads, size_t sme
         cfg.attrs = attr;
         cfg.numAttrs = 1;
     }
-    if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return host_cuda_fail(e, what);
-    }
-    if (r.C > 8) {
-        const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (smem > 48 * 1024 || r.C > 8) {
+        const cudaError_t e = allow_launch((const void*)kernel, smem, r.C);
         if (e != cudaSuccess) return host_cuda_fail(e, what);
     }
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p, extra...);
@@ -283,7 +305,7 @@ int ears_top_logits(int dtype, const void* logits, int B, int R, int V, int64_t 
     EARS_TRY(check_rows(c));
     if (k < 1 || k > EARS_MAX_TOP) return EARS_ERR_SHAPE;
     TopParams p{};
-    EARS_TRY(make_span(c, false, &p.rows));
+    EARS_TRY(make_span(c, false, &p.rows, 64u << 10));   // every CTA has a list of its own to sort
     p.k = k; p.accept_len = accept_len;
     p.out_values = out_values; p.out_ids = out_ids; p.out_lse = out_lse; p.status = status;
     if (short_threads(p.rows) == 32)

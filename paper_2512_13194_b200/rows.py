@@ -16,7 +16,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import binding
-from .binding import EarsError, _check, _stream_ptr, load_library
+from .binding import _check, load_library
 
 MAX_TOP = 128
 DISTILL_KINDS = {"forward_kl": 0, "reverse_kl": 1, "jsd": 2}
@@ -37,49 +37,59 @@ class PolicyTerms(NamedTuple):
 
 
 class _Rows:
-    """The common head of a call: dtype, pointer, sizes, strides, temperature."""
+    """The common head of a call: dtype, pointer, sizes, strides, temperature.  Small calls are bound by the host, so
+    nothing is converted, viewed or looked up that is as it should be already."""
+
+    __slots__ = ("logits", "lead", "device", "index", "B", "R", "V", "seq_T", "status", "args")
 
     def __init__(self, logits: torch.Tensor, temperature, seq_temperature, status):
-        if logits.dtype not in _DTYPES:
+        code = _DTYPES.get(logits.dtype)
+        if code is None:
             raise TypeError(f"logits must be float32, bfloat16 or float16, got {logits.dtype}")
-        if logits.dim() not in (2, 3):
+        shape = logits.shape
+        if len(shape) not in (2, 3):
             raise ValueError("expected logits [B,R,V] or [R,V]")
         if not logits.is_cuda:
             raise ValueError("logits must be a CUDA tensor")
-        if 0 in logits.shape:
+        if 0 in shape:
             raise ValueError("logits must not be empty")
-        if logits.shape[-1] > 1 and logits.stride(-1) != 1 or min(logits.stride()) < 0:
+        strides = logits.stride()
+        if strides[-1] != 1 and shape[-1] > 1 or min(strides) < 0:
             logits = logits.contiguous()
-        self.logits, self.lead = logits, tuple(logits.shape[:-1])
-        self.device = logits.device
-        if logits.dim() == 3:
-            (self.B, self.R, self.V), (sb, sr, _) = logits.shape, logits.stride()
+            strides = logits.stride()
+        self.logits, self.lead, self.device = logits, shape[:-1], logits.device
+        self.index = self.device.index
+        self.V = shape[-1]
+        if len(shape) == 3:
+            self.B, self.R = shape[0], shape[1]
+            sb, sr = strides[0], strides[1]
         else:
-            (self.R, self.V), (sr, _) = logits.shape, logits.stride()
-            self.B, sb = 1, 0
-        self.T = float(temperature)
-        self.seq_T = self.per(seq_temperature, torch.float32, (self.B,), "seq_temperature")
+            self.B, self.R = 1, shape[0]
+            sb, sr = 0, strides[0]
+        self.seq_T = None if seq_temperature is None else self.per(seq_temperature, torch.float32, (self.B,), "seq_temperature")
         if status is not None and (status.device != self.device or status.dtype != torch.int32 or status.numel() != 1):
             raise ValueError("status must be an int32 CUDA tensor of one element on the logits' device")
         self.status = status
-        self.args = (_DTYPES[logits.dtype], logits.data_ptr(), self.B, self.R, self.V, sb, sr, self.T, _ptr(self.seq_T))
+        self.args = (code, logits.data_ptr(), self.B, self.R, self.V, sb, sr, float(temperature), _ptr(self.seq_T))
 
-    def per(self, t, dtype, shape, name, extra=()):
+    def per(self, t, dtype, shape, name):
         if t is None:
             return None
         if t.device != self.device:
             raise ValueError(f"{name} must live on the logits' device")
-        if tuple(t.shape) != tuple(shape) + tuple(extra):
-            raise ValueError(f"{name} must have shape {list(shape) + list(extra)}, got {list(t.shape)}")
-        if dtype == torch.int32 and (t.dtype.is_floating_point or t.dtype == torch.bool):
-            raise TypeError(f"{name} must hold integers")
-        return t.detach().to(dtype).contiguous()
+        if t.shape != shape:
+            raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
+        if t.dtype is not dtype:
+            if dtype is torch.int32 and (t.dtype.is_floating_point or t.dtype is torch.bool):
+                raise TypeError(f"{name} must hold integers")
+            t = t.detach().to(dtype)
+        return t if t.is_contiguous() else t.contiguous()
 
     def row(self, t, name, dtype=torch.float32):
-        return self.per(t, dtype, self.lead, name)
+        return None if t is None else self.per(t, dtype, self.lead, name)
 
     def out(self, extra=(), dtype=torch.float32):
-        return torch.empty(self.lead + tuple(extra), dtype=dtype, device=self.device)
+        return torch.empty(self.lead + extra, dtype=dtype, device=self.device)
 
     def grad(self, out_grad):
         if out_grad is None:
@@ -93,11 +103,24 @@ class _Rows:
 
     def call(self, fn, *tail, stream=None):
         """fn(*head, *tail, status, stream) with the logits' device current."""
-        if torch.cuda.current_device() == self.device.index:
-            _check(fn(*self.args, *tail, _ptr(self.status), _stream_ptr(stream)))
+        if _current_device() == self.index:
+            rc = fn(*self.args, *tail, _ptr(self.status), self.stream(stream))
         else:
             with torch.cuda.device(self.device):
-                _check(fn(*self.args, *tail, _ptr(self.status), _stream_ptr(stream)))
+                rc = fn(*self.args, *tail, _ptr(self.status), self.stream(stream))
+        if rc:
+            _check(rc)
+
+    def stream(self, stream):
+        return _raw_stream(self.index) if stream is None else stream.cuda_stream
+
+
+def _current_device() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _raw_stream(index: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _ptr(t):
@@ -272,8 +295,8 @@ def _distill_inputs(rows, teacher, kind, mix):
     k = int(ids.shape[-1]) if ids.dim() else 0
     if not 1 <= k <= MAX_TOP:
         raise ValueError(f"the teacher's lists must have 1..{MAX_TOP} entries")
-    held = (rows.per(values, torch.float32, rows.lead, "teacher values", (k,)),
-            rows.per(ids, torch.int32, rows.lead, "teacher ids", (k,)), rows.row(lse, "teacher lse"))
+    held = (rows.per(values, torch.float32, rows.lead + (k,), "teacher values"),
+            rows.per(ids, torch.int32, rows.lead + (k,), "teacher ids"), rows.row(lse, "teacher lse"))
     return held, (k,) + tuple(_ptr(t) for t in held) + (DISTILL_KINDS[kind], float(mix))
 
 
