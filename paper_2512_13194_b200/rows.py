@@ -88,12 +88,19 @@ class _Rows:
     def row(self, t, name, dtype=torch.float32):
         return None if t is None else self.per(t, dtype, self.lead, name)
 
-    def out(self, extra=(), dtype=torch.float32):
-        return torch.empty(self.lead + extra, dtype=dtype, device=self.device)
+    def out(self, like=None):
+        """A float32 output per row; ``like``, an input of that kind, spares torch the parsing of shape and type."""
+        return torch.empty(self.lead, dtype=torch.float32, device=self.device) if like is None else torch.empty_like(like)
+
+    def saved(self):
+        return torch.empty(self.lead + (4,), dtype=torch.float32, device=self.device)
 
     def grad(self, out_grad):
         if out_grad is None:
-            out_grad = torch.empty(self.logits.shape, dtype=self.logits.dtype, device=self.device)
+            if self.logits.is_contiguous():
+                out_grad = torch.empty_like(self.logits)
+            else:
+                out_grad = torch.empty(self.logits.shape, dtype=self.logits.dtype, device=self.device)
         elif out_grad.shape != self.logits.shape or out_grad.dtype != self.logits.dtype or out_grad.device != self.device:
             raise ValueError("out_grad must have the logits' shape, type and device")
         elif out_grad.shape[-1] > 1 and out_grad.stride(-1) != 1:
@@ -151,7 +158,8 @@ def top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0, *, accept
     k = int(k)
     if not 1 <= k <= MAX_TOP:
         raise ValueError(f"k must lie in 1..{MAX_TOP}")
-    values, ids, lse = rows.out((k,)), rows.out((k,), torch.int32), rows.out()
+    values = torch.empty(rows.lead + (k,), dtype=torch.float32, device=rows.device)
+    ids, lse = torch.empty_like(values, dtype=torch.int32), rows.out()
     rows.call(load_library().ears_top_logits, _ptr(acc), k, values.data_ptr(), ids.data_ptr(), lse.data_ptr(), stream=stream)
     return TopLogits(values, ids, lse)
 
@@ -159,7 +167,8 @@ def top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0, *, accept
 # ---- token log probabilities --------------------------------------------------------------------
 
 def _token_forward(rows, tokens, entropy, saved, stream):
-    logp, H = rows.out(), rows.out() if entropy else None
+    logp = rows.out()
+    H = rows.out(logp) if entropy else None
     rows.call(load_library().ears_token_logprobs, tokens.data_ptr(), logp.data_ptr(), _ptr(H), _ptr(saved), stream=stream)
     return logp, H
 
@@ -169,7 +178,7 @@ class _TokenLogprobs(torch.autograd.Function):
     def forward(ctx, logits, tokens, temperature, seq_temperature, entropy, status, stream):
         _refuse_capture()
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
-        saved = rows.out((4,))
+        saved = rows.saved()
         ctx.rows, ctx.tokens, ctx.saved = rows, rows.row(tokens, "tokens", torch.int32), saved
         ctx.save_for_backward(logits)          # notices a change of the logits before the backward pass
         logp, H = _token_forward(rows, ctx.tokens, entropy, saved, stream)
@@ -206,9 +215,9 @@ def token_logprobs_step(logits: torch.Tensor, tokens: torch.Tensor, d_logp: torc
                         seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
     """(logp, entropy or None, gradient) for upstream gradients known beforehand (ears_token_logprobs_step):
     ``d_logp`` and, optionally, ``d_entropy`` per row.  ``out_grad=logits`` writes the gradient over them."""
-    rows = _Rows(logits.detach(), temperature, seq_temperature, status)
+    rows = _Rows(logits, temperature, seq_temperature, status)
     tok, dl, dh = rows.row(tokens, "tokens", torch.int32), rows.row(d_logp, "d_logp"), rows.row(d_entropy, "d_entropy")
-    logp, H = rows.out(), rows.out() if dh is not None else None
+    logp, H = rows.out(dl), rows.out(dl) if dh is not None else None
     g, place = rows.grad(out_grad)
     rows.call(load_library().ears_token_logprobs_step, tok.data_ptr(), dl.data_ptr(), _ptr(dh), logp.data_ptr(), _ptr(H),
               *place, stream=stream)
@@ -223,8 +232,9 @@ def _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, clip_low, clip_h
     return held, tuple(_ptr(t) for t in held) + (float(clip_low), float(clip_high), float(kl_coef), float(entropy_coef))
 
 
-def _policy_outputs(rows, ref, entropy):
-    return PolicyTerms(rows.out(), rows.out(), rows.out() if ref is not None else None, rows.out() if entropy else None)
+def _policy_outputs(rows, held, entropy):
+    _, old, ref, _ = held
+    return PolicyTerms(rows.out(old), rows.out(old), rows.out(old) if ref is not None else None, rows.out(old) if entropy else None)
 
 
 class _PolicyLoss(torch.autograd.Function):
@@ -233,9 +243,9 @@ class _PolicyLoss(torch.autograd.Function):
         _refuse_capture()
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
         ctx.held, ctx.args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, *coefs)
-        ctx.rows, ctx.saved = rows, rows.out((4,))
+        ctx.rows, ctx.saved = rows, rows.saved()
         ctx.save_for_backward(logits)
-        t = _policy_outputs(rows, ref_logp, entropy)
+        t = _policy_outputs(rows, ctx.held, entropy)
         rows.call(load_library().ears_policy_loss, *ctx.args, *(_ptr(o) for o in t), ctx.saved.data_ptr(), stream=stream)
         ctx.mark_non_differentiable(*(o for o in t[1:] if o is not None))
         return tuple(t)
@@ -266,7 +276,7 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
                                               with_entropy, status, stream))
     rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, *coefs)
-    t = _policy_outputs(rows, ref_logp, with_entropy)
+    t = _policy_outputs(rows, held, with_entropy)
     rows.call(load_library().ears_policy_loss, *args, *(_ptr(o) for o in t), None, stream=stream)
     return t
 
@@ -277,10 +287,10 @@ def policy_step(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
                 row_weight: Optional[torch.Tensor] = None, out_grad: Optional[torch.Tensor] = None,
                 seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
     """(PolicyTerms, gradient of sum row_weight * loss) in one call (ears_policy_step)."""
-    rows = _Rows(logits.detach(), temperature, seq_temperature, status)
+    rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, clip_low, clip_high, kl_coef, entropy_coef)
     w = rows.row(row_weight, "row_weight")
-    t = _policy_outputs(rows, ref_logp, bool(entropy) or entropy_coef != 0.0)
+    t = _policy_outputs(rows, held, bool(entropy) or entropy_coef != 0.0)
     g, place = rows.grad(out_grad)
     rows.call(load_library().ears_policy_step, *args, _ptr(w), *(_ptr(o) for o in t), *place, stream=stream)
     return t, g
@@ -306,9 +316,9 @@ class _DistillLoss(torch.autograd.Function):
         _refuse_capture()
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
         ctx.held, ctx.args = _distill_inputs(rows, teacher, kind, mix)
-        ctx.rows, ctx.saved = rows, rows.out((4,))
+        ctx.rows, ctx.saved = rows, rows.saved()
         ctx.save_for_backward(logits)
-        loss = rows.out()
+        loss = rows.out(ctx.held[2])
         rows.call(load_library().ears_distill_loss, *ctx.args, loss.data_ptr(), ctx.saved.data_ptr(), stream=stream)
         return loss
 
@@ -335,7 +345,7 @@ def distill_loss(logits: torch.Tensor, teacher: TopLogits, temperature: float = 
         return _DistillLoss.apply(logits, teacher, temperature, kind, mix, seq_temperature, status, stream)
     rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _distill_inputs(rows, teacher, kind, mix)
-    loss = rows.out()
+    loss = rows.out(held[2])
     rows.call(load_library().ears_distill_loss, *args, loss.data_ptr(), None, stream=stream)
     return loss
 
@@ -344,10 +354,10 @@ def distill_step(logits: torch.Tensor, teacher: TopLogits, temperature: float = 
                  mix: float = 0.5, row_weight: Optional[torch.Tensor] = None, out_grad: Optional[torch.Tensor] = None,
                  seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
     """(loss per row, gradient of sum row_weight * loss) in one call (ears_distill_step)."""
-    rows = _Rows(logits.detach(), temperature, seq_temperature, status)
+    rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _distill_inputs(rows, teacher, kind, mix)
     w = rows.row(row_weight, "row_weight")
-    loss = rows.out()
+    loss = rows.out(w)
     g, place = rows.grad(out_grad)
     rows.call(load_library().ears_distill_step, *args, _ptr(w), loss.data_ptr(), *place, stream=stream)
     return loss, g
