@@ -40,16 +40,11 @@ struct DistillParams {
     int32_t* status;
 };
 
-constexpr int kListSlots = 256;
-
 struct ListSmem {
     alignas(16) int col[kMaxTop];   // listed ids, -1: absent
-    int vec[kMaxTop];            // vector that holds the listed entry, -1: absent
     float x[kMaxTop];            // draft logit of the listed entry
     float t[kMaxTop];            // teacher logit
     float entry[kMaxTop];        // gradient of the listed entry
-    int head[kListSlots];        // first of the listed entries whose vector falls into the slot, -1: none
-    int next[kMaxTop];
     float factor;
     int zero;
     int seen;                    // bit 0: an entry is present, bit 1: something is wrong
@@ -106,55 +101,103 @@ __device__ __forceinline__ TeacherPart teacher_part(const DistillParams& p, cons
     return t;
 }
 
-template <int MODE>
-__device__ __forceinline__ void distill_scalars(const DistillParams& p, ListSmem& sm, long long row, int rank, double invT, bool ok,
-                                                const TeacherPart& te, float weight, Part tail) {
+// The draft's listed entries, relative to their own maximum.
+struct DraftPart { double xm, lq[kTopPer], e[kTopPer], sum; };
+
+__device__ __forceinline__ DraftPart draft_part(const DistillParams& p, const ListSmem& sm, double invT) {
     const int lane = threadIdx.x & 31;
-    double lq[kTopPer], qr[kTopPer], gs[kTopPer];
-    double xm = (double)tail.m;
+    DraftPart d;
+    d.xm = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kTopPer; ++i)
-        if (listed(p, sm, i)) xm = fmax(xm, (double)sm.x[lane + 32 * i]);
-    const bool has_tail = tail.m > -INFINITY;
-    const double M = warp_max(xm);
-    // draft: Z relative to M
-    double zs = 0.0;
+        if (listed(p, sm, i)) d.xm = fmax(d.xm, (double)sm.x[lane + 32 * i]);
+    d.xm = warp_max(d.xm);
+    const double ref = d.xm > -INFINITY ? d.xm : 0.0;   // every listed entry masked: e = 0
+    d.sum = 0.0;
 #pragma unroll
     for (int i = 0; i < kTopPer; ++i) {
-        lq[i] = qr[i] = gs[i] = 0.0;
+        d.lq[i] = d.e[i] = 0.0;
         if (listed(p, sm, i)) {
-            lq[i] = ((double)sm.x[lane + 32 * i] - M) * invT;
-            qr[i] = exp(lq[i]);
-            zs += qr[i];
+            d.lq[i] = ((double)sm.x[lane + 32 * i] - ref) * invT;
+            d.e[i] = exp(d.lq[i]);
+            d.sum += d.e[i];
         }
     }
+    d.sum = warp_sum(d.sum);
+    return d;
+}
+
+// published() is called when the gradient's scalars stand in sm.
+template <int MODE, class F>
+__device__ __forceinline__ void distill_scalars(const DistillParams& p, ListSmem& sm, long long row, int rank, double invT, bool ok,
+                                                const TeacherPart& te, const DraftPart& dr, float weight, Part tail, F published) {
+    const int lane = threadIdx.x & 31;
+    double lq[kTopPer], qr[kTopPer], gs[kTopPer];
+    const bool has_tail = tail.m > -INFINITY;
+    const double M = fmax(dr.xm, (double)tail.m);
+    // Z relative to M
+    const double td = dr.xm > -INFINITY ? (dr.xm - M) * invT : 0.0, fd = exp(td);
     const double tt = has_tail ? ((double)tail.m - M) * invT : 0.0;
     const double zt = has_tail ? exp(tt) * (double)tail.s : 0.0;
-    const double Z = warp_sum(zs) + zt, lnZ = log(Z), invZ = 1.0 / Z;
+    const double Z = dr.sum * fd + zt, invZ = 1.0 / Z;
     const double rho = zt * invZ;
-    const double ln_rho = has_tail ? tt + log((double)tail.s) - lnZ : -INFINITY;
 #pragma unroll
     for (int i = 0; i < kTopPer; ++i) {
-        lq[i] -= lnZ;
-        qr[i] *= invZ;
+        qr[i] = dr.e[i] * (fd * invZ);
+        gs[i] = 0.0;
     }
     double rt = 0.0;
     if (p.lse) {
         rt = 1.0 - te.ps;
         if (rt < kTailFloor) rt = rho > 0.0 ? kTailFloor : 0.0;
     }
-    const double ln_rt = log(rt);
-    // loss; q (g - cbar) of every outcome.  Entries that are not listed have p = q = 0 and stay out of every sum.
-    const double a = p.mix;
-    double part = 0.0, loss, gt;
-    if (p.kind == kForwardKl) {
+    ok = ok && M > -INFINITY && M < INFINITY && isfinite(te.L);
+    const double w = (double)weight * invT;
+    double gt = 0.0;
+    // sm gets q (g - cbar) of the listed entries and the factor of the others
+    const auto publish = [&] {
+        if (MODE == kForward) return;
+        bool finite = true;
 #pragma unroll
         for (int i = 0; i < kTopPer; ++i) {
-            part += te.pr[i] > 0.0 ? te.pr[i] * (te.lp[i] - lq[i]) : 0.0;
-            gs[i] = qr[i] * (te.ps + rt) - te.pr[i];
+            if (listed(p, sm, i)) {
+                sm.entry[lane + 32 * i] = (float)(w * gs[i]);
+                finite = finite && isfinite(gs[i]);
+            }
         }
-        loss = warp_sum(part) + (rt > 0.0 ? rt * (ln_rt - ln_rho) : 0.0);
+        // relative to the tail's own maximum: nothing underflows before the product
+        const double f = has_tail ? gt / (double)tail.s : 0.0;
+        finite = __all_sync(0xffffffffu, finite) && isfinite(f);
+        ok = ok && finite;
+        if (lane == 0) {
+            sm.factor = (float)(w * f);
+            sm.zero = (!ok || w == 0.0) ? 1 : 0;
+        }
+        __syncwarp();
+        published();
+    };
+    if (p.kind == kForwardKl) {   // needs no logarithm for the gradient
+#pragma unroll
+        for (int i = 0; i < kTopPer; ++i) gs[i] = qr[i] * (te.ps + rt) - te.pr[i];
         gt = rho * (te.ps + rt) - rt;
+        publish();
+        if (MODE == kBackward) {
+            if (lane == 0 && rank == 0 && !ok && p.status) atomicOr(p.status, kDevInvalidInput);
+            return;
+        }
+    }
+    const double lnZ = log(Z);
+    const double ln_rho = has_tail ? tt + log((double)tail.s) - lnZ : -INFINITY;
+    const double ln_rt = log(rt);
+#pragma unroll
+    for (int i = 0; i < kTopPer; ++i) lq[i] = dr.lq[i] + td - lnZ;
+    // loss; q (g - cbar) of every outcome.  Entries that are not listed have p = q = 0 and stay out of every sum.
+    const double a = p.mix;
+    double part = 0.0, loss;
+    if (p.kind == kForwardKl) {
+#pragma unroll
+        for (int i = 0; i < kTopPer; ++i) part += te.pr[i] > 0.0 ? te.pr[i] * (te.lp[i] - lq[i]) : 0.0;
+        loss = warp_sum(part) + (rt > 0.0 ? rt * (ln_rt - ln_rho) : 0.0);
     } else if (p.kind == kReverseKl) {
 #pragma unroll
         for (int i = 0; i < kTopPer; ++i) {
@@ -185,26 +228,8 @@ __device__ __forceinline__ void distill_scalars(const DistillParams& p, ListSmem
         for (int i = 0; i < kTopPer; ++i) gs[i] = qr[i] * ((1.0 - a) * gs[i] - cq);
         gt = rho * ((1.0 - a) * kt - cq);
     }
-    ok = ok && M > -INFINITY && M < INFINITY && isfinite(te.L) && loss == loss;
-    if (MODE != kForward) {
-        const double w = (double)weight * invT;
-        bool finite = true;
-#pragma unroll
-        for (int i = 0; i < kTopPer; ++i) {
-            if (listed(p, sm, i)) {
-                sm.entry[lane + 32 * i] = (float)(w * gs[i]);
-                finite = finite && isfinite(gs[i]);
-            }
-        }
-        // relative to the tail's own maximum: nothing underflows before the product
-        const double f = has_tail ? gt / (double)tail.s : 0.0;
-        finite = __all_sync(0xffffffffu, finite) && isfinite(f);
-        ok = ok && finite;
-        if (lane == 0) {
-            sm.factor = (float)(w * f);
-            sm.zero = (!ok || w == 0.0) ? 1 : 0;
-        }
-    }
+    ok = ok && loss == loss;
+    if (p.kind != kForwardKl) publish();
     if (lane == 0 && rank == 0) {
         const float nan = __int_as_float(0x7fc00000);
         if (MODE != kBackward) p.out_loss[row] = ok ? (float)loss : nan;
@@ -220,11 +245,16 @@ __device__ __forceinline__ void row_sync() {
     else __syncthreads();
 }
 
-// The row's list, by the THREADS threads that share the row (tid among them): into sm, with a flag for every vector
-// among [base, base + count) that holds a listed entry -- byte (i / (PER SWEEP)) SWEEP + i % SWEEP, bit i / SWEEP % PER, for
-// vector base + i: what the thread that folds the vector, one of SWEEP, looks at.  -> sm.seen.
+// Of every vector the bits of its listed entries, one byte: byte q of word (i / (PER SWEEP)) SWEEP + i % SWEEP, q = i / SWEEP % PER,
+// for vector base + i -- what the thread that folds PER vectors a round, one of SWEEP, looks at in one load.
+template <int PER> struct ListWord;
+template <> struct ListWord<4> { typedef uint32_t type; };
+template <> struct ListWord<8> { typedef uint2 type; };
+
+// The row's list, by the THREADS threads that share the row (tid among them): into sm, and the bits of the vectors
+// among [base, base + count) into bits.  -> sm.seen.
 template <typename E, int PER, int SWEEP, int THREADS>
-__device__ __forceinline__ int distill_list(const DistillParams& p, ListSmem& sm, uint32_t* flags, int tid, long long row_index, const E* row,
+__device__ __forceinline__ int distill_list(const DistillParams& p, ListSmem& sm, uint32_t* bits, int tid, long long row_index, const E* row,
                                             int lead, int base, int count) {
     constexpr int N = Words<E>::N;
     constexpr int HAND = THREADS < kMaxTop ? kMaxTop / THREADS : 1;   // entries per thread
@@ -242,9 +272,8 @@ __device__ __forceinline__ int distill_list(const DistillParams& p, ListSmem& sm
         }
     }
     if (tid == 0) sm.seen = 0;
-    const int words = (count + PER * SWEEP - 1) / (PER * SWEEP) * (SWEEP / 4);
-    for (int i = tid; i < words; i += THREADS) flags[i] = 0;
-    for (int i = tid; i < kListSlots; i += THREADS) sm.head[i] = -1;
+    const int words = (count + PER * SWEEP - 1) / (PER * SWEEP) * (SWEEP * PER / 4);
+    for (int i = tid; i < words / 4; i += THREADS) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
     bool wrong = false, present[HAND];
 #pragma unroll
     for (int h = 0; h < HAND; ++h) {
@@ -259,7 +288,6 @@ __device__ __forceinline__ int distill_list(const DistillParams& p, ListSmem& sm
                 Words<E>::unpack(make_uint4(raw_bits(row + id[h]), 0, 0, 0), xx);
                 x = xx[0];
             }
-            sm.vec[j] = present[h] ? (lead + id[h]) / N : -1;
             sm.col[j] = present[h] ? id[h] : -1;
             sm.x[j] = x;
             sm.t[j] = tv[h];
@@ -281,12 +309,10 @@ __device__ __forceinline__ int distill_list(const DistillParams& p, ListSmem& sm
                 same += (c.x == id[h]) + (c.y == id[h]) + (c.z == id[h]) + (c.w == id[h]);
             }
             wrong = wrong || same > 1;
-            const int j = tid + h * THREADS;
-            sm.next[j] = atomicExch(&sm.head[sm.vec[j] % kListSlots], j);
-            const int i = sm.vec[j] - base;
+            const int e = lead + id[h], i = e / N - base;
             if (i >= 0 && i < count) {
-                const int byte = (i / (PER * SWEEP)) * SWEEP + i % SWEEP, bit = (i / SWEEP) % PER;
-                atomicOr(&flags[byte >> 2], 1u << ((byte & 3) * 8 + bit));
+                const int byte = ((i / (PER * SWEEP)) * SWEEP + i % SWEEP) * PER + i / SWEEP % PER;
+                atomicOr(&bits[byte >> 2], 1u << ((byte & 3) * 8 + e % N));
             }
         }
         const unsigned some = __ballot_sync(0xffffffffu, any), bad = __ballot_sync(0xffffffffu, wrong);
@@ -296,11 +322,47 @@ __device__ __forceinline__ int distill_list(const DistillParams& p, ListSmem& sm
     return sm.seen;
 }
 
-// Vector v with the entries that are listed taken out: the entries of its slot, a few at most.
+// The entries of w whose bits are set go to -inf.
+__device__ __forceinline__ void mask_half(uint32_t& h, uint32_t two, uint32_t ninf) {
+    if (two & 1u) h = (h & 0xffff0000u) | ninf;
+    if (two & 2u) h = (h & 0xffffu) | (ninf << 16);
+}
 template <typename E>
-__device__ __forceinline__ void mask_listed(const ListSmem& sm, int lead, int v, uint4& w) {
-    for (int q = sm.head[v % kListSlots]; q >= 0; q = sm.next[q])
-        if (sm.vec[q] == v) put_entry(w, (lead + sm.col[q]) % Words<E>::N, minus_inf_bits<E>(), E{});
+__device__ __forceinline__ void mask_entries(uint4& w, uint32_t b) {
+    const uint32_t ninf = minus_inf_bits<E>();
+    if constexpr (sizeof(E) == 4) {
+        if (b & 1u) w.x = ninf;
+        if (b & 2u) w.y = ninf;
+        if (b & 4u) w.z = ninf;
+        if (b & 8u) w.w = ninf;
+    } else {
+        mask_half(w.x, b, ninf);
+        mask_half(w.y, b >> 2, ninf);
+        mask_half(w.z, b >> 4, ninf);
+        mask_half(w.w, b >> 6, ninf);
+    }
+}
+template <typename E>
+__device__ __forceinline__ void mask_listed(uint4 (&w)[4], uint32_t b) {
+    if (b == 0) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        if (b >> 8 * q & 0xffu) mask_entries<E>(w[q], b >> 8 * q);
+}
+template <typename E>
+__device__ __forceinline__ void mask_listed(uint4 (&w)[8], uint2 b) {
+    if ((b.x | b.y) == 0) return;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        const uint32_t v = (q < 4 ? b.x : b.y) >> 8 * (q & 3) & 0xffu;
+        if (v) mask_entries<E>(w[q], v);
+    }
+}
+// A vector outside the ones with bits (at an end of the row).
+template <typename E>
+__device__ __forceinline__ void mask_edge(const ListSmem& sm, int k, int lead, int v, uint4& w) {
+    for (int q = 0; q < k; ++q)
+        if (sm.col[q] >= 0 && (lead + sm.col[q]) / Words<E>::N == v) put_entry(w, (lead + sm.col[q]) % Words<E>::N, minus_inf_bits<E>(), E{});
 }
 
 // Nothing listed, or a list that cannot be used.
@@ -345,14 +407,9 @@ __global__ void __launch_bounds__(kLThreads) ears_distill_kernel(const DistillPa
         Stat<false> a;
         stat_open(a);
         const uint64_t pol = l2_policy_evict_first();
-        const unsigned char* flag_bytes = reinterpret_cast<const unsigned char*>(flags);
+        const uint2* bits = reinterpret_cast<const uint2*>(flags) + tid;
         sweep_rounds(s, pol, [&](uint4 (&w)[kLUnroll], int round) {
-            const unsigned f = flag_bytes[round * kLThreads + tid];
-            if (f) {
-#pragma unroll
-                for (int j = 0; j < kLUnroll; ++j)
-                    if (f >> j & 1u) mask_listed<E>(sm, s.lead, s.v0 + round * kLRound + tid + j * kLThreads, w[j]);
-            }
+            mask_listed<E>(w, bits[round * kLThreads]);
             stat_fold<E, kLUnroll, false>(w, r.c, a);
         });
         st = exchange_parts<false>(a, xs, p.rows.C, r.rank, r.c);
@@ -362,7 +419,7 @@ __global__ void __launch_bounds__(kLThreads) ears_distill_kernel(const DistillPa
         const double invT = 1.0 / r.T;
         const float weight = MODE != kForward && p.weight ? __ldg(p.weight + r.row) : 1.f;
         distill_scalars<MODE>(p, sm, r.row, r.rank, invT, r.T_ok && (empty || rowstat_ok(st.m, st.s)),
-                              teacher_part(p, sm, r.row, invT), weight, st);
+                              teacher_part(p, sm, r.row, invT), draft_part(p, sm, invT), weight, st, [] {});
     }
     if (MODE == kForward) return;
     __syncthreads();
@@ -397,9 +454,10 @@ __global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(c
         bool any = false;
         for (int j = tid - kRingConsumers; j < k; j += 32)
             any = any || (__ldg(p.ids + r.row * k + j) >= 0 && __ldg(p.values + r.row * k + j) > -INFINITY);
-        if (__any_sync(0xffffffffu, any) && tid == kRingConsumers) {
+        any = __any_sync(0xffffffffu, any);
+        if (tid == kRingConsumers) {
             ring_init(&bars, stages);
-            issued = ring_load(ring, 0, ring.H, keep, drop);
+            if (any) issued = ring_load(ring, 0, ring.H, keep, drop);
         }
     }
     const int seen = distill_list<E, kRingPer, kRingConsumers, kDistillThreads>(p, sm, flags, tid, r.row, row, s.lead, ring.v0, ring.vecs);
@@ -413,11 +471,11 @@ __global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(c
         const double invT = 1.0 / r.T;
         const float weight = p.weight ? __ldg(p.weight + r.row) : 1.f;
         const TeacherPart te = teacher_part(p, sm, r.row, invT);
+        const DraftPart dr = draft_part(p, sm, invT);
         exchange_join(C);
         const Part st = merge_parts<false>(xs, C * kRingWarps, r.c);
-        distill_scalars<kStep>(p, sm, r.row, r.rank, invT, r.T_ok && (tail_empty(st) || rowstat_ok(st.m, st.s)), te, weight, st);
-        __syncwarp();
-        asm volatile("bar.arrive 1, %0;" ::"n"(kRingConsumers + 32) : "memory");
+        distill_scalars<kStep>(p, sm, r.row, r.rank, invT, r.T_ok && (tail_empty(st) || rowstat_ok(st.m, st.s)), te, dr, weight, st,
+                               [] { asm volatile("bar.arrive 1, %0;" ::"n"(kRingConsumers + 32) : "memory"); });
         return;
     }
     if (tid >= kRingConsumers) {
@@ -426,14 +484,9 @@ __global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(c
     }
     Stat<false> a;
     stat_open(a);
-    const unsigned char* flag_bytes = reinterpret_cast<const unsigned char*>(flags) + tid;
+    const uint32_t* bits = flags + tid;
     const bool swept = ring_stats(ring, [&](uint4 (&w)[kRingPer], int chunk) {
-        const unsigned f = flag_bytes[chunk * kLThreads];
-        if (f) {
-#pragma unroll
-            for (int j = 0; j < kRingPer; ++j)
-                if (f >> j & 1u) mask_listed<E>(sm, s.lead, ring.v0 + chunk * kRingVecs + tid + j * kRingConsumers, w[j]);
-        }
+        mask_listed<E>(w, bits[chunk * kRingConsumers]);
         stat_fold<E, kRingPer, false>(w, r.c, a);
     });
     if (!swept) {
@@ -443,7 +496,7 @@ __global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(c
     const int v = edge_vector(ring, s);
     if (v >= 0) {
         uint4 w[1] = {load_partial(s.base, v, s.lead, s.end)};
-        mask_listed<E>(sm, s.lead, v, w[0]);
+        mask_edge<E>(sm, k, s.lead, v, w[0]);
         stat_fold<E, 1, false>(w, r.c, a);
     }
     const Part st = exchange_parts<false, kRingWarps>(a, xs, C, r.rank, r.c);

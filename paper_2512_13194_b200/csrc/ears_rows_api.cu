@@ -4,6 +4,7 @@
 #include "../../include/ears.h"
 
 #include <atomic>
+#include <climits>
 #include <cmath>
 #include <cstdint>
 #include <cstdlib>
@@ -85,7 +86,7 @@ int choose_cluster(long long rows, size_t row_bytes, bool twice, size_t min_slic
     return C;
 }
 
-int make_span(const RowCall& c, bool twice, RowSpan* out, size_t min_slice = 16u << 10) {
+int make_span(const RowCall& c, bool twice, RowSpan* out, size_t min_slice = 16u << 10, int max_vectors = INT_MAX) {
     int sms = 0;
     const int rc = host_device_sms(&sms);
     if (rc) return rc;
@@ -96,6 +97,7 @@ int make_span(const RowCall& c, bool twice, RowSpan* out, size_t min_slice = 16u
     s.C = choose_cluster(s.rows, (size_t)c.V * esize_of(c.dtype), twice, min_slice, sms);
     const int n = 16 / esize_of(c.dtype);
     s.vectors = (int)(((long long)c.V + 2 * n - 2) / n);
+    while (s.C < kLMaxCluster && s.vectors / s.C > max_vectors) s.C *= 2;
     const int per = (s.vectors + s.C - 1) / s.C;
     s.slice = (per + kSliceAlign - 1) / kSliceAlign * kSliceAlign;
     *out = s;
@@ -236,8 +238,9 @@ int launch_token_step(int dtype, const TokenParams& p, bool ent, void* stream) {
 
 int launch_distill_step(int dtype, const DistillParams& p, void* stream) {
     if (const int g = short_threads(p.rows)) return launch_distill_short<kStep>(dtype, p, g, stream);
-    const int stages = ring_stages(p.rows.slice);
-    const size_t flags = (size_t)((p.rows.slice + kRingVecs - 1) / kRingVecs) * kLThreads;
+    int stages = ring_stages(p.rows.slice);
+    const size_t flags = (size_t)((p.rows.slice + kRingVecs - 1) / kRingVecs) * kRingVecs;   // a byte per vector
+    while (stages > 2 && (size_t)stages * kRingChunk + flags > (100u << 10)) --stages;   // two CTAs per SM
     return with_type(dtype, [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
         return launch_rows(ears_distill_step_kernel<E>, p, kDistillThreads, (size_t)stages * kRingChunk + flags, (cudaStream_t)stream,
@@ -248,7 +251,7 @@ int launch_distill_step(int dtype, const DistillParams& p, void* stream) {
 template <int MODE>
 int launch_distill(int dtype, const DistillParams& p, void* stream) {
     if (const int g = short_threads(p.rows)) return launch_distill_short<MODE>(dtype, p, g, stream);
-    const size_t smem = MODE == kBackward ? 0 : (size_t)((p.rows.slice + kLRound - 1) / kLRound) * kLThreads;
+    const size_t smem = MODE == kBackward ? 0 : (size_t)((p.rows.slice + kLRound - 1) / kLRound) * kLRound;   // a byte per vector
     return with_type(dtype, [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
         return launch_rows(ears_distill_kernel<E, MODE>, p, kLThreads, smem, (cudaStream_t)stream, "ears_distill_kernel launch");
@@ -279,6 +282,7 @@ int check_distill(int V, int k, int kind, double mix, const float* lse) {
     return EARS_OK;
 }
 
+constexpr int kDistillSlice = 1 << 16;   // vectors per CTA, each with a byte of shared memory
 static_assert(kMaxTop == EARS_MAX_TOP, "list length");
 
 }  // namespace
@@ -433,7 +437,7 @@ int ears_distill_loss(int dtype, const void* logits, int B, int R, int V, int64_
     EARS_TRY(check_distill(V, k, kind, mix, lse));
     if (misaligned(out_saved, 16)) return EARS_ERR_ALIGN;
     DistillParams p{};
-    EARS_TRY(make_span(c, false, &p.rows));
+    EARS_TRY(make_span(c, false, &p.rows, 16u << 10, kDistillSlice));
     p.k = k; p.kind = kind; p.mix = mix; p.values = values; p.ids = ids; p.lse = lse;
     p.out_loss = out_loss; p.stats = (float4*)out_saved; p.status = status;
     return launch_distill<kForward>(dtype, p, stream);
@@ -450,7 +454,7 @@ int ears_distill_backward(int dtype, const void* logits, int B, int R, int V, in
     EARS_TRY(check_grad(c, out_grad, grad_stride_b, grad_stride_r));
     if (misaligned(saved, 16)) return EARS_ERR_ALIGN;
     DistillParams p{};
-    EARS_TRY(make_span(c, false, &p.rows));
+    EARS_TRY(make_span(c, false, &p.rows, 16u << 10, kDistillSlice));
     p.k = k; p.kind = kind; p.mix = mix; p.values = values; p.ids = ids; p.lse = lse; p.weight = d_loss;
     p.stats = (float4*)const_cast<float*>(saved); p.status = status;
     p.grad = out_grad; p.gsb = grad_stride_b; p.gsr = grad_stride_r;
@@ -467,7 +471,7 @@ int ears_distill_step(int dtype, const void* logits, int B, int R, int V, int64_
     EARS_TRY(check_distill(V, k, kind, mix, lse));
     EARS_TRY(check_grad(c, out_grad, grad_stride_b, grad_stride_r));
     DistillParams p{};
-    EARS_TRY(make_span(c, true, &p.rows));
+    EARS_TRY(make_span(c, true, &p.rows, 16u << 10, kDistillSlice));
     p.k = k; p.kind = kind; p.mix = mix; p.values = values; p.ids = ids; p.lse = lse; p.weight = row_weight;
     p.out_loss = out_loss; p.status = status;
     p.grad = out_grad; p.gsb = grad_stride_b; p.gsr = grad_stride_r;

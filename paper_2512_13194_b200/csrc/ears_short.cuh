@@ -150,17 +150,17 @@ template <typename E, int G, int MODE>
 __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas) ears_distill_short_kernel(const DistillParams p) {
     __shared__ float4 xs[G / 32];
     __shared__ ListSmem lists[ShortShape<G>::kRows];
-    __shared__ uint32_t all_flags[ShortShape<G>::kThreads / 4];
+    __shared__ alignas(16) uint2 all_bits[ShortShape<G>::kThreads];
     RowSetup r;
     if (!short_setup<G>(p.rows, &r)) return;
     const int tid = threadIdx.x % G, k = p.k;
     ListSmem& sm = lists[threadIdx.x / G];
-    uint32_t* flags = all_flags + threadIdx.x / G * (G / 4);
+    uint2* bits = all_bits + threadIdx.x / G * G;
     const E* row = row_ptr<E>(p.rows, r);
     const Slice<E> s = make_slice<E>(row, p.rows.V, p.rows.slice, 0);
     E* grad = MODE == kForward ? nullptr : grad_ptr<E>(p.grad, p.gsb, p.gsr, r) - s.lead;
     const int v0 = s.lead > 0 ? 1 : 0;   // the first whole vector
-    const int seen = distill_list<E, kShortSlots, G, G>(p, sm, flags, tid, r.row, row, s.lead, v0, max(0, s.end / Words<E>::N - v0));
+    const int seen = distill_list<E, kShortSlots, G, G>(p, sm, reinterpret_cast<uint32_t*>(bits), tid, r.row, row, s.lead, v0, max(0, s.end / Words<E>::N - v0));
     if (seen != 1) {
         if (tid == 0) distill_unused<MODE>(p, r.row, (seen & 2) != 0);
         if (MODE != kForward) short_zero<E, G>(s, tid, grad);
@@ -174,13 +174,8 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas)
         st = Part{q.x, q.y, 0.f};
     } else {
         // the gradient of a listed entry is written on its own, so its place may go to -inf for good
-        const unsigned f = reinterpret_cast<const unsigned char*>(flags)[tid];
-        if (f) {
-#pragma unroll
-            for (int j = 0; j < kShortSlots; ++j)
-                if (f >> j & 1u) mask_listed<E>(sm, s.lead, v0 + tid + j * G, x.w[j]);
-        }
-        if (x.edge >= 0) mask_listed<E>(sm, s.lead, x.edge, x.we);
+        mask_listed<E>(x.w, bits[tid]);
+        if (x.edge >= 0) mask_edge<E>(sm, k, s.lead, x.edge, x.we);
         st = short_merge<G, false>(short_stats<E, G, false>(x, r.c), xs, r.c);
     }
     const bool empty = tail_empty(st);
@@ -188,7 +183,7 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas)
         const double invT = 1.0 / r.T;
         const float weight = MODE != kForward && p.weight ? __ldg(p.weight + r.row) : 1.f;
         distill_scalars<MODE>(p, sm, r.row, 0, invT, r.T_ok && (empty || rowstat_ok(st.m, st.s)), teacher_part(p, sm, r.row, invT),
-                              weight, st);
+                              draft_part(p, sm, invT), weight, st, [] {});
     }
     if (MODE == kForward) return;
     row_sync<G>();

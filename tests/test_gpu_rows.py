@@ -453,6 +453,19 @@ def test_distill_lists_at_the_edges(ears):
     close(loss, o.loss, o.loss_scale * (3 * LOG_TOL))
 
 
+def test_distill_longest_rows(ears):
+    V, k, T = 1 << 20, 128, 1.0
+    for dtype, cluster in (("fp32", 1), ("fp32", 0), ("bf16", 0)):
+        ears.set_row_cluster(cluster)
+        x, vals, ids, lse, g = teacher_case(2, V, k, dtype, T, 70)
+        o = R.distill(x, T, vals, ids, lse=lse)
+        teacher = ears.TopLogits(vals.to(DEV), ids.to(DEV), lse.to(DEV))
+        loss, grad = ears.distill_step(x.to(DEV), teacher, T)
+        for l in (loss, ears.distill_loss(x.to(DEV), teacher, T)):
+            close(l, o.loss, o.loss_scale * (3 * LOG_TOL))
+        close_grad(grad, o.grad, o.scale, G_TOL, dtype)
+
+
 def test_distill_lists_that_cannot_be_used(ears):
     n, V, k = 6, 300, 4
     x, vals, ids, lse, g = teacher_case(n, V, k, "fp32", 1.0, 12)
