@@ -40,16 +40,18 @@ class _Rows:
     """The common head of a call: dtype, pointer, sizes, strides, temperature.  Small calls are bound by the host, so
     nothing is converted, viewed or looked up that is as it should be already."""
 
-    __slots__ = ("logits", "lead", "device", "index", "B", "R", "V", "seq_T", "status", "args")
+    __slots__ = ("logits", "lead", "index", "B", "R", "V", "seq_T", "status", "args")
 
     def __init__(self, logits: torch.Tensor, temperature, seq_temperature, status):
         code = _DTYPES.get(logits.dtype)
         if code is None:
             raise TypeError(f"logits must be float32, bfloat16 or float16, got {logits.dtype}")
         shape = logits.shape
-        if len(shape) not in (2, 3):
+        dims = len(shape)
+        if dims != 3 and dims != 2:
             raise ValueError("expected logits [B,R,V] or [R,V]")
-        if not logits.is_cuda:
+        self.index = index = logits.get_device()
+        if index < 0:
             raise ValueError("logits must be a CUDA tensor")
         if 0 in shape:
             raise ValueError("logits must not be empty")
@@ -57,25 +59,24 @@ class _Rows:
         if strides[-1] != 1 and shape[-1] > 1 or min(strides) < 0:
             logits = logits.contiguous()
             strides = logits.stride()
-        self.logits, self.lead, self.device = logits, shape[:-1], logits.device
-        self.index = self.device.index
-        self.V = shape[-1]
-        if len(shape) == 3:
+        self.logits, self.lead, self.V = logits, shape[:-1], shape[-1]
+        if dims == 3:
             self.B, self.R = shape[0], shape[1]
             sb, sr = strides[0], strides[1]
         else:
             self.B, self.R = 1, shape[0]
             sb, sr = 0, strides[0]
         self.seq_T = None if seq_temperature is None else self.per(seq_temperature, torch.float32, (self.B,), "seq_temperature")
-        if status is not None and (status.device != self.device or status.dtype != torch.int32 or status.numel() != 1):
+        if status is not None and (status.get_device() != index or status.dtype != torch.int32 or status.numel() != 1):
             raise ValueError("status must be an int32 CUDA tensor of one element on the logits' device")
-        self.status = status
-        self.args = (code, logits.data_ptr(), self.B, self.R, self.V, sb, sr, float(temperature), _ptr(self.seq_T))
+        self.status = None if status is None else status.data_ptr()
+        self.args = (code, logits.data_ptr(), self.B, self.R, self.V, sb, sr, float(temperature),
+                     None if self.seq_T is None else self.seq_T.data_ptr())
 
     def per(self, t, dtype, shape, name):
         if t is None:
             return None
-        if t.device != self.device:
+        if t.get_device() != self.index:
             raise ValueError(f"{name} must live on the logits' device")
         if t.shape != shape:
             raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
@@ -88,20 +89,11 @@ class _Rows:
     def row(self, t, name, dtype=torch.float32):
         return None if t is None else self.per(t, dtype, self.lead, name)
 
-    def out(self, like=None):
-        """A float32 output per row; ``like``, an input of that kind, spares torch the parsing of shape and type."""
-        return torch.empty(self.lead, dtype=torch.float32, device=self.device) if like is None else torch.empty_like(like)
-
-    def saved(self):
-        return torch.empty(self.lead + (4,), dtype=torch.float32, device=self.device)
-
     def grad(self, out_grad):
+        x = self.logits
         if out_grad is None:
-            if self.logits.is_contiguous():
-                out_grad = torch.empty_like(self.logits)
-            else:
-                out_grad = torch.empty(self.logits.shape, dtype=self.logits.dtype, device=self.device)
-        elif out_grad.shape != self.logits.shape or out_grad.dtype != self.logits.dtype or out_grad.device != self.device:
+            out_grad = torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        elif out_grad.shape != x.shape or out_grad.dtype != x.dtype or out_grad.get_device() != self.index:
             raise ValueError("out_grad must have the logits' shape, type and device")
         elif out_grad.shape[-1] > 1 and out_grad.stride(-1) != 1:
             raise ValueError("the entries of out_grad's rows must be contiguous")
@@ -111,27 +103,25 @@ class _Rows:
     def call(self, fn, *tail, stream=None):
         """fn(*head, *tail, status, stream) with the logits' device current."""
         if _current_device() == self.index:
-            rc = fn(*self.args, *tail, _ptr(self.status), self.stream(stream))
+            rc = fn(*self.args, *tail, self.status, _raw_stream(self.index) if stream is None else stream.cuda_stream)
         else:
-            with torch.cuda.device(self.device):
-                rc = fn(*self.args, *tail, _ptr(self.status), self.stream(stream))
+            with torch.cuda.device(self.index):
+                rc = fn(*self.args, *tail, self.status, _raw_stream(self.index) if stream is None else stream.cuda_stream)
         if rc:
             _check(rc)
 
-    def stream(self, stream):
-        return _raw_stream(self.index) if stream is None else stream.cuda_stream
 
-
-def _current_device() -> int:
-    return torch._C._cuda_getDevice()
-
-
-def _raw_stream(index: int) -> int:
-    return torch._C._cuda_getCurrentRawStream(index)
+_current_device = torch._C._cuda_getDevice
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_F32 = torch.float32
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _saved(rows):
+    return torch.empty(rows.lead + (4,), dtype=_F32, device=rows.logits.device)
 
 
 def _refuse_capture():
@@ -158,8 +148,9 @@ def top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0, *, accept
     k = int(k)
     if not 1 <= k <= MAX_TOP:
         raise ValueError(f"k must lie in 1..{MAX_TOP}")
-    values = torch.empty(rows.lead + (k,), dtype=torch.float32, device=rows.device)
-    ids, lse = torch.empty_like(values, dtype=torch.int32), rows.out()
+    values = torch.empty(rows.lead + (k,), dtype=_F32, device=rows.logits.device)
+    ids = torch.empty_like(values, dtype=torch.int32)
+    lse = torch.empty(rows.lead, dtype=_F32, device=rows.logits.device)
     rows.call(load_library().ears_top_logits, _ptr(acc), k, values.data_ptr(), ids.data_ptr(), lse.data_ptr(), stream=stream)
     return TopLogits(values, ids, lse)
 
@@ -167,8 +158,8 @@ def top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0, *, accept
 # ---- token log probabilities --------------------------------------------------------------------
 
 def _token_forward(rows, tokens, entropy, saved, stream):
-    logp = rows.out()
-    H = rows.out(logp) if entropy else None
+    logp = torch.empty_like(tokens, dtype=_F32)
+    H = torch.empty_like(logp) if entropy else None
     rows.call(load_library().ears_token_logprobs, tokens.data_ptr(), logp.data_ptr(), _ptr(H), _ptr(saved), stream=stream)
     return logp, H
 
@@ -178,7 +169,7 @@ class _TokenLogprobs(torch.autograd.Function):
     def forward(ctx, logits, tokens, temperature, seq_temperature, entropy, status, stream):
         _refuse_capture()
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
-        saved = rows.saved()
+        saved = _saved(rows)
         ctx.rows, ctx.tokens, ctx.saved = rows, rows.row(tokens, "tokens", torch.int32), saved
         ctx.save_for_backward(logits)          # notices a change of the logits before the backward pass
         logp, H = _token_forward(rows, ctx.tokens, entropy, saved, stream)
@@ -217,7 +208,8 @@ def token_logprobs_step(logits: torch.Tensor, tokens: torch.Tensor, d_logp: torc
     ``d_logp`` and, optionally, ``d_entropy`` per row.  ``out_grad=logits`` writes the gradient over them."""
     rows = _Rows(logits, temperature, seq_temperature, status)
     tok, dl, dh = rows.row(tokens, "tokens", torch.int32), rows.row(d_logp, "d_logp"), rows.row(d_entropy, "d_entropy")
-    logp, H = rows.out(dl), rows.out(dl) if dh is not None else None
+    logp = torch.empty_like(dl)
+    H = None if dh is None else torch.empty_like(dl)
     g, place = rows.grad(out_grad)
     rows.call(load_library().ears_token_logprobs_step, tok.data_ptr(), dl.data_ptr(), _ptr(dh), logp.data_ptr(), _ptr(H),
               *place, stream=stream)
@@ -234,7 +226,8 @@ def _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, clip_low, clip_h
 
 def _policy_outputs(rows, held, entropy):
     _, old, ref, _ = held
-    return PolicyTerms(rows.out(old), rows.out(old), rows.out(old) if ref is not None else None, rows.out(old) if entropy else None)
+    new = torch.empty_like
+    return PolicyTerms(new(old), new(old), None if ref is None else new(old), new(old) if entropy else None)
 
 
 class _PolicyLoss(torch.autograd.Function):
@@ -243,7 +236,7 @@ class _PolicyLoss(torch.autograd.Function):
         _refuse_capture()
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
         ctx.held, ctx.args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, *coefs)
-        ctx.rows, ctx.saved = rows, rows.saved()
+        ctx.rows, ctx.saved = rows, _saved(rows)
         ctx.save_for_backward(logits)
         t = _policy_outputs(rows, ctx.held, entropy)
         rows.call(load_library().ears_policy_loss, *ctx.args, *(_ptr(o) for o in t), ctx.saved.data_ptr(), stream=stream)
@@ -310,15 +303,19 @@ def _distill_inputs(rows, teacher, kind, mix):
     return held, (k,) + tuple(_ptr(t) for t in held) + (DISTILL_KINDS[kind], float(mix))
 
 
+def _loss_like(rows, t):
+    return torch.empty(rows.lead, dtype=_F32, device=rows.logits.device) if t is None else torch.empty_like(t)
+
+
 class _DistillLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, teacher, temperature, kind, mix, seq_temperature, status, stream):
         _refuse_capture()
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
         ctx.held, ctx.args = _distill_inputs(rows, teacher, kind, mix)
-        ctx.rows, ctx.saved = rows, rows.saved()
+        ctx.rows, ctx.saved = rows, _saved(rows)
         ctx.save_for_backward(logits)
-        loss = rows.out(ctx.held[2])
+        loss = _loss_like(rows, ctx.held[2])
         rows.call(load_library().ears_distill_loss, *ctx.args, loss.data_ptr(), ctx.saved.data_ptr(), stream=stream)
         return loss
 
@@ -345,7 +342,7 @@ def distill_loss(logits: torch.Tensor, teacher: TopLogits, temperature: float = 
         return _DistillLoss.apply(logits, teacher, temperature, kind, mix, seq_temperature, status, stream)
     rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _distill_inputs(rows, teacher, kind, mix)
-    loss = rows.out(held[2])
+    loss = _loss_like(rows, held[2])
     rows.call(load_library().ears_distill_loss, *args, loss.data_ptr(), None, stream=stream)
     return loss
 
@@ -357,7 +354,7 @@ def distill_step(logits: torch.Tensor, teacher: TopLogits, temperature: float = 
     rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _distill_inputs(rows, teacher, kind, mix)
     w = rows.row(row_weight, "row_weight")
-    loss = rows.out(w)
+    loss = _loss_like(rows, w)
     g, place = rows.grad(out_grad)
     rows.call(load_library().ears_distill_step, *args, _ptr(w), loss.data_ptr(), *place, stream=stream)
     return loss, g
