@@ -55,5 +55,28 @@ def build(force: bool = False, verbose: bool = False, trace: bool = False) -> st
     return out
 
 
+TORCH_LIB = os.path.join(HERE, "ears_torch.so")
+
+
+def build_torch(force: bool = False) -> str:
+    """The Python entry of the row operators (csrc/ears_torch.cpp): host code only, against torch's C++ headers."""
+    import sysconfig
+
+    import torch
+    src = os.path.join(CSRC, "ears_torch.cpp")
+    header = os.path.join(os.path.dirname(HERE), "include", "ears.h")
+    if not force and os.path.exists(TORCH_LIB) and all(os.path.getmtime(f) <= os.path.getmtime(TORCH_LIB) for f in (src, header)):
+        return TORCH_LIB
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{root}/include",
+           f"-I{root}/include/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}", f"-I{cuda}/include", "-o", TORCH_LIB, src,
+           f"-L{root}/lib", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python", f"-Wl,-rpath,{root}/lib"]
+    subprocess.run(cmd, check=True)
+    return TORCH_LIB
+
+
 if __name__ == "__main__":
+    print(build_torch(force="--force" in sys.argv))
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv, trace="--trace" in sys.argv))

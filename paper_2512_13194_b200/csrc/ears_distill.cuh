@@ -42,7 +42,6 @@ struct DistillParams {
 
 struct ListSmem {
     alignas(16) int col[kMaxTop];   // listed ids, -1: absent
-    float x[kMaxTop];            // draft logit of the listed entry
     float t[kMaxTop];            // teacher logit
     float entry[kMaxTop];        // gradient of the listed entry
     float factor;
@@ -101,16 +100,34 @@ __device__ __forceinline__ TeacherPart teacher_part(const DistillParams& p, cons
     return t;
 }
 
+// The draft's logits of the listed entries: asked for when the list stands, used later.
+struct DraftLogits { float x[kTopPer]; };
+
+template <typename E>
+__device__ __forceinline__ DraftLogits draft_logits(const DistillParams& p, const ListSmem& sm, const E* row) {
+    const int lane = threadIdx.x & 31;
+    DraftLogits d;
+#pragma unroll
+    for (int i = 0; i < kTopPer; ++i) {
+        d.x[i] = -INFINITY;
+        if (listed(p, sm, i)) {
+            float x[Words<E>::N];
+            Words<E>::unpack(make_uint4(raw_bits(row + sm.col[lane + 32 * i]), 0, 0, 0), x);
+            d.x[i] = x[0];
+        }
+    }
+    return d;
+}
+
 // The draft's listed entries, relative to their own maximum.
 struct DraftPart { double xm, lq[kTopPer], e[kTopPer], sum; };
 
-__device__ __forceinline__ DraftPart draft_part(const DistillParams& p, const ListSmem& sm, double invT) {
-    const int lane = threadIdx.x & 31;
+__device__ __forceinline__ DraftPart draft_part(const DistillParams& p, const ListSmem& sm, const DraftLogits& dl, double invT) {
     DraftPart d;
     d.xm = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kTopPer; ++i)
-        if (listed(p, sm, i)) d.xm = fmax(d.xm, (double)sm.x[lane + 32 * i]);
+        if (listed(p, sm, i)) d.xm = fmax(d.xm, (double)dl.x[i]);
     d.xm = warp_max(d.xm);
     const double ref = d.xm > -INFINITY ? d.xm : 0.0;   // every listed entry masked: e = 0
     d.sum = 0.0;
@@ -118,7 +135,7 @@ __device__ __forceinline__ DraftPart draft_part(const DistillParams& p, const Li
     for (int i = 0; i < kTopPer; ++i) {
         d.lq[i] = d.e[i] = 0.0;
         if (listed(p, sm, i)) {
-            d.lq[i] = ((double)sm.x[lane + 32 * i] - ref) * invT;
+            d.lq[i] = ((double)dl.x[i] - ref) * invT;
             d.e[i] = exp(d.lq[i]);
             d.sum += d.e[i];
         }
@@ -254,8 +271,8 @@ template <> struct ListWord<8> { typedef uint2 type; };
 // The row's list, by the THREADS threads that share the row (tid among them): into sm, and the bits of the vectors
 // among [base, base + count) into bits.  -> sm.seen.
 template <typename E, int PER, int SWEEP, int THREADS>
-__device__ __forceinline__ int distill_list(const DistillParams& p, ListSmem& sm, uint32_t* bits, int tid, long long row_index, const E* row,
-                                            int lead, int base, int count) {
+__device__ __forceinline__ int distill_list(const DistillParams& p, ListSmem& sm, uint32_t* bits, int tid, long long row_index, int lead,
+                                            int base, int count) {
     constexpr int N = Words<E>::N;
     constexpr int HAND = THREADS < kMaxTop ? kMaxTop / THREADS : 1;   // entries per thread
     const int k = p.k;
@@ -282,14 +299,7 @@ __device__ __forceinline__ int distill_list(const DistillParams& p, ListSmem& sm
         wrong = wrong || off;
         present[h] = !off && id[h] >= 0 && tv[h] > -INFINITY;
         if (j < kMaxTop) {
-            float x = -INFINITY;
-            if (present[h]) {
-                float xx[N];
-                Words<E>::unpack(make_uint4(raw_bits(row + id[h]), 0, 0, 0), xx);
-                x = xx[0];
-            }
             sm.col[j] = present[h] ? id[h] : -1;
-            sm.x[j] = x;
             sm.t[j] = tv[h];
         }
     }
@@ -388,12 +398,14 @@ __global__ void __launch_bounds__(kLThreads) ears_distill_kernel(const DistillPa
     const E* row = row_ptr<E>(p.rows, r);
     const Slice<E> s = make_slice<E>(row, p.rows.V, p.rows.slice, r.rank);
     E* grad = MODE == kForward ? nullptr : grad_ptr<E>(p.grad, p.gsb, p.gsr, r) - s.lead;
-    const int seen = distill_list<E, kLUnroll, kLThreads, kLThreads>(p, sm, flags, tid, r.row, row, s.lead, s.v0, MODE == kBackward ? 0 : s.n);
+    const int seen = distill_list<E, kLUnroll, kLThreads, kLThreads>(p, sm, flags, tid, r.row, s.lead, s.v0, MODE == kBackward ? 0 : s.n);
     if (seen != 1) {   // the same in every CTA of the cluster
         if (tid == 0 && r.rank == 0) distill_unused<MODE>(p, r.row, (seen & 2) != 0);
         if (MODE != kForward) dense_pass<E, false>(s, grad, true, 0.f, 0.f, 0.f, 0.f);
         return;
     }
+    DraftLogits dl{};
+    if (tid < 32) dl = draft_logits(p, sm, row);
     Part st;
     if (MODE == kBackward) {
         const float4 q = p.stats[r.row];
@@ -419,7 +431,7 @@ __global__ void __launch_bounds__(kLThreads) ears_distill_kernel(const DistillPa
         const double invT = 1.0 / r.T;
         const float weight = MODE != kForward && p.weight ? __ldg(p.weight + r.row) : 1.f;
         distill_scalars<MODE>(p, sm, r.row, r.rank, invT, r.T_ok && (empty || rowstat_ok(st.m, st.s)),
-                              teacher_part(p, sm, r.row, invT), draft_part(p, sm, invT), weight, st, [] {});
+                              teacher_part(p, sm, r.row, invT), draft_part(p, sm, dl, invT), weight, st, [] {});
     }
     if (MODE == kForward) return;
     __syncthreads();
@@ -460,7 +472,7 @@ __global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(c
             if (any) issued = ring_load(ring, 0, ring.H, keep, drop);
         }
     }
-    const int seen = distill_list<E, kRingPer, kRingConsumers, kDistillThreads>(p, sm, flags, tid, r.row, row, s.lead, ring.v0, ring.vecs);
+    const int seen = distill_list<E, kRingPer, kRingConsumers, kDistillThreads>(p, sm, flags, tid, r.row, s.lead, ring.v0, ring.vecs);
     if (seen != 1) {   // the same in every CTA of the cluster
         if (tid == 0 && r.rank == 0) distill_unused<kStep>(p, r.row, (seen & 2) != 0);
         if (tid < kLThreads) dense_pass<E, false>(s, grad, true, 0.f, 0.f, 0.f, 0.f);
@@ -470,8 +482,9 @@ __global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(c
     if (tid >= kRingThreads) {   // scalars
         const double invT = 1.0 / r.T;
         const float weight = p.weight ? __ldg(p.weight + r.row) : 1.f;
+        const DraftLogits dl = draft_logits(p, sm, row);
         const TeacherPart te = teacher_part(p, sm, r.row, invT);
-        const DraftPart dr = draft_part(p, sm, invT);
+        const DraftPart dr = draft_part(p, sm, dl, invT);
         exchange_join(C);
         const Part st = merge_parts<false>(xs, C * kRingWarps, r.c);
         distill_scalars<kStep>(p, sm, r.row, r.rank, invT, r.T_ok && (tail_empty(st) || rowstat_ok(st.m, st.s)), te, dr, weight, st,

@@ -160,12 +160,14 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas)
     const Slice<E> s = make_slice<E>(row, p.rows.V, p.rows.slice, 0);
     E* grad = MODE == kForward ? nullptr : grad_ptr<E>(p.grad, p.gsb, p.gsr, r) - s.lead;
     const int v0 = s.lead > 0 ? 1 : 0;   // the first whole vector
-    const int seen = distill_list<E, kShortSlots, G, G>(p, sm, reinterpret_cast<uint32_t*>(bits), tid, r.row, row, s.lead, v0, max(0, s.end / Words<E>::N - v0));
+    const int seen = distill_list<E, kShortSlots, G, G>(p, sm, reinterpret_cast<uint32_t*>(bits), tid, r.row, s.lead, v0, max(0, s.end / Words<E>::N - v0));
     if (seen != 1) {
         if (tid == 0) distill_unused<MODE>(p, r.row, (seen & 2) != 0);
         if (MODE != kForward) short_zero<E, G>(s, tid, grad);
         return;
     }
+    DraftLogits dl{};
+    if (tid < 32) dl = draft_logits(p, sm, row);
     ShortRow<E> x;
     short_load<E, G>(s, tid, x);
     Part st;
@@ -183,7 +185,7 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas)
         const double invT = 1.0 / r.T;
         const float weight = MODE != kForward && p.weight ? __ldg(p.weight + r.row) : 1.f;
         distill_scalars<MODE>(p, sm, r.row, 0, invT, r.T_ok && (empty || rowstat_ok(st.m, st.s)), teacher_part(p, sm, r.row, invT),
-                              draft_part(p, sm, invT), weight, st, [] {});
+                              draft_part(p, sm, dl, invT), weight, st, [] {});
     }
     if (MODE == kForward) return;
     row_sync<G>();

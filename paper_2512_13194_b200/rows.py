@@ -7,15 +7,20 @@ lie as long as the entries of a row are contiguous (a slice ``target[:, :K]`` is
 have the logits' shape without V and are converted to contiguous float32 / int32 where they are not.
 ``*_loss`` and ``token_logprobs`` can be differentiated by autograd; ``*_step`` return the gradient at once,
 reading the logits from memory a single time, and are what a step recorded into a CUDA graph uses.
+Calls whose tensors are in their plain form already go through csrc/ears_torch.cpp, which makes the same C-ABI call
+with less work on the host; everything else is converted, checked and refused here.
 ``status``: optional int32 CUDA tensor of one element that gets EARS_DEV_INVALID_INPUT OR-ed in.
 """
 from __future__ import annotations
 
+import ctypes
+import os
 from typing import NamedTuple, Optional
 
 import torch
 
 from . import binding
+from . import build as _build
 from .binding import _check, load_library
 
 MAX_TOP = 128
@@ -34,6 +39,33 @@ class PolicyTerms(NamedTuple):
     logp: torch.Tensor
     kl: Optional[torch.Tensor]
     entropy: Optional[torch.Tensor]
+
+
+_plain = None          # the ears_torch module, bound to the library in use
+_plain_for = None
+
+
+def _plain_calls():
+    """csrc/ears_torch.cpp, calling the library that load_library() returns."""
+    global _plain, _plain_for
+    lib = binding._lib
+    if lib is not None and lib is _plain_for:
+        return _plain
+    lib = load_library()
+    if _plain is None:
+        if not os.path.exists(_build.TORCH_LIB):
+            _build.build_torch()
+        from . import ears_torch
+        _plain = ears_torch
+    names = ("ears_top_logits", "ears_token_logprobs", "ears_token_logprobs_step", "ears_policy_loss", "ears_policy_step",
+             "ears_distill_loss", "ears_distill_step")
+    _plain.bind({n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names})
+    _plain_for = lib
+    return _plain
+
+
+def _raw(stream):
+    return None if stream is None else stream.cuda_stream
 
 
 class _Rows:
@@ -143,6 +175,9 @@ def top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0, *, accept
     normaliser at ``temperature`` (ears_top_logits).  Entries of -inf are not listed (id -1, value -inf).
     ``accept_len`` [B] int32, as a verification call returns it: rows behind a sequence's first rejection
     are left out."""
+    out = _plain_calls().top_logits(logits, accept_len, k, temperature, seq_temperature, status, _raw(stream))
+    if out is not None:
+        return TopLogits(*out)
     rows = _Rows(logits, temperature, seq_temperature, status)
     acc = rows.per(accept_len, torch.int32, (rows.B,), "accept_len")
     k = int(k)
@@ -196,6 +231,9 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, temperature: floa
     ``entropy=True`` the pair (logp, entropy in nats).  Differentiable (ears_token_logprobs, _backward)."""
     if _wants_grad(logits):
         return _TokenLogprobs.apply(logits, tokens, temperature, seq_temperature, bool(entropy), status, stream)
+    out = _plain_calls().token_logprobs(logits, tokens, bool(entropy), temperature, seq_temperature, status, _raw(stream))
+    if out is not None:
+        return out if entropy else out[0]
     rows = _Rows(logits, temperature, seq_temperature, status)
     logp, H = _token_forward(rows, rows.row(tokens, "tokens", torch.int32), entropy, None, stream)
     return (logp, H) if entropy else logp
@@ -206,6 +244,9 @@ def token_logprobs_step(logits: torch.Tensor, tokens: torch.Tensor, d_logp: torc
                         seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
     """(logp, entropy or None, gradient) for upstream gradients known beforehand (ears_token_logprobs_step):
     ``d_logp`` and, optionally, ``d_entropy`` per row.  ``out_grad=logits`` writes the gradient over them."""
+    out = _plain_calls().token_logprobs_step(logits, tokens, d_logp, d_entropy, out_grad, temperature, seq_temperature, status, _raw(stream))
+    if out is not None:
+        return out
     rows = _Rows(logits, temperature, seq_temperature, status)
     tok, dl, dh = rows.row(tokens, "tokens", torch.int32), rows.row(d_logp, "d_logp"), rows.row(d_entropy, "d_entropy")
     logp = torch.empty_like(dl)
@@ -267,6 +308,10 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
     if _wants_grad(logits):
         return PolicyTerms(*_PolicyLoss.apply(logits, tokens, old_logp, advantage, ref_logp, temperature, coefs, seq_temperature,
                                               with_entropy, status, stream))
+    out = _plain_calls().policy(logits, tokens, old_logp, ref_logp, advantage, *coefs, with_entropy, False, None, None, temperature,
+                                seq_temperature, status, _raw(stream))
+    if out is not None:
+        return PolicyTerms(*out[:4])
     rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, *coefs)
     t = _policy_outputs(rows, held, with_entropy)
@@ -280,10 +325,15 @@ def policy_step(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
                 row_weight: Optional[torch.Tensor] = None, out_grad: Optional[torch.Tensor] = None,
                 seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
     """(PolicyTerms, gradient of sum row_weight * loss) in one call (ears_policy_step)."""
+    with_entropy = bool(entropy) or entropy_coef != 0.0
+    out = _plain_calls().policy(logits, tokens, old_logp, ref_logp, advantage, clip_low, clip_high, kl_coef, entropy_coef, with_entropy,
+                                True, row_weight, out_grad, temperature, seq_temperature, status, _raw(stream))
+    if out is not None:
+        return PolicyTerms(*out[:4]), out[4]
     rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, clip_low, clip_high, kl_coef, entropy_coef)
     w = rows.row(row_weight, "row_weight")
-    t = _policy_outputs(rows, held, bool(entropy) or entropy_coef != 0.0)
+    t = _policy_outputs(rows, held, with_entropy)
     g, place = rows.grad(out_grad)
     rows.call(load_library().ears_policy_step, *args, _ptr(w), *(_ptr(o) for o in t), *place, stream=stream)
     return t, g
@@ -340,6 +390,10 @@ def distill_loss(logits: torch.Tensor, teacher: TopLogits, temperature: float = 
     kind: "forward_kl", "reverse_kl" (needs lse) or "jsd" with weight ``mix``.  Rows without entries are left out."""
     if _wants_grad(logits):
         return _DistillLoss.apply(logits, teacher, temperature, kind, mix, seq_temperature, status, stream)
+    out = _plain_calls().distill(logits, *teacher, DISTILL_KINDS.get(kind), mix, False, None, None, temperature, seq_temperature, status,
+                                 _raw(stream))
+    if out is not None:
+        return out[0]
     rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _distill_inputs(rows, teacher, kind, mix)
     loss = _loss_like(rows, held[2])
@@ -351,6 +405,10 @@ def distill_step(logits: torch.Tensor, teacher: TopLogits, temperature: float = 
                  mix: float = 0.5, row_weight: Optional[torch.Tensor] = None, out_grad: Optional[torch.Tensor] = None,
                  seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
     """(loss per row, gradient of sum row_weight * loss) in one call (ears_distill_step)."""
+    out = _plain_calls().distill(logits, *teacher, DISTILL_KINDS.get(kind), mix, True, row_weight, out_grad, temperature, seq_temperature,
+                                 status, _raw(stream))
+    if out is not None:
+        return out
     rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _distill_inputs(rows, teacher, kind, mix)
     w = rows.row(row_weight, "row_weight")

@@ -547,6 +547,72 @@ def test_captured_steps_replay_on_new_inputs(ears):
     assert torch.isfinite(leaf.grad).all()
 
 
+def test_inputs_that_need_converting_give_the_same_results(ears):
+    n, V, k = 7, 3001, 9
+    x, vals, ids, lse, g = teacher_case(n, V, k, "fp32", 1.0, 17)
+    xg = x.to(DEV)
+    tok = ids[:, 0].contiguous().to(DEV)
+    f = [torch.randn(n, generator=g).to(DEV) for _ in range(4)]
+    wide = [torch.stack([t, t], 1)[:, 0] for t in f]                 # strided
+    double = [t.double() for t in f]
+    transposed = xg.t().contiguous().t()
+    teacher = ears.TopLogits(vals.to(DEV), ids.to(DEV), lse.to(DEV))
+    other = ears.TopLogits(vals.double().to(DEV), ids.long().to(DEV), lse.double().to(DEV))
+
+    def same(a, b):
+        for u, v in zip(a, b):
+            assert (u is None and v is None) or torch.equal(u, v)
+    for a, b in ((f, wide), (f, double)):
+        for logits, t in ((xg, tok.long()), (transposed, tok)):
+            same(ears.token_logprobs_step(xg, tok, a[0], a[1]), ears.token_logprobs_step(logits, t, b[0], b[1]))
+            pa, ga = ears.policy_step(xg, tok, a[0], a[1], ref_logp=a[2], kl_coef=0.1, entropy_coef=0.01, row_weight=a[3])
+            pb, gb = ears.policy_step(logits, t, b[0], b[1], ref_logp=b[2], kl_coef=0.1, entropy_coef=0.01, row_weight=b[3])
+            same(pa + (ga,), pb + (gb,))
+            same(ears.policy_loss(xg, tok, a[0], a[1], entropy=1), ears.policy_loss(logits, t, b[0], b[1], entropy=True))
+            same(ears.distill_step(xg, teacher, kind="jsd", row_weight=a[3]), ears.distill_step(logits, other, kind="jsd", row_weight=b[3]))
+            same([ears.distill_loss(xg, teacher)], [ears.distill_loss(logits, other)])
+            same(ears.token_logprobs(xg, tok, entropy=1), ears.token_logprobs(logits, t, entropy=True))
+    same(ears.top_logits(xg, 4), ears.top_logits(transposed, 4))
+    same(ears.top_logits(xg, 4), [t.squeeze(0) for t in ears.top_logits(xg.unsqueeze(0), torch.tensor(4).item(), 1)])
+
+
+def test_calls_that_are_refused(ears):
+    x = torch.zeros(3, 50, device=DEV)
+    tok, f = torch.zeros(3, dtype=torch.int32, device=DEV), torch.zeros(3, device=DEV)
+    teacher = ears.top_logits(x, 4)
+    for bad in (0.0, -1.0, float("nan"), float("inf")):
+        with pytest.raises(ears.EarsError):
+            ears.token_logprobs(x, tok, bad)
+    for k in (0, 129, -3):
+        with pytest.raises(ValueError):
+            ears.top_logits(x, k)
+    with pytest.raises(ValueError):
+        ears.token_logprobs(x, tok[:2])
+    with pytest.raises(ValueError):
+        ears.token_logprobs(x, tok.cpu())
+    with pytest.raises(TypeError):
+        ears.token_logprobs(x, f)
+    with pytest.raises(ValueError):
+        ears.distill_loss(x, teacher, kind="no such kind")
+    with pytest.raises(ears.EarsError):
+        ears.distill_loss(x, teacher, kind="jsd", mix=1.0)
+    with pytest.raises(ears.EarsError):
+        ears.distill_loss(x, ears.TopLogits(teacher.values, teacher.ids, None), kind="reverse_kl")
+    with pytest.raises(ears.EarsError):
+        ears.policy_loss(x, tok, f, f, kl_coef=0.1)
+    with pytest.raises(ValueError):
+        ears.token_logprobs_step(x, tok, f, out_grad=torch.zeros(3, 51, device=DEV))
+    with pytest.raises(ears.EarsError):                               # rows that share memory
+        ears.token_logprobs_step(x, tok, f, out_grad=torch.zeros(50, device=DEV).expand(3, 50))
+    with pytest.raises(ears.EarsError):                               # overlaps the logits in part
+        buf = torch.zeros(200, device=DEV)
+        ears.token_logprobs_step(buf[:150].view(3, 50), tok, f, out_grad=buf[50:].view(3, 50))
+    with pytest.raises(ValueError):
+        ears.top_logits(x[:0], 2)
+    with pytest.raises(ValueError):
+        ears.top_logits(x, 2, status=torch.zeros(1, device=DEV))
+
+
 def test_autograd_matches_the_step_and_notices_changed_logits(ears):
     n, V = 6, 9001
     x, g = logits(n, V, "bf16", 16)
