@@ -155,7 +155,7 @@ __device__ __forceinline__ void distill_scalars(const DistillParams& p, ListSmem
     // Z relative to M
     const double td = dr.xm > -INFINITY ? (dr.xm - M) * invT : 0.0, fd = exp(td);
     const double tt = has_tail ? ((double)tail.m - M) * invT : 0.0;
-    const double zt = has_tail ? exp(tt) * (double)tail.s : 0.0;
+    const double mass = row_mass(tail.s), zt = has_tail ? exp(tt) * mass : 0.0;
     const double Z = dr.sum * fd + zt, invZ = 1.0 / Z;
     const double rho = zt * invZ;
 #pragma unroll
@@ -183,7 +183,7 @@ __device__ __forceinline__ void distill_scalars(const DistillParams& p, ListSmem
             }
         }
         // relative to the tail's own maximum: nothing underflows before the product
-        const double f = has_tail ? gt / (double)tail.s : 0.0;
+        const double f = has_tail ? gt / mass : 0.0;
         finite = __all_sync(0xffffffffu, finite) && isfinite(f);
         ok = ok && finite;
         if (lane == 0) {
@@ -204,7 +204,7 @@ __device__ __forceinline__ void distill_scalars(const DistillParams& p, ListSmem
         }
     }
     const double lnZ = log(Z);
-    const double ln_rho = has_tail ? tt + log((double)tail.s) - lnZ : -INFINITY;
+    const double ln_rho = has_tail ? tt + log(mass) - lnZ : -INFINITY;
     const double ln_rt = log(rt);
 #pragma unroll
     for (int i = 0; i < kTopPer; ++i) lq[i] = dr.lq[i] + td - lnZ;
@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(kLThreads) ears_distill_kernel(const DistillPa
     if (MODE == kForward) return;
     __syncthreads();
     const bool zero = sm.zero != 0;
-    dense_pass<E, false>(s, grad, zero, empty ? 0.f : st.m, r.c, sm.factor, 0.f);
+    dense_pass<E, false>(s, grad, zero, empty ? 0.f : st.m, r.c.near, sm.factor, 0.f);
     if (zero) return;
     __syncthreads();   // the dense values of the listed entries have been written
     if (tid < k && sm.col[tid] >= 0 && in_slice(s, sm.col[tid])) store_entry(grad + s.lead + sm.col[tid], sm.entry[tid]);
@@ -515,7 +515,7 @@ __global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(c
     const Part st = exchange_parts<false, kRingWarps>(a, xs, C, r.rank, r.c);
     asm volatile("bar.sync 1, %0;" ::"n"(kRingConsumers + 32) : "memory");   // the scalars
     const bool zero = sm.zero != 0;
-    ring_gradient<E, false>(ring, s, grad, zero, tail_empty(st) ? 0.f : st.m, r.c, sm.factor, 0.f, drop, p.status);
+    ring_gradient<E, false>(ring, s, grad, zero, tail_empty(st) ? 0.f : st.m, r.c.near, sm.factor, 0.f, drop, p.status);
     if (zero) return;
     asm volatile("bar.sync 2, %0;" ::"n"(kRingConsumers) : "memory");   // the dense values of the listed entries have been written
     if (tid < k && sm.col[tid] >= 0 && in_slice(s, sm.col[tid])) store_entry(grad + s.lead + sm.col[tid], sm.entry[tid]);

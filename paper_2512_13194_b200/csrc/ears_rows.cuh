@@ -9,7 +9,9 @@
 //
 // Statistics are (m, s, w): the maximum, s = sum 2^t and, where the entropy is wanted, w = sum 2^t t
 // with t = (l - m) c, c = log2(e) / temperature.  The difference is taken before the product: every t
-// is <= 0 and neither masks of the type's lowest value nor rows made of nothing else overflow it.
+// is <= 0 and neither masks of the type's lowest value nor rows made of nothing else overflow it.  c enters in
+// two parts: rounded to 32 bits it would be off by up to 6e-8, the same in every term, and a row's log normaliser
+// by that times its mean |t| (13 and more), against 1e-7 from everything else.
 #pragma once
 #include "ears_cluster.cuh"
 #include "ears_common.cuh"
@@ -39,6 +41,26 @@ struct RowSpan {           // rows r = b R + k of [B, R, V] with strides in entr
     int slice;             // vectors per CTA (a multiple of kSliceAlign)
 };
 constexpr int kSliceAlign = 8;   // 128-byte lines are not shared between slices
+
+// c = log2(e) / temperature: hi < c and lo = c - hi > 0 (a masked entry's -inf times lo must stay -inf), and the
+// nearest 32-bit value.
+struct Scale { float hi, lo, near; };
+
+__device__ __forceinline__ Scale make_scale(double T) {
+    const double c = kLog2e / T;
+    Scale s;
+    s.hi = __double2float_rd(c);
+    if ((double)s.hi == c) s.hi = __uint_as_float(__float_as_uint(s.hi) - 1u);
+    s.lo = (float)(c - (double)s.hi);
+    s.near = (float)c;
+    return s;
+}
+__device__ __forceinline__ float scaled(float d, const Scale& c) { return __fmaf_rn(d, c.hi, d * c.lo); }
+
+// The special-function unit's exp2 falls short by this much on average (measured over the fractions; single results by
+// up to 2^-22 either way): added to sums of it, all but the maximum's own term, which is exactly 1.
+constexpr double kEx2Short = 1.25e-7;
+__device__ __forceinline__ double row_mass(float s) { return (double)s + kEx2Short * ((double)s - 1.0); }
 
 // The vectors of one row that one CTA handles.
 template <typename E>
@@ -158,15 +180,15 @@ __device__ __forceinline__ f32x2 clamp_masked(f32x2 t) {
     return pack2(fmaxf(lo, kMaskedT), fmaxf(hi, kMaskedT));
 }
 
-// G vectors: the maximum first, one rescale of the sums if it grew, then per entry a subtraction,
-// a multiplication, an exp2 and an addition, all but the exp2 on pairs.
+// G vectors: the maximum first, one rescale of the sums if it grew, then per entry a subtraction, a
+// multiplication, a multiply-add, an exp2 and an addition, all but the exp2 on pairs.
 // -> the vectors' maximum.
 template <typename E, int G, bool ENT>
-__device__ __forceinline__ float stat_fold(const uint4 (&w)[G], float c, Stat<ENT>& a) {
+__device__ __forceinline__ float stat_fold(const uint4 (&w)[G], const Scale& c, Stat<ENT>& a) {
     constexpr int PN = Words<E>::N / 2;
     const float cm = Words<E>::template vmax_all<G>(w);
     if (cm > a.m) {
-        const float dl = a.m == -INFINITY ? 0.f : fmaxf((a.m - cm) * c, kMaskedT);
+        const float dl = a.m == -INFINITY ? 0.f : fmaxf(scaled(a.m - cm, c), kMaskedT);
         const float sc = a.m == -INFINITY ? 0.f : ex2_approx(dl);
         const f32x2 sc2 = pack2(sc, sc), dl2 = pack2(dl, dl);
 #pragma unroll
@@ -177,18 +199,31 @@ __device__ __forceinline__ float stat_fold(const uint4 (&w)[G], float c, Stat<EN
         a.m = cm;
     }
     const float ref = a.m == -INFINITY ? 0.f : a.m;
-    const f32x2 c2 = pack2(c, c), nr2 = pack2(-ref, -ref);
+    const f32x2 c2 = pack2(c.hi, c.hi), l2 = pack2(c.lo, c.lo), nr2 = pack2(-ref, -ref);
+    // The call's terms are added up among themselves first, in eight lanes: a row with one large entry (a sum of 1.01, say)
+    // would otherwise lose most of its small terms, each below half a step of the running sum.
+    f32x2 ns[4], nw[ENT ? 2 : 1];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) ns[q] = pack2(0.f, 0.f);
+    nw[0] = nw[ENT ? 1 : 0] = pack2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < G; ++j) {
         f32x2 p[PN];
         Words<E>::pairs(w[j], p);
 #pragma unroll
         for (int i = 0; i < PN; ++i) {
-            const f32x2 t = mul2(add2(p[i], nr2), c2);
+            const f32x2 d = add2(p[i], nr2), t = fma2(d, c2, mul2(d, l2));
             const f32x2 e = ex2_pair(t);
-            a.s[i & 1] = add2(a.s[i & 1], e);
-            if (ENT) a.w[i & 1] = fma2(e, clamp_masked(t), a.w[i & 1]);
+            f32x2& lane = ns[(j * PN + i) & 3];
+            lane = add2(lane, e);
+            if (ENT) nw[i & 1] = fma2(e, clamp_masked(t), nw[i & 1]);
         }
+    }
+    a.s[0] = add2(a.s[0], add2(ns[0], ns[2]));
+    a.s[1] = add2(a.s[1], add2(ns[1], ns[3]));
+    if (ENT) {
+        a.w[0] = add2(a.w[0], nw[0]);
+        a.w[ENT ? 1 : 0] = add2(a.w[ENT ? 1 : 0], nw[ENT ? 1 : 0]);
     }
     return cm;
 }
@@ -197,11 +232,11 @@ __device__ __forceinline__ float stat_fold(const uint4 (&w)[G], float c, Stat<EN
 struct Part { float m, s, w; };
 
 // Merges the 32 lanes' parts; all lanes get the result.
-__device__ __forceinline__ Part merge_lanes(Part a, float c, bool ent) {
+__device__ __forceinline__ Part merge_lanes(Part a, const Scale& c, bool ent) {
     float M = a.m;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
-    const float dl = a.m == -INFINITY ? 0.f : fmaxf((a.m - M) * c, kMaskedT);   // nothing seen: s is 0, or NaN
+    const float dl = a.m == -INFINITY ? 0.f : fmaxf(scaled(a.m - M, c), kMaskedT);   // nothing seen: s is 0, or NaN
     const float sc = exp2f(dl);   // full precision: the factor scales a whole part
     a.w = ent ? sc * __fmaf_rn(dl, a.s, a.w) : 0.f;
     a.s *= sc;
@@ -222,7 +257,7 @@ __device__ __forceinline__ void cluster_wait_peers() {
 
 // One warp: the n parts that the exchange left in xs -> the row's; the same in every warp and CTA.
 template <bool ENT>
-__device__ __forceinline__ Part merge_parts(const float4* xs, int n, float c) {
+__device__ __forceinline__ Part merge_parts(const float4* xs, int n, const Scale& c) {
     const int lane = threadIdx.x & 31;
     Part q{-INFINITY, 0.f, 0.f};
     if (n <= 32) {
@@ -231,7 +266,7 @@ __device__ __forceinline__ Part merge_parts(const float4* xs, int n, float c) {
         // lane i takes parts i, i + 32, ..
         for (int i = lane; i < n; i += 32) q.m = fmaxf(q.m, xs[i].x);
         for (int i = lane; i < n; i += 32) {
-            const float dl = xs[i].x == -INFINITY ? 0.f : fmaxf((xs[i].x - q.m) * c, kMaskedT);
+            const float dl = xs[i].x == -INFINITY ? 0.f : fmaxf(scaled(xs[i].x - q.m, c), kMaskedT);
             const float sc = exp2f(dl);
             if (ENT) q.w += sc * __fmaf_rn(dl, xs[i].y, xs[i].z);
             q.s = __fmaf_rn(sc, xs[i].y, q.s);
@@ -243,7 +278,7 @@ __device__ __forceinline__ Part merge_parts(const float4* xs, int n, float c) {
 // Every warp's part goes to every CTA of the cluster through distributed shared memory; after one
 // barrier every warp merges the same C x WARPS parts in the same order, so all CTAs hold identical bits.
 template <bool ENT, int WARPS = kLWarps>
-__device__ __forceinline__ Part exchange_parts(const Stat<ENT>& a, float4* xs /* [kLMaxCluster * WARPS] */, int C, int rank, float c) {
+__device__ __forceinline__ Part exchange_parts(const Stat<ENT>& a, float4* xs /* [kLMaxCluster * WARPS] */, int C, int rank, const Scale& c) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     float s0, s1, w0 = 0.f, w1 = 0.f;
     unpack2(add2(a.s[0], a.s[1]), s0, s1);
@@ -384,7 +419,7 @@ __device__ __forceinline__ bool in_slice(const Slice<E>& s, int col) {
 }
 
 // ---- what every kernel does first ---------------------------------------------------------------
-struct RowSetup { long long row; unsigned b, k; int rank; double T; float c; bool T_ok; };
+struct RowSetup { long long row; unsigned b, k; int rank; double T; Scale c; bool T_ok; };
 
 __device__ __forceinline__ RowSetup row_setup_at(const RowSpan& p, unsigned row) {   // rows fit 32 bits
     RowSetup r;
@@ -393,8 +428,8 @@ __device__ __forceinline__ RowSetup row_setup_at(const RowSpan& p, unsigned row)
     r.b = row / (unsigned)p.R;
     r.k = row - r.b * (unsigned)p.R;
     r.T = p.seq_T ? (double)__ldg(p.seq_T + r.b) : p.T;
-    r.c = (float)(kLog2e / r.T);
-    r.T_ok = r.T > 0.0 && r.T < (double)INFINITY && r.c < INFINITY;
+    r.c = make_scale(r.T);
+    r.T_ok = r.T > 0.0 && r.T < (double)INFINITY && r.c.near < INFINITY;
     return r;
 }
 

@@ -49,7 +49,7 @@ __device__ __forceinline__ void short_load(const Slice<E>& s, int tid, ShortRow<
 }
 
 template <typename E, int G, bool ENT>
-__device__ __forceinline__ Stat<ENT> short_stats(const ShortRow<E>& x, float c) {
+__device__ __forceinline__ Stat<ENT> short_stats(const ShortRow<E>& x, const Scale& c) {
     Stat<ENT> a;
     stat_open(a);
     stat_fold<E, kShortSlots, ENT>(x.w, c, a);
@@ -91,7 +91,7 @@ __device__ __forceinline__ void short_zero(const Slice<E>& s, int tid, E* g) {
 
 // The statistics of the whole row, in every thread.
 template <int G, bool ENT>
-__device__ __forceinline__ Part short_merge(const Stat<ENT>& a, float4* xs, float c) {
+__device__ __forceinline__ Part short_merge(const Stat<ENT>& a, float4* xs, const Scale& c) {
     float s0, s1, w0 = 0.f, w1 = 0.f;
     unpack2(add2(a.s[0], a.s[1]), s0, s1);
     if (ENT) unpack2(add2(a.w[0], a.w[ENT ? 1 : 0]), w0, w1);
@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas)
     if (MODE == kForward) return;
     row_sync<G>();
     const TokenScalars t = sc;
-    short_gradient<E, G, ENT>(s, tid, grad, x, t.zero != 0, st.m, r.c, t.A, t.Bt);
+    short_gradient<E, G, ENT>(s, tid, grad, x, t.zero != 0, st.m, r.c.near, t.A, t.Bt);
     if (t.zero) return;
     row_sync<G>();   // the dense value of the token's entry has been written
     if (tid == 0) store_entry(grad + s.lead + tok, t.entry);
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas)
     if (MODE == kForward) return;
     row_sync<G>();
     const bool zero = sm.zero != 0;
-    short_gradient<E, G, false>(s, tid, grad, x, zero, empty ? 0.f : st.m, r.c, sm.factor, 0.f);
+    short_gradient<E, G, false>(s, tid, grad, x, zero, empty ? 0.f : st.m, r.c.near, sm.factor, 0.f);
     if (zero) return;
     row_sync<G>();   // the dense values of the listed entries have been written
     for (int j = tid; j < k; j += G)
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(ShortShape<32>::kThreads, ShortShape<32>::kCta
     }
     const bool ok = live && r.T_ok && rowstat_ok(st.m, st.s);
     if (lane == 0) {
-        p.out_lse[r.row] = !live ? -INFINITY : ok ? (float)((double)st.m / r.T + log((double)st.s)) : __int_as_float(0x7fc00000);
+        p.out_lse[r.row] = !live ? -INFINITY : ok ? (float)((double)st.m / r.T + log(row_mass(st.s))) : __int_as_float(0x7fc00000);
         if (live && !ok && p.status) atomicOr(p.status, kDevInvalidInput);
         sm.total = 0;
     }

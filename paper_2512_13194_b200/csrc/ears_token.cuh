@@ -71,9 +71,9 @@ template <bool ENT, int MODE>
 __device__ __forceinline__ TokenScalars token_scalars(const TokenParams& p, long long row, int rank, double T, bool T_ok, const TokenInputs& in, Part st) {
     const float lt = in.lt;
     const bool ok = T_ok && rowstat_ok(st.m, st.s) && (!ENT || st.w == st.w);
-    const double Z = st.s, lnZ = log(Z), invT = 1.0 / T;
+    const double Z = row_mass(st.s), lnZ = log(Z), invT = 1.0 / T;
     double logp = ((double)lt - (double)st.m) * invT - lnZ;
-    double H = ENT ? lnZ - kLn2 * (double)st.w / Z : 0.0;
+    double H = ENT ? lnZ - kLn2 * ((1.0 + kEx2Short) * (double)st.w) / Z : 0.0;
     double loss = 0.0, kl = 0.0, g = 0.0, h = 0.0;
     bool fine = ok;
     if (p.policy) {
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kLThreads) ears_token_kernel(const TokenParams
     }
     __syncthreads();
     const TokenScalars t = sc;
-    dense_pass<E, ENT>(s, grad, t.zero != 0, st.m, r.c, t.A, t.Bt);
+    dense_pass<E, ENT>(s, grad, t.zero != 0, st.m, r.c.near, t.A, t.Bt);
     if (!t.zero && in_slice(s, tok)) {
         __syncthreads();   // the dense value of this entry has been written
         if (threadIdx.x == 0) store_entry(grad + s.lead + tok, t.entry);
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) ears_token_step_kernel(const 
     if (tid == 0) sc = token_scalars<ENT, kStep>(p, r.row, r.rank, r.T, r.T_ok, in, st);
     ring_sync_consumers();
     const TokenScalars t = sc;
-    ring_gradient<E, ENT>(ring, s, grad, t.zero != 0, st.m, r.c, t.A, t.Bt, drop, p.status);
+    ring_gradient<E, ENT>(ring, s, grad, t.zero != 0, st.m, r.c.near, t.A, t.Bt, drop, p.status);
     if (!t.zero && in_slice(s, tok)) {
         ring_sync_consumers();   // the dense value of this entry has been written
         if (tid == 0) store_entry(grad + s.lead + tok, t.entry);

@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(kLThreads, 4) ears_top_kernel(const TopParams 
     const Part st = exchange_parts<false>(a, sm.xs, p.rows.C, r.rank, r.c);
     const bool ok = r.T_ok && rowstat_ok(st.m, st.s);
     if (r.rank == 0 && tid == 0) {
-        p.out_lse[r.row] = ok ? (float)((double)st.m / r.T + log((double)st.s)) : __int_as_float(0x7fc00000);
+        p.out_lse[r.row] = ok ? (float)((double)st.m / r.T + log(row_mass(st.s))) : __int_as_float(0x7fc00000);
         if (!ok && p.status) atomicOr(p.status, kDevInvalidInput);
     }
     const int C = p.rows.C;
