@@ -388,7 +388,7 @@ __device__ __forceinline__ bool tail_empty(Part st) { return st.m == -INFINITY &
 
 // Forward and backward calls: one sweep, straight from memory.
 template <typename E, int MODE>
-__global__ void __launch_bounds__(kLThreads) ears_distill_kernel(const DistillParams p) {
+__global__ void __launch_bounds__(kLThreads, 4) ears_distill_kernel(const DistillParams p) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     __shared__ ListSmem sm;
     __shared__ float4 xs[kLMaxCluster * kLWarps];

@@ -146,7 +146,7 @@ __device__ __forceinline__ void token_unused(const TokenParams& p, long long row
 
 // Forward and backward calls: one sweep, straight from memory.
 template <typename E, bool ENT, int MODE>
-__global__ void __launch_bounds__(kLThreads) ears_token_kernel(const TokenParams p) {
+__global__ void __launch_bounds__(kLThreads, 4) ears_token_kernel(const TokenParams p) {
     __shared__ float4 xs[kLMaxCluster * kLWarps];
     __shared__ TokenScalars sc;
     const RowSetup r = row_setup(p.rows);
