@@ -182,11 +182,10 @@ __device__ __forceinline__ f32x2 clamp_masked(f32x2 t) {
 
 // G vectors: the maximum first, one rescale of the sums if it grew, then per entry a subtraction, a
 // multiplication, a multiply-add, an exp2 and an addition, all but the exp2 on pairs.
-// -> the vectors' maximum.
+// cm: the vectors' maximum.
 template <typename E, int G, bool ENT>
-__device__ __forceinline__ float stat_fold(const uint4 (&w)[G], const Scale& c, Stat<ENT>& a) {
+__device__ __forceinline__ void stat_add(const uint4 (&w)[G], float cm, const Scale& c, Stat<ENT>& a) {
     constexpr int PN = Words<E>::N / 2;
-    const float cm = Words<E>::template vmax_all<G>(w);
     if (cm > a.m) {
         const float dl = a.m == -INFINITY ? 0.f : fmaxf(scaled(a.m - cm, c), kMaskedT);
         const float sc = a.m == -INFINITY ? 0.f : ex2_approx(dl);
@@ -225,7 +224,10 @@ __device__ __forceinline__ float stat_fold(const uint4 (&w)[G], const Scale& c, 
         a.w[0] = add2(a.w[0], nw[0]);
         a.w[ENT ? 1 : 0] = add2(a.w[ENT ? 1 : 0], nw[ENT ? 1 : 0]);
     }
-    return cm;
+}
+template <typename E, int G, bool ENT>
+__device__ __forceinline__ void stat_fold(const uint4 (&w)[G], const Scale& c, Stat<ENT>& a) {
+    stat_add<E, G, ENT>(w, Words<E>::template vmax_all<G>(w), c, a);
 }
 
 // The statistics of a part: what one warp hands on, and what the whole row ends with.

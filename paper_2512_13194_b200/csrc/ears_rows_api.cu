@@ -187,6 +187,14 @@ int launch_short(void (*kernel)(P), P p, int threads_per_row, cudaStream_t strea
     return e == cudaSuccess ? EARS_OK : host_cuda_fail(e, what);
 }
 
+// Rows that a warp streams (ears_top_warp_kernel): when there are more of them than CTAs fit on the device at once, four per
+// SM; fewer are done sooner by a CTA each.
+bool top_by_warps(const RowSpan& r) {
+    int sms = 0;
+    if (g_row_cluster.load(std::memory_order_relaxed) || host_device_sms(&sms) != EARS_OK) return false;
+    return r.vectors <= 32 * kShortSlots * kWarpTopRounds && r.rows > 4ll * sms;
+}
+
 template <int MODE>
 int launch_token_short(int dtype, const TokenParams& p, bool ent, int g, void* stream) {
     return with_type(dtype, [&](auto* e) {
@@ -316,6 +324,11 @@ int ears_top_logits(int dtype, const void* logits, int B, int R, int V, int64_t 
         return with_type(dtype, [&](auto* e) {
             return launch_short(ears_top_short_kernel<std::remove_pointer_t<decltype(e)>>, p, 32, (cudaStream_t)stream,
                                 "ears_top_short_kernel launch");
+        });
+    if (top_by_warps(p.rows))
+        return with_type(dtype, [&](auto* e) {
+            return launch_short(ears_top_warp_kernel<std::remove_pointer_t<decltype(e)>>, p, 32, (cudaStream_t)stream,
+                                "ears_top_warp_kernel launch");
         });
     return with_type(dtype, [&](auto* e) {
         return launch_rows(ears_top_kernel<std::remove_pointer_t<decltype(e)>>, p, kLThreads, 0, (cudaStream_t)stream, "ears_top_kernel launch");

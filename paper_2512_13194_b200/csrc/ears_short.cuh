@@ -202,6 +202,28 @@ constexpr int kShortTopBuf = 256;            // candidates per row; kMaxTop and 
 
 struct ShortTopSmem { alignas(16) top_key buf[kShortTopBuf]; int total; };
 
+// One warp: the candidates buf[0 .. n) to their ranks below k, absent entries behind them.
+__device__ __forceinline__ void write_ranked(top_key* buf, int n, int k, float* values, int32_t* ids) {
+    const int lane = threadIdx.x & 31;
+    if (lane == 0 && (n & 1)) buf[n] = 0ull;   // kShortTopBuf is even
+    __syncwarp();
+    const ulonglong2* pairs = reinterpret_cast<const ulonglong2*>(buf);
+    for (int at = lane; at < n; at += 32) {
+        const top_key mine = buf[at];
+        int rank = 0;
+#pragma unroll 4
+        for (int j = 0; j < (n + 1) / 2; ++j) {
+            const ulonglong2 q = pairs[j];
+            rank += (q.x > mine) + (q.y > mine);
+        }
+        if (rank < k) {
+            values[rank] = unorder_bits((uint32_t)(mine >> 32));
+            ids[rank] = (int32_t)~(uint32_t)mine;
+        }
+    }
+    for (int j = n + lane; j < k; j += 32) { values[j] = -INFINITY; ids[j] = -1; }   // fewer than k finite entries
+}
+
 template <typename E>
 __global__ void __launch_bounds__(ShortShape<32>::kThreads, ShortShape<32>::kCtas) ears_top_short_kernel(const TopParams p) {
     constexpr int N = Words<E>::N;
@@ -323,23 +345,186 @@ __global__ void __launch_bounds__(ShortShape<32>::kThreads, ShortShape<32>::kCta
         __syncwarp();
         n = min(above, k);
     }
-    if (lane == 0 && (n & 1)) sm.buf[n] = 0ull;   // kShortTopBuf is even
-    __syncwarp();
-    const ulonglong2* pairs = reinterpret_cast<const ulonglong2*>(sm.buf);
-    for (int at = lane; at < n; at += 32) {
-        const top_key mine = sm.buf[at];
-        int rank = 0;
-#pragma unroll 4
-        for (int j = 0; j < (n + 1) / 2; ++j) {
-            const ulonglong2 q = pairs[j];
-            rank += (q.x > mine) + (q.y > mine);
+    write_ranked(sm.buf, n, k, values, ids);
+}
+
+// ---- top logits of many rows of middling length: a warp streams its row -------------------------------
+// The CTA-wide kernel spends some 10 us on a row whatever its length, with four rows in flight per SM; here 24 are.
+constexpr int kWarpTopRounds = 8;            // of 32 lanes x kShortSlots vectors: rows up to 32 KB
+constexpr int kWarpTopReach = 384;           // vectors fetched again
+
+struct WarpTopSmem {
+    alignas(16) top_key buf[kShortTopBuf];
+    uint4 peak[kWarpTopRounds][32];          // upper halves of the vectors' maxima, eight a round and lane
+    uint16_t reach[kWarpTopReach];
+    int total, vectors;
+};
+
+__device__ __forceinline__ float peak_of(uint4 p, int j) {
+    const uint32_t two = j < 2 ? p.x : j < 4 ? p.y : j < 6 ? p.z : p.w;
+    return __uint_as_float(j & 1 ? two & 0xffff0000u : two << 16);
+}
+
+// Too many entries reach the threshold: the k-th largest value bit by bit, then all entries above it and the first
+// equal ones, the row fetched again for every bit.  -> entries in buf, exactly k.
+template <typename E>
+__device__ __noinline__ int warp_top_exact(const Slice<E>& s, WarpTopSmem& sm, int k) {
+    constexpr int N = Words<E>::N;
+    const int lane = threadIdx.x & 31;
+    uint32_t u = 0;
+    for (int b = 31; b >= 0; --b) {
+        const uint32_t t = u | 1u << b;
+        int c = 0;
+        for (int v = lane; v < s.n; v += 32) {
+            float x[N];
+            Words<E>::unpack(slice_vector(s, v), x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) c += order_bits(x[i]) >= t ? 1 : 0;
         }
-        if (rank < k) {
-            values[rank] = unorder_bits((uint32_t)(mine >> 32));
-            ids[rank] = (int32_t)~(uint32_t)mine;
+        if (__reduce_add_sync(0xffffffffu, c) >= k) u = t;
+    }
+    int above = 0, equal = 0;   // entries above the value so far, equal ones so far, in the order of the columns
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int v0 = 0; v0 < s.n; v0 += 32) {
+            const int v = v0 + lane;
+            const uint4 w = v < s.n ? slice_vector(s, v) : Words<E>::minus_inf();
+            float x[N];
+            Words<E>::unpack(w, x);
+            int mine = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) mine += (pass == 0 ? order_bits(x[i]) > u : order_bits(x[i]) == u) ? 1 : 0;
+            int sum = mine;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, sum, off);
+                if (lane >= off) sum += o;
+            }
+            int at = above + (pass == 0 ? 0 : equal) + sum - mine;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (pass == 0 ? order_bits(x[i]) > u : order_bits(x[i]) == u) {
+                    if (at < k) sm.buf[at] = make_key(x[i], v * N + i - s.lead);
+                    ++at;
+                }
+            }
+            const int all = __shfl_sync(0xffffffffu, sum, 31);
+            if (pass == 0) above += all; else equal += all;
         }
     }
-    for (int j = n + lane; j < k; j += 32) { values[j] = -INFINITY; ids[j] = -1; }   // fewer than k finite entries
+    __syncwarp();
+    return min(above + equal, k);
+}
+
+template <typename E>
+__global__ void __launch_bounds__(ShortShape<32>::kThreads, ShortShape<32>::kCtas) ears_top_warp_kernel(const TopParams p) {
+    constexpr int N = Words<E>::N;
+    __shared__ WarpTopSmem rows[ShortShape<32>::kRows];
+    RowSetup r;
+    if (!short_setup<32>(p.rows, &r)) return;
+    const int lane = threadIdx.x & 31, k = p.k;
+    WarpTopSmem& sm = rows[threadIdx.x / 32];
+    float* values = p.out_values + r.row * k;
+    int32_t* ids = p.out_ids + r.row * k;
+    const bool live = !p.accept_len || (int)r.k <= __ldg(p.accept_len + r.b);
+    const Slice<E> s = make_slice<E>(row_ptr<E>(p.rows, r), p.rows.V, p.rows.slice, 0);
+    const int rounds = live ? (s.n + 32 * kShortSlots - 1) / (32 * kShortSlots) : 0;
+    Stat<false> a;
+    stat_open(a);
+    float best[kShortSlots];   // of the vectors at the same place of every round
+#pragma unroll
+    for (int j = 0; j < kShortSlots; ++j) best[j] = -INFINITY;
+    for (int round = 0; round < rounds; ++round) {
+        uint4 w[kShortSlots];
+        uint32_t half[kShortSlots];
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < kShortSlots; ++j) {
+            const int v = (round * kShortSlots + j) * 32 + lane;
+            w[j] = Words<E>::minus_inf();
+            if (v < s.n) w[j] = slice_vector(s, v);
+        }
+#pragma unroll
+        for (int j = 0; j < kShortSlots; ++j) {
+            const uint4 one[1] = {w[j]};
+            const float m = Words<E>::template vmax_all<1>(one);
+            half[j] = __float_as_uint(m);
+            best[j] = fmaxf(best[j], m);
+            top = fmaxf(top, m);
+        }
+        sm.peak[round][lane] = make_uint4(__byte_perm(half[0], half[1], 0x7632), __byte_perm(half[2], half[3], 0x7632),
+                                          __byte_perm(half[4], half[5], 0x7632), __byte_perm(half[6], half[7], 0x7632));
+        stat_add<E, kShortSlots, false>(w, top, r.c, a);
+    }
+    const Part st = short_merge<32, false>(a, nullptr, r.c);
+    const bool ok = live && r.T_ok && rowstat_ok(st.m, st.s);
+    if (lane == 0) {
+        p.out_lse[r.row] = !live ? -INFINITY : ok ? (float)((double)st.m / r.T + log(row_mass(st.s))) : __int_as_float(0x7fc00000);
+        if (live && !ok && p.status) atomicOr(p.status, kDevInvalidInput);
+        sm.total = sm.vectors = 0;
+    }
+    __syncwarp();
+    if (!ok) {
+        for (int j = lane; j < k; j += 32) { values[j] = -INFINITY; ids[j] = -1; }
+        return;
+    }
+    uint32_t bv[kShortSlots];
+#pragma unroll
+    for (int j = 0; j < kShortSlots; ++j) bv[j] = order_bits(best[j]) >> 16;
+    const float reach = unorder_bits(warp_kth(bv, kShortSlots, k) << 16);
+    // the lane's own vectors that reach it
+    int mine = 0;
+    for (int round = 0; round < rounds; ++round) {
+        const uint4 q = sm.peak[round][lane];
+#pragma unroll
+        for (int j = 0; j < kShortSlots; ++j) mine += peak_of(q, j) >= reach ? 1 : 0;
+    }
+    int place = warp_reserve(mine, &sm.vectors);
+    if (mine > 0 && place + mine <= kWarpTopReach) {
+        for (int round = 0; round < rounds; ++round) {
+            const uint4 q = sm.peak[round][lane];
+#pragma unroll
+            for (int j = 0; j < kShortSlots; ++j)
+                if (peak_of(q, j) >= reach) sm.reach[place++] = (uint16_t)((round * kShortSlots + j) * 32 + lane);
+        }
+    }
+    __syncwarp();
+    const int reached = sm.vectors;
+    int n = kShortTopBuf + 1;
+    if (reached <= kWarpTopReach) {
+        constexpr int BATCH = 4;
+        for (int q0 = 0; q0 < reached; q0 += 32 * BATCH) {
+            uint4 w[BATCH];
+            int v[BATCH], hits = 0;
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const int q = q0 + j * 32 + lane;
+                v[j] = q < reached ? sm.reach[q] : 0;
+                w[j] = q < reached ? slice_vector(s, v[j]) : Words<E>::minus_inf();
+            }
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                float x[N];
+                Words<E>::unpack(w[j], x);
+#pragma unroll
+                for (int i = 0; i < N; ++i) hits += x[i] >= reach ? 1 : 0;
+            }
+            int at = warp_reserve(hits, &sm.total);
+            if (hits > 0 && at + hits <= kShortTopBuf) {
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j) {
+                    float x[N];
+                    Words<E>::unpack(w[j], x);
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        if (x[i] >= reach) sm.buf[at++] = make_key(x[i], v[j] * N + i - s.lead);
+                }
+            }
+        }
+        __syncwarp();
+        n = sm.total;
+    }
+    if (n > kShortTopBuf) n = warp_top_exact(s, sm, k);
+    write_ranked(sm.buf, n, k, values, ids);
 }
 
 }  // namespace ears

@@ -5,9 +5,9 @@
 // complement of its index, all keys of a row are distinct, and the k largest keys are unique.
 //
 // One sweep of the slice yields the statistics of the row's softmax and, as a by-product, the maximum of
-// every group of entries that one thread held in registers together (64 of them; at most kTopRounds groups
-// per thread).  Of these maxima, folded to two per thread, the k-th largest is a threshold: at least k
-// entries reach it.  For rows in no particular order few others do (of G folded groups about G ln(G / (G - k))
+// every group of entries that one thread held in registers together (two vectors, 16 entries of two bytes; rounds
+// beyond kTopRounds share groups with earlier ones).  Of these maxima, folded to two per thread, the k-th largest is
+// a threshold: at least k entries reach it.  For rows in no particular order few others do (of G folded groups about G ln(G / (G - k))
 // entries: 147 for k = 128 and G = 512, 177 had each thread one, 137 four), so only the groups that reach it are
 // fetched again, and their entries are candidates.
 //   * the threshold is kept as the upper 16 bits of an ordered pattern, which is exact for bf16 and a little lower
@@ -27,10 +27,11 @@
 namespace ears {
 
 typedef unsigned long long top_key;
-constexpr int kTopBuf = 2048;                // candidates a CTA holds: 128 + 64 < 2048, so each offer takes one thread's at least
-constexpr int kTopRounds = 16;               // groups per thread: round r of the sweep counts to group r % kTopRounds
+constexpr int kTopBuf = 1024;                // candidates a CTA holds: 128 + 64 < 1024, so each offer takes one thread's at least
+constexpr int kTopRounds = 16;               // round r of the sweep counts to the groups of r % kTopRounds
+constexpr int kTopParts = 4;                 // groups per thread and round: two vectors each
 constexpr int kTopGroups = 1024;             // groups fetched again
-constexpr int kTopBatch = 10;                // groups fetched at a time by a warp
+constexpr int kTopBatch = 6;                 // groups fetched at a time by eight lanes: 192 by the CTA
 
 struct TopParams {
     RowSpan rows;
@@ -47,7 +48,7 @@ struct TopSmem {
     alignas(16) top_key buf[kTopBuf];
     union {
         top_key list[kLMaxCluster][kMaxTop];          // sorted lists of the cluster's CTAs
-        float group[kTopRounds][kLThreads];           // before them: the group maxima
+        uint2 group[kTopRounds][kLThreads];           // before them: the upper halves of the group maxima, four a round
     };
     float best[2 * kLThreads];
     int count[kLMaxCluster];
@@ -283,6 +284,13 @@ __device__ __noinline__ void offer_rounds(const Slice<E>& s, TopSmem& sm, int ro
     }
 }
 
+// Group q of a round: its maximum with the lower half of its bits cut off, which a threshold without those bits (or, below
+// zero, with all of them set) does not notice.
+__device__ __forceinline__ float group_max(uint2 g, int q) {
+    const uint32_t two = q < 2 ? g.x : g.y;
+    return __uint_as_float(q & 1 ? two & 0xffff0000u : two << 16);
+}
+
 template <typename E>
 __global__ void __launch_bounds__(kLThreads, 4) ears_top_kernel(const TopParams p) {
     __shared__ TopSmem sm;
@@ -306,10 +314,23 @@ __global__ void __launch_bounds__(kLThreads, 4) ears_top_kernel(const TopParams 
     const int rounds = (s.n + kLRound - 1) / kLRound, groups = min(rounds, kTopRounds);
     float best[2] = {-INFINITY, -INFINITY};   // the thread's group maxima, folded to those of even and of odd rounds
     sweep_rounds(s, pol, [&](uint4 (&w)[kLUnroll], int round) {
-        const float top = stat_fold<E, kLUnroll, false>(w, r.c, a);
-        float* g = &sm.group[round % kTopRounds][tid];
-        *g = round < kTopRounds ? top : fmaxf(*g, top);
+        float part[kTopParts];
+#pragma unroll
+        for (int q = 0; q < kTopParts; ++q) {
+            const uint4 two[2] = {w[2 * q], w[2 * q + 1]};
+            part[q] = Words<E>::template vmax_all<2>(two);
+        }
+        const float top = fmaxf(max3(part[0], part[1], part[2]), part[3]);
+        uint2* g = &sm.group[round % kTopRounds][tid];
+        if (round >= kTopRounds) {
+            const uint2 old = *g;
+#pragma unroll
+            for (int q = 0; q < kTopParts; ++q) part[q] = fmaxf(part[q], group_max(old, q));
+        }
+        *g = make_uint2(__byte_perm(__float_as_uint(part[0]), __float_as_uint(part[1]), 0x7632),
+                        __byte_perm(__float_as_uint(part[2]), __float_as_uint(part[3]), 0x7632));
         best[round & 1] = fmaxf(best[round & 1], top);
+        stat_add<E, kLUnroll, false>(w, top, r.c, a);
     });
     sm.best[tid] = best[0];
     sm.best[kLThreads + tid] = best[1];
@@ -326,26 +347,38 @@ __global__ void __launch_bounds__(kLThreads, 4) ears_top_kernel(const TopParams 
     const float reach = unorder_bits(t16 << 16);
     // the thread's own groups; false for NaN: the row is unusable anyway
     int mine = 0;
-    for (int i = 0; i < groups; ++i) mine += sm.group[i][tid] >= reach ? 1 : 0;
+    for (int i = 0; i < groups; ++i) {
+        const uint2 g = sm.group[i][tid];
+#pragma unroll
+        for (int q = 0; q < kTopParts; ++q) mine += group_max(g, q) >= reach ? 1 : 0;
+    }
     int place = warp_reserve(mine, &sm.groups);
-    if (mine > 0 && place + mine <= kTopGroups)
-        for (int i = 0; i < groups; ++i)
-            if (sm.group[i][tid] >= reach) sm.reach[place++] = (uint16_t)(i * kLThreads + tid);
+    if (mine > 0 && place + mine <= kTopGroups) {
+        for (int i = 0; i < groups; ++i) {
+            const uint2 g = sm.group[i][tid];
+#pragma unroll
+            for (int q = 0; q < kTopParts; ++q)
+                if (group_max(g, q) >= reach) sm.reach[place++] = (uint16_t)((i * kTopParts + q) * kLThreads + tid);
+        }
+    }
     __syncthreads();
     const int reached = sm.groups;
     if (reached <= kTopGroups) {
-        // a warp to a group, 32 lanes to its eight vectors, kTopBatch groups in flight
-        for (int q0 = tid / 32; q0 < reached; q0 += kTopBatch * kLWarps) {
+        // eight lanes to a group's two vectors, kTopBatch groups of theirs in flight
+        constexpr int TEAMS = kLThreads / 8;
+        for (int q0 = tid / 32 * 4; q0 < reached; q0 += kTopBatch * TEAMS) {   // the same for a warp
+            const int team = (tid & 31) / 8, sub = tid & 7;
             for (int turn = 0; turn < rounds; turn += kTopRounds) {   // once, unless a slice has more rounds than groups
                 uint32_t w[kTopBatch];
-                const auto entry = [&](int j) {   // of the run: vector, word lane % 4
-                    const int q = q0 + j * kLWarps, lane = tid & 31, g = q < reached ? sm.reach[q] : 0;
-                    return ((s.v0 + (turn + g / kLThreads) * kLRound + (lane / 4) * kLThreads + g % kLThreads) * 4 + lane % 4) * kTopWord<E>;
+                const auto entry = [&](int j) {   // of the run: vector, word sub % 4
+                    const int q = q0 + team + j * TEAMS, g = q < reached ? sm.reach[q] : 0;
+                    const int round = turn + g / (kTopParts * kLThreads), part = g / kLThreads % kTopParts;
+                    return ((s.v0 + round * kLRound + (2 * part + sub / 4) * kLThreads + g % kLThreads) * 4 + sub % 4) * kTopWord<E>;
                 };
 #pragma unroll
                 for (int j = 0; j < kTopBatch; ++j) {
                     w[j] = Words<E>::minus_inf().x;
-                    if (q0 + j * kLWarps < reached) {
+                    if (q0 + team + j * TEAMS < reached) {
                         const int e = entry(j);
                         if (e < (s.v0 + s.n) * Words<E>::N) w[j] = load_word(s, e);
                     }

@@ -126,6 +126,35 @@ def test_top_logits_of_short_rows_in_hard_orders(ears, dtype, name, V):
         close(top.lse, lse, LOG_TOL * 2)
 
 
+@pytest.mark.parametrize("dtype,V", [("bf16", 2100), ("bf16", 16370), ("fp16", 7001), ("fp32", 1100), ("fp32", 8181)])
+def test_top_logits_of_many_rows(ears, dtype, V):
+    """More rows than CTAs fit on the device at once, a few of them hard: those first and last are checked."""
+    n, k = 1300, 100
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn(n, V + 3, generator=g)
+    hard = [(0, "ascending"), (1, "constant"), (2, "two_values"), (3, "three_finite"), (n - 2, "signed_zeros"), (n - 1, "descending")]
+    for row, name in hard:
+        x[row, 2:2 + V] = PATTERNS[name](V)
+    x[5, 2:2 + V] = -math.inf
+    x[7, 9] = math.nan
+    x = x.to(DT[dtype])[:, 2:2 + V]
+    acc = torch.full((n,), 0, dtype=torch.int32)
+    acc[9] = -1
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    wide = torch.zeros(n, V + 3, dtype=DT[dtype], device=DEV)
+    wide[:, 2:2 + V] = x.to(DEV)
+    dev = wide[:, 2:2 + V].unsqueeze(1)
+    top = ears.top_logits(dev, k, 0.9, accept_len=acc.to(DEV), status=st)
+    assert int(st) == ears.DEV_INVALID_INPUT
+    bad = [5, 7]
+    assert torch.isnan(top.lse[bad, 0]).all() and (top.ids[bad + [9]] == -1).all() and float(top.lse[9, 0]) == -math.inf
+    pick = [r for r in list(range(0, 40)) + list(range(n - 40, n)) if r not in bad + [9]]
+    v, i, lse = R.top_logits(x[pick], k, 0.9)
+    assert torch.equal(top.ids[pick, 0].cpu().long(), i)
+    assert torch.equal(top.values[pick, 0].cpu().double(), v)
+    close(top.lse[pick, 0], lse, LOG_TOL * 2)
+
+
 def test_many_short_rows_and_rows_that_start_anywhere(ears):
     for dtype in ("fp32", "bf16"):
         for V in (3, 17, 700, 2030, 6001, 12001):
