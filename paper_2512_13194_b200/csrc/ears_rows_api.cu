@@ -187,12 +187,12 @@ int launch_short(void (*kernel)(P), P p, int threads_per_row, cudaStream_t strea
     return e == cudaSuccess ? EARS_OK : host_cuda_fail(e, what);
 }
 
-// Rows that a warp streams (ears_top_warp_kernel): when there are more of them than CTAs fit on the device at once, four per
-// SM; fewer are done sooner by a CTA each.
+// Rows that a warp streams (ears_top_warp_kernel): up to 4 KB, and up to 32 KB when there are more of them than CTAs fit on the
+// device at once, four per SM; fewer are done sooner by a CTA each.
 bool top_by_warps(const RowSpan& r) {
     int sms = 0;
     if (g_row_cluster.load(std::memory_order_relaxed) || host_device_sms(&sms) != EARS_OK) return false;
-    return r.vectors <= 32 * kShortSlots * kWarpTopRounds && r.rows > 4ll * sms;
+    return r.vectors <= 32 * kShortSlots || (r.vectors <= 32 * kShortSlots * kWarpTopRounds && r.rows > 4ll * sms);
 }
 
 template <int MODE>
@@ -320,11 +320,6 @@ int ears_top_logits(int dtype, const void* logits, int B, int R, int V, int64_t 
     EARS_TRY(make_span(c, false, &p.rows, 64u << 10));   // every CTA has a list of its own to sort
     p.k = k; p.accept_len = accept_len;
     p.out_values = out_values; p.out_ids = out_ids; p.out_lse = out_lse; p.status = status;
-    if (short_threads(p.rows) == 32)
-        return with_type(dtype, [&](auto* e) {
-            return launch_short(ears_top_short_kernel<std::remove_pointer_t<decltype(e)>>, p, 32, (cudaStream_t)stream,
-                                "ears_top_short_kernel launch");
-        });
     if (top_by_warps(p.rows))
         return with_type(dtype, [&](auto* e) {
             return launch_short(ears_top_warp_kernel<std::remove_pointer_t<decltype(e)>>, p, 32, (cudaStream_t)stream,

@@ -197,10 +197,12 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas)
         if (sm.col[j] >= 0) store_entry(grad + s.lead + sm.col[j], sm.entry[j]);
 }
 
-// ---- top logits of short rows: a warp per row -------------------------------------------------------
+// ---- top logits: a warp streams its row ----------------------------------------------------------------
+// The CTA-wide kernel spends some 10 us on a row whatever its length, with four rows in flight per SM; here 24 are
+// (8192 rows of 6000 bf16: 147 us and 50).
 constexpr int kShortTopBuf = 256;            // candidates per row; kMaxTop and more
-
-struct ShortTopSmem { alignas(16) top_key buf[kShortTopBuf]; int total; };
+constexpr int kWarpTopRounds = 8;            // of 32 lanes x kShortSlots vectors: rows up to 32 KB
+constexpr int kWarpTopReach = 384;           // vectors fetched again
 
 // One warp: the candidates buf[0 .. n) to their ranks below k, absent entries behind them.
 __device__ __forceinline__ void write_ranked(top_key* buf, int n, int k, float* values, int32_t* ids) {
@@ -223,135 +225,6 @@ __device__ __forceinline__ void write_ranked(top_key* buf, int n, int k, float* 
     }
     for (int j = n + lane; j < k; j += 32) { values[j] = -INFINITY; ids[j] = -1; }   // fewer than k finite entries
 }
-
-template <typename E>
-__global__ void __launch_bounds__(ShortShape<32>::kThreads, ShortShape<32>::kCtas) ears_top_short_kernel(const TopParams p) {
-    constexpr int N = Words<E>::N;
-    __shared__ ShortTopSmem rows[ShortShape<32>::kRows];
-    RowSetup r;
-    if (!short_setup<32>(p.rows, &r)) return;
-    const int lane = threadIdx.x & 31, k = p.k;
-    ShortTopSmem& sm = rows[threadIdx.x / 32];
-    float* values = p.out_values + r.row * k;
-    int32_t* ids = p.out_ids + r.row * k;
-    const bool live = !p.accept_len || (int)r.k <= __ldg(p.accept_len + r.b);
-    const Slice<E> s = make_slice<E>(row_ptr<E>(p.rows, r), p.rows.V, p.rows.slice, 0);
-    Part st{-INFINITY, 0.f, 0.f};
-    ShortRow<E> row;
-    if (live) {
-        short_load<E, 32>(s, lane, row);
-        st = short_merge<32, false>(short_stats<E, 32, false>(row, r.c), nullptr, r.c);
-    }
-    const bool ok = live && r.T_ok && rowstat_ok(st.m, st.s);
-    if (lane == 0) {
-        p.out_lse[r.row] = !live ? -INFINITY : ok ? (float)((double)st.m / r.T + log(row_mass(st.s))) : __int_as_float(0x7fc00000);
-        if (live && !ok && p.status) atomicOr(p.status, kDevInvalidInput);
-        sm.total = 0;
-    }
-    __syncwarp();
-    if (!ok) {
-        for (int j = lane; j < k; j += 32) { values[j] = -INFINITY; ids[j] = -1; }
-        return;
-    }
-    // threshold from the vectors' maxima; the vector at an end is the first of nine
-    const auto vec = [&](int j) { return j == 0 ? row.we : row.w[j == 0 ? 0 : j - 1]; };
-    const auto col = [&](int j) { return (j == 0 ? row.edge : row.v0 + lane + 32 * (j - 1)) * N - s.lead; };
-    uint32_t v[kShortSlots + 1];
-#pragma unroll
-    for (int j = 0; j <= kShortSlots; ++j) {
-        const uint4 one[1] = {vec(j)};
-        v[j] = order_bits(Words<E>::template vmax_all<1>(one)) >> 16;
-    }
-    const uint32_t t16 = warp_kth(v, 1 + (row.vecs + 31) / 32, k);
-#pragma unroll
-    for (int j = 0; j <= kShortSlots; ++j) {
-        if (v[j] < t16) continue;
-        float x[N];
-        Words<E>::unpack(vec(j), x);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if ((order_bits(x[i]) >> 16) < t16) continue;
-            const int at = atomicAdd(&sm.total, 1);
-            if (at < kShortTopBuf) sm.buf[at] = make_key(x[i], col(j) + i);
-        }
-    }
-    __syncwarp();
-    int n = sm.total;
-    if (n > kShortTopBuf) {
-        // too many reach it: the k-th largest value bit by bit, then all entries above it and the first equal ones
-        uint32_t u = 0;
-#pragma unroll 1
-        for (int b = 31; b >= 0; --b) {
-            const uint32_t t = u | 1u << b;
-            int c = 0;
-#pragma unroll
-            for (int j = 0; j <= kShortSlots; ++j) {
-                float x[N];
-                Words<E>::unpack(vec(j), x);
-#pragma unroll
-                for (int i = 0; i < N; ++i) c += order_bits(x[i]) >= t ? 1 : 0;
-            }
-            if (__reduce_add_sync(0xffffffffu, c) >= k) u = t;
-        }
-        __syncwarp();
-        if (lane == 0) sm.total = 0;
-        __syncwarp();
-        // the greater ones, fewer than k
-#pragma unroll
-        for (int j = 0; j <= kShortSlots; ++j) {
-            float x[N];
-            Words<E>::unpack(vec(j), x);
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (order_bits(x[i]) > u) sm.buf[atomicAdd(&sm.total, 1)] = make_key(x[i], col(j) + i);
-        }
-        __syncwarp();
-        // equal ones in the order of their columns: the first vector (lane 0 has it), the whole ones, the last (lane 1)
-        int above = sm.total;   // places taken
-#pragma unroll 1
-        for (int q = 0; q < kShortSlots + 2 && above < k; ++q) {
-            uint4 one = Words<E>::minus_inf();
-            int first = 0;
-            if (q == 0) { if (lane == 0) one = row.we; first = -s.lead; }
-            else if (q == kShortSlots + 1) { if (lane == 1) one = row.we; first = row.edge * N - s.lead; }
-            else {
-#pragma unroll
-                for (int j = 0; j < kShortSlots; ++j)
-                    if (j == q - 1) one = row.w[j];
-                first = (row.v0 + lane + 32 * (q - 1)) * N - s.lead;
-            }
-            float x[N];
-            Words<E>::unpack(one, x);
-            int mine = 0;
-#pragma unroll
-            for (int i = 0; i < N; ++i) mine += order_bits(x[i]) == u ? 1 : 0;
-            int before = mine;
-#pragma unroll
-            for (int off = 1; off < 32; off <<= 1) {
-                const int o = __shfl_up_sync(0xffffffffu, before, off);
-                if (lane >= off) before += o;
-            }
-            const int all = __shfl_sync(0xffffffffu, before, 31);
-            before += above - mine;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if (order_bits(x[i]) == u) {
-                    if (before < k) sm.buf[before] = make_key(x[i], first + i);
-                    ++before;
-                }
-            }
-            above += all;
-        }
-        __syncwarp();
-        n = min(above, k);
-    }
-    write_ranked(sm.buf, n, k, values, ids);
-}
-
-// ---- top logits of many rows of middling length: a warp streams its row -------------------------------
-// The CTA-wide kernel spends some 10 us on a row whatever its length, with four rows in flight per SM; here 24 are.
-constexpr int kWarpTopRounds = 8;            // of 32 lanes x kShortSlots vectors: rows up to 32 KB
-constexpr int kWarpTopReach = 384;           // vectors fetched again
 
 struct WarpTopSmem {
     alignas(16) top_key buf[kShortTopBuf];
