@@ -38,6 +38,7 @@ struct RowSpan {           // rows r = b R + k of [B, R, V] with strides in entr
     const float* seq_T;    // [B] temperature per sequence, or NULL
     int vectors;           // 16-byte vectors that a row, starting anywhere, covers at most
     int C;                 // CTAs per row
+    int sms;               // of the device
     int slice;             // vectors per CTA (a multiple of kSliceAlign)
 };
 constexpr int kSliceAlign = 8;   // 128-byte lines are not shared between slices

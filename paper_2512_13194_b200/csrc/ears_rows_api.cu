@@ -91,6 +91,7 @@ int make_span(const RowCall& c, bool twice, RowSpan* out, size_t min_slice = 16u
     const int rc = host_device_sms(&sms);
     if (rc) return rc;
     RowSpan s;
+    s.sms = sms;
     s.x = c.x; s.stride_b = c.sb; s.stride_r = c.sr;
     s.rows = (long long)c.B * c.R;
     s.R = c.R; s.V = c.V; s.T = c.T; s.seq_T = c.seq_T;
@@ -160,12 +161,15 @@ int with_type(int dtype, F&& f) {
     return f((uint16_t*)nullptr);
 }
 
-// Threads that hold a row in registers (ears_short.cuh), 0 where the row is too long for that or a number of CTAs per
-// row is asked for.
-int short_threads(const RowSpan& r) {
+// Threads that have a row to themselves (ears_short.cuh), 0 where it is too long for that or a number of CTAs per row is asked
+// for.  Up to 4 KB a warp; up to 16 KB 128 threads, or a warp where there are more than eight rows per SM (steps on 1200
+// rows of 12 KB: 12.2 us with 128 threads, 13.3 with a warp; on 8192: 65 and 57, distillation 103 and 77); up to 32 KB a warp
+// for forward calls on many rows (4096 of 32 KB: 33 us with a CTA per row, 30 with a warp; steps 74 and 86).
+int short_threads(const RowSpan& r, bool step) {
     if (g_row_cluster.load(std::memory_order_relaxed)) return 0;
-    for (int g : {32, 128, 256})
-        if (r.vectors <= g * kShortSlots) return g;
+    if (r.vectors <= 32 * kShortSlots) return 32;
+    if (r.vectors <= 128 * kShortSlots) return r.rows > 8ll * r.sms ? 32 : 128;
+    if (!step && r.vectors <= 32 * kShortSlots * ShortShape<32>::kRounds && r.rows > 16ll * r.sms) return 32;
     return 0;
 }
 
@@ -173,8 +177,7 @@ int short_threads(const RowSpan& r) {
 template <typename F>
 int with_short(int g, F&& f) {
     if (g == 32) return f(std::integral_constant<int, 32>());
-    if (g == 128) return f(std::integral_constant<int, 128>());
-    return f(std::integral_constant<int, 256>());
+    return f(std::integral_constant<int, 128>());
 }
 
 template <typename P>
@@ -190,9 +193,8 @@ int launch_short(void (*kernel)(P), P p, int threads_per_row, cudaStream_t strea
 // Rows that a warp streams (ears_top_warp_kernel): up to 4 KB, and up to 32 KB when there are more of them than CTAs fit on the
 // device at once, four per SM; fewer are done sooner by a CTA each.
 bool top_by_warps(const RowSpan& r) {
-    int sms = 0;
-    if (g_row_cluster.load(std::memory_order_relaxed) || host_device_sms(&sms) != EARS_OK) return false;
-    return r.vectors <= 32 * kShortSlots || (r.vectors <= 32 * kShortSlots * kWarpTopRounds && r.rows > 4ll * sms);
+    if (g_row_cluster.load(std::memory_order_relaxed)) return false;
+    return r.vectors <= 32 * kShortSlots || (r.vectors <= 32 * kShortSlots * kWarpTopRounds && r.rows > 4ll * r.sms);
 }
 
 template <int MODE>
@@ -220,7 +222,7 @@ int launch_distill_short(int dtype, const DistillParams& p, int g, void* stream)
 
 template <int MODE>
 int launch_token(int dtype, const TokenParams& p, bool ent, void* stream) {
-    if (const int g = short_threads(p.rows)) return launch_token_short<MODE>(dtype, p, ent, g, stream);
+    if (const int g = short_threads(p.rows, false)) return launch_token_short<MODE>(dtype, p, ent, g, stream);
     return with_type(dtype, [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
         return launch_rows(ent ? ears_token_kernel<E, true, MODE> : ears_token_kernel<E, false, MODE>, p, kLThreads, 0,
@@ -235,7 +237,7 @@ int ring_stages(int slice) {
 }
 
 int launch_token_step(int dtype, const TokenParams& p, bool ent, void* stream) {
-    if (const int g = short_threads(p.rows)) return launch_token_short<kStep>(dtype, p, ent, g, stream);
+    if (const int g = short_threads(p.rows, true)) return launch_token_short<kStep>(dtype, p, ent, g, stream);
     const int stages = ring_stages(p.rows.slice);
     return with_type(dtype, [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
@@ -245,7 +247,7 @@ int launch_token_step(int dtype, const TokenParams& p, bool ent, void* stream) {
 }
 
 int launch_distill_step(int dtype, const DistillParams& p, void* stream) {
-    if (const int g = short_threads(p.rows)) return launch_distill_short<kStep>(dtype, p, g, stream);
+    if (const int g = short_threads(p.rows, true)) return launch_distill_short<kStep>(dtype, p, g, stream);
     int stages = ring_stages(p.rows.slice);
     const size_t flags = (size_t)((p.rows.slice + kRingVecs - 1) / kRingVecs) * kRingVecs;   // a byte per vector
     while (stages > 2 && (size_t)stages * kRingChunk + flags > (100u << 10)) --stages;   // two CTAs per SM
@@ -258,7 +260,7 @@ int launch_distill_step(int dtype, const DistillParams& p, void* stream) {
 
 template <int MODE>
 int launch_distill(int dtype, const DistillParams& p, void* stream) {
-    if (const int g = short_threads(p.rows)) return launch_distill_short<MODE>(dtype, p, g, stream);
+    if (const int g = short_threads(p.rows, false)) return launch_distill_short<MODE>(dtype, p, g, stream);
     const size_t smem = MODE == kBackward ? 0 : (size_t)((p.rows.slice + kLRound - 1) / kLRound) * kLRound;   // a byte per vector
     return with_type(dtype, [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;

@@ -1,10 +1,10 @@
-// Short rows: a warp (up to 4 KB of logits) or a CTA of 128 or 256 threads (up to 16 and 32 KB) holds a whole row
-// in registers, eight 16-byte vectors per thread, so that it is read once whatever is computed from it.
+// Short rows: a warp, or a CTA of 128 threads, has a row to itself.  It takes the row in rounds of eight 16-byte vectors
+// per thread and keeps the last round in registers, so that a row of one round (4 KB for a warp, 16 KB for 128 threads) is
+// read once whatever is computed from it; the gradient of a longer one fetches the other rounds again, out of L2.
 //
-// Bound by latency: a row passes through about 3 us of dependent steps (its token or list, its logits, the
-// reduction, the 64-bit scalars), so what counts is the number of rows an SM has in flight, 24 with a warp per row
-// against the 3 or 4 that CTAs of 256 threads and more leave room for.  8192 rows of 4 KB take a step of token log
-// probabilities from 85 us (a CTA with a ring of stages per row) to the figure in the table of measurements.
+// Bound by latency: a row passes through some 3 us of dependent steps (its token or list, its logits, the
+// reduction, the 64-bit scalars), so what counts is the number of rows an SM has in flight: 24 with a warp per row, 6 with
+// 128 threads, 2 to 4 with the CTAs of the other kernels.
 #pragma once
 #include "ears_distill.cuh"
 #include "ears_rows.cuh"
@@ -19,40 +19,50 @@ constexpr int kShortWarpRows = 4;            // rows per CTA where a warp has a 
 template <int G> struct ShortShape {
     static constexpr int kRows = G == 32 ? kShortWarpRows : 1;   // rows per CTA
     static constexpr int kThreads = G * kRows;
-    static constexpr int kCtas = G == 256 ? 3 : 6;              // per SM: leaves 80 registers a thread
+    static constexpr int kRounds = G == 32 ? 8 : 1;              // longest rows: 32 and 16 KB
+    static constexpr int kCtas = 6;                              // per SM: leaves 80 registers a thread
 };
 
-// A row's whole vectors, tid + j G of them in w[j], and the one vector at an end that the row covers in part which falls to
-// this thread: thread 0 has the first, thread 1 the last (index `edge`, -1: none).  Beyond the row: -inf.
-template <typename E>
-struct ShortRow {
-    uint4 w[kShortSlots], we;
-    int v0, vecs, edge;
-};
-
+// A row's whole vectors, in rounds: vector (round kShortSlots + j) G + tid in w[j]; and the one vector at an end that the row
+// covers in part which falls to this thread: thread 0 has the first, thread 1 the last (index `edge`, -1: none).  Beyond
+// the row: -inf.
 template <typename E, int G>
-__device__ __forceinline__ void short_load(const Slice<E>& s, int tid, ShortRow<E>& x) {
-    constexpr int N = Words<E>::N;
-    x.v0 = s.lead > 0 ? 1 : 0;
-    x.vecs = max(0, s.end / N - x.v0);
-    x.edge = -1;
-    if (tid == 0 && x.v0 > 0) x.edge = 0;
-    if (tid == 1 && s.n > x.v0 + x.vecs) x.edge = s.n - 1;
-    const uint4* p = reinterpret_cast<const uint4*>(s.base) + x.v0 + tid;
-#pragma unroll
-    for (int j = 0; j < kShortSlots; ++j) {
-        x.w[j] = Words<E>::minus_inf();
-        if (tid + j * G < x.vecs) x.w[j] = ld_row16(p + j * G);
-    }
-    x.we = Words<E>::minus_inf();
-    if (x.edge >= 0) x.we = load_partial(s.base, x.edge, s.lead, s.end);
-}
+struct ShortRow {
+    const Slice<E>& s;
+    int tid, v0, vecs, edge, rounds;
+    uint4 w[kShortSlots], we;
 
-template <typename E, int G, bool ENT>
-__device__ __forceinline__ Stat<ENT> short_stats(const ShortRow<E>& x, const Scale& c) {
+    __device__ __forceinline__ ShortRow(const Slice<E>& slice, int thread) : s(slice), tid(thread) {
+        v0 = s.lead > 0 ? 1 : 0;
+        vecs = max(0, s.end / Words<E>::N - v0);
+        rounds = (vecs + kShortSlots * G - 1) / (kShortSlots * G);
+        edge = -1;
+        if (tid == 0 && v0 > 0) edge = 0;
+        if (tid == 1 && s.n > v0 + vecs) edge = s.n - 1;
+        we = Words<E>::minus_inf();
+        if (edge >= 0) we = load_partial(s.base, edge, s.lead, s.end);
+    }
+    __device__ __forceinline__ void load(int round) {
+        const int first = round * kShortSlots * G + tid;
+        const uint4* p = reinterpret_cast<const uint4*>(s.base) + v0 + first;
+#pragma unroll
+        for (int j = 0; j < kShortSlots; ++j) {
+            w[j] = Words<E>::minus_inf();
+            if (first + j * G < vecs) w[j] = ld_row16(p + j * G);
+        }
+    }
+};
+
+// The statistics of the thread's vectors; mask(w, round) may take entries out, of the last round for good.
+template <typename E, int G, bool ENT, class F>
+__device__ __forceinline__ Stat<ENT> short_stats(ShortRow<E, G>& x, const Scale& c, F mask) {
     Stat<ENT> a;
     stat_open(a);
-    stat_fold<E, kShortSlots, ENT>(x.w, c, a);
+    for (int round = 0; round < x.rounds; ++round) {
+        x.load(round);
+        mask(x.w, round);
+        stat_fold<E, kShortSlots, ENT>(x.w, c, a);
+    }
     if (x.edge >= 0) {
         const uint4 one[1] = {x.we};
         stat_fold<E, 1, ENT>(one, c, a);
@@ -60,18 +70,22 @@ __device__ __forceinline__ Stat<ENT> short_stats(const ShortRow<E>& x, const Sca
     return a;
 }
 
-// The gradient row, 2^t (A + Bt t) or zeros.
+// The gradient row, 2^t (A + Bt t) or zeros: the last round, which w holds, first.
 template <typename E, int G, bool ENT>
-__device__ __forceinline__ void short_gradient(const Slice<E>& s, int tid, E* g, const ShortRow<E>& x, bool zero, float ref, float c, float A, float Bt) {
+__device__ __forceinline__ void short_gradient(ShortRow<E, G>& x, E* g, bool zero, float ref, float c, float A, float Bt) {
+    const Slice<E>& s = x.s;
     const bool aligned = ((uintptr_t)g & 15) == 0;
-    uint4* out = reinterpret_cast<uint4*>(g) + x.v0 + tid;
+    for (int round = x.rounds - 1; round >= 0; --round) {
+        if (round < x.rounds - 1 && !zero) x.load(round);
+        const int first = round * kShortSlots * G + x.tid;
+        uint4* out = reinterpret_cast<uint4*>(g) + x.v0 + first;
 #pragma unroll
-    for (int j = 0; j < kShortSlots; ++j) {
-        if (j * G >= x.vecs) break;
-        const uint4 d = zero ? make_uint4(0, 0, 0, 0) : dense_words<E, ENT>(x.w[j], ref, c, A, Bt);
-        if (tid + j * G < x.vecs) {
-            if (aligned) out[j * G] = d;
-            else store_partial(g, x.v0 + tid + j * G, d, s.lead, s.end);
+        for (int j = 0; j < kShortSlots; ++j) {
+            const uint4 d = zero ? make_uint4(0, 0, 0, 0) : dense_words<E, ENT>(x.w[j], ref, c, A, Bt);
+            if (first + j * G < x.vecs) {
+                if (aligned) out[j * G] = d;
+                else store_partial(g, x.v0 + first + j * G, d, s.lead, s.end);
+            }
         }
     }
     if (x.edge >= 0)
@@ -131,16 +145,19 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas)
     }
     TokenInputs in{};
     if (tid == 0) in = token_inputs<E, ENT, MODE>(p, row, r.row, tok);
-    ShortRow<E> x;
-    short_load<E, G>(s, tid, x);
+    ShortRow<E, G> x(s, tid);
     Part st;
-    if (MODE == kBackward) st = token_saved<ENT>(p.stats[r.row]);
-    else st = short_merge<G, ENT>(short_stats<E, G, ENT>(x, r.c), xs, r.c);
+    if (MODE == kBackward) {
+        if (x.rounds > 0) x.load(x.rounds - 1);
+        st = token_saved<ENT>(p.stats[r.row]);
+    } else {
+        st = short_merge<G, ENT>(short_stats<E, G, ENT>(x, r.c, [](uint4 (&)[kShortSlots], int) {}), xs, r.c);
+    }
     if (tid == 0) sc = token_scalars<ENT, MODE>(p, r.row, 0, r.T, r.T_ok, in, st);
     if (MODE == kForward) return;
     row_sync<G>();
     const TokenScalars t = sc;
-    short_gradient<E, G, ENT>(s, tid, grad, x, t.zero != 0, st.m, r.c.near, t.A, t.Bt);
+    short_gradient<E, G, ENT>(x, grad, t.zero != 0, st.m, r.c.near, t.A, t.Bt);
     if (t.zero) return;
     row_sync<G>();   // the dense value of the token's entry has been written
     if (tid == 0) store_entry(grad + s.lead + tok, t.entry);
@@ -150,17 +167,18 @@ template <typename E, int G, int MODE>
 __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas) ears_distill_short_kernel(const DistillParams p) {
     __shared__ float4 xs[G / 32];
     __shared__ ListSmem lists[ShortShape<G>::kRows];
-    __shared__ alignas(16) uint2 all_bits[ShortShape<G>::kThreads];
+    __shared__ alignas(16) uint2 all_bits[ShortShape<G>::kThreads * ShortShape<G>::kRounds];
     RowSetup r;
     if (!short_setup<G>(p.rows, &r)) return;
     const int tid = threadIdx.x % G, k = p.k;
     ListSmem& sm = lists[threadIdx.x / G];
-    uint2* bits = all_bits + threadIdx.x / G * G;
+    uint2* bits = all_bits + threadIdx.x / G * (G * ShortShape<G>::kRounds);
     const E* row = row_ptr<E>(p.rows, r);
     const Slice<E> s = make_slice<E>(row, p.rows.V, p.rows.slice, 0);
     E* grad = MODE == kForward ? nullptr : grad_ptr<E>(p.grad, p.gsb, p.gsr, r) - s.lead;
     const int v0 = s.lead > 0 ? 1 : 0;   // the first whole vector
-    const int seen = distill_list<E, kShortSlots, G, G>(p, sm, reinterpret_cast<uint32_t*>(bits), tid, r.row, s.lead, v0, max(0, s.end / Words<E>::N - v0));
+    const int seen = distill_list<E, kShortSlots, G, G>(p, sm, reinterpret_cast<uint32_t*>(bits), tid, r.row, s.lead, v0,
+                                                             max(0, s.end / Words<E>::N - v0));
     if (seen != 1) {
         if (tid == 0) distill_unused<MODE>(p, r.row, (seen & 2) != 0);
         if (MODE != kForward) short_zero<E, G>(s, tid, grad);
@@ -168,17 +186,18 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas)
     }
     DraftLogits dl{};
     if (tid < 32) dl = draft_logits(p, sm, row);
-    ShortRow<E> x;
-    short_load<E, G>(s, tid, x);
+    ShortRow<E, G> x(s, tid);
     Part st;
     if (MODE == kBackward) {
+        if (x.rounds > 0) x.load(x.rounds - 1);
         const float4 q = p.stats[r.row];
         st = Part{q.x, q.y, 0.f};
     } else {
         // the gradient of a listed entry is written on its own, so its place may go to -inf for good
-        mask_listed<E>(x.w, bits[tid]);
         if (x.edge >= 0) mask_edge<E>(sm, k, s.lead, x.edge, x.we);
-        st = short_merge<G, false>(short_stats<E, G, false>(x, r.c), xs, r.c);
+        st = short_merge<G, false>(short_stats<E, G, false>(x, r.c, [&](uint4 (&w)[kShortSlots], int round) {
+            mask_listed<E>(w, bits[round * G + tid]);
+        }), xs, r.c);
     }
     const bool empty = tail_empty(st);
     if (tid < 32) {
@@ -190,7 +209,7 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas)
     if (MODE == kForward) return;
     row_sync<G>();
     const bool zero = sm.zero != 0;
-    short_gradient<E, G, false>(s, tid, grad, x, zero, empty ? 0.f : st.m, r.c.near, sm.factor, 0.f);
+    short_gradient<E, G, false>(x, grad, zero, empty ? 0.f : st.m, r.c.near, sm.factor, 0.f);
     if (zero) return;
     row_sync<G>();   // the dense values of the listed entries have been written
     for (int j = tid; j < k; j += G)

@@ -155,6 +155,40 @@ def test_top_logits_of_many_rows(ears, dtype, V):
     close(top.lse[pick, 0], lse, LOG_TOL * 2)
 
 
+@pytest.mark.parametrize("dtype,V", [("bf16", 2100), ("bf16", 8100), ("fp16", 16001), ("fp32", 1100), ("fp32", 4090), ("fp32", 8001)])
+def test_many_rows_that_a_warp_streams(ears, dtype, V):
+    n, k, T = 2500, 12, 1.1
+    g = torch.Generator().manual_seed(V)
+    wide = (torch.randn(n, V + 3, generator=g) * 2).to(DT[dtype])
+    wide[:, 2 + V // 2:2 + V // 2 + 40] = -math.inf
+    x = wide[:, 2:2 + V]
+    dev = wide.to(DEV)[:, 2:2 + V]
+    tok = torch.randint(0, V // 2, (n,), generator=g, dtype=torch.int32)
+    dl, dh = torch.randn(n, generator=g), torch.randn(n, generator=g)
+    tok[11], dl[13], dh[13] = -1, 0.0, 0.0
+    teacher = ears.top_logits((dev.float() * 0.6).to(DT[dtype]), k, T)
+    pick = list(range(20)) + list(range(n - 20, n))
+    o = R.token_logprobs(x[pick], tok[pick], T, dl[pick], dh[pick])
+    logp, H, grad = ears.token_logprobs_step(dev, tok.to(DEV), dl.to(DEV), dh.to(DEV), T)
+    close(logp[pick], o.logp, LOG_TOL)
+    close(H[pick], o.entropy, H_TOL)
+    close_grad(grad[pick], o.grad, o.scale, 2 * H_TOL, dtype)
+    close(ears.token_logprobs(dev, tok.to(DEV), T)[pick], o.logp, LOG_TOL)
+    w = dl.abs()
+    for kind in ("forward_kl", "jsd"):
+        od = R.distill(x[pick], T, *(t[pick].cpu() for t in teacher[:2]), lse=teacher.lse[pick].cpu(), kind=kind, weight=w[pick])
+        loss, grad = ears.distill_step(dev, teacher, T, kind=kind, row_weight=w.to(DEV))
+        close(loss[pick], od.loss, od.loss_scale * (3 * LOG_TOL))
+        close(ears.distill_loss(dev, teacher, T, kind=kind)[pick], od.loss, od.loss_scale * (3 * LOG_TOL))
+        close_grad(grad[pick], od.grad, od.scale, G_TOL, dtype)
+        leaf = dev.clone().requires_grad_(True)
+        (ears.distill_loss(leaf, teacher, T, kind=kind) * w.to(DEV)).sum().backward()
+        close_grad(leaf.grad[pick], od.grad, od.scale, G_TOL, dtype)
+        over = wide.to(DEV)
+        ears.distill_step(over[:, 2:2 + V], teacher, T, kind=kind, row_weight=w.to(DEV), out_grad=over[:, 2:2 + V])
+        assert torch.equal(over[:, 2:2 + V], grad) and torch.equal(over[:, :2].cpu(), wide[:, :2]) and torch.equal(over[:, 2 + V:].cpu(), wide[:, 2 + V:])
+
+
 def test_many_short_rows_and_rows_that_start_anywhere(ears):
     for dtype in ("fp32", "bf16"):
         for V in (3, 17, 700, 2030, 6001, 12001):
