@@ -7,7 +7,6 @@
 #include <climits>
 #include <cmath>
 #include <cstdint>
-#include <cstdlib>
 #include <initializer_list>
 #include <map>
 #include <mutex>
@@ -25,7 +24,6 @@ namespace {
 
 using namespace ears;
 
-const int g_ring_stages = getenv("RING_S") ? atoi(getenv("RING_S")) : 6;
 std::atomic<int> g_row_cluster{0};   // ears_set_row_cluster
 
 int esize_of(int dtype) { return dtype == EARS_DTYPE_F32 ? 4 : 2; }
@@ -105,7 +103,10 @@ int make_span(const RowCall& c, bool twice, RowSpan* out, size_t min_slice = 16u
     return EARS_OK;
 }
 
-// Opts a kernel in to shared memory above 48 KB and to clusters of 16, once per kernel and device.
+// Dynamic shared memory that fits the 48 KB every kernel may have beside what it declares itself.
+constexpr size_t kPlainSmem = 32 * 1024;
+
+// Opts a kernel in to more shared memory than that and to clusters of 16, once per kernel and device.
 cudaError_t allow_launch(const void* kernel, size_t smem, int C) {
     static std::mutex mutex;
     static std::map<std::pair<const void*, int>, std::pair<size_t, bool>> allowed;
@@ -114,7 +115,7 @@ cudaError_t allow_launch(const void* kernel, size_t smem, int C) {
     if (e != cudaSuccess) return e;
     std::lock_guard<std::mutex> lock(mutex);
     auto& have = allowed[{kernel, dev}];
-    if (smem > 48 * 1024 && smem > have.first) {
+    if (smem > kPlainSmem && smem > have.first) {
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         have.first = smem;
@@ -142,7 +143,7 @@ int launch_rows(void (*kernel)(P, Extra...), const P& p, int threads, size_t sme
         cfg.attrs = attr;
         cfg.numAttrs = 1;
     }
-    if (smem > 48 * 1024 || r.C > 8) {
+    if (smem > kPlainSmem || r.C > 8) {
         const cudaError_t e = allow_launch((const void*)kernel, smem, r.C);
         if (e != cudaSuccess) return host_cuda_fail(e, what);
     }
@@ -232,8 +233,7 @@ int launch_token(int dtype, const TokenParams& p, bool ent, void* stream) {
 
 int ring_stages(int slice) {
     const int chunks = (slice + kRingVecs - 1) / kRingVecs;
-    const int most = g_ring_stages;
-    return chunks < most ? chunks : most;
+    return chunks < kRingStages ? chunks : kRingStages;
 }
 
 int launch_token_step(int dtype, const TokenParams& p, bool ent, void* stream) {

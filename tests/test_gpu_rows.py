@@ -155,6 +155,24 @@ def test_top_logits_of_many_rows(ears, dtype, V):
     close(top.lse[pick, 0], lse, LOG_TOL * 2)
 
 
+@pytest.mark.parametrize("V", [8200, 16390, 20000, 24600, 33000, 41000, 49200, 57300, 70001])
+def test_steps_at_every_number_of_stages(ears, V):
+    """Rows of one to nine 16 KB chunks, held whole or fetched again, by one and by two CTAs."""
+    n, k = 3, 10
+    x, vals, ids, lse, g = teacher_case(n, V, k, "bf16", 1.0, 80 + V)
+    tok, dl = ids[:, 1].contiguous(), torch.randn(n, generator=g)
+    teacher = ears.TopLogits(vals.to(DEV), ids.to(DEV), lse.to(DEV))
+    o, od = R.token_logprobs(x, tok, 1.0, dl), R.distill(x, 1.0, vals, ids, lse=lse, weight=dl.abs())
+    for cluster in (0, 1, 2):
+        ears.set_row_cluster(cluster)
+        logp, _, grad = ears.token_logprobs_step(x.to(DEV), tok.to(DEV), dl.to(DEV))
+        close(logp, o.logp, LOG_TOL)
+        close_grad(grad, o.grad, o.scale, G_TOL, "bf16")
+        loss, grad = ears.distill_step(x.to(DEV), teacher, row_weight=dl.abs().to(DEV))
+        close(loss, od.loss, od.loss_scale * (3 * LOG_TOL))
+        close_grad(grad, od.grad, od.scale, G_TOL, "bf16")
+
+
 @pytest.mark.parametrize("dtype,V", [("bf16", 2100), ("bf16", 8100), ("fp16", 16001), ("fp32", 1100), ("fp32", 4090), ("fp32", 8001)])
 def test_many_rows_that_a_warp_streams(ears, dtype, V):
     n, k, T = 2500, 12, 1.1
