@@ -82,7 +82,7 @@ bool per_row(const Rows& r, const at::Tensor* t, at::ScalarType type, at::IntArr
     return t->is_cuda() && t->get_device() == r.device && t->scalar_type() == type && t->sizes() == shape && t->is_contiguous();
 }
 
-// logits, then (after the operator's own arguments) temperature, seq_temperature, status, stream
+// logits, then (after the operator's own arguments) temperature, seq_temperature, status; the current stream
 bool take_logits(Args& a, Rows* r) {
     r->x = a.tensor(false);
     if (!a.plain) return false;
@@ -112,7 +112,6 @@ bool take_rest(Args& a, Rows* r) {
     r->T = a.number();
     const at::Tensor* seq = a.tensor(true);
     const at::Tensor* status = a.tensor(true);
-    PyObject* stream = a.next();
     if (!a.plain) return false;
     if (seq) {
         const int64_t b = r->B;
@@ -123,12 +122,7 @@ bool take_rest(Args& a, Rows* r) {
         if (!status->is_cuda() || status->get_device() != r->device || status->scalar_type() != at::kInt || status->numel() != 1) return false;
         r->status = status->mutable_data_ptr<int32_t>();
     }
-    if (stream == Py_None) {
-        r->stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)r->device).stream();
-    } else {
-        r->stream = PyLong_AsVoidPtr(stream);
-        if (!r->stream && PyErr_Occurred()) { PyErr_Clear(); return false; }
-    }
+    r->stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)r->device).stream();
     return true;
 }
 
@@ -196,7 +190,7 @@ PyObject* guarded(F&& f) {
     }
 }
 
-// (logits, accept_len, k, T, seq_T, status, stream)
+// (logits, accept_len, k, T, seq_T, status)
 PyObject* top_logits(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         Args a{argv, n};
@@ -218,7 +212,7 @@ PyObject* top_logits(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     });
 }
 
-// (logits, tokens, entropy, T, seq_T, status, stream)
+// (logits, tokens, entropy, T, seq_T, status)
 PyObject* token_logprobs(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         Args a{argv, n};
@@ -239,7 +233,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     });
 }
 
-// (logits, tokens, d_logp, d_entropy, out_grad, T, seq_T, status, stream)
+// (logits, tokens, d_logp, d_entropy, out_grad, T, seq_T, status)
 PyObject* token_logprobs_step(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         Args a{argv, n};
@@ -262,7 +256,7 @@ PyObject* token_logprobs_step(PyObject*, PyObject* const* argv, Py_ssize_t n) {
 }
 
 // (logits, tokens, old_logp, ref_logp, advantage, clip_low, clip_high, kl_coef, entropy_coef, entropy, step, row_weight,
-//  out_grad, T, seq_T, status, stream)
+//  out_grad, T, seq_T, status)
 PyObject* policy(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         Args a{argv, n};
@@ -293,7 +287,7 @@ PyObject* policy(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     });
 }
 
-// (logits, values, ids, lse, kind, mix, step, row_weight, out_grad, T, seq_T, status, stream)
+// (logits, values, ids, lse, kind, mix, step, row_weight, out_grad, T, seq_T, status)
 PyObject* distill(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         Args a{argv, n};

@@ -14,6 +14,7 @@ with less work on the host; everything else is converted, checked and refused he
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import NamedTuple, Optional
 
@@ -64,8 +65,15 @@ def _plain_calls():
     return _plain
 
 
-def _raw(stream):
-    return None if stream is None else stream.cuda_stream
+def _on_stream(fn):
+    """``stream=``: the whole call, its conversions and outputs included, belongs to that stream as under torch.cuda.stream."""
+    @functools.wraps(fn)
+    def call(*args, stream=None, **kwargs):
+        if stream is None:
+            return fn(*args, **kwargs)
+        with torch.cuda.stream(stream):
+            return fn(*args, **kwargs)
+    return call
 
 
 class _Rows:
@@ -132,13 +140,13 @@ class _Rows:
         st = out_grad.stride()
         return out_grad, (out_grad.data_ptr(), st[0] if len(st) == 3 else 0, st[-2])
 
-    def call(self, fn, *tail, stream=None):
-        """fn(*head, *tail, status, stream) with the logits' device current."""
+    def call(self, fn, *tail):
+        """fn(*head, *tail, status, stream) with the logits' device current, on its current stream."""
         if _current_device() == self.index:
-            rc = fn(*self.args, *tail, self.status, _raw_stream(self.index) if stream is None else stream.cuda_stream)
+            rc = fn(*self.args, *tail, self.status, _raw_stream(self.index))
         else:
             with torch.cuda.device(self.index):
-                rc = fn(*self.args, *tail, self.status, _raw_stream(self.index) if stream is None else stream.cuda_stream)
+                rc = fn(*self.args, *tail, self.status, _raw_stream(self.index))
         if rc:
             _check(rc)
 
@@ -169,13 +177,14 @@ def _wants_grad(logits) -> bool:
 
 # ---- top logits ------------------------------------------------------------------------------
 
+@_on_stream
 def top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0, *, accept_len: Optional[torch.Tensor] = None,
-               seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None) -> TopLogits:
+               seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> TopLogits:
     """The k largest logits of every row (1 <= k <= 128), equal values by ascending index, and the row's log
     normaliser at ``temperature`` (ears_top_logits).  Entries of -inf are not listed (id -1, value -inf).
     ``accept_len`` [B] int32, as a verification call returns it: rows behind a sequence's first rejection
     are left out."""
-    out = _plain_calls().top_logits(logits, accept_len, k, temperature, seq_temperature, status, _raw(stream))
+    out = _plain_calls().top_logits(logits, accept_len, k, temperature, seq_temperature, status)
     if out is not None:
         return TopLogits(*out)
     rows = _Rows(logits, temperature, seq_temperature, status)
@@ -186,28 +195,28 @@ def top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0, *, accept
     values = torch.empty(rows.lead + (k,), dtype=_F32, device=rows.logits.device)
     ids = torch.empty_like(values, dtype=torch.int32)
     lse = torch.empty(rows.lead, dtype=_F32, device=rows.logits.device)
-    rows.call(load_library().ears_top_logits, _ptr(acc), k, values.data_ptr(), ids.data_ptr(), lse.data_ptr(), stream=stream)
+    rows.call(load_library().ears_top_logits, _ptr(acc), k, values.data_ptr(), ids.data_ptr(), lse.data_ptr())
     return TopLogits(values, ids, lse)
 
 
 # ---- token log probabilities --------------------------------------------------------------------
 
-def _token_forward(rows, tokens, entropy, saved, stream):
+def _token_forward(rows, tokens, entropy, saved):
     logp = torch.empty_like(tokens, dtype=_F32)
     H = torch.empty_like(logp) if entropy else None
-    rows.call(load_library().ears_token_logprobs, tokens.data_ptr(), logp.data_ptr(), _ptr(H), _ptr(saved), stream=stream)
+    rows.call(load_library().ears_token_logprobs, tokens.data_ptr(), logp.data_ptr(), _ptr(H), _ptr(saved))
     return logp, H
 
 
 class _TokenLogprobs(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, logits, tokens, temperature, seq_temperature, entropy, status, stream):
+    def forward(ctx, logits, tokens, temperature, seq_temperature, entropy, status):
         _refuse_capture()
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
         saved = _saved(rows)
         ctx.rows, ctx.tokens, ctx.saved = rows, rows.row(tokens, "tokens", torch.int32), saved
-        ctx.save_for_backward(logits)          # notices a change of the logits before the backward pass
-        logp, H = _token_forward(rows, ctx.tokens, entropy, saved, stream)
+        ctx.save_for_backward(logits, ctx.tokens)   # notices a change of either before the backward pass
+        logp, H = _token_forward(rows, ctx.tokens, entropy, saved)
         ctx.with_entropy = entropy
         return (logp, H) if entropy else logp
 
@@ -222,29 +231,31 @@ class _TokenLogprobs(torch.autograd.Function):
         dh = rows.row(d_entropy, "d_entropy")
         rows.call(load_library().ears_token_logprobs_backward, ctx.tokens.data_ptr(), ctx.saved.data_ptr(), dl.data_ptr(),
                   _ptr(dh), *place)
-        return (g,) + (None,) * 6
+        return (g,) + (None,) * 5
 
 
+@_on_stream
 def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, temperature: float = 1.0, *, entropy: bool = False,
-                   seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+                   seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
     """Log probability of ``tokens`` (one per row, int; -1 leaves the row out: 0) at ``temperature``; with
     ``entropy=True`` the pair (logp, entropy in nats).  Differentiable (ears_token_logprobs, _backward)."""
     if _wants_grad(logits):
-        return _TokenLogprobs.apply(logits, tokens, temperature, seq_temperature, bool(entropy), status, stream)
-    out = _plain_calls().token_logprobs(logits, tokens, bool(entropy), temperature, seq_temperature, status, _raw(stream))
+        return _TokenLogprobs.apply(logits, tokens, temperature, seq_temperature, bool(entropy), status)
+    out = _plain_calls().token_logprobs(logits, tokens, bool(entropy), temperature, seq_temperature, status)
     if out is not None:
         return out if entropy else out[0]
     rows = _Rows(logits, temperature, seq_temperature, status)
-    logp, H = _token_forward(rows, rows.row(tokens, "tokens", torch.int32), entropy, None, stream)
+    logp, H = _token_forward(rows, rows.row(tokens, "tokens", torch.int32), entropy, None)
     return (logp, H) if entropy else logp
 
 
+@_on_stream
 def token_logprobs_step(logits: torch.Tensor, tokens: torch.Tensor, d_logp: torch.Tensor, d_entropy: Optional[torch.Tensor] = None,
                         temperature: float = 1.0, *, out_grad: Optional[torch.Tensor] = None,
-                        seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+                        seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
     """(logp, entropy or None, gradient) for upstream gradients known beforehand (ears_token_logprobs_step):
     ``d_logp`` and, optionally, ``d_entropy`` per row.  ``out_grad=logits`` writes the gradient over them."""
-    out = _plain_calls().token_logprobs_step(logits, tokens, d_logp, d_entropy, out_grad, temperature, seq_temperature, status, _raw(stream))
+    out = _plain_calls().token_logprobs_step(logits, tokens, d_logp, d_entropy, out_grad, temperature, seq_temperature, status)
     if out is not None:
         return out
     rows = _Rows(logits, temperature, seq_temperature, status)
@@ -253,7 +264,7 @@ def token_logprobs_step(logits: torch.Tensor, tokens: torch.Tensor, d_logp: torc
     H = None if dh is None else torch.empty_like(dl)
     g, place = rows.grad(out_grad)
     rows.call(load_library().ears_token_logprobs_step, tok.data_ptr(), dl.data_ptr(), _ptr(dh), logp.data_ptr(), _ptr(H),
-              *place, stream=stream)
+              *place)
     return logp, H, g
 
 
@@ -273,14 +284,14 @@ def _policy_outputs(rows, held, entropy):
 
 class _PolicyLoss(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, logits, tokens, old_logp, advantage, ref_logp, temperature, coefs, seq_temperature, entropy, status, stream):
+    def forward(ctx, logits, tokens, old_logp, advantage, ref_logp, temperature, coefs, seq_temperature, entropy, status):
         _refuse_capture()
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
         ctx.held, ctx.args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, *coefs)
         ctx.rows, ctx.saved = rows, _saved(rows)
-        ctx.save_for_backward(logits)
+        ctx.save_for_backward(logits, *(t for t in ctx.held if t is not None))
         t = _policy_outputs(rows, ctx.held, entropy)
-        rows.call(load_library().ears_policy_loss, *ctx.args, *(_ptr(o) for o in t), ctx.saved.data_ptr(), stream=stream)
+        rows.call(load_library().ears_policy_loss, *ctx.args, *(_ptr(o) for o in t), ctx.saved.data_ptr())
         ctx.mark_non_differentiable(*(o for o in t[1:] if o is not None))
         return tuple(t)
 
@@ -293,13 +304,14 @@ class _PolicyLoss(torch.autograd.Function):
         g, place = rows.grad(None)
         dl = rows.row(d_loss, "d_loss")
         rows.call(load_library().ears_policy_backward, *ctx.args, ctx.saved.data_ptr(), dl.data_ptr(), *place)
-        return (g,) + (None,) * 10
+        return (g,) + (None,) * 9
 
 
+@_on_stream
 def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tensor, advantage: torch.Tensor,
                 temperature: float = 1.0, *, ref_logp: Optional[torch.Tensor] = None, clip_low: float = 0.2,
                 clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0, entropy: bool = False,
-                seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None) -> PolicyTerms:
+                seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> PolicyTerms:
     """Clipped policy loss per row with a KL term and an entropy bonus (ears_policy_loss), differentiable in the
     logits through ``loss``; the other terms (kl with ``ref_logp``, entropy when its coefficient is not 0 or
     ``entropy=True``) come without gradients.  Token -1 leaves a row out."""
@@ -307,27 +319,28 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
     coefs = (clip_low, clip_high, kl_coef, entropy_coef)
     if _wants_grad(logits):
         return PolicyTerms(*_PolicyLoss.apply(logits, tokens, old_logp, advantage, ref_logp, temperature, coefs, seq_temperature,
-                                              with_entropy, status, stream))
+                                              with_entropy, status))
     out = _plain_calls().policy(logits, tokens, old_logp, ref_logp, advantage, *coefs, with_entropy, False, None, None, temperature,
-                                seq_temperature, status, _raw(stream))
+                                seq_temperature, status)
     if out is not None:
         return PolicyTerms(*out[:4])
     rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, *coefs)
     t = _policy_outputs(rows, held, with_entropy)
-    rows.call(load_library().ears_policy_loss, *args, *(_ptr(o) for o in t), None, stream=stream)
+    rows.call(load_library().ears_policy_loss, *args, *(_ptr(o) for o in t), None)
     return t
 
 
+@_on_stream
 def policy_step(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tensor, advantage: torch.Tensor,
                 temperature: float = 1.0, *, ref_logp: Optional[torch.Tensor] = None, clip_low: float = 0.2,
                 clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0, entropy: bool = False,
                 row_weight: Optional[torch.Tensor] = None, out_grad: Optional[torch.Tensor] = None,
-                seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+                seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
     """(PolicyTerms, gradient of sum row_weight * loss) in one call (ears_policy_step)."""
     with_entropy = bool(entropy) or entropy_coef != 0.0
     out = _plain_calls().policy(logits, tokens, old_logp, ref_logp, advantage, clip_low, clip_high, kl_coef, entropy_coef, with_entropy,
-                                True, row_weight, out_grad, temperature, seq_temperature, status, _raw(stream))
+                                True, row_weight, out_grad, temperature, seq_temperature, status)
     if out is not None:
         return PolicyTerms(*out[:4]), out[4]
     rows = _Rows(logits, temperature, seq_temperature, status)
@@ -335,7 +348,7 @@ def policy_step(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
     w = rows.row(row_weight, "row_weight")
     t = _policy_outputs(rows, held, with_entropy)
     g, place = rows.grad(out_grad)
-    rows.call(load_library().ears_policy_step, *args, _ptr(w), *(_ptr(o) for o in t), *place, stream=stream)
+    rows.call(load_library().ears_policy_step, *args, _ptr(w), *(_ptr(o) for o in t), *place)
     return t, g
 
 
@@ -359,14 +372,14 @@ def _loss_like(rows, t):
 
 class _DistillLoss(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, logits, teacher, temperature, kind, mix, seq_temperature, status, stream):
+    def forward(ctx, logits, teacher, temperature, kind, mix, seq_temperature, status):
         _refuse_capture()
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
         ctx.held, ctx.args = _distill_inputs(rows, teacher, kind, mix)
         ctx.rows, ctx.saved = rows, _saved(rows)
-        ctx.save_for_backward(logits)
+        ctx.save_for_backward(logits, *(t for t in ctx.held if t is not None))
         loss = _loss_like(rows, ctx.held[2])
-        rows.call(load_library().ears_distill_loss, *ctx.args, loss.data_ptr(), ctx.saved.data_ptr(), stream=stream)
+        rows.call(load_library().ears_distill_loss, *ctx.args, loss.data_ptr(), ctx.saved.data_ptr())
         return loss
 
     @staticmethod
@@ -378,35 +391,35 @@ class _DistillLoss(torch.autograd.Function):
         g, place = rows.grad(None)
         dl = rows.row(d_loss, "d_loss")
         rows.call(load_library().ears_distill_backward, *ctx.args, ctx.saved.data_ptr(), dl.data_ptr(), *place)
-        return (g,) + (None,) * 7
+        return (g,) + (None,) * 6
 
 
+@_on_stream
 def distill_loss(logits: torch.Tensor, teacher: TopLogits, temperature: float = 1.0, *, kind: str = "forward_kl",
-                 mix: float = 0.5, seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
-                 stream=None) -> torch.Tensor:
+                 mix: float = 0.5, seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Divergence of the draft rows from a teacher's top logits, per row (ears_distill_loss), differentiable in
     the draft's logits.  ``teacher``: what ``top_logits`` returned for the matching rows at the same temperature;
     with ``lse=None`` its entries are renormalised, else the rest of the vocabulary is one more outcome.
     kind: "forward_kl", "reverse_kl" (needs lse) or "jsd" with weight ``mix``.  Rows without entries are left out."""
     if _wants_grad(logits):
-        return _DistillLoss.apply(logits, teacher, temperature, kind, mix, seq_temperature, status, stream)
-    out = _plain_calls().distill(logits, *teacher, DISTILL_KINDS.get(kind), mix, False, None, None, temperature, seq_temperature, status,
-                                 _raw(stream))
+        return _DistillLoss.apply(logits, teacher, temperature, kind, mix, seq_temperature, status)
+    out = _plain_calls().distill(logits, *teacher, DISTILL_KINDS.get(kind), mix, False, None, None, temperature, seq_temperature, status)
     if out is not None:
         return out[0]
     rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _distill_inputs(rows, teacher, kind, mix)
     loss = _loss_like(rows, held[2])
-    rows.call(load_library().ears_distill_loss, *args, loss.data_ptr(), None, stream=stream)
+    rows.call(load_library().ears_distill_loss, *args, loss.data_ptr(), None)
     return loss
 
 
+@_on_stream
 def distill_step(logits: torch.Tensor, teacher: TopLogits, temperature: float = 1.0, *, kind: str = "forward_kl",
                  mix: float = 0.5, row_weight: Optional[torch.Tensor] = None, out_grad: Optional[torch.Tensor] = None,
-                 seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+                 seq_temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
     """(loss per row, gradient of sum row_weight * loss) in one call (ears_distill_step)."""
     out = _plain_calls().distill(logits, *teacher, DISTILL_KINDS.get(kind), mix, True, row_weight, out_grad, temperature, seq_temperature,
-                                 status, _raw(stream))
+                                 status)
     if out is not None:
         return out
     rows = _Rows(logits, temperature, seq_temperature, status)
@@ -414,7 +427,7 @@ def distill_step(logits: torch.Tensor, teacher: TopLogits, temperature: float = 
     w = rows.row(row_weight, "row_weight")
     loss = _loss_like(rows, w)
     g, place = rows.grad(out_grad)
-    rows.call(load_library().ears_distill_step, *args, _ptr(w), loss.data_ptr(), *place, stream=stream)
+    rows.call(load_library().ears_distill_step, *args, _ptr(w), loss.data_ptr(), *place)
     return loss, g
 
 

@@ -707,9 +707,13 @@ def test_autograd_matches_the_step_and_notices_changed_logits(ears):
     leaf2 = x.to(DEV).requires_grad_(True)
     y = leaf2 * 1.0
     out = ears.token_logprobs(y, tok)
-    y.data_ptr()
     with torch.no_grad():
         y.add_(1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
+    old = torch.zeros(n, device=DEV)
+    out = ears.policy_loss(leaf2, tok, old, dl).loss
+    old.add_(1.0)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         out.sum().backward()
     # the entropy's gradient alone, and only the log probability's
