@@ -136,12 +136,15 @@ int launch_rows(void (*kernel)(P, Extra...), const P& p, int threads, size_t sme
     cfg.blockDim = dim3((unsigned)threads, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // wait_for_stream
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
     if (r.C > 1) {
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)r.C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)r.C; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
     }
     if (smem > kPlainSmem || r.C > 8) {
         const cudaError_t e = allow_launch((const void*)kernel, smem, r.C);
@@ -186,9 +189,19 @@ int launch_short(void (*kernel)(P), P p, int threads_per_row, cudaStream_t strea
     const int rows = threads_per_row == 32 ? kShortWarpRows : 1;   // per CTA
     p.rows.slice = p.rows.vectors;
     p.rows.C = 1;
-    kernel<<<(unsigned)((p.rows.rows + rows - 1) / rows), threads_per_row * rows, 0, stream>>>(p);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? EARS_OK : host_cuda_fail(e, what);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((p.rows.rows + rows - 1) / rows), 1, 1);
+    cfg.blockDim = dim3((unsigned)(threads_per_row * rows), 1, 1);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // wait_for_stream
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+    if (e == cudaSuccess) return EARS_OK;
+    (void)cudaGetLastError();
+    return host_cuda_fail(e, what);
 }
 
 // Rows that a warp streams (ears_top_warp_kernel): up to 4 KB, and up to 32 KB when there are more of them than CTAs fit on the

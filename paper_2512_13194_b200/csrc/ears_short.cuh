@@ -119,6 +119,7 @@ __device__ __forceinline__ Part short_merge(const Stat<ENT>& a, float4* xs, cons
 // The row of this thread, or false when the grid's last CTA has none left for it.
 template <int G>
 __device__ __forceinline__ bool short_setup(const RowSpan& p, RowSetup* r) {
+    wait_for_stream();
     const unsigned row = blockIdx.x * (unsigned)ShortShape<G>::kRows + (G == 32 ? threadIdx.x / 32u : 0u);
     if (row >= p.rows) return false;
     *r = row_setup_at(p, row);

@@ -599,6 +599,30 @@ def test_another_stream_and_side_by_side_calls(ears):
         assert torch.equal(o[0], want[0]) and torch.equal(o[2], want[2])
 
 
+def test_calls_queued_behind_one_another_see_what_came_before(ears):
+    """A chain in which every call reads what the one before wrote, alternating with other kernels, long and short."""
+    g = torch.Generator().manual_seed(18)
+    for n, V in ((3, 900), (40, 30000), (700, 5000)):
+        x = torch.randn(n, V, generator=g)
+        tok = torch.randint(0, V, (n,), generator=g, dtype=torch.int32).to(DEV)
+        dl = torch.ones(n, device=DEV)
+
+        def chain(sync):
+            y, logps = x.to(DEV), []
+            for i in range(12):
+                if i % 3 == 2:
+                    y.mul_(1.01)
+                logp, _, grad = ears.token_logprobs_step(y, tok, dl)
+                ears.token_logprobs_step(grad, tok, dl, out_grad=grad)
+                y = y + grad * 0.1
+                logps.append(logp)
+                if sync:
+                    torch.cuda.synchronize()
+            return torch.stack(logps), y
+        want, got = chain(True), chain(False)
+        assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
 def test_captured_steps_replay_on_new_inputs(ears):
     n, V, k = 9, 20011, 16
     x, vals, ids, lse, g = teacher_case(n, V, k, "bf16", 1.0, 15)
