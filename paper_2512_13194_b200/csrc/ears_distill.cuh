@@ -497,7 +497,7 @@ __global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(c
     }
     Stat<false> a;
     stat_open(a);
-    const uint32_t* bits = flags + tid;
+    const auto* bits = reinterpret_cast<const typename ListWord<kRingPer>::type*>(flags) + tid;
     const bool swept = ring_stats(ring, [&](uint4 (&w)[kRingPer], int chunk) {
         mask_listed<E>(w, bits[chunk * kRingConsumers]);
         stat_fold<E, kRingPer, false>(w, r.c, a);
