@@ -12,8 +12,13 @@
 // outside the list share one factor, so a gradient row is factor * 2^t plus k entries of their own.
 //
 // rho is the sum over the entries outside the list, never 1 - sum q (a trained draft leaves a tail of
-// 1e-4 and less, of which the difference would keep no digits): the sweep skips the listed entries.  One
-// byte of shared memory per thread and round says which of its eight vectors hold any.
+// 1e-4 and less, of which the difference would keep no digits): the sweep skips the listed entries, found by one bit
+// per logit in shared memory, looked at a word per thread and round.
+//
+// Bound by HBM like ears_token.cuh; what comes on top is the list (two dependent loads before the sweep may begin, hidden by the
+// ring's first loads) and the scalars, which a warp of their own prepares during the sweep.  2044 rows of 128256 bf16
+// with 64 listed entries: 354 us with a linear search for the listed entries, 203 with a slot table, 194 with the bits and with the
+// forward divergence's gradient published before its logarithms (0.78 of the measured copy rate).
 #pragma once
 #include "ears_ring.cuh"
 #include "ears_rows.cuh"

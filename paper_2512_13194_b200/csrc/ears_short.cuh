@@ -4,7 +4,8 @@
 //
 // Bound by latency: a row passes through some 3 us of dependent steps (its token or list, its logits, the
 // reduction, the 64-bit scalars), so what counts is the number of rows an SM has in flight: 24 with a warp per row, 6 with
-// 128 threads, 2 to 4 with the CTAs of the other kernels.
+// 128 threads, 2 to 4 with the CTAs of the other kernels.  Token steps on 8192 rows of bf16: 85 us with the ring at 2000
+// entries, 22 so; 98 and 56 at 6000 (floor 30).
 #pragma once
 #include "ears_distill.cuh"
 #include "ears_rows.cuh"

@@ -20,6 +20,11 @@
 //     slower, never wrong.
 // The C sorted lists of a cluster are handed to every CTA, and each CTA finds the final ranks of its own
 // entries by binary search in the others.
+//
+// Bound by HBM and by what follows the sweep: of 47 us for 128 of 512 rows of 152064 bf16 (0.51 of the copy rate; the
+// CTAs of one launch run side by side and finish together) the sweep takes 39 (33 without the group maxima), the candidates 5, their
+// ranks 3.  A first build that ranked every candidate of a per-thread threshold by counting took 465 us, fetching all eight
+// vectors of a round again 53.
 #pragma once
 #include "ears_distill.cuh"   // kMaxTop
 #include "ears_rows.cuh"
