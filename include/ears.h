@@ -439,19 +439,21 @@ int ears_profile_end(float* kernel_ms, int capacity, int* n_calls);
  *   temperature   l / temperature enters every softmax; seq_temperature [B] replaces it where not NULL.  It is
  *                 taken in 64 bits: rounding it to 32 would move logits of 20 by 1e-6.
  *   status        optional DEVICE word into which EARS_DEV_INVALID_INPUT is OR-ed when a row could not be
- *                 used; the caller clears it.
+ *                 used, and EARS_DEV_TIMEOUT when a bounded wait gave up; the caller clears it.
  *   out_grad      [B, R, V] in the logits' type, with strides of its own; rows must not overlap.  It may be
  *                 the logits themselves (same pointer, same strides): the gradient then replaces them.
- *                 Any other overlap with the logits is refused.
+ *                 Any other overlap of the two address ranges is refused.
  *   out_saved     optional, 4 floats per row, 16-byte aligned: what the backward call of the same
  *                 operator needs (`saved`); logits and the other inputs must be unchanged until then.
  * -inf logits (masked vocabulary) are legal, and so are masks of the type's lowest value.  A row left out
  * (see each operator) is not read: its outputs are 0 and its gradient row is zeros.  A row that cannot be
  * used (NaN or +inf logit, no finite logit, index outside [0, V), unusable temperature) gives NaN outputs
  * and a gradient row of zeros, and sets the status bit.  Other rows are unaffected.
- * Sums and row scalars are kept in 32 bits and 64 bits; a gradient entry is rounded once, to its type.
+ * Sums and row scalars are kept in 32 bits and 64 bits; a gradient entry is rounded once, to its type, and what lies
+ * below 2^-126 of its row's largest exponential is 0.
  * The calls use no workspace, allocate nothing and may be recorded into CUDA graphs and run side by side
- * on any streams.  Results do not depend on anything but the inputs and the launch's CTAs per row.
+ * on any streams (the driver loads a kernel at its first launch: make that one outside any capture).  Results do not
+ * depend on anything but the inputs and the launch's CTAs per row.
  */
 #define EARS_MAX_TOP 128
 #define EARS_MAX_DISTILL_V (1 << 20)

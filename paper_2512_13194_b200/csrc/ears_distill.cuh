@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(kLThreads, 4) ears_distill_kernel(const Distil
         stat_open(a);
         const uint64_t pol = l2_policy_evict_first();
         const uint2* bits = reinterpret_cast<const uint2*>(flags) + tid;
-        sweep_rounds(s, pol, [&](uint4 (&w)[kLUnroll], int round) {
+        sweep_rounds<E, false>(s, pol, [&](uint4 (&w)[kLUnroll], int round) {
             mask_listed<E>(w, bits[round * kLThreads]);
             stat_fold<E, kLUnroll, false>(w, r.c, a);
         });

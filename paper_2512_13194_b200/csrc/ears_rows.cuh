@@ -154,14 +154,31 @@ __device__ __forceinline__ void load_round(const Slice<E>& s, int i0, uint4 (&w)
     }
 }
 
-// f(w, round) for every round of the thread's vectors.  Four CTAs per SM cover the wait for a round's loads; fetching the
-// next round ahead instead leaves room for two and was slower (2048 rows of 256000 fp32: 330 us against 306).
-template <typename E, class F>
+// f(w, round) for every round of the thread's vectors.  Four CTAs per SM cover the wait for a round's loads.  AHEAD fetches
+// the next round while one is worked on, which leaves room for two CTAs per SM: for launches of the top-logits kernel that have no
+// more (64 of 250 rows of 128256 bf16: 25.1 us and 22.7; with more CTAs it loses, scoring 2048 rows of 256000 fp32: 306 us
+// and 330, and so do the leaner forward kernels, 200 rows of 33000: 6.2 us and 7.2).
+template <typename E, bool AHEAD, class F>
 __device__ __forceinline__ void sweep_rounds(const Slice<E>& s, uint64_t pol, F f) {
-    for (int i0 = threadIdx.x, r = 0; i0 < s.n; i0 += kLRound, ++r) {
-        uint4 w[kLUnroll];
-        load_round(s, i0, w, pol);
-        f(w, r);
+    const int tid = threadIdx.x, rounds = (s.n + kLRound - 1) / kLRound;
+    if (!AHEAD) {
+        for (int r = 0; r < rounds; ++r) {
+            uint4 w[kLUnroll];
+            load_round(s, r * kLRound + tid, w, pol);
+            f(w, r);
+        }
+    } else if (rounds > 0) {
+        uint4 w[kLUnroll], x[kLUnroll];
+        load_round(s, tid, w, pol);
+#pragma unroll 1
+        for (int r = 0;; r += 2) {
+            if (r + 1 < rounds) load_round(s, (r + 1) * kLRound + tid, x, pol);
+            f(w, r);
+            if (r + 1 >= rounds) break;
+            if (r + 2 < rounds) load_round(s, (r + 2) * kLRound + tid, w, pol);
+            f(x, r + 1);
+            if (r + 2 >= rounds) break;
+        }
     }
 }
 

@@ -341,7 +341,10 @@ int ears_top_logits(int dtype, const void* logits, int B, int R, int V, int64_t 
                                 "ears_top_warp_kernel launch");
         });
     return with_type(dtype, [&](auto* e) {
-        return launch_rows(ears_top_kernel<std::remove_pointer_t<decltype(e)>>, p, kLThreads, 0, (cudaStream_t)stream, "ears_top_kernel launch");
+        typedef std::remove_pointer_t<decltype(e)> E;
+        const bool ahead = p.rows.rows * p.rows.C <= 2ll * p.rows.sms;   // all CTAs run at once, two per SM
+        return launch_rows(ahead ? ears_top_kernel<E, true> : ears_top_kernel<E, false>, p, kLThreads, 0, (cudaStream_t)stream,
+                           "ears_top_kernel launch");
     });
 }
 

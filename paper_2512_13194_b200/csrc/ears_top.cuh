@@ -296,8 +296,8 @@ __device__ __forceinline__ float group_max(uint2 g, int q) {
     return __uint_as_float(q & 1 ? two & 0xffff0000u : two << 16);
 }
 
-template <typename E>
-__global__ void __launch_bounds__(kLThreads, 4) ears_top_kernel(const TopParams p) {
+template <typename E, bool AHEAD>
+__global__ void __launch_bounds__(kLThreads, AHEAD ? 2 : 4) ears_top_kernel(const TopParams p) {
     __shared__ TopSmem sm;
     const int tid = threadIdx.x, k = p.k;
     const RowSetup r = row_setup(p.rows);
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(kLThreads, 4) ears_top_kernel(const TopParams 
     const uint64_t pol = l2_policy_normal();   // some of it is fetched again
     const int rounds = (s.n + kLRound - 1) / kLRound, groups = min(rounds, kTopRounds);
     float best[2] = {-INFINITY, -INFINITY};   // the thread's group maxima, folded to those of even and of odd rounds
-    sweep_rounds(s, pol, [&](uint4 (&w)[kLUnroll], int round) {
+    sweep_rounds<E, AHEAD>(s, pol, [&](uint4 (&w)[kLUnroll], int round) {
         float part[kTopParts];
 #pragma unroll
         for (int q = 0; q < kTopParts; ++q) {
