@@ -1,5 +1,5 @@
 """64-bit definitions of the operators on rows of logits, with the gradients taken by differentiating
-them (torch float64 on the CPU).  Checker side only: shares nothing with the CUDA library.
+them (torch float64 on the CPU).  Test side only: shares nothing with the CUDA library.
 
 Every function takes logits as [n, V] of any float type and returns float64 tensors.  Besides outputs and
 gradients the results carry ``scale`` [n, V]: the size of the terms a gradient entry is made of, which is

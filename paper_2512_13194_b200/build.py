@@ -51,7 +51,9 @@ def build(force: bool = False, verbose: bool = False, trace: bool = False) -> st
         for u, code in zip(UNITS, codes):
             if code:
                 raise subprocess.CalledProcessError(code, f"nvcc -c {u}")
-        subprocess.run([_nvcc()] + NVCC_FLAGS + ["-shared", "-o", out] + objects, check=True)
+        linked = f"{out}.{os.getpid()}"      # put in place whole: another process may be loading the library
+        subprocess.run([_nvcc()] + NVCC_FLAGS + ["-shared", "-o", linked] + objects, check=True)
+        os.replace(linked, out)
     return out
 
 
@@ -69,11 +71,13 @@ def build_torch(force: bool = False) -> str:
         return TORCH_LIB
     root = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
+    linked = f"{TORCH_LIB}.{os.getpid()}"
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{root}/include",
-           f"-I{root}/include/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}", f"-I{cuda}/include", "-o", TORCH_LIB, src,
+           f"-I{root}/include/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}", f"-I{cuda}/include", "-o", linked, src,
            f"-L{root}/lib", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python", f"-Wl,-rpath,{root}/lib"]
     subprocess.run(cmd, check=True)
+    os.replace(linked, TORCH_LIB)
     return TORCH_LIB
 
 

@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(kLThreads, 4) ears_token_kernel(const TokenPar
     } else {
         Stat<ENT> a;
         stat_open(a);
-    const uint64_t pol = l2_policy_evict_first();
+        const uint64_t pol = l2_policy_evict_first();
         sweep_rounds<E, false>(s, pol, [&](uint4 (&w)[kLUnroll], int) { stat_fold<E, kLUnroll, ENT>(w, r.c, a); });
         st = exchange_parts<ENT>(a, xs, p.rows.C, r.rank, r.c);
     }

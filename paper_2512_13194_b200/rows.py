@@ -71,9 +71,19 @@ def _on_stream(fn):
     def call(*args, stream=None, **kwargs):
         if stream is None:
             return fn(*args, **kwargs)
+        logits = args[0] if args else kwargs["logits"]
+        if stream.device_index != logits.get_device():
+            raise ValueError("the stream must belong to the logits' device")
         with torch.cuda.stream(stream):
             return fn(*args, **kwargs)
     return call
+
+
+def _overwritten(out_grad) -> None:
+    """A gradient has been written over a tensor of the caller's (the logits, say): an autograd graph that saved
+    it notices in its backward pass."""
+    if out_grad is not None:
+        torch.autograd.graph.increment_version(out_grad)
 
 
 class _Rows:
@@ -257,6 +267,7 @@ def token_logprobs_step(logits: torch.Tensor, tokens: torch.Tensor, d_logp: torc
     ``d_logp`` and, optionally, ``d_entropy`` per row.  ``out_grad=logits`` writes the gradient over them."""
     out = _plain_calls().token_logprobs_step(logits, tokens, d_logp, d_entropy, out_grad, temperature, seq_temperature, status)
     if out is not None:
+        _overwritten(out_grad)
         return out
     rows = _Rows(logits, temperature, seq_temperature, status)
     tok, dl, dh = rows.row(tokens, "tokens", torch.int32), rows.row(d_logp, "d_logp"), rows.row(d_entropy, "d_entropy")
@@ -265,6 +276,7 @@ def token_logprobs_step(logits: torch.Tensor, tokens: torch.Tensor, d_logp: torc
     g, place = rows.grad(out_grad)
     rows.call(load_library().ears_token_logprobs_step, tok.data_ptr(), dl.data_ptr(), _ptr(dh), logp.data_ptr(), _ptr(H),
               *place)
+    _overwritten(out_grad)
     return logp, H, g
 
 
@@ -342,6 +354,7 @@ def policy_step(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
     out = _plain_calls().policy(logits, tokens, old_logp, ref_logp, advantage, clip_low, clip_high, kl_coef, entropy_coef, with_entropy,
                                 True, row_weight, out_grad, temperature, seq_temperature, status)
     if out is not None:
+        _overwritten(out_grad)
         return PolicyTerms(*out[:4]), out[4]
     rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, clip_low, clip_high, kl_coef, entropy_coef)
@@ -349,6 +362,7 @@ def policy_step(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
     t = _policy_outputs(rows, held, with_entropy)
     g, place = rows.grad(out_grad)
     rows.call(load_library().ears_policy_step, *args, _ptr(w), *(_ptr(o) for o in t), *place)
+    _overwritten(out_grad)
     return t, g
 
 
@@ -421,6 +435,7 @@ def distill_step(logits: torch.Tensor, teacher: TopLogits, temperature: float = 
     out = _plain_calls().distill(logits, *teacher, DISTILL_KINDS.get(kind), mix, True, row_weight, out_grad, temperature, seq_temperature,
                                  status)
     if out is not None:
+        _overwritten(out_grad)
         return out
     rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _distill_inputs(rows, teacher, kind, mix)
@@ -428,6 +443,7 @@ def distill_step(logits: torch.Tensor, teacher: TopLogits, temperature: float = 
     loss = _loss_like(rows, w)
     g, place = rows.grad(out_grad)
     rows.call(load_library().ears_distill_step, *args, _ptr(w), loss.data_ptr(), *place)
+    _overwritten(out_grad)
     return loss, g
 
 

@@ -56,6 +56,8 @@ class EarsSampler:
         self.uncertainty, self.stop_at_first_reject = uncertainty, bool(stop_at_first_reject)
         self.b_first, self.report_entropy = int(b_first), bool(report_entropy)
         self.report_logprobs, self.teacher_k = bool(report_logprobs), int(teacher_k)
+        if not 0 <= self.teacher_k <= rows.MAX_TOP:
+            raise ValueError(f"teacher_k must lie in 0..{rows.MAX_TOP}")
         self.steps = 0
         self.accepted = 0          # draft tokens accepted so far (read from the outputs on request only)
         self._pending = []         # accept_len tensors not yet folded into `accepted`

@@ -749,6 +749,31 @@ def test_autograd_matches_the_step_and_notices_changed_logits(ears):
         close_grad(leaf.grad, o.grad, o.scale, 2 * H_TOL, "bf16")
 
 
+@pytest.mark.parametrize("convert", [False, True])
+def test_a_gradient_written_over_saved_logits_is_noticed(ears, convert):
+    n, V = 3, 700
+    x, _ = logits(n, V, "bf16", 18)
+    leaf = x.to(DEV).requires_grad_(True)
+    tok = torch.zeros(n, dtype=torch.int64 if convert else torch.int32, device=DEV)   # converted tensors go through ctypes
+    f = torch.ones(n, dtype=torch.float64 if convert else torch.float32, device=DEV)
+    teacher = ears.top_logits(x.to(DEV), 4)
+    if convert:
+        teacher = teacher._replace(ids=teacher.ids.long())
+    steps = (lambda y: ears.token_logprobs_step(y, tok, f, out_grad=y), lambda y: ears.policy_step(y, tok, f, f, out_grad=y),
+             lambda y: ears.distill_step(y, teacher, out_grad=y))
+    for step in steps:
+        y = leaf * 1.0
+        out = ears.token_logprobs(y, tok)
+        step(y.detach())                       # shares its memory and its version with y
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            out.sum().backward()
+        y = leaf * 1.0                         # the gradient handed on from where the logits were
+        step(y.detach())
+        leaf.grad = None
+        y.backward(y.detach())
+        assert torch.equal(leaf.grad, y.detach())
+
+
 def test_a_round_of_drafting_and_learning(ears):
     """Verification, capture of the teacher, scoring, one distillation step and one policy step, as a program
     that trains its draft and its policy from the same rows runs them."""

@@ -1,5 +1,6 @@
 """Refusals of the operators on rows of logits that the host decides: no device is touched."""
 import ctypes
+import types
 
 import pytest
 import torch
@@ -103,3 +104,18 @@ def test_binding_refuses_what_is_not_on_a_device():
         ears.token_logprobs(x.double(), torch.zeros(2, dtype=torch.int32))
     with pytest.raises(ValueError):
         ears.distill_step(x, ears.TopLogits(x[:, :2], torch.zeros(2, 2, dtype=torch.int32), None))
+
+
+def test_a_stream_of_another_device_is_refused():
+    logits = types.SimpleNamespace(get_device=lambda: 1)
+    stream = types.SimpleNamespace(device_index=0)
+    for call in (lambda: ears.top_logits(logits, 2, stream=stream), lambda: ears.top_logits(logits=logits, k=2, stream=stream)):
+        with pytest.raises(ValueError, match="stream"):
+            call()
+
+
+def test_the_sampler_refuses_a_teacher_that_cannot_be_kept():
+    for k in (-1, 129):
+        with pytest.raises(ValueError):
+            ears.EarsSampler(teacher_k=k)
+    assert ears.EarsSampler(teacher_k=128).teacher_k == 128
