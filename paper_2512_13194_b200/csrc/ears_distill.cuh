@@ -52,6 +52,7 @@ struct ListSmem {
     float factor;
     int zero;
     int seen;                    // bit 0: an entry is present, bit 1: something is wrong
+    uint32_t edge[2];            // listed entries of the vectors just before and just behind those with bits
 };
 
 __device__ __forceinline__ double warp_sum(double v) {
@@ -293,7 +294,7 @@ __device__ __forceinline__ int distill_list(const DistillParams& p, ListSmem& sm
             tv[h] = __ldg(p.values + row_index * k + j);
         }
     }
-    if (tid == 0) sm.seen = 0;
+    if (tid == 0) sm.seen = 0, sm.edge[0] = sm.edge[1] = 0;
     const int words = (count + PER * SWEEP - 1) / (PER * SWEEP) * (SWEEP * PER / 4);
     for (int i = tid; i < words / 4; i += THREADS) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
     bool wrong = false, present[HAND];
@@ -328,6 +329,8 @@ __device__ __forceinline__ int distill_list(const DistillParams& p, ListSmem& sm
             if (i >= 0 && i < count) {
                 const int byte = ((i / (PER * SWEEP)) * SWEEP + i % SWEEP) * PER + i / SWEEP % PER;
                 atomicOr(&bits[byte >> 2], 1u << ((byte & 3) * 8 + e % N));
+            } else if (i == -1 || i == count) {
+                atomicOr(&sm.edge[i < 0 ? 0 : 1], 1u << e % N);
             }
         }
         const unsigned some = __ballot_sync(0xffffffffu, any), bad = __ballot_sync(0xffffffffu, wrong);
@@ -373,13 +376,6 @@ __device__ __forceinline__ void mask_listed(uint4 (&w)[8], uint2 b) {
         if (v) mask_entries<E>(w[q], v);
     }
 }
-// A vector outside the ones with bits (at an end of the row).
-template <typename E>
-__device__ __forceinline__ void mask_edge(const ListSmem& sm, int k, int lead, int v, uint4& w) {
-    for (int q = 0; q < k; ++q)
-        if (sm.col[q] >= 0 && (lead + sm.col[q]) / Words<E>::N == v) put_entry(w, (lead + sm.col[q]) % Words<E>::N, minus_inf_bits<E>(), E{});
-}
-
 // Nothing listed, or a list that cannot be used.
 template <int MODE>
 __device__ __forceinline__ void distill_unused(const DistillParams& p, long long row, bool bad) {
@@ -514,7 +510,7 @@ __global__ void __launch_bounds__(kDistillThreads, 2) ears_distill_step_kernel(c
     const int v = edge_vector(ring, s);
     if (v >= 0) {
         uint4 w[1] = {load_partial(s.base, v, s.lead, s.end)};
-        mask_edge<E>(sm, k, s.lead, v, w[0]);
+        mask_entries<E>(w[0], sm.edge[v < ring.v0 ? 0 : 1]);
         stat_fold<E, 1, false>(w, r.c, a);
     }
     const Part st = exchange_parts<false, kRingWarps>(a, xs, C, r.rank, r.c);

@@ -168,9 +168,12 @@ int with_type(int dtype, F&& f) {
 // Threads that have a row to themselves (ears_short.cuh), 0 where it is too long for that or a number of CTAs per row is asked
 // for.  Up to 4 KB a warp; up to 16 KB 128 threads, or a warp where there are more than eight rows per SM (steps on 1200
 // rows of 12 KB: 12.2 us with 128 threads, 13.3 with a warp; on 8192: 65 and 57, distillation 103 and 77); up to 32 KB a warp
-// for forward calls on many rows (4096 of 32 KB: 33 us with a CTA per row, 30 with a warp; steps 74 and 86).
-int short_threads(const RowSpan& r, bool step) {
+// for forward calls on many rows (4096 of 32 KB: 33 us with a CTA per row, 30 with a warp; steps 74 and 86).  A step on no more rows than
+// SMs is done sooner by a CTA each, from a list on twice as many (148 rows of 1991 bf16: policy 6.0 us with a warp and 5.5,
+// distillation from 64 entries 10.9 and 8.5; on 592 rows policy 6.2 and 11.1, distillation 11.1 and 16.6).
+int short_threads(const RowSpan& r, bool step, bool list) {
     if (g_row_cluster.load(std::memory_order_relaxed)) return 0;
+    if (step && r.rows <= (list ? 2ll : 1ll) * r.sms) return 0;
     if (r.vectors <= 32 * kShortSlots) return 32;
     if (r.vectors <= 128 * kShortSlots) return r.rows > 8ll * r.sms ? 32 : 128;
     if (!step && r.vectors <= 32 * kShortSlots * ShortShape<32>::kRounds && r.rows > 16ll * r.sms) return 32;
@@ -205,9 +208,12 @@ int launch_short(void (*kernel)(P), P p, int threads_per_row, cudaStream_t strea
 }
 
 // Rows that a warp streams (ears_top_warp_kernel): up to 4 KB, and up to 32 KB when there are more of them than CTAs fit on the
-// device at once, four per SM; fewer are done sooner by a CTA each.
-bool top_by_warps(const RowSpan& r) {
+// device at once, four per SM; fewer are done sooner by a CTA each.  So are long lists from few rows of any length (128 of 1026
+// bf16: 27.9 us with a warp, 10.0 with a CTA on 148 rows, 28.4 and 17.2 on 592, 36.9 and 35.9 on 1200; 64 of 300: 15.9 and 9.0
+// on 148, 16.3 and 14.3 on 592, but 64 of 1026 8.1 and 11.7; 8 of 1026: 6.2 and 7.1 on 148).
+bool top_by_warps(const RowSpan& r, int k) {
     if (g_row_cluster.load(std::memory_order_relaxed)) return false;
+    if ((k > 32 && r.rows <= 2ll * r.sms) || (k > 64 && r.rows <= 4ll * r.sms)) return false;
     return r.vectors <= 32 * kShortSlots || (r.vectors <= 32 * kShortSlots * kWarpTopRounds && r.rows > 4ll * r.sms);
 }
 
@@ -236,7 +242,7 @@ int launch_distill_short(int dtype, const DistillParams& p, int g, void* stream)
 
 template <int MODE>
 int launch_token(int dtype, const TokenParams& p, bool ent, void* stream) {
-    if (const int g = short_threads(p.rows, false)) return launch_token_short<MODE>(dtype, p, ent, g, stream);
+    if (const int g = short_threads(p.rows, false, false)) return launch_token_short<MODE>(dtype, p, ent, g, stream);
     return with_type(dtype, [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
         return launch_rows(ent ? ears_token_kernel<E, true, MODE> : ears_token_kernel<E, false, MODE>, p, kLThreads, 0,
@@ -250,7 +256,7 @@ int ring_stages(int slice) {
 }
 
 int launch_token_step(int dtype, const TokenParams& p, bool ent, void* stream) {
-    if (const int g = short_threads(p.rows, true)) return launch_token_short<kStep>(dtype, p, ent, g, stream);
+    if (const int g = short_threads(p.rows, true, false)) return launch_token_short<kStep>(dtype, p, ent, g, stream);
     const int stages = ring_stages(p.rows.slice);
     return with_type(dtype, [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
@@ -260,7 +266,7 @@ int launch_token_step(int dtype, const TokenParams& p, bool ent, void* stream) {
 }
 
 int launch_distill_step(int dtype, const DistillParams& p, void* stream) {
-    if (const int g = short_threads(p.rows, true)) return launch_distill_short<kStep>(dtype, p, g, stream);
+    if (const int g = short_threads(p.rows, true, true)) return launch_distill_short<kStep>(dtype, p, g, stream);
     int stages = ring_stages(p.rows.slice);
     const size_t flags = (size_t)((p.rows.slice + kRingVecs - 1) / kRingVecs) * kRingVecs;   // a byte per vector
     while (stages > 2 && (size_t)stages * kRingChunk + flags > (100u << 10)) --stages;   // two CTAs per SM
@@ -273,7 +279,7 @@ int launch_distill_step(int dtype, const DistillParams& p, void* stream) {
 
 template <int MODE>
 int launch_distill(int dtype, const DistillParams& p, void* stream) {
-    if (const int g = short_threads(p.rows, false)) return launch_distill_short<MODE>(dtype, p, g, stream);
+    if (const int g = short_threads(p.rows, false, true)) return launch_distill_short<MODE>(dtype, p, g, stream);
     const size_t smem = MODE == kBackward ? 0 : (size_t)((p.rows.slice + kLRound - 1) / kLRound) * kLRound;   // a byte per vector
     return with_type(dtype, [&](auto* e) {
         typedef std::remove_pointer_t<decltype(e)> E;
@@ -335,7 +341,7 @@ int ears_top_logits(int dtype, const void* logits, int B, int R, int V, int64_t 
     EARS_TRY(make_span(c, false, &p.rows, 64u << 10));   // every CTA has a list of its own to sort
     p.k = k; p.accept_len = accept_len;
     p.out_values = out_values; p.out_ids = out_ids; p.out_lse = out_lse; p.status = status;
-    if (top_by_warps(p.rows))
+    if (top_by_warps(p.rows, p.k))
         return with_type(dtype, [&](auto* e) {
             return launch_short(ears_top_warp_kernel<std::remove_pointer_t<decltype(e)>>, p, 32, (cudaStream_t)stream,
                                 "ears_top_warp_kernel launch");

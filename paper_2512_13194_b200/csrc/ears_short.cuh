@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas)
         st = Part{q.x, q.y, 0.f};
     } else {
         // the gradient of a listed entry is written on its own, so its place may go to -inf for good
-        if (x.edge >= 0) mask_edge<E>(sm, k, s.lead, x.edge, x.we);
+        if (x.edge >= 0) mask_entries<E>(x.we, sm.edge[x.edge < v0 ? 0 : 1]);
         st = short_merge<G, false>(short_stats<E, G, false>(x, r.c, [&](uint4 (&w)[kShortSlots], int round) {
             mask_listed<E>(w, bits[round * G + tid]);
         }), xs, r.c);
@@ -225,25 +225,42 @@ constexpr int kShortTopBuf = 256;            // candidates per row; kMaxTop and 
 constexpr int kWarpTopRounds = 8;            // of 32 lanes x kShortSlots vectors: rows up to 32 KB
 constexpr int kWarpTopReach = 384;           // vectors fetched again
 
+// One warp: the candidates from + lane, from + lane + 32, .. (W of a lane) to their ranks among buf[0 .. n).
+template <int W>
+__device__ __forceinline__ void rank_some(const top_key* buf, int from, int n, int k, float* values, int32_t* ids) {
+    const int at = from + (threadIdx.x & 31);
+    const ulonglong2* pairs = reinterpret_cast<const ulonglong2*>(buf);
+    top_key mine[W];
+    int rank[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        const bool have = at + 32 * i < n;
+        mine[i] = have ? buf[at + 32 * i] : 0ull;
+        rank[i] = have ? 0 : k;
+    }
+#pragma unroll 4
+    for (int j = 0; j < (n + 1) / 2; ++j) {
+        const ulonglong2 q = pairs[j];
+#pragma unroll
+        for (int i = 0; i < W; ++i) rank[i] += (q.x > mine[i]) + (q.y > mine[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        if (rank[i] < k) {
+            values[rank[i]] = unorder_bits((uint32_t)(mine[i] >> 32));
+            ids[rank[i]] = (int32_t)~(uint32_t)mine[i];
+        }
+    }
+}
+
 // One warp: the candidates buf[0 .. n) to their ranks below k, absent entries behind them.
 __device__ __forceinline__ void write_ranked(top_key* buf, int n, int k, float* values, int32_t* ids) {
     const int lane = threadIdx.x & 31;
     if (lane == 0 && (n & 1)) buf[n] = 0ull;   // kShortTopBuf is even
     __syncwarp();
-    const ulonglong2* pairs = reinterpret_cast<const ulonglong2*>(buf);
-    for (int at = lane; at < n; at += 32) {
-        const top_key mine = buf[at];
-        int rank = 0;
-#pragma unroll 4
-        for (int j = 0; j < (n + 1) / 2; ++j) {
-            const ulonglong2 q = pairs[j];
-            rank += (q.x > mine) + (q.y > mine);
-        }
-        if (rank < k) {
-            values[rank] = unorder_bits((uint32_t)(mine >> 32));
-            ids[rank] = (int32_t)~(uint32_t)mine;
-        }
-    }
+    int from = 0;
+    for (; n - from > 64; from += 128) rank_some<4>(buf, from, n, k, values, ids);
+    for (; n - from > 0; from += 32) rank_some<1>(buf, from, n, k, values, ids);
     for (int j = n + lane; j < k; j += 32) { values[j] = -INFINITY; ids[j] = -1; }   // fewer than k finite entries
 }
 
@@ -259,26 +276,52 @@ __device__ __forceinline__ float peak_of(uint4 p, int j) {
     return __uint_as_float(j & 1 ? two & 0xffff0000u : two << 16);
 }
 
-// Too many entries reach the threshold: the k-th largest value bit by bit, then all entries above it and the first
-// equal ones, the row fetched again for every bit.  -> entries in buf, exactly k.
+// Too many entries reach `lo`, the threshold from the vectors' maxima: the k-th largest value is approached two bits at a
+// time, from the bits that lo and the row's largest share, the row fetched again for every step, until no more entries reach
+// the threshold than buf holds.  If its last bit leaves too many (equal entries), buf gets those above it and the first
+// equal ones.  -> entries in buf, k or more.
 template <typename E>
-__device__ __noinline__ int warp_top_exact(const Slice<E>& s, WarpTopSmem& sm, int k) {
+__device__ __noinline__ int warp_top_exact(const Slice<E>& s, WarpTopSmem& sm, int k, uint32_t lo, uint32_t hi) {
     constexpr int N = Words<E>::N;
     const int lane = threadIdx.x & 31;
-    uint32_t u = 0;
-    for (int b = 31; b >= 0; --b) {
-        const uint32_t t = u | 1u << b;
-        int c = 0;
-        for (int v = lane; v < s.n; v += 32) {
-            float x[N];
-            Words<E>::unpack(slice_vector(s, v), x);
+    uint32_t u = hi;
+    int reaching = kShortTopBuf + 1;
+    if (hi != lo) {
+        int b = (31 - __clz(hi ^ lo)) & ~1;   // of the two bits tried first
+        u = b == 30 ? 0u : hi >> (b + 2) << (b + 2);
+        for (; b >= 0 && reaching > kShortTopBuf; b -= 2) {
+            // all of k reach lo, and what lies below it need not be told apart (nor be the order of a number)
+            const float t1 = unorder_bits(max(u | 1u << b, lo)), t2 = unorder_bits(max(u | 2u << b, lo)), t3 = unorder_bits(max(u | 3u << b, lo));
+            uint32_t c12 = 0, c3 = 0;
+            for (int v0 = lane; v0 < s.n; v0 += 32 * kShortSlots) {
+                uint4 w[kShortSlots];
 #pragma unroll
-            for (int i = 0; i < N; ++i) c += order_bits(x[i]) >= t ? 1 : 0;
+                for (int j = 0; j < kShortSlots; ++j) w[j] = v0 + 32 * j < s.n ? slice_vector(s, v0 + 32 * j) : Words<E>::minus_inf();
+#pragma unroll
+                for (int j = 0; j < kShortSlots; ++j) {
+                    float x[N];
+                    Words<E>::unpack(w[j], x);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        c12 += (x[i] >= t1 ? 1u : 0u) + (x[i] >= t2 ? 1u << 16 : 0u);
+                        c3 += x[i] >= t3 ? 1u : 0u;
+                    }
+                }
+            }
+            c12 = __reduce_add_sync(0xffffffffu, c12);   // at most 16384 each
+            c3 = __reduce_add_sync(0xffffffffu, c3);
+            const int n3 = (int)c3, n2 = (int)(c12 >> 16), n1 = (int)(c12 & 0xffffu);
+            if (n3 >= k) { u |= 3u << b; reaching = n3; }
+            else if (n2 >= k) { u |= 2u << b; reaching = n2; }
+            else if (n1 >= k) { u |= 1u << b; reaching = n1; }
         }
-        if (__reduce_add_sync(0xffffffffu, c) >= k) u = t;
+        u = max(u, lo);
     }
+    const bool ties = reaching > kShortTopBuf;
+    const int room = ties ? k : kShortTopBuf;
+    const uint32_t over = ties ? u : u - 1;
     int above = 0, equal = 0;   // entries above the value so far, equal ones so far, in the order of the columns
-    for (int pass = 0; pass < 2; ++pass) {
+    for (int pass = 0; pass < (ties ? 2 : 1); ++pass) {
         for (int v0 = 0; v0 < s.n; v0 += 32) {
             const int v = v0 + lane;
             const uint4 w = v < s.n ? slice_vector(s, v) : Words<E>::minus_inf();
@@ -286,7 +329,7 @@ __device__ __noinline__ int warp_top_exact(const Slice<E>& s, WarpTopSmem& sm, i
             Words<E>::unpack(w, x);
             int mine = 0;
 #pragma unroll
-            for (int i = 0; i < N; ++i) mine += (pass == 0 ? order_bits(x[i]) > u : order_bits(x[i]) == u) ? 1 : 0;
+            for (int i = 0; i < N; ++i) mine += (pass == 0 ? order_bits(x[i]) > over : order_bits(x[i]) == u) ? 1 : 0;
             int sum = mine;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
@@ -296,8 +339,8 @@ __device__ __noinline__ int warp_top_exact(const Slice<E>& s, WarpTopSmem& sm, i
             int at = above + (pass == 0 ? 0 : equal) + sum - mine;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                if (pass == 0 ? order_bits(x[i]) > u : order_bits(x[i]) == u) {
-                    if (at < k) sm.buf[at] = make_key(x[i], v * N + i - s.lead);
+                if (pass == 0 ? order_bits(x[i]) > over : order_bits(x[i]) == u) {
+                    if (at < room) sm.buf[at] = make_key(x[i], v * N + i - s.lead);
                     ++at;
                 }
             }
@@ -306,7 +349,7 @@ __device__ __noinline__ int warp_top_exact(const Slice<E>& s, WarpTopSmem& sm, i
         }
     }
     __syncwarp();
-    return min(above + equal, k);
+    return min(above + equal, room);
 }
 
 template <typename E>
@@ -364,7 +407,8 @@ __global__ void __launch_bounds__(ShortShape<32>::kThreads, ShortShape<32>::kCta
     uint32_t bv[kShortSlots];
 #pragma unroll
     for (int j = 0; j < kShortSlots; ++j) bv[j] = order_bits(best[j]) >> 16;
-    const float reach = unorder_bits(warp_kth(bv, kShortSlots, k) << 16);
+    const uint32_t reach_bits = warp_kth(bv, kShortSlots, k) << 16;
+    const float reach = unorder_bits(reach_bits);
     // the lane's own vectors that reach it
     int mine = 0;
     for (int round = 0; round < rounds; ++round) {
@@ -417,7 +461,7 @@ __global__ void __launch_bounds__(ShortShape<32>::kThreads, ShortShape<32>::kCta
         __syncwarp();
         n = sm.total;
     }
-    if (n > kShortTopBuf) n = warp_top_exact(s, sm, k);
+    if (n > kShortTopBuf) n = warp_top_exact(s, sm, k, reach_bits, order_bits(st.m));
     write_ranked(sm.buf, n, k, values, ids);
 }
 

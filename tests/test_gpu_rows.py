@@ -155,6 +155,25 @@ def test_top_logits_of_many_rows(ears, dtype, V):
     close(top.lse[pick, 0], lse, LOG_TOL * 2)
 
 
+@pytest.mark.parametrize("V", [300, 1026, 1501, 2043])
+@pytest.mark.parametrize("name", sorted(PATTERNS) + ["normal"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_top_logits_of_many_short_rows_in_hard_orders(ears, dtype, name, V):
+    """As many rows as it takes for each to fall to a single warp."""
+    x = PATTERNS[name](V) if name in PATTERNS else torch.randn(V, generator=torch.Generator().manual_seed(V))
+    if dtype == "fp16":
+        x = x.clamp(-65504.0, 65504.0) if name != "three_finite" else x
+    x = torch.stack([x, x.flip(0), x.roll(7)]).to(DT[dtype])
+    many = x.to(DEV).repeat(300, 1)
+    for k in (2, 33, 64, 100, 128):
+        top = ears.top_logits(many, k, 1.0)
+        v, i, lse = R.top_logits(x, k, 1.0)
+        assert torch.equal(top.ids.cpu().long().view(300, 3, k), i.expand(300, 3, k))
+        assert torch.equal(top.values.cpu().double().view(300, 3, k), v.expand(300, 3, k))
+        # equal rows that start at different places of a 16-byte vector are summed in a different order
+        close(top.lse, lse.repeat(300), LOG_TOL * 2)
+
+
 @pytest.mark.parametrize("V", [8200, 16390, 20000, 24600, 33000, 41000, 49200, 57300, 70001])
 def test_steps_at_every_number_of_stages(ears, V):
     """Rows of one to nine 16 KB chunks, held whole or fetched again, by one and by two CTAs."""
@@ -747,6 +766,35 @@ def test_autograd_matches_the_step_and_notices_changed_logits(ears):
         outs[pick].sum().backward()
         o = R.token_logprobs(x, tok.cpu(), 1.0, *((torch.ones(n), None) if pick == 0 else (torch.zeros(n), torch.ones(n))))
         close_grad(leaf.grad, o.grad, o.scale, 2 * H_TOL, "bf16")
+
+
+@pytest.mark.parametrize("n", [330, 700])
+@pytest.mark.parametrize("V", [3, 17, 700, 2030, 6001])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_short_rows_in_numbers(ears, dtype, V, n):
+    """Rows of one round of a warp and more, more of them than SMs and than four per SM, at every kind of start."""
+    x, g = logits(n, V + 3, dtype, 90 + V, mask=False)
+    dev = x.to(DEV)
+    tok, dl = torch.randint(0, V, (n,), generator=g, dtype=torch.int32), torch.randn(n, generator=g)
+    k = min(V, 40)
+    pick = list(range(12)) + list(range(n - 12, n))
+    for off in (0, 1, 3):
+        rows, at = x[pick][:, off:off + V], dev[:, off:off + V]
+        o = R.token_logprobs(rows, tok[pick], 0.9, dl[pick])
+        logp, _, grad = ears.token_logprobs_step(at, tok.to(DEV), dl.to(DEV), None, 0.9)
+        close(logp[pick], o.logp, LOG_TOL)
+        close_grad(grad[pick], o.grad, o.scale, G_TOL, dtype)
+        close(ears.token_logprobs(at, tok.to(DEV), 0.9)[pick], o.logp, LOG_TOL)
+        teacher = ears.top_logits((at.float() * 0.7).to(DT[dtype]), k)
+        held = [t[pick].cpu() for t in teacher]
+        od = R.distill(rows, 1.0, held[0], held[1], lse=held[2], kind="jsd", weight=dl[pick].abs())
+        loss, grad = ears.distill_step(at, teacher, kind="jsd", row_weight=dl.abs().to(DEV))
+        close(loss[pick], od.loss, od.loss_scale * (3 * LOG_TOL))
+        close_grad(grad[pick], od.grad, od.scale, G_TOL, dtype)
+        close(ears.distill_loss(at, teacher, kind="jsd")[pick], od.loss, od.loss_scale * (3 * LOG_TOL))
+        leaf = at.clone().requires_grad_(True)
+        (ears.distill_loss(leaf, teacher, kind="jsd") * dl.abs().to(DEV)).sum().backward()
+        close_grad(leaf.grad[pick], od.grad, od.scale, G_TOL, dtype)
 
 
 @pytest.mark.parametrize("convert", [False, True])
