@@ -168,9 +168,9 @@ int with_type(int dtype, F&& f) {
 // Threads that have a row to themselves (ears_short.cuh), 0 where it is too long for that or a number of CTAs per row is asked
 // for.  Up to 4 KB a warp; up to 16 KB 128 threads, or a warp where there are more than eight rows per SM (steps on 1200
 // rows of 12 KB: 12.2 us with 128 threads, 13.3 with a warp; on 8192: 65 and 57, distillation 103 and 77); up to 32 KB a warp
-// for forward calls on many rows (4096 of 32 KB: 33 us with a CTA per row, 30 with a warp; steps 74 and 86).  A step on no more rows than
-// SMs is done sooner by a CTA each, from a list on twice as many (148 rows of 1991 bf16: policy 6.0 us with a warp and 5.5,
-// distillation from 64 entries 10.9 and 8.5; on 592 rows policy 6.2 and 11.1, distillation 11.1 and 16.6).
+// for forward calls on many rows (4096 of 32 KB: 33 us with a CTA per row, 30 with a warp; steps 74 and 86).  A step on no
+// more rows than SMs is done sooner by a CTA each, from a list on twice as many (148 rows of 1991 bf16: policy 6.0 us with a
+// warp and 5.5, distillation from 64 entries 10.9 and 8.5; on 592 rows policy 6.2 and 11.1, distillation 11.1 and 16.6).
 int short_threads(const RowSpan& r, bool step, bool list) {
     if (g_row_cluster.load(std::memory_order_relaxed)) return 0;
     if (step && r.rows <= (list ? 2ll : 1ll) * r.sms) return 0;

@@ -220,7 +220,8 @@ __global__ void __launch_bounds__(ShortShape<G>::kThreads, ShortShape<G>::kCtas)
 
 // ---- top logits: a warp streams its row ----------------------------------------------------------------
 // The CTA-wide kernel spends some 10 us on a row whatever its length, with four rows in flight per SM; here 24 are
-// (8192 rows of 6000 bf16: 147 us and 50).
+// (8192 rows of 6000 bf16: 147 us and 50).  Where the vectors' maxima leave too many candidates, as in a row with few more
+// vectors than the list has entries, warp_top_exact narrows them (128 of 20000 x 1026 bf16: 383 us, of 20000 x 2000 183).
 constexpr int kShortTopBuf = 256;            // candidates per row; kMaxTop and more
 constexpr int kWarpTopRounds = 8;            // of 32 lanes x kShortSlots vectors: rows up to 32 KB
 constexpr int kWarpTopReach = 384;           // vectors fetched again
