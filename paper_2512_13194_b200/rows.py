@@ -119,7 +119,7 @@ class _Rows:
         self.seq_T = None if seq_temperature is None else self.per(seq_temperature, torch.float32, (self.B,), "seq_temperature")
         if status is not None and (status.get_device() != index or status.dtype != torch.int32 or status.numel() != 1):
             raise ValueError("status must be an int32 CUDA tensor of one element on the logits' device")
-        self.status = None if status is None else status.data_ptr()
+        self.status = status           # held, not its address: a backward call writes to it again
         self.args = (code, logits.data_ptr(), self.B, self.R, self.V, sb, sr, float(temperature),
                      None if self.seq_T is None else self.seq_T.data_ptr())
 
@@ -153,10 +153,10 @@ class _Rows:
     def call(self, fn, *tail):
         """fn(*head, *tail, status, stream) with the logits' device current, on its current stream."""
         if _current_device() == self.index:
-            rc = fn(*self.args, *tail, self.status, _raw_stream(self.index))
+            rc = fn(*self.args, *tail, _ptr(self.status), _raw_stream(self.index))
         else:
             with torch.cuda.device(self.index):
-                rc = fn(*self.args, *tail, self.status, _raw_stream(self.index))
+                rc = fn(*self.args, *tail, _ptr(self.status), _raw_stream(self.index))
         if rc:
             _check(rc)
 

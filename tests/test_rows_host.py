@@ -1,0 +1,85 @@
+"""What the Python side of the row operators hands to the library and keeps between calls: tensors on the CPU pass for
+device tensors, and a stand-in for the library records its arguments and touches none of them."""
+import gc
+import weakref
+
+import pytest
+import torch
+
+import paper_2512_13194_b200 as ears
+from paper_2512_13194_b200 import rows
+
+
+class Library:
+    """Every entry point: records (name, arguments) and succeeds."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def entry(*args):
+            self.calls.append((name, args))
+            return 0
+        return entry
+
+    def last(self, name):
+        return [args for n, args in self.calls if n == name][-1]
+
+
+class NoPlainCalls:
+    """The extension module when nothing is in its plain form."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
+@pytest.fixture
+def lib(monkeypatch):
+    fake = Library()
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda self: 0)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(rows, "load_library", lambda: fake)
+    monkeypatch.setattr(rows, "_plain_calls", NoPlainCalls)
+    monkeypatch.setattr(rows, "_current_device", lambda: 0)
+    monkeypatch.setattr(rows, "_raw_stream", lambda index: 0)
+    return fake
+
+
+N, V, K = 3, 16, 4
+STATUS = -2                # place of the status word among every entry point's arguments
+
+
+class Inputs:
+    """One call's inputs besides the logits."""
+
+    def __init__(self):
+        self.tokens = torch.zeros(N, dtype=torch.int32)
+        self.f = [torch.zeros(N) for _ in range(3)]
+        self.teacher = ears.TopLogits(torch.zeros(N, K), torch.arange(K, dtype=torch.int32).repeat(N, 1), torch.zeros(N))
+
+
+# name of the entry points -> (differentiable call, returning what backward starts from)
+LOSSES = {
+    "ears_token_logprobs": lambda x, i, **kw: ears.token_logprobs(x, i.tokens, **kw),
+    "ears_policy": lambda x, i, **kw: ears.policy_loss(x, i.tokens, i.f[0], i.f[1], ref_logp=i.f[2], kl_coef=0.1, **kw).loss,
+    "ears_distill": lambda x, i, **kw: ears.distill_loss(x, i.teacher, **kw),
+}
+
+
+def leaf():
+    return torch.zeros(N, V).requires_grad_(True)
+
+
+@pytest.mark.parametrize("name", sorted(LOSSES))
+def test_the_status_word_lives_until_the_backward_pass_is_over(lib, name):
+    x, status = leaf(), torch.zeros(1, dtype=torch.int32)
+    out = LOSSES[name](x, Inputs(), status=status)
+    place, held = status.data_ptr(), weakref.ref(status)
+    del status
+    gc.collect()
+    assert held() is not None                       # its memory may not be handed out again
+    out.sum().backward()
+    assert lib.last(name + "_backward")[STATUS] == place
+    del out
+    gc.collect()
+    assert held() is None
