@@ -225,7 +225,7 @@ class _TokenLogprobs(torch.autograd.Function):
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
         saved = _saved(rows)
         ctx.rows, ctx.tokens, ctx.saved = rows, rows.row(tokens, "tokens", torch.int32), saved
-        ctx.save_for_backward(logits, ctx.tokens)   # notices a change of either before the backward pass
+        ctx.save_for_backward(logits, ctx.tokens, rows.seq_T)   # notices a change of any before the backward pass
         logp, H = _token_forward(rows, ctx.tokens, entropy, saved)
         ctx.with_entropy = entropy
         return (logp, H) if entropy else logp
@@ -301,7 +301,7 @@ class _PolicyLoss(torch.autograd.Function):
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
         ctx.held, ctx.args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, *coefs)
         ctx.rows, ctx.saved = rows, _saved(rows)
-        ctx.save_for_backward(logits, *(t for t in ctx.held if t is not None))
+        ctx.save_for_backward(logits, rows.seq_T, *ctx.held)
         t = _policy_outputs(rows, ctx.held, entropy)
         rows.call(load_library().ears_policy_loss, *ctx.args, *(_ptr(o) for o in t), ctx.saved.data_ptr())
         ctx.mark_non_differentiable(*(o for o in t[1:] if o is not None))
@@ -391,7 +391,7 @@ class _DistillLoss(torch.autograd.Function):
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
         ctx.held, ctx.args = _distill_inputs(rows, teacher, kind, mix)
         ctx.rows, ctx.saved = rows, _saved(rows)
-        ctx.save_for_backward(logits, *(t for t in ctx.held if t is not None))
+        ctx.save_for_backward(logits, rows.seq_T, *ctx.held)
         loss = _loss_like(rows, ctx.held[2])
         rows.call(load_library().ears_distill_loss, *ctx.args, loss.data_ptr(), ctx.saved.data_ptr())
         return loss

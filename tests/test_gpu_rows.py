@@ -861,3 +861,60 @@ def test_a_round_of_drafting_and_learning(ears):
     r2 = s2(tg, dg, xg)
     o2 = R.token_logprobs(t.view(-1, V), r2.tokens.cpu().view(-1), Ts.repeat_interleave(K + 1))
     close(r2.logprobs.view(-1), o2.logp, LOG_TOL)
+
+
+@pytest.mark.parametrize("dtype,V", [("fp32", 1003), ("bf16", 9001), ("fp16", 33001)])
+@pytest.mark.parametrize("cluster", [0, 1, 4])
+def test_a_temperature_per_sequence_in_every_loss_step_and_backward_call(ears, dtype, V, cluster):
+    ears.set_row_cluster(cluster)
+    B, Rr, k = 4, 3, 9
+    n = B * Rr
+    Ts = torch.tensor([0.5, 0.9, 1.0, 1.7])
+    T = Ts.repeat_interleave(Rr)
+    x, g = logits(n, V, dtype, 200 + V)
+    t = (x.float() + 0.8 * torch.randn(n, V, generator=g)).to(DT[dtype])
+    tok = torch.randint(V // 8, V - V // 16, (n,), generator=g, dtype=torch.int32)
+    dl, dh, w = torch.randn(n, generator=g), torch.randn(n, generator=g), torch.rand(n, generator=g)
+    vals, ids, lse = R.top_logits(t, k, T)
+    held = (vals.float(), ids.to(torch.int32), lse.float())
+    logp = R.token_logprobs(x, tok, T).logp
+    old, ref = (logp + 0.3).float(), (logp - 0.2).float()
+    row = lambda a: a.view(B, Rr, *a.shape[1:]).to(DEV)
+    flat = lambda a: a.reshape(n, *a.shape[2:])
+    xg, tg, seq = row(x), row(tok), Ts.to(DEV)
+    coefs = dict(kl_coef=0.1, entropy_coef=0.02)
+
+    top = ears.top_logits(row(t), k, seq_temperature=seq)
+    assert torch.equal(flat(top.ids).cpu(), held[1])
+    close(flat(top.lse), lse, LOG_TOL)
+    o = R.token_logprobs(x, tok, T, dl, dh)
+    lp, H, grad = ears.token_logprobs_step(xg, tg, row(dl), row(dh), seq_temperature=seq)
+    close(flat(lp), o.logp, LOG_TOL)
+    close(flat(H), o.entropy, H_TOL)
+    close_grad(flat(grad), o.grad, o.scale, 2 * H_TOL, dtype)
+    leaf = xg.clone().requires_grad_(True)
+    torch.autograd.backward(ears.token_logprobs(leaf, tg, entropy=True, seq_temperature=seq), [row(dl), row(dh)])
+    close_grad(flat(leaf.grad), o.grad, o.scale, 2 * H_TOL, dtype)
+
+    o = R.policy(x, tok, T, old, dl, ref=ref, weight=w, **coefs)
+    args = (tg, row(old), row(dl))
+    terms, grad = ears.policy_step(xg, *args, ref_logp=row(ref), row_weight=row(w), seq_temperature=seq, **coefs)
+    close(flat(terms.loss), o.loss, o.loss_scale * (2 * LOG_TOL) + 0.02 * H_TOL)
+    close_grad(flat(grad), o.grad, o.scale, 2 * H_TOL, dtype)
+    leaf.grad = None
+    terms = ears.policy_loss(leaf, *args, ref_logp=row(ref), seq_temperature=seq, **coefs)
+    close(flat(terms.loss), o.loss, o.loss_scale * (2 * LOG_TOL) + 0.02 * H_TOL)
+    (terms.loss * row(w)).sum().backward()
+    close_grad(flat(leaf.grad), o.grad, o.scale, 2 * H_TOL, dtype)
+
+    teacher = ears.TopLogits(*map(row, held))
+    for kind in ("forward_kl", "reverse_kl", "jsd"):
+        o = R.distill(x, T, *held[:2], lse=held[2], kind=kind, weight=w)
+        loss, grad = ears.distill_step(xg, teacher, kind=kind, row_weight=row(w), seq_temperature=seq)
+        close(flat(loss), o.loss, o.loss_scale * (3 * LOG_TOL))
+        close_grad(flat(grad), o.grad, o.scale, G_TOL, dtype)
+        leaf.grad = None
+        loss = ears.distill_loss(leaf, teacher, kind=kind, seq_temperature=seq)
+        close(flat(loss), o.loss, o.loss_scale * (3 * LOG_TOL))
+        (loss * row(w)).sum().backward()
+        close_grad(flat(leaf.grad), o.grad, o.scale, G_TOL, dtype)

@@ -83,3 +83,16 @@ def test_the_status_word_lives_until_the_backward_pass_is_over(lib, name):
     del out
     gc.collect()
     assert held() is None
+
+
+@pytest.mark.parametrize("name", sorted(LOSSES))
+def test_a_changed_temperature_is_noticed_by_the_backward_pass(lib, name):
+    T = torch.ones(1)                                # logits [R, V] are one sequence
+    out = LOSSES[name](leaf(), Inputs(), seq_temperature=T)
+    T.mul_(0.9)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
+    assert not any(n == name + "_backward" for n, _ in lib.calls)
+    T = torch.ones(1)
+    LOSSES[name](leaf(), Inputs(), seq_temperature=T).sum().backward()
+    assert lib.last(name + "_backward")[8] == T.data_ptr()
