@@ -170,8 +170,25 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _addresses(ts):
+    return tuple(_ptr(t) for t in ts)
+
+
 def _saved(rows):
     return torch.empty(rows.lead + (4,), dtype=_F32, device=rows.logits.device)
+
+
+def _keep(ctx, rows, logits, status, saved, *held):
+    """What the backward call reads goes through autograd, which notices changes, frees it and may move it meanwhile: the logits
+    (or the copy made of them), the temperatures, the statistics, the per-row inputs.  The status word is written to."""
+    ctx.temperature, ctx.status = rows.args[7], status
+    ctx.save_for_backward(logits if rows.logits.data_ptr() == logits.data_ptr() else rows.logits, rows.seq_T, saved, *held)
+
+
+def _kept(ctx):
+    """-> the rows again, the statistics, the per-row inputs"""
+    logits, seq_T, saved, *held = ctx.saved_tensors
+    return _Rows(logits, ctx.temperature, seq_T, ctx.status), saved, held
 
 
 def _refuse_capture():
@@ -223,24 +240,20 @@ class _TokenLogprobs(torch.autograd.Function):
     def forward(ctx, logits, tokens, temperature, seq_temperature, entropy, status):
         _refuse_capture()
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
-        saved = _saved(rows)
-        ctx.rows, ctx.tokens, ctx.saved = rows, rows.row(tokens, "tokens", torch.int32), saved
-        ctx.save_for_backward(logits, ctx.tokens, rows.seq_T)   # notices a change of any before the backward pass
-        logp, H = _token_forward(rows, ctx.tokens, entropy, saved)
-        ctx.with_entropy = entropy
+        saved, tokens = _saved(rows), rows.row(tokens, "tokens", torch.int32)
+        _keep(ctx, rows, logits, status, saved, tokens)
+        logp, H = _token_forward(rows, tokens, entropy, saved)
         return (logp, H) if entropy else logp
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_logp, d_entropy=None):
         _refuse_capture()
-        ctx.saved_tensors
-        rows = ctx.rows
+        rows, saved, (tokens,) = _kept(ctx)
         g, place = rows.grad(None)
         dl = rows.row(d_logp, "d_logp")
         dh = rows.row(d_entropy, "d_entropy")
-        rows.call(load_library().ears_token_logprobs_backward, ctx.tokens.data_ptr(), ctx.saved.data_ptr(), dl.data_ptr(),
-                  _ptr(dh), *place)
+        rows.call(load_library().ears_token_logprobs_backward, tokens.data_ptr(), saved.data_ptr(), dl.data_ptr(), _ptr(dh), *place)
         return (g,) + (None,) * 5
 
 
@@ -285,7 +298,7 @@ def token_logprobs_step(logits: torch.Tensor, tokens: torch.Tensor, d_logp: torc
 def _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, clip_low, clip_high, kl_coef, entropy_coef):
     held = (rows.row(tokens, "tokens", torch.int32), rows.row(old_logp, "old_logp"), rows.row(ref_logp, "ref_logp"),
             rows.row(advantage, "advantage"))
-    return held, tuple(_ptr(t) for t in held) + (float(clip_low), float(clip_high), float(kl_coef), float(entropy_coef))
+    return held, _addresses(held) + (float(clip_low), float(clip_high), float(kl_coef), float(entropy_coef))
 
 
 def _policy_outputs(rows, held, entropy):
@@ -299,11 +312,11 @@ class _PolicyLoss(torch.autograd.Function):
     def forward(ctx, logits, tokens, old_logp, advantage, ref_logp, temperature, coefs, seq_temperature, entropy, status):
         _refuse_capture()
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
-        ctx.held, ctx.args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, *coefs)
-        ctx.rows, ctx.saved = rows, _saved(rows)
-        ctx.save_for_backward(logits, rows.seq_T, *ctx.held)
-        t = _policy_outputs(rows, ctx.held, entropy)
-        rows.call(load_library().ears_policy_loss, *ctx.args, *(_ptr(o) for o in t), ctx.saved.data_ptr())
+        held, args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, *coefs)
+        saved, ctx.coefs = _saved(rows), args[len(held):]
+        _keep(ctx, rows, logits, status, saved, *held)
+        t = _policy_outputs(rows, held, entropy)
+        rows.call(load_library().ears_policy_loss, *args, *_addresses(t), saved.data_ptr())
         ctx.mark_non_differentiable(*(o for o in t[1:] if o is not None))
         return tuple(t)
 
@@ -311,11 +324,10 @@ class _PolicyLoss(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_loss, *_):
         _refuse_capture()
-        ctx.saved_tensors
-        rows = ctx.rows
+        rows, saved, held = _kept(ctx)
         g, place = rows.grad(None)
         dl = rows.row(d_loss, "d_loss")
-        rows.call(load_library().ears_policy_backward, *ctx.args, ctx.saved.data_ptr(), dl.data_ptr(), *place)
+        rows.call(load_library().ears_policy_backward, *_addresses(held), *ctx.coefs, saved.data_ptr(), dl.data_ptr(), *place)
         return (g,) + (None,) * 9
 
 
@@ -339,7 +351,7 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
     rows = _Rows(logits, temperature, seq_temperature, status)
     held, args = _policy_inputs(rows, tokens, old_logp, advantage, ref_logp, *coefs)
     t = _policy_outputs(rows, held, with_entropy)
-    rows.call(load_library().ears_policy_loss, *args, *(_ptr(o) for o in t), None)
+    rows.call(load_library().ears_policy_loss, *args, *_addresses(t), None)
     return t
 
 
@@ -361,7 +373,7 @@ def policy_step(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
     w = rows.row(row_weight, "row_weight")
     t = _policy_outputs(rows, held, with_entropy)
     g, place = rows.grad(out_grad)
-    rows.call(load_library().ears_policy_step, *args, _ptr(w), *(_ptr(o) for o in t), *place)
+    rows.call(load_library().ears_policy_step, *args, _ptr(w), *_addresses(t), *place)
     _overwritten(out_grad)
     return t, g
 
@@ -377,7 +389,7 @@ def _distill_inputs(rows, teacher, kind, mix):
         raise ValueError(f"the teacher's lists must have 1..{MAX_TOP} entries")
     held = (rows.per(values, torch.float32, rows.lead + (k,), "teacher values"),
             rows.per(ids, torch.int32, rows.lead + (k,), "teacher ids"), rows.row(lse, "teacher lse"))
-    return held, (k,) + tuple(_ptr(t) for t in held) + (DISTILL_KINDS[kind], float(mix))
+    return held, (k,) + _addresses(held) + (DISTILL_KINDS[kind], float(mix))
 
 
 def _loss_like(rows, t):
@@ -389,22 +401,21 @@ class _DistillLoss(torch.autograd.Function):
     def forward(ctx, logits, teacher, temperature, kind, mix, seq_temperature, status):
         _refuse_capture()
         rows = _Rows(logits.detach(), temperature, seq_temperature, status)
-        ctx.held, ctx.args = _distill_inputs(rows, teacher, kind, mix)
-        ctx.rows, ctx.saved = rows, _saved(rows)
-        ctx.save_for_backward(logits, rows.seq_T, *ctx.held)
-        loss = _loss_like(rows, ctx.held[2])
-        rows.call(load_library().ears_distill_loss, *ctx.args, loss.data_ptr(), ctx.saved.data_ptr())
+        held, args = _distill_inputs(rows, teacher, kind, mix)
+        saved, ctx.kind = _saved(rows), args[1 + len(held):]
+        _keep(ctx, rows, logits, status, saved, *held)
+        loss = _loss_like(rows, held[2])
+        rows.call(load_library().ears_distill_loss, *args, loss.data_ptr(), saved.data_ptr())
         return loss
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_loss):
         _refuse_capture()
-        ctx.saved_tensors
-        rows = ctx.rows
+        rows, saved, held = _kept(ctx)
         g, place = rows.grad(None)
         dl = rows.row(d_loss, "d_loss")
-        rows.call(load_library().ears_distill_backward, *ctx.args, ctx.saved.data_ptr(), dl.data_ptr(), *place)
+        rows.call(load_library().ears_distill_backward, held[1].shape[-1], *_addresses(held), *ctx.kind, saved.data_ptr(), dl.data_ptr(), *place)
         return (g,) + (None,) * 6
 
 

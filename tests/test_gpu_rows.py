@@ -918,3 +918,50 @@ def test_a_temperature_per_sequence_in_every_loss_step_and_backward_call(ears, d
         close(flat(loss), o.loss, o.loss_scale * (3 * LOG_TOL))
         (loss * row(w)).sum().backward()
         close_grad(flat(leaf.grad), o.grad, o.scale, G_TOL, dtype)
+
+
+@pytest.mark.parametrize("sliced", [False, True])
+def test_backward_through_hooks_checkpoints_and_twice(ears, sliced):
+    """Logits offloaded between the passes, recomputed, or kept for a second backward pass: the same gradient; and nothing of
+    their size is left behind it."""
+    from torch.utils.checkpoint import checkpoint
+    B, Rr, V, k = 3, 5, 40003, 8
+    x, vals, ids, lse, g = teacher_case(B * Rr, V, k, "bf16", 1.0, 19)
+    base = x.view(B, Rr, V).to(DEV)
+    leaf = base.clone().requires_grad_(True)
+    at = (lambda t: t[:, :-1]) if sliced else (lambda t: t)
+    n = at(base).shape[:2]
+    row = lambda t: at(t.view(B, Rr, *t.shape[1:])).contiguous().to(DEV)
+    teacher, tok, f = ears.TopLogits(row(vals.float()), row(ids.to(torch.int32)), row(lse.float())), row(ids[:, 0].to(torch.int32)), torch.ones(n, device=DEV)
+    losses = (lambda y: ears.distill_loss(y, teacher, kind="jsd"), lambda y: ears.token_logprobs(y, tok),
+              lambda y: ears.policy_loss(y, tok, -f, f, entropy_coef=0.01).loss)
+    for loss in losses:
+        def grad(run):
+            leaf.grad = None
+            run()
+            torch.cuda.synchronize()
+            return leaf.grad
+        want = grad(lambda: loss(at(leaf * 1.0)).sum().backward())
+        assert want.any()
+
+        def offloaded():
+            with torch.autograd.graph.save_on_cpu():
+                loss(at(leaf * 1.0)).sum().backward()
+
+        def twice():
+            out = loss(at(leaf * 1.0)).sum()
+            out.backward(retain_graph=True)
+            first, leaf.grad = leaf.grad, None
+            out.backward()
+            assert torch.equal(first, leaf.grad)
+            with pytest.raises(RuntimeError, match="second time"):
+                out.backward()
+        for run in (offloaded, twice, lambda: checkpoint(lambda y: loss(at(y * 1.0)), leaf, use_reentrant=False).sum().backward()):
+            assert torch.equal(grad(run), want)
+        leaf.grad = None
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        out = loss(at(leaf * 1.0))
+        out.sum().backward()
+        leaf.grad = None
+        assert torch.cuda.memory_allocated() - before < V * 2 and out.grad_fn is not None

@@ -96,3 +96,45 @@ def test_a_changed_temperature_is_noticed_by_the_backward_pass(lib, name):
     T = torch.ones(1)
     LOSSES[name](leaf(), Inputs(), seq_temperature=T).sum().backward()
     assert lib.last(name + "_backward")[8] == T.data_ptr()
+
+
+@pytest.mark.parametrize("name", sorted(LOSSES))
+@pytest.mark.parametrize("copied", [False, True])
+def test_nothing_of_the_logits_size_outlives_the_backward_pass(lib, monkeypatch, name, copied):
+    memory, contiguous = [], torch.Tensor.contiguous
+
+    def watched(t):
+        t = contiguous(t)
+        memory.append(weakref.ref(t.untyped_storage()))
+        return t
+    x = leaf()
+    y = x.t().contiguous().t() if copied else x * 1.0          # entries of a row apart: the call works on a copy
+    memory.append(weakref.ref(y.untyped_storage()))
+    monkeypatch.setattr(torch.Tensor, "contiguous", watched)
+    out = LOSSES[name](y, Inputs())
+    assert len(memory) == 1 + copied
+    if copied:
+        assert memory[1]() is not None
+    del y
+    out.sum().backward()
+    gc.collect()
+    assert out.grad_fn is not None                              # the loss is still there
+    assert all(m() is None for m in memory[:1 + copied])
+
+
+@pytest.mark.parametrize("name", sorted(LOSSES))
+def test_saved_tensor_hooks_stand_between_the_passes(lib, name):
+    """What the backward call reads is what the hooks hand back, the statistics among it."""
+    back = []
+
+    def unpack(t):
+        back.append(t.clone())
+        return back[-1]
+    x, T = leaf(), torch.ones(1)
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t.detach(), unpack):
+        out = LOSSES[name](x, Inputs(), seq_temperature=T)
+        out.sum().backward()
+    places = {t.data_ptr() for t in back}
+    args = lib.last(name + "_backward")
+    assert args[1] in places and args[8] in places              # logits, temperatures
+    assert sum(a in places for a in args) == len(back)
