@@ -5,8 +5,9 @@ policy loss.  Argument marshalling only; every computation runs in the CUDA libr
 Logits are CUDA tensors [B, R, V] or [R, V] (float32, bfloat16, float16); rows are used where they
 lie as long as the entries of a row are contiguous (a slice ``target[:, :K]`` is not copied).  Per-row tensors
 have the logits' shape without V and are converted to contiguous float32 / int32 where they are not.
-``*_loss`` and ``token_logprobs`` can be differentiated by autograd; ``*_step`` return the gradient at once,
-reading the logits from memory a single time, and are what a step recorded into a CUDA graph uses.
+``*_loss`` and ``token_logprobs`` can be differentiated by autograd, in the logits alone (every other input counts as a
+constant; forward mode is refused); ``*_step`` return the gradient at once, reading the logits from memory a single
+time, and are what a step recorded into a CUDA graph uses.
 Calls whose tensors are in their plain form already go through csrc/ears_torch.cpp, which makes the same C-ABI call
 with less work on the host; everything else is converted, checked and refused here.
 ``status``: optional int32 CUDA tensor of one element that gets EARS_DEV_INVALID_INPUT OR-ed in.
@@ -19,6 +20,7 @@ import os
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding
 from . import build as _build
@@ -65,10 +67,22 @@ def _plain_calls():
     return _plain
 
 
+def _refuse_tangents(values) -> None:
+    # a dual tensor does not say requires_grad: its tangent would be dropped without a word
+    for v in values:
+        if isinstance(v, tuple):
+            _refuse_tangents(v)
+        elif isinstance(v, torch.Tensor) and forward_ad.unpack_dual(v).tangent is not None:
+            raise NotImplementedError("the row operators have no forward-mode derivatives")
+
+
 def _on_stream(fn):
     """``stream=``: the whole call, its conversions and outputs included, belongs to that stream as under torch.cuda.stream."""
     @functools.wraps(fn)
     def call(*args, stream=None, **kwargs):
+        if forward_ad._current_level >= 0:
+            _refuse_tangents(args)
+            _refuse_tangents(kwargs.values())
         if stream is None:
             return fn(*args, **kwargs)
         logits = args[0] if args else kwargs["logits"]

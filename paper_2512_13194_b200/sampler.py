@@ -84,7 +84,7 @@ class EarsSampler:
         if self.report_logprobs:
             res.logprobs = rows.token_logprobs(target_logits.detach(), res.tokens, T, seq_temperature=seq_T, stream=stream)
         if self.teacher_k:
-            res.teacher = rows.top_logits(target_logits[:, :-1], self.teacher_k, T, accept_len=res.accept_len,
+            res.teacher = rows.top_logits(target_logits.detach()[:, :-1], self.teacher_k, T, accept_len=res.accept_len,
                                           seq_temperature=seq_T, stream=stream)
         self.offset += 1
         self.steps += 1

@@ -138,3 +138,30 @@ def test_saved_tensor_hooks_stand_between_the_passes(lib, name):
     args = lib.last(name + "_backward")
     assert args[1] in places and args[8] in places              # logits, temperatures
     assert sum(a in places for a in args) == len(back)
+
+
+ALL_CALLS = dict(LOSSES, **{
+    "ears_top_logits": lambda x, i: ears.top_logits(x, K),
+    "ears_token_logprobs_step": lambda x, i: ears.token_logprobs_step(x, i.tokens, i.f[0]),
+    "ears_policy_step": lambda x, i: ears.policy_step(x, i.tokens, i.f[0], i.f[1]),
+    "ears_distill_step": lambda x, i: ears.distill_step(x, i.teacher),
+})
+
+
+@pytest.mark.parametrize("name", sorted(ALL_CALLS))
+def test_forward_mode_derivatives_are_refused(lib, name):
+    from torch.autograd import forward_ad
+    call = ALL_CALLS[name]
+    with forward_ad.dual_level():
+        dual = lambda t: forward_ad.make_dual(t, torch.ones_like(t))
+        with pytest.raises(NotImplementedError, match="forward-mode"):
+            call(dual(torch.zeros(N, V)), Inputs())
+        i = Inputs()
+        i.f, i.teacher = [dual(t) for t in i.f], i.teacher._replace(values=dual(i.teacher.values))
+        if name not in ("ears_top_logits", "ears_token_logprobs"):      # which take integers beside the logits
+            with pytest.raises(NotImplementedError, match="forward-mode"):
+                call(torch.zeros(N, V), i)
+        assert not lib.calls
+        call(torch.zeros(N, V), Inputs())                       # no tangent: as ever
+        call(dual(torch.zeros(N, V)).detach(), Inputs())
+        assert lib.calls
