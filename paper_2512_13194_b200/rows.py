@@ -28,6 +28,7 @@ from .binding import _check, load_library
 
 MAX_TOP = 128
 DISTILL_KINDS = {"forward_kl": 0, "reverse_kl": 1, "jsd": 2}
+_INT32_MAX = 2**31 - 1
 _DTYPES = {torch.float32: binding.EARS_DTYPE_F32, torch.bfloat16: binding.EARS_DTYPE_BF16, torch.float16: binding.EARS_DTYPE_F16}
 
 
@@ -100,6 +101,16 @@ def _overwritten(out_grad) -> None:
         torch.autograd.graph.increment_version(out_grad)
 
 
+def _within_int32(t):
+    """Integers beyond 32 bits go to the nearest that 32 bits hold, which is an index of no row either."""
+    if t.dtype is torch.uint64:
+        t = t.to(torch.int64)
+        t = torch.where(t < 0, _INT32_MAX, t)       # 2^63 and more
+    elif t.dtype is torch.uint32:
+        t = t.to(torch.int64)
+    return t.clamp(-_INT32_MAX - 1, _INT32_MAX) if t.dtype is torch.int64 else t
+
+
 class _Rows:
     """The common head of a call: dtype, pointer, sizes, strides, temperature.  Small calls are bound by the host, so
     nothing is converted, viewed or looked up that is as it should be already."""
@@ -147,7 +158,10 @@ class _Rows:
         if t.dtype is not dtype:
             if dtype is torch.int32 and (t.dtype.is_floating_point or t.dtype is torch.bool):
                 raise TypeError(f"{name} must hold integers")
-            t = t.detach().to(dtype)
+            t = t.detach()
+            if dtype is torch.int32:
+                t = _within_int32(t)
+            t = t.to(dtype)
         return t if t.is_contiguous() else t.contiguous()
 
     def row(self, t, name, dtype=torch.float32):

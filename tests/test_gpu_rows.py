@@ -965,3 +965,25 @@ def test_backward_through_hooks_checkpoints_and_twice(ears, sliced):
         out.sum().backward()
         leaf.grad = None
         assert torch.cuda.memory_allocated() - before < V * 2 and out.grad_fn is not None
+
+
+def test_ids_beyond_32_bits_make_their_rows_unusable(ears):
+    V, wide = 300, [2**32 + 5, 2**31, -2**32 - 1, -1]
+    x, g = logits(5, V, "fp32", 21)
+    tok = torch.tensor(wide + [100])
+    for logits_ in (x.to(DEV), x.to(DEV).requires_grad_(True)):
+        st = torch.zeros(1, dtype=torch.int32, device=DEV)
+        logp = ears.token_logprobs(logits_, tok.to(DEV), status=st)
+        assert int(st) == ears.DEV_INVALID_INPUT
+        logp = logp.detach()
+        assert torch.isnan(logp[:3]).all() and float(logp[3]) == 0.0
+        close(logp[4:], R.token_logprobs(x[4:], tok[4:], 1.0).logp, LOG_TOL)
+    ids = torch.tensor([[5, w] for w in wide + [100]])
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    loss, grad = ears.distill_step(x.to(DEV), ears.TopLogits(torch.zeros(5, 2, device=DEV), ids.to(DEV), None), status=st)
+    assert int(st) == ears.DEV_INVALID_INPUT
+    assert torch.isnan(loss[:3]).all() and not grad[:3].any()
+    o = R.distill(x[3:], 1.0, torch.tensor([[0.0, -math.inf], [0.0, 0.0]]), ids[3:])
+    close(loss[3:], o.loss, o.loss_scale * (3 * LOG_TOL))      # entry 5 of the last row is masked: infinite
+    close_grad(grad[3:4], o.grad[:1], o.scale[:1], G_TOL, "fp32")
+    assert torch.isfinite(grad[4]).all()

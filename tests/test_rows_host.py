@@ -1,5 +1,6 @@
 """What the Python side of the row operators hands to the library and keeps between calls: tensors on the CPU pass for
 device tensors, and a stand-in for the library records its arguments and touches none of them."""
+import ctypes
 import gc
 import weakref
 
@@ -165,3 +166,53 @@ def test_forward_mode_derivatives_are_refused(lib, name):
         call(torch.zeros(N, V), Inputs())                       # no tangent: as ever
         call(dual(torch.zeros(N, V)).detach(), Inputs())
         assert lib.calls
+
+
+def entries(place, n, ctype):
+    """What a recorded address holds (the tensor must still be alive)."""
+    return list((ctype * n).from_address(place))
+
+
+WIDE = [2**32 + 5, 2**31, -2**32 - 1, 2**63 - 1, -2**63, 2**32]
+
+
+@pytest.mark.parametrize("dtype", [torch.int64, torch.uint64, torch.uint32])
+def test_ids_that_32_bits_cannot_hold_do_not_become_others(lib, monkeypatch, dtype):
+    wide = WIDE if dtype is torch.int64 else [2**32 - 1, 2**31 + 3] + ([2**64 - 1, 2**63 + 7] if dtype is torch.uint64 else [])
+    n = len(wide) + 3
+    t = torch.tensor(wide + [7, 15, 0], dtype=dtype)
+    x, f = torch.zeros(n, V), torch.zeros(n)
+    got = []
+
+    def entry(*args):
+        got.append(entries(args[9], n, ctypes.c_int32))
+        return 0
+    monkeypatch.setattr(lib, "ears_token_logprobs", entry, raising=False)
+    ears.token_logprobs(x, t)
+    monkeypatch.setattr(lib, "ears_policy_step", entry, raising=False)
+    ears.policy_step(x, t, f, f)
+    monkeypatch.setattr(lib, "ears_distill_step", lambda *args: got.append(entries(args[11], n, ctypes.c_int32)) or 0, raising=False)
+    ears.distill_step(x, ears.TopLogits(torch.zeros(n, 1), t.view(n, 1), None))
+    assert len(got) == 3
+    for ids in got:
+        assert ids[-3:] == [7, 15, 0]
+        for i in ids[:-3]:
+            assert i < -1 or i >= 2**30                         # neither left out nor an entry of any row
+
+
+def test_lengths_that_32_bits_cannot_hold(lib, monkeypatch):
+    got = []
+    monkeypatch.setattr(lib, "ears_top_logits", lambda *args: got.extend(entries(args[9], 3, ctypes.c_int32)) or 0, raising=False)
+    ears.top_logits(torch.zeros(3, 2, V), 2, accept_len=torch.tensor([1, 2**32 + 1, -2**33 - 1]))
+    assert got[0] == 1 and got[1] >= 2 and got[2] < 0
+
+
+def test_ids_in_narrow_types_and_their_refusals(lib, monkeypatch):
+    got = []
+    monkeypatch.setattr(lib, "ears_token_logprobs", lambda *args: got.append(entries(args[9], N, ctypes.c_int32)) or 0, raising=False)
+    for dtype in (torch.int8, torch.int16, torch.int64, torch.uint8):
+        ears.token_logprobs(torch.zeros(N, V), torch.tensor([3, 1, 2], dtype=dtype))
+    assert got == [[3, 1, 2]] * 4
+    for dtype in (torch.float32, torch.bool, torch.float64):
+        with pytest.raises(TypeError):
+            ears.token_logprobs(torch.zeros(N, V), torch.zeros(N, dtype=dtype))
