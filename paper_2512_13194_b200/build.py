@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import glob
+import hashlib
 import os
 import subprocess
 import sys
@@ -60,20 +61,36 @@ def build(force: bool = False, verbose: bool = False, trace: bool = False) -> st
 TORCH_LIB = os.path.join(HERE, "ears_torch.so")
 
 
+def torch_stamp() -> str:
+    """What csrc/ears_torch.cpp is compiled from and for, as the module carries it: its source, the C header, torch and Python."""
+    import torch
+    h = hashlib.sha256(f"{torch.__version__} {sys.version}".encode())
+    for path in (os.path.join(CSRC, "ears_torch.cpp"), os.path.join(os.path.dirname(HERE), "include", "ears.h")):
+        with open(path, "rb") as f:
+            h.update(f.read())
+    return "ears_torch:" + h.hexdigest()
+
+
+def torch_is_stale() -> bool:
+    if not os.path.exists(TORCH_LIB):
+        return True
+    with open(TORCH_LIB, "rb") as f:
+        return torch_stamp().encode() not in f.read()
+
+
 def build_torch(force: bool = False) -> str:
     """The Python entry of the row operators (csrc/ears_torch.cpp): host code only, against torch's C++ headers."""
     import sysconfig
 
     import torch
     src = os.path.join(CSRC, "ears_torch.cpp")
-    header = os.path.join(os.path.dirname(HERE), "include", "ears.h")
-    if not force and os.path.exists(TORCH_LIB) and all(os.path.getmtime(f) <= os.path.getmtime(TORCH_LIB) for f in (src, header)):
+    if not force and not torch_is_stale():
         return TORCH_LIB
     root = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
     linked = f"{TORCH_LIB}.{os.getpid()}"
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{root}/include",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DEARS_TORCH_STAMP="{torch_stamp()}"', f"-I{root}/include",
            f"-I{root}/include/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}", f"-I{cuda}/include", "-o", linked, src,
            f"-L{root}/lib", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python", f"-Wl,-rpath,{root}/lib"]
     subprocess.run(cmd, check=True)

@@ -343,4 +343,12 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "ears_torch", nullptr, -1, g_meth
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit_ears_torch(void) { return PyModule_Create(&g_module); }
+PyMODINIT_FUNC PyInit_ears_torch(void) {
+    PyObject* m = PyModule_Create(&g_module);
+    // what build.py compares before it takes a module that is there already, and the C interface's version
+    if (m && (PyModule_AddStringConstant(m, "stamp", EARS_TORCH_STAMP) || PyModule_AddIntConstant(m, "version", EARS_VERSION))) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}

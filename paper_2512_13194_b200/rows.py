@@ -16,7 +16,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
-import os
+import warnings
 from typing import NamedTuple, Optional
 
 import torch
@@ -45,8 +45,13 @@ class PolicyTerms(NamedTuple):
     entropy: Optional[torch.Tensor]
 
 
-_plain = None          # the ears_torch module, bound to the library in use
+_plain = None          # the ears_torch module, bound to the library in use, or _Ctypes
 _plain_for = None
+
+
+class _Ctypes:
+    """In the module's place where it cannot be had: no call is in its plain form."""
+    top_logits = token_logprobs = token_logprobs_step = policy = distill = staticmethod(lambda *args: None)
 
 
 def _plain_calls():
@@ -56,16 +61,24 @@ def _plain_calls():
     if lib is not None and lib is _plain_for:
         return _plain
     lib = load_library()
-    if _plain is None:
-        if not os.path.exists(_build.TORCH_LIB):
-            _build.build_torch()
-        from . import ears_torch
-        _plain = ears_torch
-    names = ("ears_top_logits", "ears_token_logprobs", "ears_token_logprobs_step", "ears_policy_loss", "ears_policy_step",
-             "ears_distill_loss", "ears_distill_step")
-    _plain.bind({n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names})
+    try:
+        _plain = _bind_module(lib)
+    except Exception as e:
+        warnings.warn(f"ears: the row operators' calls go through ctypes, which takes the host some 10 us more each: {e}", RuntimeWarning)
+        _plain = _Ctypes
     _plain_for = lib
     return _plain
+
+
+def _bind_module(lib):
+    _build.build_torch()       # nothing to do when what is there was built from these sources for this torch
+    from . import ears_torch
+    if ears_torch.version != lib.ears_version():
+        raise RuntimeError(f"ears_torch is for version {ears_torch.version} of the library, which has {lib.ears_version()}")
+    names = ("ears_top_logits", "ears_token_logprobs", "ears_token_logprobs_step", "ears_policy_loss", "ears_policy_step",
+             "ears_distill_loss", "ears_distill_step")
+    ears_torch.bind({n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names})
+    return ears_torch
 
 
 def _refuse_tangents(values) -> None:

@@ -987,3 +987,10 @@ def test_ids_beyond_32_bits_make_their_rows_unusable(ears):
     close(loss[3:], o.loss, o.loss_scale * (3 * LOG_TOL))      # entry 5 of the last row is masked: infinite
     close_grad(grad[3:4], o.grad[:1], o.scale[:1], G_TOL, "fp32")
     assert torch.isfinite(grad[4]).all()
+
+
+def test_plain_calls_go_through_the_module(ears):
+    from paper_2512_13194_b200 import rows
+    assert rows._plain_calls().__name__.endswith("ears_torch")
+    out = rows._plain_calls().token_logprobs(torch.zeros(3, 50, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV), False, 1.0, None, None)
+    assert out is not None and out[1] is None

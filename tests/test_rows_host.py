@@ -2,6 +2,8 @@
 device tensors, and a stand-in for the library records its arguments and touches none of them."""
 import ctypes
 import gc
+import shutil
+import warnings
 import weakref
 
 import pytest
@@ -216,3 +218,64 @@ def test_ids_in_narrow_types_and_their_refusals(lib, monkeypatch):
     for dtype in (torch.float32, torch.bool, torch.float64):
         with pytest.raises(TypeError):
             ears.token_logprobs(torch.zeros(N, V), torch.zeros(N, dtype=dtype))
+
+
+# ---- the extension module -----------------------------------------------------------------------------
+
+@pytest.fixture
+def unbound(monkeypatch):
+    """No call has been made yet."""
+    monkeypatch.setattr(rows, "_plain", None)
+    monkeypatch.setattr(rows, "_plain_for", None)
+
+
+def test_a_module_built_from_other_sources_is_built_again(tmp_path, monkeypatch):
+    build = rows._build
+    path = build.build_torch()
+    assert not build.torch_is_stale()
+    made = []
+
+    def compile(cmd, **kw):
+        made.append(cmd)
+        shutil.copy(path, cmd[cmd.index("-o") + 1])
+    monkeypatch.setattr(build, "TORCH_LIB", str(tmp_path / "ears_torch.so"))
+    monkeypatch.setattr(build.subprocess, "run", compile)
+    build.build_torch()                                          # absent
+    build.build_torch()                                          # current
+    assert len(made) == 1
+    monkeypatch.setattr(torch, "__version__", "1.0.0")           # compiled against another torch
+    assert build.torch_is_stale()
+    monkeypatch.undo()
+    copy = tmp_path / "csrc"
+    shutil.copytree(build.CSRC, copy)
+    monkeypatch.setattr(build, "CSRC", str(copy))
+    assert not build.torch_is_stale()                            # whatever the files' times
+    with open(copy / "ears_torch.cpp", "a") as f:
+        f.write("// changed\n")
+    assert build.torch_is_stale()
+
+
+def test_without_the_module_calls_go_through_ctypes(unbound, monkeypatch):
+    def no_compiler(*a, **kw):
+        raise OSError("no compiler")
+    monkeypatch.setattr(rows._build, "build_torch", no_compiler)
+    with pytest.warns(RuntimeWarning, match="no compiler"):
+        plain = rows._plain_calls()
+    for name in ("top_logits", "token_logprobs", "token_logprobs_step", "policy", "distill"):
+        assert getattr(plain, name)(1, 2, 3) is None             # "not in its plain form"
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        assert rows._plain_calls() is plain                      # said once
+
+
+def test_a_library_of_another_version_is_not_called_through_the_module(unbound, monkeypatch):
+    lib = ears.load_library()
+    assert rows._plain_calls().version == lib.ears_version()
+
+    class Other:
+        def __getattr__(self, name):
+            return (lambda: lib.ears_version() + 1) if name == "ears_version" else getattr(lib, name)
+    monkeypatch.setattr(rows.binding, "_lib", Other())
+    monkeypatch.setattr(rows, "load_library", lambda: rows.binding._lib)
+    with pytest.warns(RuntimeWarning, match="version"):
+        assert rows._plain_calls().policy() is None
