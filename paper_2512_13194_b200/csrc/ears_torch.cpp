@@ -10,6 +10,7 @@
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #define PY_SSIZE_T_CLEAN
@@ -179,15 +180,12 @@ PyObject* tuple_of(std::initializer_list<at::Tensor> ts) {
 #define EARS_ROWS(r) (r).dtype, (r).x->const_data_ptr(), (r).B, (r).R, (r).V, (r).sb, (r).sr, (r).T, (r).seq_T
 #define EARS_NOT_PLAIN Py_RETURN_NONE
 
-// C++ exceptions (an allocation that fails, say) become Python's
+// C++ exceptions become the Python exceptions that torch makes of them: an allocation that fails is torch.OutOfMemoryError
 template <typename F>
 PyObject* guarded(F&& f) {
-    try {
-        return f();
-    } catch (const std::exception& e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
-    }
+    HANDLE_TH_ERRORS
+    return f();
+    END_HANDLE_TH_ERRORS
 }
 
 // (logits, accept_len, k, T, seq_T, status)

@@ -994,3 +994,16 @@ def test_plain_calls_go_through_the_module(ears):
     assert rows._plain_calls().__name__.endswith("ears_torch")
     out = rows._plain_calls().token_logprobs(torch.zeros(3, 50, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV), False, 1.0, None, None)
     assert out is not None and out[1] is None
+
+
+def test_running_out_of_memory_is_told_as_such(ears):
+    """A broadcast row has a gradient of 8 TB."""
+    n = 1 << 21
+    x = torch.zeros(1, 1 << 20, device=DEV).expand(n, 1 << 20)
+    tok, f = torch.zeros(n, dtype=torch.int32, device=DEV), torch.zeros(n, device=DEV)
+    teacher = ears.TopLogits(torch.zeros(n, 1, device=DEV), torch.zeros(n, 1, dtype=torch.int32, device=DEV), None)
+    for step in (lambda t: ears.token_logprobs_step(x, t, f), lambda t: ears.policy_step(x, t, f, f), lambda t: ears.distill_step(x, teacher)):
+        for t in (tok, tok.long()):                      # through the module, through ctypes
+            with pytest.raises(torch.OutOfMemoryError):
+                step(t)
+    ears.token_logprobs(x[:3], tok[:3])
