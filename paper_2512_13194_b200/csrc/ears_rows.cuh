@@ -43,8 +43,9 @@ struct RowSpan {           // rows r = b R + k of [B, R, V] with strides in entr
 };
 constexpr int kSliceAlign = 8;   // 128-byte lines are not shared between slices
 
-// c = log2(e) / temperature: hi < c and lo = c - hi > 0 (a masked entry's -inf times lo must stay -inf), and the
-// nearest 32-bit value.
+// c = log2(e) / temperature: hi < c and lo = c - hi > 0, and the nearest 32-bit value.  None of them is 0, since a masked
+// entry's -inf times each must stay -inf: from T = 1e29 on lo may round to 0, from 1e45 on the others do, and 2^-149 takes
+// its place (2^-149 times the largest difference of two logits is 1e-6, in entries whose exponent is 0).
 struct Scale { float hi, lo, near; };
 
 __device__ __forceinline__ Scale make_scale(double T) {
@@ -52,8 +53,10 @@ __device__ __forceinline__ Scale make_scale(double T) {
     Scale s;
     s.hi = __double2float_rd(c);
     if ((double)s.hi == c) s.hi = __uint_as_float(__float_as_uint(s.hi) - 1u);
-    s.lo = (float)(c - (double)s.hi);
-    s.near = (float)c;
+    const float least = __uint_as_float(1u);
+    s.hi = fmaxf(s.hi, least);
+    s.lo = fmaxf((float)(c - (double)s.hi), least);
+    s.near = fmaxf((float)c, least);
     return s;
 }
 __device__ __forceinline__ float scaled(float d, const Scale& c) { return __fmaf_rn(d, c.hi, d * c.lo); }

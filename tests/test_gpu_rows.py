@@ -1007,3 +1007,33 @@ def test_running_out_of_memory_is_told_as_such(ears):
             with pytest.raises(torch.OutOfMemoryError):
                 step(t)
     ears.token_logprobs(x[:3], tok[:3])
+
+
+@pytest.mark.parametrize("T", [1e30, 3e38, 2e45, 1e300])
+@pytest.mark.parametrize("dtype,V,n", [("fp32", 1003, 6), ("bf16", 9001, 6), ("fp16", 40, 400)])
+def test_temperatures_so_high_that_32_bits_hold_nothing_of_their_inverse(ears, dtype, V, n, T):
+    """Every entry that is not masked has the same probability; masked ones have none."""
+    x, g = logits(n, V, dtype, 22)
+    k = 5
+    tok = torch.randint(V // 8 + 1, V - V // 16 - 1, (n,), generator=g, dtype=torch.int32)
+    dl, dh = torch.randn(n, generator=g), torch.randn(n, generator=g)
+    vals, ids, lse = R.top_logits(x, k, T)
+    Ts = [(T, {})] + ([(1.0, dict(seq_temperature=torch.tensor([T], device=DEV)))] if T < 1e38 or T == 3e38 else [])
+    for scalar, kw in Ts:
+        exact = T if not kw else float(torch.tensor(T))
+        o = R.token_logprobs(x, tok, exact, dl, dh)
+        top = ears.top_logits(x.to(DEV), k, scalar, **kw)
+        assert torch.equal(top.ids.cpu().long(), ids)
+        close(top.lse, lse, LOG_TOL)
+        logp, H, grad = ears.token_logprobs_step(x.to(DEV), tok.to(DEV), dl.to(DEV), dh.to(DEV), scalar, **kw)
+        close(logp, o.logp, LOG_TOL)
+        close(H, o.entropy, H_TOL)
+        close_grad(grad, o.grad, o.scale, 2 * H_TOL, dtype)
+        leaf = x.to(DEV).requires_grad_(True)
+        torch.autograd.backward(ears.token_logprobs(leaf, tok.to(DEV), scalar, entropy=True, **kw), [dl.to(DEV), dh.to(DEV)])
+        close_grad(leaf.grad, o.grad, o.scale, 2 * H_TOL, dtype)
+        teacher = ears.TopLogits(vals.float().to(DEV), ids.to(torch.int32).to(DEV), lse.float().to(DEV))
+        o = R.distill(x, exact, vals.float(), ids, lse=lse.float(), kind="jsd")
+        loss, grad = ears.distill_step(x.to(DEV), teacher, scalar, kind="jsd", **kw)
+        close(loss, o.loss, o.loss_scale * (3 * LOG_TOL))
+        close_grad(grad, o.grad, o.scale, G_TOL, dtype)
