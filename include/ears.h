@@ -494,7 +494,8 @@ int ears_token_logprobs_step(int dtype, const void* logits, int B, int R, int V,
 /*
  * Clipped policy loss per token, with rho = exp(logp - old_logp), logp as above:
  *   loss = -min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A) + kl_coef kl - entropy_coef H,
- *   kl   = exp(ref_logp - logp) - (ref_logp - logp) - 1     (0 without ref_logp; kl_coef > 0 needs it).
+ *   kl   = exp(ref_logp - logp) - (ref_logp - logp) - 1     (0 without ref_logp; kl_coef > 0 needs it; with kl_coef = 0
+ *          it is reported and enters neither the loss nor the gradient, infinite or not).
  * tokens, old_logp, ref_logp, advantage [B R]; token -1 leaves the row out.  out_logp, out_kl and out_entropy
  * are optional (not differentiated).  Where the clipped branch is taken the ratio's gradient is 0; on a tie
  * it is the unclipped branch's.  The gradient is that of sum_r w_r loss_r with w = d_loss (backward) or

@@ -87,9 +87,11 @@ __device__ __forceinline__ TokenScalars token_scalars(const TokenParams& p, long
         g = plain <= clipped ? -plain : 0.0;
         if (p.ref_logp) {
             const double d = (double)in.ref_logp - logp, ed = exp(d);
-            kl = ed - d - 1.0;
-            loss += p.kl_coef * kl;
-            g += p.kl_coef * (1.0 - ed);
+            kl = d < INFINITY ? ed - d - 1.0 : d;
+            if (p.kl_coef != 0.0) {   // an infinite term without weight is reported, no more
+                loss += p.kl_coef * kl;
+                g += p.kl_coef * (1.0 - ed);
+            }
         }
         if (ENT) loss -= p.entropy_coef * H;
         fine = fine && isfinite(old) && isfinite(A) && isfinite(loss) && isfinite(g);

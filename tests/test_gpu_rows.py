@@ -1037,3 +1037,34 @@ def test_temperatures_so_high_that_32_bits_hold_nothing_of_their_inverse(ears, d
         loss, grad = ears.distill_step(x.to(DEV), teacher, scalar, kind="jsd", **kw)
         close(loss, o.loss, o.loss_scale * (3 * LOG_TOL))
         close_grad(grad, o.grad, o.scale, G_TOL, dtype)
+
+
+@pytest.mark.parametrize("cluster", [0, 1, 4])
+def test_a_kl_term_without_weight_stays_out_of_the_loss(ears, cluster):
+    """ref_logp with kl_coef = 0 only reports the term: infinite where the token is masked or the reference far above, and
+    neither the loss nor the gradient take notice."""
+    ears.set_row_cluster(cluster)
+    n, V = 6, 7001
+    x, g = logits(n, V, "fp32", 23)
+    tok = torch.tensor([V - 1, 2000, 2001, -1, 2002, V - 2], dtype=torch.int32)      # the first and last are masked
+    adv, w = torch.randn(n, generator=g), torch.rand(n, generator=g)
+    logp = R.token_logprobs(x, tok, 1.0).logp
+    old = torch.where(torch.isinf(logp), -5.0, logp + 0.1).float()
+    ref = torch.tensor([-3.0, 0.0, 1000.0, 0.0, -math.inf, -2.0])
+    d = lambda t: t.to(DEV)
+    args = (d(x), d(tok), d(old), d(adv))
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    want, gw = ears.policy_step(*args, row_weight=d(w), entropy_coef=0.01)
+    assert torch.isfinite(want.loss).all()
+    got, gg = ears.policy_step(*args, row_weight=d(w), entropy_coef=0.01, ref_logp=d(ref), status=st)
+    assert torch.equal(got.loss, want.loss) and torch.equal(got.logp, want.logp) and torch.equal(gg, gw) and int(st) == 0
+    o = R.policy(x, tok, 1.0, old, adv, entropy_coef=0.01, weight=w)
+    close(got.loss, o.loss, o.loss_scale * (2 * LOG_TOL) + 0.01 * H_TOL)
+    delta = ref[1].double() - logp[1]
+    kl = torch.tensor([math.inf, float(delta.exp() - delta - 1), math.inf, 0.0, math.inf, math.inf], dtype=torch.float64)
+    close(got.kl, kl, LOG_TOL * (1 + float(delta.exp())))
+    leaf = d(x).requires_grad_(True)
+    terms = ears.policy_loss(leaf, *args[1:], entropy_coef=0.01, ref_logp=d(ref), status=st)
+    (terms.loss * d(w)).sum().backward()
+    assert int(st) == 0
+    close_grad(leaf.grad, o.grad, o.scale, 2 * H_TOL, "fp32")
