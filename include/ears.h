@@ -427,8 +427,9 @@ int ears_profile_end(float* kernel_ms, int capacity, int* n_calls);
  * What a program that verifies drafts does with the same rows next to the verification: take the
  * target's top logits as a teacher for the draft (ears_top_logits), train the draft towards them
  * (ears_distill_*), score the emitted tokens (ears_token_logprobs*), and train a policy on sampled
- * tokens (ears_policy_*; with beta > 0 the emitted tokens follow a wider law than P_t, so their
- * log probability at sampling time enters as `old`).
+ * tokens (ears_policy_*; `old` is their log probability under the law that they were drawn from.  For tokens
+ * that a verification call emitted that is ln P_t, as ears_token_logprobs scores it on the target rows, only if
+ * beta was 0: with beta > 0 they follow a wider law, whose probabilities no call here returns).
  *
  * Common arguments:
  *   logits        [B, R, V], entries of a row contiguous; row (b, k) starts at logits + b stride_b +

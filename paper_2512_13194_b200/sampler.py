@@ -23,7 +23,8 @@ class StepResult:
     tokens: torch.Tensor          # [B,K+1] int32: accepted prefix, then the resampled or bonus token, then -1
     offset: int                   # the random stream's offset this step used
     entropy: Optional[torch.Tensor] = None   # [B,K] float64 H(P_t) per position, when asked for
-    logprobs: Optional[torch.Tensor] = None  # [B,K+1] float32 ln P_t of the emitted tokens (0 behind the last), when asked for
+    logprobs: Optional[torch.Tensor] = None  # [B,K+1] float32 ln P_t of the emitted tokens (0 behind the last), when asked for;
+                                             # their log probability at sampling time only with beta = 0
     teacher: Optional[rows.TopLogits] = None # top logits of the target rows 0..K-1 up to the first rejection, when asked for
 
     def emitted(self):
@@ -42,8 +43,10 @@ class EarsSampler:
     (H(P_t) / ln V, Sec. 5 item 1).  seed: the random stream of this sampler; the offset starts at
     ``first_offset`` and goes up by one per step, so that a run can be replayed from (seed, offset).
     b_first: global index of this rank's first sequence when a batch is sharded across GPUs.
-    report_logprobs: every step also scores the tokens it emits under the target rows (the log probability a
-    later policy loss needs as ``old_logp``).  teacher_k: every step also keeps the ``teacher_k`` largest logits of
+    report_logprobs: every step also scores the tokens it emits under the target rows: ln P_t.  With beta = 0 and draft
+    tokens drawn from the draft's own distribution that is the law they were drawn from, and what a later policy loss
+    needs as ``old_logp``; with beta > 0 tokens are accepted more readily than P_t would have them, and a ratio
+    built on ln P_t is biased.  teacher_k: every step also keeps the ``teacher_k`` largest logits of
     the target rows that a draft row stands beside, positions behind the first rejection left out: the
     ``teacher`` of ``distill_step`` on the step's draft logits.
     """
