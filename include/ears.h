@@ -453,8 +453,10 @@ int ears_profile_end(float* kernel_ms, int capacity, int* n_calls);
  * Sums and row scalars are kept in 32 bits and 64 bits; a gradient entry is rounded once, to its type, and what lies
  * below 2^-126 of its row's largest exponential is 0.
  * The calls use no workspace, allocate nothing and may be recorded into CUDA graphs and run side by side
- * on any streams (the driver loads a kernel at its first launch: make that one outside any capture).  Results do not
- * depend on anything but the inputs and the launch's CTAs per row.
+ * on any streams (the driver loads a kernel at its first launch: make that one outside any capture).  The same call on
+ * the same kind of device gives the same bits.  Which threads share a row, and with that the order of its sums, goes by
+ * the number of rows, their length and type, the device's SM count, ears_set_row_cluster and the row's start within 16
+ * bytes: the same row may come out with other last bits in a larger batch or at another address.
  */
 #define EARS_MAX_TOP 128
 #define EARS_MAX_DISTILL_V (1 << 20)
@@ -547,7 +549,7 @@ int ears_distill_step(int dtype, const void* logits, int B, int R, int V, int64_
 
 /*
  * CTAs per row of the operators above, for tests and measurements: 1, 2, 4, 8 or 16; 0 = automatic.
- * Results differ only through floating-point summation order.
+ * Results differ only through floating-point summation order.  (0 may give short rows to a warp or to 128 threads.)
  */
 int ears_set_row_cluster(int cluster);
 

@@ -1068,3 +1068,24 @@ def test_a_kl_term_without_weight_stays_out_of_the_loss(ears, cluster):
     (terms.loss * d(w)).sum().backward()
     assert int(st) == 0
     close_grad(leaf.grad, o.grad, o.scale, 2 * H_TOL, "fp32")
+
+
+def test_the_same_call_gives_the_same_bits(ears):
+    """Over every form that rows may take: many short rows, few, middling, long, split."""
+    g = torch.Generator().manual_seed(24)
+    for n, V, dtype in ((20, 700, "bf16"), (700, 700, "fp32"), (3000, 6000, "bf16"), (40, 33001, "fp16"), (3, 128256, "bf16")):
+        x = (torch.randn(n, V + 3, generator=g) * 2).to(DT[dtype]).to(DEV)
+        k = 12
+        f, tok = torch.randn(n, generator=g).to(DEV), torch.randint(0, V, (n,), generator=g, dtype=torch.int32).to(DEV)
+
+        def run(at):
+            teacher = ears.top_logits(at, k)
+            yield from teacher
+            yield from ears.token_logprobs(at, tok, entropy=True)
+            yield from ears.token_logprobs_step(at, tok, f, f)
+            yield from ears.distill_step(at * 0.5, teacher, kind="jsd")
+        for at in (x[:, :V], x[:, 1:V + 1]):
+            first = list(run(at))
+            for _ in range(3):
+                for a, b in zip(first, run(at)):
+                    assert torch.equal(a, b)
