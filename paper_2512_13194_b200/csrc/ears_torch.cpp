@@ -1,11 +1,12 @@
 // The row operators' calls from Python without its per-argument cost: a small call is bound by the host (a clipped
-// policy step on 24 rows runs 6 us on the device; marshalled in Python it takes 20 us on the host, from here 9).
+// policy step on 24 rows runs 5.6 us on the device; marshalled in Python it takes 20 us on the host, from here 7.5; scores of
+// 24 tokens with ids of 64 bits 24 and 20).
 //
 // Every function takes the arguments of its Python wrapper in rows.py in one fixed order, allocates the outputs
 // and makes the C-ABI call of include/ears.h, if and only if everything is in its plain form already: CUDA tensors on
-// the current device, of the exact type and shape, contiguous per-row arrays.  Anything else, a refusal by the library
-// included, returns None, and the wrapper goes its ordinary way, which converts, checks and raises.  Nothing is
-// decided here that is not decided there.
+// the current device, of the exact type and shape, contiguous per-row arrays, ids of 32 or 64 bits.  Anything else, a refusal
+// by the library included, returns None, and the wrapper goes its ordinary way, which converts, checks and raises.
+// Nothing is decided here that is not decided there.
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
@@ -132,9 +133,15 @@ const float* row_floats(const Rows& r, const at::Tensor* t, bool* plain) {
     if (!per_row(r, t, at::kFloat, r.lead)) { *plain = false; return nullptr; }
     return t->const_data_ptr<float>();
 }
-const int32_t* row_ints(const Rows& r, const at::Tensor* t, bool* plain) {
+// 64-bit integers, as torch's own index tensors are, count as plain too; those that 32 bits cannot hold go to the nearest that
+// they can, an index of no row.  `narrow` keeps what they become.
+const int32_t* ints(const Rows& r, const at::Tensor* t, at::IntArrayRef shape, at::Tensor* narrow, bool* plain) {
     if (!t) return nullptr;
-    if (!per_row(r, t, at::kInt, r.lead)) { *plain = false; return nullptr; }
+    if (per_row(r, t, at::kLong, shape)) {
+        *narrow = at::clamp(*t, INT32_MIN, INT32_MAX).to(at::kInt);
+        t = narrow;
+    }
+    if (!per_row(r, t, at::kInt, shape)) { *plain = false; return nullptr; }
     return t->const_data_ptr<int32_t>();
 }
 
@@ -198,12 +205,15 @@ PyObject* top_logits(PyObject*, PyObject* const* argv, Py_ssize_t n) {
         const long k = a.integer();
         if (!take_rest(a, &r) || k < 1 || k > EARS_MAX_TOP) EARS_NOT_PLAIN;
         const int64_t b = r.B;
-        if (acc && !per_row(r, acc, at::kInt, at::IntArrayRef(&b, 1))) EARS_NOT_PLAIN;
+        bool plain = true;
+        at::Tensor narrow;
+        const int32_t* lengths = ints(r, acc, at::IntArrayRef(&b, 1), &narrow, &plain);
+        if (!plain) EARS_NOT_PLAIN;
         c10::SmallVector<int64_t, 4> shape(r.lead.begin(), r.lead.end());
         shape.push_back(k);
         at::Tensor values = new_out(r, shape), ids = new_out(r, shape, at::kInt), lse = row_out(r);
         const int rc = ((decltype(&ears_top_logits))g_entries[kTop].fn)(
-            EARS_ROWS(r), acc ? acc->const_data_ptr<int32_t>() : nullptr, (int)k, data_of(values), ids.mutable_data_ptr<int32_t>(),
+            EARS_ROWS(r), lengths, (int)k, data_of(values), ids.mutable_data_ptr<int32_t>(),
             data_of(lse), r.status, r.stream);
         if (rc) EARS_NOT_PLAIN;
         return tuple_of({values, ids, lse});
@@ -220,7 +230,8 @@ PyObject* token_logprobs(PyObject*, PyObject* const* argv, Py_ssize_t n) {
         const bool entropy = a.flag();
         if (!take_rest(a, &r)) EARS_NOT_PLAIN;
         bool plain = true;
-        const int32_t* t = row_ints(r, tok, &plain);
+        at::Tensor narrow;
+        const int32_t* t = ints(r, tok, r.lead, &narrow, &plain);
         if (!plain) EARS_NOT_PLAIN;
         at::Tensor logp = row_out(r), H;
         if (entropy) H = row_out(r);
@@ -240,7 +251,8 @@ PyObject* token_logprobs_step(PyObject*, PyObject* const* argv, Py_ssize_t n) {
         const at::Tensor *tok = a.tensor(false), *dl = a.tensor(false), *dh = a.tensor(true), *og = a.tensor(true);
         if (!take_rest(a, &r)) EARS_NOT_PLAIN;
         bool plain = true;
-        const int32_t* t = row_ints(r, tok, &plain);
+        at::Tensor narrow;
+        const int32_t* t = ints(r, tok, r.lead, &narrow, &plain);
         const float *l = row_floats(r, dl, &plain), *h = row_floats(r, dh, &plain);
         Grad g;
         if (!plain || !take_grad(r, og, &g)) EARS_NOT_PLAIN;
@@ -266,7 +278,8 @@ PyObject* policy(PyObject*, PyObject* const* argv, Py_ssize_t n) {
         const at::Tensor *weight = a.tensor(true), *og = a.tensor(true);
         if (!take_rest(a, &r)) EARS_NOT_PLAIN;
         bool plain = true;
-        const int32_t* t = row_ints(r, tok, &plain);
+        at::Tensor narrow;
+        const int32_t* t = ints(r, tok, r.lead, &narrow, &plain);
         const float *o = row_floats(r, old, &plain), *f = row_floats(r, ref, &plain), *ad = row_floats(r, adv, &plain),
                     *w = row_floats(r, weight, &plain);
         Grad g;
@@ -301,14 +314,15 @@ PyObject* distill(PyObject*, PyObject* const* argv, Py_ssize_t n) {
         if (k < 1 || k > EARS_MAX_TOP) EARS_NOT_PLAIN;
         c10::SmallVector<int64_t, 4> shape(r.lead.begin(), r.lead.end());
         shape.push_back(k);
-        if (!per_row(r, values, at::kFloat, shape) || !per_row(r, ids, at::kInt, shape)) EARS_NOT_PLAIN;
+        if (!per_row(r, values, at::kFloat, shape)) EARS_NOT_PLAIN;
         bool plain = true;
+        at::Tensor narrow;
+        const int32_t* id = ints(r, ids, shape, &narrow, &plain);
         const float *l = row_floats(r, lse, &plain), *w = row_floats(r, weight, &plain);
         Grad g;
         if (!plain || (step && !take_grad(r, og, &g))) EARS_NOT_PLAIN;
         at::Tensor loss = row_out(r);
         const float* v = values->const_data_ptr<float>();
-        const int32_t* id = ids->const_data_ptr<int32_t>();
         const int rc = step ? ((decltype(&ears_distill_step))g_entries[kDistillStep].fn)(EARS_ROWS(r), (int)k, v, id, l, (int)kind, mix, w,
                                                                                        data_of(loss), g.t.mutable_data_ptr(), g.sb,
                                                                                        g.sr, r.status, r.stream)

@@ -4,7 +4,8 @@ policy loss.  Argument marshalling only; every computation runs in the CUDA libr
 
 Logits are CUDA tensors [B, R, V] or [R, V] (float32, bfloat16, float16); rows are used where they
 lie as long as the entries of a row are contiguous (a slice ``target[:, :K]`` is not copied).  Per-row tensors
-have the logits' shape without V and are converted to contiguous float32 / int32 where they are not.
+have the logits' shape without V and are converted to contiguous float32 / int32 where they are not (integers that 32 bits
+cannot hold stay unusable).
 ``*_loss`` and ``token_logprobs`` can be differentiated by autograd, in the logits alone (every other input counts as a
 constant; forward mode is refused); ``*_step`` return the gradient at once, reading the logits from memory a single
 time, and are what a step recorded into a CUDA graph uses.

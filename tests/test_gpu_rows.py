@@ -1089,3 +1089,25 @@ def test_the_same_call_gives_the_same_bits(ears):
             for _ in range(3):
                 for a, b in zip(first, run(at)):
                     assert torch.equal(a, b)
+
+
+def test_ids_of_64_bits_go_through_the_module(ears):
+    from paper_2512_13194_b200 import rows
+    n, V, k = 6, 900, 5
+    x, g = logits(2 * n, V, "bf16", 25)
+    x3 = x.view(2, n, V).to(DEV)
+    tok = torch.randint(V // 8, V - V // 16, (2, n), generator=g).to(DEV)
+    f = torch.randn(2, n, generator=g).to(DEV)
+    acc = torch.tensor([2, -1], device=DEV)
+    narrow = lambda t: t.to(torch.int32)
+    teacher = ears.top_logits(x3, k)
+    plain = rows._plain_calls()
+    for of in (lambda i: plain.token_logprobs(x3, i(tok), True, 1.0, None, None), lambda i: plain.top_logits(x3, i(acc), k, 1.0, None, None),
+               lambda i: plain.token_logprobs_step(x3, i(tok), f, None, None, 1.0, None, None),
+               lambda i: plain.policy(x3, i(tok), f, None, f, 0.2, 0.2, 0.0, 0.0, False, True, None, None, 1.0, None, None),
+               lambda i: plain.distill(x3, teacher.values, i(teacher.ids.long()), teacher.lse, 2, 0.5, True, None, None, 1.0, None, None)):
+        wide, small = of(lambda t: t), of(narrow)
+        assert wide is not None and len(wide) == len(small)
+        for a, b in zip(wide, small):
+            assert (a is None and b is None) or torch.equal(a, b)
+    assert plain.token_logprobs(x3, tok.t(), True, 1.0, None, None) is None
