@@ -88,7 +88,7 @@ def _bind_module(lib):
 def _refuse_tangents(values) -> None:
     # a dual tensor does not say requires_grad: its tangent would be dropped without a word
     for v in values:
-        if isinstance(v, tuple):
+        if isinstance(v, (tuple, list)):
             _refuse_tangents(v)
         elif isinstance(v, torch.Tensor) and forward_ad.unpack_dual(v).tangent is not None:
             raise NotImplementedError("the row operators have no forward-mode derivatives")

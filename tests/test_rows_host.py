@@ -164,6 +164,11 @@ def test_forward_mode_derivatives_are_refused(lib, name):
         if name not in ("ears_top_logits", "ears_token_logprobs"):      # which take integers beside the logits
             with pytest.raises(NotImplementedError, match="forward-mode"):
                 call(torch.zeros(N, V), i)
+            if "distill" in name:
+                i = Inputs()
+                i.teacher = [dual(i.teacher.values), *i.teacher[1:]]    # the list as a plain list
+                with pytest.raises(NotImplementedError, match="forward-mode"):
+                    call(torch.zeros(N, V), i)
         assert not lib.calls
         call(torch.zeros(N, V), Inputs())                       # no tangent: as ever
         call(dual(torch.zeros(N, V)).detach(), Inputs())
