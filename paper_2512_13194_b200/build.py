@@ -74,6 +74,8 @@ def torch_stamp() -> str:
 def torch_is_stale() -> bool:
     if not os.path.exists(TORCH_LIB):
         return True
+    if not os.path.exists(os.path.join(CSRC, "ears_torch.cpp")):
+        return False               # a package without its sources
     with open(TORCH_LIB, "rb") as f:
         return torch_stamp().encode() not in f.read()
 

@@ -258,6 +258,8 @@ def test_a_module_built_from_other_sources_is_built_again(tmp_path, monkeypatch)
     with open(copy / "ears_torch.cpp", "a") as f:
         f.write("// changed\n")
     assert build.torch_is_stale()
+    (copy / "ears_torch.cpp").unlink()
+    assert not build.torch_is_stale()                            # nothing to build it from
 
 
 def test_without_the_module_calls_go_through_ctypes(unbound, monkeypatch):
