@@ -436,7 +436,7 @@ int ears_profile_end(float* kernel_ms, int capacity, int* n_calls);
  *                 k stride_r (strides in entries, >= 0), so that the first K rows of a target
  *                 [B, K+1, V], or rows padded to a longer pitch, are used in place.  Any alignment of at
  *                 least the element size and any V serve; rows that share their start within 16 bytes with the
- *                 gradient's rows run at full speed, others store the gradient entry by entry, three to four
+ *                 gradient's rows run at full speed, others store the gradient entry by entry, two to four
  *                 times slower where rows are long.  Per-row arrays are contiguous, row b R + k.
  *   temperature   l / temperature enters every softmax; seq_temperature [B] replaces it where not NULL.  It is
  *                 taken in 64 bits: rounding it to 32 would move logits of 20 by 1e-6.

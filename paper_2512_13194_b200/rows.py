@@ -8,7 +8,7 @@ have the logits' shape without V and are converted to contiguous float32 / int32
 cannot hold stay unusable).
 A gradient is allocated contiguous where the logits are not.  With V x element size no multiple of 16 (``logits[:, :-1]`` of a
 vocabulary of 50257) its rows then start elsewhere within 16 bytes than the logits' and are stored entry by entry, at a
-third to a quarter of the speed; a step is spared that by an ``out_grad`` with the logits' strides.
+half to a quarter of the speed; a step is spared that by an ``out_grad`` with the logits' strides.
 ``*_loss`` and ``token_logprobs`` can be differentiated by autograd, in the logits alone (every other input counts as a
 constant; forward mode is refused); ``*_step`` return the gradient at once, reading the logits from memory a single
 time, and are what a step recorded into a CUDA graph uses.

@@ -1111,3 +1111,15 @@ def test_ids_of_64_bits_go_through_the_module(ears):
         for a, b in zip(wide, small):
             assert (a is None and b is None) or torch.equal(a, b)
     assert plain.token_logprobs(x3, tok.t(), True, 1.0, None, None) is None
+
+
+def test_tokens_of_every_integer_type(ears):
+    x, g = logits(4, 100, "fp32", 26)
+    tok = torch.tensor([20, 50, 93, 13], dtype=torch.int32)
+    want = ears.token_logprobs(x.to(DEV), tok.to(DEV))
+    for dtype in (torch.int8, torch.uint8, torch.int16, torch.int64, torch.uint16, torch.uint32, torch.uint64):
+        assert torch.equal(ears.token_logprobs(x.to(DEV), tok.to(dtype).to(DEV)), want)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    far = torch.tensor([2**64 - 1, 2**63 + 7, 2**32, 13], dtype=torch.uint64)
+    logp = ears.token_logprobs(x.to(DEV), far.to(DEV), status=st)
+    assert torch.isnan(logp[:3]).all() and torch.equal(logp[3], want[3]) and int(st) == ears.DEV_INVALID_INPUT
