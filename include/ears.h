@@ -554,6 +554,79 @@ int ears_distill_step(int dtype, const void* logits, int B, int R, int V, int64_
  */
 int ears_set_row_cluster(int cluster);
 
+/*
+ * ---- A key/value cache held in 4 bits -----------------------------------------------------------------
+ *
+ * What stands before a verification step and after it: the forward pass whose logits the step verifies writes the
+ * K + 1 newest tokens of every sequence into the cache (ears_kv_write) and attends from them over it
+ * (ears_kv_attention); of those tokens the step keeps accept_len + 1, so that `start` of the next pass is
+ * start + accept_len + 1 (an unusable sequence, accept_len -1, stays where it is).  What was written behind is
+ * overwritten by the next pass and never seen.  Serving only: nothing here has a gradient.
+ *
+ * The cache is a pool of pages of page_size tokens (a multiple of 16), keys and values of all heads:
+ *   codes   uint8 [pages, 2, heads, page_size, head_dim / 2]: 0 keys, 1 values; two codes a byte, the even
+ *           dimension's in the low half
+ *   params  bfloat16 [pages, 2, heads, page_size, head_dim / EARS_KV_GROUP, 2]: scale s and minimum m of each group
+ *           of EARS_KV_GROUP = 64 consecutive dimensions; a code c stands for m + s c
+ * 4.5 bits a value; both 16-byte aligned and contiguous.  head_dim is 64, 128 or 256.
+ * Writing a group x: m = min x rounded down to bfloat16; s = (max x - m) / 15 in 32 bits, rounded up to bfloat16, at least
+ * 2^-126; c = (x - m) / s, the difference rounded to 32 bits, to the nearest whole number, ties to even.  A value comes back
+ * within s / 2 of what was written.  A group with a NaN or an infinity, or whose range overflows 32 bits, reads back as NaN.
+ *
+ * Common arguments:
+ *   page_table   [B, table_width] int32, rows table_stride apart: token t of sequence b lies in page
+ *                page_table[b, t / page_size], place t % page_size.  Sequences may share pages that are only read; two
+ *                tokens written to the same place by one call leave either there, or codes of one and scales of the other.
+ *   start        [B] int32: position i of the call is token start[b] + i.
+ *   counts       [B] int32 or NULL: positions i >= counts[b] are left out (NULL, or more than Q: none is).
+ *   strides      in elements, >= 0; the head_dim elements of a head are contiguous.  Any alignment of at least the
+ *                element size serves; starts on 16 bytes are fetched at full speed.
+ *   status       as above: EARS_DEV_INVALID_INPUT where a position lies outside the table, or a page outside the pool.
+ * Every address is formed in 64 bits.  A position outside is not written, reads as NaN, and makes NaN of the rows that see it.
+ * The calls allocate nothing and may be recorded into CUDA graphs and run side by side on any streams, as long as calls
+ * that overlap have workspaces of their own.
+ */
+#define EARS_KV_GROUP 64
+typedef struct {
+    void* codes;
+    void* params;
+    int pages;       /* in the pool */
+    int heads;
+    int page_size;   /* tokens, a multiple of 16 */
+    int head_dim;
+} ears_kv_cache;
+
+/* Quantises keys and values [B, Q, heads, head_dim] of type `dtype` into the cache. */
+int ears_kv_write(int dtype, const ears_kv_cache* cache, const void* k, const void* v, int B, int Q, int64_t k_stride_b, int64_t k_stride_q,
+                  int64_t k_stride_h, int64_t v_stride_b, int64_t v_stride_q, int64_t v_stride_h, const int32_t* page_table,
+                  int table_width, int64_t table_stride, const int32_t* start, const int32_t* counts, int32_t* status, void* stream);
+
+/* The values m + s c of Q tokens per sequence, in 32 bits and rounded once to `dtype`: out_k, out_v [B, Q, heads, head_dim],
+   contiguous, 16-byte aligned.  Positions that are left out are zeros. */
+int ears_kv_read(int dtype, const ears_kv_cache* cache, int B, int Q, const int32_t* page_table, int table_width, int64_t table_stride,
+                 const int32_t* start, const int32_t* counts, void* out_k, void* out_v, int32_t* status, void* stream);
+
+/*
+ * Attention of Q positions per sequence, whose own tokens are in the cache already: position i, at p = start[b] + i, sees
+ * the tokens t <= p, and of those, with window > 0, the last `window` (t > p - window) and the first `sinks` (t < sinks).
+ *   out = sum_t softmax_t(scale q . k_t) v_t,    out_lse = ln sum_t exp(scale q . k_t)   (optional)
+ * q [B, Q, heads_q, head_dim] bfloat16 or half precision; query head n reads head n / (heads_q / cache->heads).  out, of q's type,
+ * [B, Q, heads_q, head_dim] contiguous, 16-byte aligned; out_lse [B, Q, heads_q].  They must not overlap the inputs.
+ * Positions that are left out get zeros and -inf.  A NaN or infinity in a row of q, or a NaN read from a token that it sees, makes
+ * that row NaN and no other.
+ * Scores, their sums and the results are kept in 32 bits; q is taken as it is, or, where its row spans more than 2^25, to within
+ * 2^-26 of the row's largest element; weights enter the second product in half precision (bfloat16 q) or in two halves.
+ * workspace: ears_kv_attention_workspace_bytes for the same arguments on the same device (0: they would be refused), 256-byte
+ * aligned; its contents before and after mean nothing.  It does not grow with the lengths.  The same call on the same kind of
+ * device gives the same bits; a row's may differ with what else is in the batch (the order of its sums).
+ * Made for few positions (Q x heads_q / heads up to some tens): more are right, and read the cache once for every 8 to 32 rows.
+ */
+size_t ears_kv_attention_workspace_bytes(int dtype, const ears_kv_cache* cache, int B, int Q, int heads_q, int table_width, int window, int sinks);
+int ears_kv_attention(int dtype, const ears_kv_cache* cache, const void* q, int B, int Q, int heads_q, int64_t q_stride_b, int64_t q_stride_q,
+                      int64_t q_stride_h, const int32_t* page_table, int table_width, int64_t table_stride, const int32_t* start,
+                      const int32_t* counts, double scale, int window, int sinks, void* out, float* out_lse, void* workspace,
+                      size_t workspace_bytes, int32_t* status, void* stream);
+
 const char* ears_status_string(int status);
 const char* ears_last_cuda_error(void); /* text of the last failing CUDA call on this thread, or "" */
 int ears_version(void);

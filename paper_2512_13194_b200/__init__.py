@@ -45,3 +45,11 @@ from .rows import (  # noqa: F401,E402
     token_logprobs_step,
     top_logits,
 )
+from .kv import (  # noqa: F401,E402
+    KVCache,
+    kv_advance,
+    kv_attention,
+    kv_cache,
+    kv_read,
+    kv_write,
+)

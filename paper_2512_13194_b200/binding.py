@@ -23,6 +23,11 @@ class EarsError(RuntimeError):
         self.status = status
 
 
+class KvCacheStruct(ctypes.Structure):       # ears_kv_cache
+    _fields_ = [("codes", ctypes.c_void_p), ("params", ctypes.c_void_p), ("pages", ctypes.c_int), ("heads", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("head_dim", ctypes.c_int)]
+
+
 def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     """Loads (and, when sources are newer, rebuilds) the in-tree CUDA library."""
     global _lib
@@ -110,6 +115,16 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                        ("ears_distill_step", distill + ptrs(2) + place)):
         getattr(lib, name).argtypes = rows + args + ptrs(2)     # ..., status, stream
         getattr(lib, name).restype = c.c_int
+    seqs = [c.c_void_p, c.c_int, c.c_int64, c.c_void_p, c.c_void_p]      # page_table, width, stride, start, counts
+    cache, strides = c.POINTER(KvCacheStruct), [c.c_int64] * 3
+    for name, args in (("ears_kv_write", [c.c_int, cache] + ptrs(2) + [c.c_int, c.c_int] + strides * 2 + seqs),
+                       ("ears_kv_read", [c.c_int, cache, c.c_int, c.c_int] + seqs + ptrs(2)),
+                       ("ears_kv_attention", [c.c_int, cache, c.c_void_p] + [c.c_int] * 3 + strides + seqs + [c.c_double, c.c_int, c.c_int]
+                        + ptrs(3) + [c.c_size_t])):
+        getattr(lib, name).argtypes = args + ptrs(2)            # ..., status, stream
+        getattr(lib, name).restype = c.c_int
+    lib.ears_kv_attention_workspace_bytes.argtypes = [c.c_int, cache] + [c.c_int] * 6
+    lib.ears_kv_attention_workspace_bytes.restype = c.c_size_t
     lib.ears_set_row_cluster.argtypes = [c.c_int]
     lib.ears_set_row_cluster.restype = c.c_int
     lib.ears_status_string.argtypes = [c.c_int]

@@ -11,7 +11,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libears.so")
-UNITS = ("ears_api.cu", "ears_rows_api.cu")      # translation units, compiled side by side
+UNITS = ("ears_api.cu", "ears_rows_api.cu", "ears_kv_api.cu")      # translation units, compiled side by side
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
 

@@ -456,11 +456,6 @@ __device__ __forceinline__ RowSetup row_setup_at(const RowSpan& p, unsigned row)
     return r;
 }
 
-// Launches may be queued behind the kernel before them while it still runs (programmatic stream serialisation): nothing is
-// read or written before that kernel is done and its writes are visible.  Calls that follow one another are spared 2 us
-// each (scoring 48 rows of 64 KB: 6.1 us a call, 4.5 so).
-__device__ __forceinline__ void wait_for_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 __device__ __forceinline__ RowSetup row_setup(const RowSpan& p) {
     wait_for_stream();
     const unsigned row = blockIdx.x / (unsigned)p.C;

@@ -24,8 +24,9 @@ namespace {
 struct Entry { const char* name; void* fn; };
 Entry g_entries[] = {{"ears_top_logits", nullptr}, {"ears_token_logprobs", nullptr}, {"ears_token_logprobs_step", nullptr},
                      {"ears_policy_loss", nullptr}, {"ears_policy_step", nullptr}, {"ears_distill_loss", nullptr},
-                     {"ears_distill_step", nullptr}};
-enum { kTop, kToken, kTokenStep, kPolicyLoss, kPolicyStep, kDistillLoss, kDistillStep };
+                     {"ears_distill_step", nullptr}, {"ears_kv_write", nullptr}, {"ears_kv_read", nullptr},
+                     {"ears_kv_attention", nullptr}, {"ears_kv_attention_workspace_bytes", nullptr}};
+enum { kTop, kToken, kTokenStep, kPolicyLoss, kPolicyStep, kDistillLoss, kDistillStep, kKvWrite, kKvRead, kKvAttention, kKvWorkspace };
 
 // The arguments of one call, taken in order; `plain` falls when one is not in its plain form.
 struct Args {
@@ -333,6 +334,138 @@ PyObject* distill(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     });
 }
 
+// ---- the key/value cache ----
+struct Kv {
+    ears_kv_cache cache = {};
+    int device = -1, B = 0, width = 0;
+    int64_t stride = 0;
+    const int32_t *table = nullptr, *start = nullptr, *counts = nullptr;
+    int32_t* status = nullptr;
+    void* stream = nullptr;
+};
+bool on(const at::Tensor* t, int device, at::ScalarType type) { return t->is_cuda() && t->get_device() == device && t->scalar_type() == type; }
+
+bool take_cache(Args& a, Kv* kv) {
+    const at::Tensor *codes = a.tensor(false), *params = a.tensor(false);
+    if (!a.plain || !codes->is_cuda() || codes->dim() != 5 || params->dim() != 6) return false;
+    kv->device = codes->get_device();
+    if (c10::cuda::current_device() != kv->device) return false;
+    if (codes->scalar_type() != at::kByte || !on(params, kv->device, at::kBFloat16) || !codes->is_contiguous() || !params->is_contiguous()) return false;
+    const auto c = codes->sizes(), p = params->sizes();
+    if (c[1] != 2 || c[4] > 128 || p[4] != c[4] * 2 / EARS_KV_GROUP || p[5] != 2 || c.slice(0, 4) != p.slice(0, 4)) return false;
+    for (int i = 0; i < 5; ++i)
+        if (c[i] > INT32_MAX) return false;
+    kv->cache = {codes->mutable_data_ptr(), params->mutable_data_ptr(), (int)c[0], (int)c[2], (int)c[3], (int)c[4] * 2};
+    return true;
+}
+bool take_seqs(Kv* kv, const at::Tensor* pages, const at::Tensor* start, const at::Tensor* counts, const at::Tensor* status) {
+    if (!on(pages, kv->device, at::kInt) || pages->dim() != 2 || pages->size(0) > INT32_MAX || pages->size(1) > INT32_MAX) return false;
+    if (pages->size(1) > 1 && pages->stride(1) != 1) return false;
+    kv->B = (int)pages->size(0);
+    kv->width = (int)pages->size(1);
+    kv->stride = pages->stride(0);
+    kv->table = pages->const_data_ptr<int32_t>();
+    const int64_t b = kv->B;
+    for (const at::Tensor* t : {start, counts})
+        if (t && (!on(t, kv->device, at::kInt) || t->sizes() != at::IntArrayRef(&b, 1) || !t->is_contiguous())) return false;
+    kv->start = start->const_data_ptr<int32_t>();
+    kv->counts = counts ? counts->const_data_ptr<int32_t>() : nullptr;
+    if (status) {
+        if (!on(status, kv->device, at::kInt) || status->numel() != 1) return false;
+        kv->status = status->mutable_data_ptr<int32_t>();
+    }
+    kv->stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)kv->device).stream();
+    return true;
+}
+int dtype_of(const at::Tensor& t) {
+    switch (t.scalar_type()) {
+        case at::kFloat: return EARS_DTYPE_F32;
+        case at::kBFloat16: return EARS_DTYPE_BF16;
+        case at::kHalf: return EARS_DTYPE_F16;
+        default: return -1;
+    }
+}
+// [B, Q, heads, head_dim], used where it lies
+bool heads_of(const Kv& kv, const at::Tensor* t) {
+    if (!t->is_cuda() || t->get_device() != kv.device || t->dim() != 4 || t->size(0) != kv.B || t->size(3) != kv.cache.head_dim) return false;
+    if (t->stride(3) != 1 || t->numel() == 0 || t->size(1) > INT32_MAX || t->size(2) > INT32_MAX) return false;
+    return t->stride(0) >= 0 && t->stride(1) >= 0 && t->stride(2) >= 0;
+}
+at::Tensor kv_out(const Kv& kv, at::IntArrayRef shape, at::ScalarType type) {
+    return at::detail::empty_cuda(shape, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)kv.device), std::nullopt);
+}
+#define EARS_SEQS(kv) (kv).table, (kv).width, (kv).stride, (kv).start, (kv).counts
+
+// (codes, params, k, v, pages, start, counts, status) -> True
+PyObject* kv_write(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        Args a{argv, n};
+        Kv kv;
+        if (!take_cache(a, &kv)) EARS_NOT_PLAIN;
+        const at::Tensor *k = a.tensor(false), *v = a.tensor(false), *pages = a.tensor(false), *start = a.tensor(false), *counts = a.tensor(true),
+                         *status = a.tensor(true);
+        if (!a.plain || !take_seqs(&kv, pages, start, counts, status) || !heads_of(kv, k) || !heads_of(kv, v)) EARS_NOT_PLAIN;
+        const int dtype = dtype_of(*k);
+        if (dtype < 0 || dtype_of(*v) != dtype || k->sizes() != v->sizes() || k->size(2) != kv.cache.heads) EARS_NOT_PLAIN;
+        const int rc = ((decltype(&ears_kv_write))g_entries[kKvWrite].fn)(
+            dtype, &kv.cache, k->const_data_ptr(), v->const_data_ptr(), kv.B, (int)k->size(1), k->stride(0), k->stride(1), k->stride(2),
+            v->stride(0), v->stride(1), v->stride(2), EARS_SEQS(kv), kv.status, kv.stream);
+        if (rc) EARS_NOT_PLAIN;
+        Py_RETURN_TRUE;
+    });
+}
+
+// (codes, params, pages, start, tokens, counts, dtype, status)
+PyObject* kv_read(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        Args a{argv, n};
+        Kv kv;
+        if (!take_cache(a, &kv)) EARS_NOT_PLAIN;
+        const at::Tensor *pages = a.tensor(false), *start = a.tensor(false);
+        const long tokens = a.integer();
+        const at::Tensor* counts = a.tensor(true);
+        const long dtype = a.integer();
+        const at::Tensor* status = a.tensor(true);
+        if (!a.plain || !take_seqs(&kv, pages, start, counts, status) || kv.B < 1 || tokens < 1 || tokens > INT32_MAX) EARS_NOT_PLAIN;
+        if (dtype != EARS_DTYPE_F32 && dtype != EARS_DTYPE_BF16 && dtype != EARS_DTYPE_F16) EARS_NOT_PLAIN;
+        const at::ScalarType type = dtype == EARS_DTYPE_F32 ? at::kFloat : dtype == EARS_DTYPE_BF16 ? at::kBFloat16 : at::kHalf;
+        const int64_t shape[4] = {kv.B, tokens, kv.cache.heads, kv.cache.head_dim};
+        at::Tensor k = kv_out(kv, shape, type), v = kv_out(kv, shape, type);
+        const int rc = ((decltype(&ears_kv_read))g_entries[kKvRead].fn)((int)dtype, &kv.cache, kv.B, (int)tokens, EARS_SEQS(kv),
+                                                                        k.mutable_data_ptr(), v.mutable_data_ptr(), kv.status, kv.stream);
+        if (rc) EARS_NOT_PLAIN;
+        return tuple_of({k, v});
+    });
+}
+
+// (codes, params, q, pages, start, counts, scale, window, sinks, lse, status)
+PyObject* kv_attention(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        Args a{argv, n};
+        Kv kv;
+        if (!take_cache(a, &kv)) EARS_NOT_PLAIN;
+        const at::Tensor *q = a.tensor(false), *pages = a.tensor(false), *start = a.tensor(false), *counts = a.tensor(true);
+        const double scale = a.number();
+        const long window = a.integer(), sinks = a.integer();
+        const bool lse = a.flag();
+        const at::Tensor* status = a.tensor(true);
+        if (!a.plain || !take_seqs(&kv, pages, start, counts, status) || !heads_of(kv, q)) EARS_NOT_PLAIN;
+        const int dtype = dtype_of(*q), Q = (int)q->size(1), heads = (int)q->size(2);
+        if ((dtype != EARS_DTYPE_BF16 && dtype != EARS_DTYPE_F16) || window < 0 || window > INT32_MAX || sinks < 0 || sinks > INT32_MAX) EARS_NOT_PLAIN;
+        const size_t need = ((decltype(&ears_kv_attention_workspace_bytes))g_entries[kKvWorkspace].fn)(dtype, &kv.cache, kv.B, Q, heads, kv.width,
+                                                                                                   (int)window, (int)sinks);
+        if (!need) EARS_NOT_PLAIN;
+        const int64_t bytes = (int64_t)need;
+        at::Tensor out = kv_out(kv, q->sizes(), q->scalar_type()), work = kv_out(kv, at::IntArrayRef(&bytes, 1), at::kByte), sums;
+        if (lse) sums = kv_out(kv, q->sizes().slice(0, 3), at::kFloat);
+        const int rc = ((decltype(&ears_kv_attention))g_entries[kKvAttention].fn)(
+            dtype, &kv.cache, q->const_data_ptr(), kv.B, Q, heads, q->stride(0), q->stride(1), q->stride(2), EARS_SEQS(kv), scale, (int)window,
+            (int)sinks, out.mutable_data_ptr(), lse ? sums.mutable_data_ptr<float>() : nullptr, work.mutable_data_ptr(), need, kv.status, kv.stream);
+        if (rc) EARS_NOT_PLAIN;
+        return tuple_of({out, sums});
+    });
+}
+
 // bind({name: address}): the entry points of the library in use
 PyObject* bind(PyObject*, PyObject* dict) {
     for (Entry& e : g_entries) {
@@ -350,7 +483,8 @@ PyObject* bind(PyObject*, PyObject* dict) {
 #define EARS_METHOD(name, fn) {name, (PyCFunction)(void (*)(void))fn, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {EARS_METHOD("top_logits", top_logits), EARS_METHOD("token_logprobs", token_logprobs),
                            EARS_METHOD("token_logprobs_step", token_logprobs_step), EARS_METHOD("policy", policy),
-                           EARS_METHOD("distill", distill), {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                           EARS_METHOD("distill", distill), EARS_METHOD("kv_write", kv_write), EARS_METHOD("kv_read", kv_read),
+                           EARS_METHOD("kv_attention", kv_attention), {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "ears_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

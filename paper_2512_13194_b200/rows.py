@@ -56,6 +56,7 @@ _plain_for = None
 class _Ctypes:
     """In the module's place where it cannot be had: no call is in its plain form."""
     top_logits = token_logprobs = token_logprobs_step = policy = distill = staticmethod(lambda *args: None)
+    kv_write = kv_read = kv_attention = top_logits
 
 
 def _plain_calls():
@@ -80,7 +81,8 @@ def _bind_module(lib):
     if ears_torch.version != lib.ears_version():
         raise RuntimeError(f"ears_torch is for version {ears_torch.version} of the library, which has {lib.ears_version()}")
     names = ("ears_top_logits", "ears_token_logprobs", "ears_token_logprobs_step", "ears_policy_loss", "ears_policy_step",
-             "ears_distill_loss", "ears_distill_step")
+             "ears_distill_loss", "ears_distill_step", "ears_kv_write", "ears_kv_read", "ears_kv_attention",
+             "ears_kv_attention_workspace_bytes")
     ears_torch.bind({n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names})
     return ears_torch
 

@@ -14,7 +14,7 @@ from typing import Optional
 
 import torch
 
-from . import binding, rows
+from . import binding, kv, rows
 
 
 @dataclass
@@ -73,9 +73,11 @@ class EarsSampler:
         return float(value), None
 
     def __call__(self, target_logits: torch.Tensor, draft_logits: torch.Tensor, draft_tokens: torch.Tensor,
-                 stream=None) -> StepResult:
+                 stream=None, kv_start: Optional[torch.Tensor] = None) -> StepResult:
         """One verification step: target_logits [B,K+1,V], draft_logits [B,K,V], draft_tokens [B,K]
-        (CUDA tensors).  Asynchronous on ``stream``; the returned tensors are ready once it is."""
+        (CUDA tensors).  Asynchronous on ``stream``; the returned tensors are ready once it is.
+        kv_start: [B] where the pass that made these logits began in the key/value cache (``kv_write``'s ``start``); it is
+        moved, in place, behind the tokens that the step keeps."""
         T, seq_T = self._split(self.temperature)
         beta, seq_beta = self._split(self.beta)
         out = binding.verify(target_logits, draft_logits, draft_tokens, T, beta if seq_beta is None else 0.0,
@@ -89,6 +91,8 @@ class EarsSampler:
         if self.teacher_k:
             res.teacher = rows.top_logits(target_logits.detach()[:, :-1], self.teacher_k, T, accept_len=res.accept_len,
                                           seq_temperature=seq_T, stream=stream)
+        if kv_start is not None:
+            kv.kv_advance(kv_start, res.accept_len, stream=stream)
         self.offset += 1
         self.steps += 1
         self._pending.append(res.accept_len)
