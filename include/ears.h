@@ -569,8 +569,8 @@ int ears_set_row_cluster(int cluster);
  *   params  bfloat16 [pages, 2, heads, page_size, head_dim / EARS_KV_GROUP, 2]: scale s and minimum m of each group
  *           of EARS_KV_GROUP = 64 consecutive dimensions; a code c stands for m + s c
  * 4.5 bits a value; both 16-byte aligned and contiguous.  head_dim is 64, 128 or 256.
- * Writing a group x: m = min x rounded down to bfloat16; s = (max x - m) / 15 in 32 bits, rounded up to bfloat16, at least
- * 2^-126; c = (x - m) / s, the difference rounded to 32 bits, to the nearest whole number, ties to even.  A value comes back
+ * Writing a group x: m = min x rounded down to bfloat16; s = (max x - m) r in 32 bits, r the 32-bit number nearest
+ * to 1 / 15 (it lies above), rounded up to bfloat16, at least 2^-126; c = (x - m) / s, the difference rounded to 32 bits, to the nearest whole number, ties to even.  A value comes back
  * within s / 2 of what was written.  A group with a NaN or an infinity, or whose range overflows 32 bits, reads back as NaN.
  *
  * Common arguments:

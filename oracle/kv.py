@@ -1,7 +1,7 @@
 """The key/value cache held in 4 bits from its definition, in 64 bits where the format does not fix 32 (torch on the CPU).
 
-A group x of 64: m = min x rounded down to bfloat16, s = (max x - m) / 15 in 32 bits rounded up to bfloat16 and at least 2^-126,
-c = (x - m) / s, the difference rounded to 32 bits, to the nearest whole number, ties to even; a code stands for m + s c.
+A group x of 64: m = min x rounded down to bfloat16, s = (max x - m) r in 32 bits, r the 32-bit number nearest to 1 / 15, rounded up
+to bfloat16 and at least 2^-126, c = (x - m) / s, the difference rounded to 32 bits, to the nearest whole number, ties to even; a code stands for m + s c.
 """
 from __future__ import annotations
 
@@ -24,7 +24,7 @@ def quantise(x):
     """[..., D] -> (codes uint8 [..., D/2], params bfloat16 [..., D/64, 2])"""
     x = x.float().unflatten(-1, (-1, GROUP))
     m = _neighbour(x.amin(-1), -1)
-    s = _neighbour((x.amax(-1) - m) / 15, 1)
+    s = _neighbour((x.amax(-1) - m) * torch.tensor(1 / 15, dtype=torch.float32), 1)
     usable = torch.isfinite(s) & torch.isfinite(m)
     s = torch.where(usable, s.clamp(min=2.0 ** -126), torch.nan)
     m = torch.where(usable, m, torch.nan)

@@ -5,7 +5,7 @@
 //     params [P, 2, H, page, D / 64]     a word per group of 64: the scale s (low half) and the minimum m, bfloat16
 // and a code c stands for m + s c.  A token's codes in one head are contiguous, and so are a page's tokens, so that a tile
 // of tokens is one run of bytes for whatever reads it.  For a group x_0 .. x_63
-//     m = min x, rounded down to bfloat16            s = (max x - m) / 15, rounded up to bfloat16, at least 2^-126
+//     m = min x, rounded down to bfloat16            s = (max x - m) fl(1 / 15) in 32 bits, rounded up to bfloat16, at least 2^-126
 //     c = (x - m) / s to the nearest, ties to even
 // with the directed roundings keeping every x inside [m, m + 15 s]: a value comes back within s / 2 of what was written.
 // bfloat16 and not half precision, since neither large keys overflow its range nor small values lose their scale.
@@ -151,9 +151,9 @@ __global__ void __launch_bounds__(kKvThreads) ears_kv_write_kernel(const KvWrite
     uint32_t mb = __float_as_uint(lo), cut = mb & 0xffff0000u;
     if ((int)mb < 0 && mb != cut) cut += 0x10000u;
     const float m = __uint_as_float(cut);
-    const float exact_s = __fdiv_rn(__fsub_rn(hi, m), 15.f);
-    const bool fine = exact_s <= FLT_MAX;             // false for NaN too
-    uint32_t sbits = __float_as_uint(exact_s);
+    const float range = __fmul_rn(__fsub_rn(hi, m), 1.f / 15.f);
+    const bool fine = range <= FLT_MAX;               // false for NaN too
+    uint32_t sbits = __float_as_uint(range);
     if (sbits & 0xffffu) sbits = (sbits & 0xffff0000u) + 0x10000u;
     float s = __uint_as_float(sbits);
     s = fmaxf(s, 0x1p-126f);
