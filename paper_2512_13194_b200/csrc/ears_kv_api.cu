@@ -149,8 +149,10 @@ int make_plan(int dtype, const ears_kv_cache* c, int B, int Q, int heads_q, int 
     // no more CTAs than chunks can be, whatever the lengths
     long long tokens = (long long)width * c->page_size;
     if (window && (long long)window + sinks + Q + 3 * kKaTile < tokens) tokens = (long long)window + sinks + Q + 3 * kKaTile;
-    const long double most = (long double)B * c->heads * plan->blocks * ((tokens + kKaChunk - 1) / kKaChunk);
-    if (most < plan->grid) plan->grid = (int)most;
+    const long long chunks = (tokens + kKaChunk - 1) / kKaChunk;
+    const long double units = (long double)B * c->heads * plan->blocks;
+    if (units * (chunks + kKaAhead) > (long double)INT_MAX) return EARS_ERR_SHAPE;    // the device counts in 31 bits
+    if (units * chunks < plan->grid) plan->grid = (int)(units * chunks);
     return EARS_OK;
 }
 

@@ -5,14 +5,16 @@
 //     q . k_t = sum_g s_tg (q_g . c_tg) + m_tg sum(q_g),      out_g = sum_t (P_t s_tg) c_tg + sum_t P_t m_tg
 // so that the products run on the codes themselves, and scales and minima touch a value per token and row only.
 //
-// What bounds it: 4.5 bits per value have to be read, and each code turned into a 16-bit operand.  A code c placed in the lowest
-// bits of a half-precision number IS the subnormal c 2^-24, and one in bits 4..7 is c 2^-20, which tensor cores take at full
-// speed: two masks and one shift make eight operands of a 32-bit word, with nothing to subtract; the powers of two go into q
-// (odd dimensions of keys / 16) and into the result (odd dimensions of values).
+// What bounds it: 4.5 bits per value have to be read, and each code turned into an operand of the tensor cores.  A code c in a byte IS
+// the 8-bit floating-point number (e4m3) c 2^-9, and one in the lowest bits of a half-precision number the subnormal c 2^-24, or
+// c 2^-20 four bits further up; tensor cores take them all at full speed.  For the keys two masks and a shift make eight
+// operands, against queries taken apart into two e4m3 numbers (bfloat16: 8 bits, exact) or three (half precision: 11 bits), whose
+// products and sums are exact or rounded once to 32 bits; the 8-bit product runs at four times the rate of the 16-bit one.
+// For the values, whose weights need half precision's range, 12 operations on a pair of tokens make sixteen operands.
 //
-// The products are m16n8k16 with tokens (or, for the values, dimensions) as the 16 rows and eight of the head group's
+// The products have 16 tokens (or, for the values, dimensions) as rows and eight of the head group's
 // queries as columns: M = Q x heads per key head is seldom more than a few eights, and no work goes into padding a tile of
-// 64 or 128.  Scores come out with a token per thread pair of rows, where a token's scale and minimum are two registers, and
+// 64 or 128.  Scores come out with a token per pair of rows of a thread, where a token's scale and minimum are two registers, and
 // become the second product's operand through an 8x8 transpose.  The order of dimensions within a product is free as long as
 // both operands agree: a thread takes consecutive codes, 8 (keys) or 4 (values) bytes of a token and group at a time.
 //
@@ -20,28 +22,46 @@
 // Every CTA of the grid, as many as are resident at once, takes an equal run of the chunks of all units, whatever the
 // sequences' lengths, which it reads on the device.  Units that are cut are joined by a second small kernel in a fixed order.
 #pragma once
+#include <climits>
 #include <type_traits>
 
 #include "ears_kv.cuh"
 
 namespace ears {
 
+#ifndef KA_SUB
+#define KA_SUB 1
+#endif
+#ifndef KA_OCC2
+#define KA_OCC2 3
+#endif
+#ifndef KA_AHEAD
+#define KA_AHEAD 2
+#endif
+#ifndef KA_OCC
+#define KA_OCC 4
+#endif
 constexpr int kKaWarps = 4, kKaThreads = kKaWarps * 32;
 constexpr int kKaTile = 16;                         // tokens of a warp's tile
 constexpr int kKaChunk = kKaWarps * kKaTile;
-constexpr float kKaSlack = 8.f;                     // the running maximum is raised when a score passes it by this much (base 2)
+constexpr int kKaAhead = KA_AHEAD;                  // what starting and ending a unit costs, in chunks
+// The running maximum is raised when a score passes it by 2^12, and the values' scales enter times a power of two that keeps
+// them below 8: their product, a weight, stays below half precision's 2^16.
+constexpr float kKaSlack = 12.f, kKaScaleCap = 8.f;
 
 template <int D> struct KaShape {
     static constexpr int NG = D / kKvGroup;
     static constexpr int RB = D / 2;                // bytes of a token's codes
-    static constexpr int kCodes = kKaTile * RB, kParams = kKaTile * NG * 4;
-    static constexpr int kStage = 2 * (kCodes + kParams);
-    static constexpr int kStages = D == 64 ? 8 : D == 128 ? 5 : 4;
+    static constexpr int kCodes = kKaTile * RB, kPars = kKaTile * NG * 4;
+    static constexpr int kTileBytes = 2 * (kCodes + kPars);        // keys' codes, values' codes, keys' parameters, values' parameters
+    static constexpr int kStage = 2 * kTileBytes;   // two tiles
+    static constexpr int kStages = D == 64 ? 5 : 3;
     static constexpr int kSmem = kKaWarps * kStages * kStage;
-    static_assert(kSmem >= kKaWarps * 8 * D * 4, "the warps' results meet in the ring's memory");
     // 16-byte pieces of row i are kept in another order, so that what a warp loads at once lies in different banks
     __device__ static __forceinline__ int swizzle(int i) { return RB == 128 ? ((i & 1) << 2) | (i & 2) : RB == 64 ? (i & 2) : 0; }
 };
+// product row i of each eight holds token (i >> 1) | (i & 1) << 2, so that the values' token pairs lie in different banks
+__device__ __forceinline__ int ka_row_of(int t) { return (t & 8) | ((t & 3) << 1) | ((t >> 2) & 1); }
 
 struct KaParams {
     KvCache cache;
@@ -68,6 +88,7 @@ struct KaSpan {
     bool bad;
     __device__ __forceinline__ int tile(int i) const { return i < sinks ? i : first + (i - sinks); }
     __device__ __forceinline__ int chunks() const { return max(1, (tiles + kKaWarps - 1) / kKaWarps); }
+    __device__ __forceinline__ int cost() const { return chunks() + kKaAhead; }
 };
 __device__ __forceinline__ KaSpan ka_span(const KaParams& p, int b) {
     KaSpan s;
@@ -92,6 +113,31 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// c = a b + c (ZERO: a b), a and b of four 8-bit floating-point numbers (e4m3) per register
+template <bool ZERO>
+__device__ __forceinline__ void mma_e4m3(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (ZERO) {
+        asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                     : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+    } else {
+        asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+}
+// four numbers as e4m3, the first in the lowest byte; x keeps what is left of them
+__device__ __forceinline__ uint32_t take_e4m3(float (&x)[4]) {
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x[1]), "f"(x[0]));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x[3]), "f"(x[2]));
+    uint32_t a, b;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(a) : "h"(lo));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(b) : "h"(hi));
+    const float2 fa = f16x2_to_float2(a), fb = f16x2_to_float2(b);
+    x[0] -= fa.x; x[1] -= fa.y; x[2] -= fb.x; x[3] -= fb.y;
+    return (uint32_t)lo | (uint32_t)hi << 16;
+}
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
     uint32_t r;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
@@ -100,6 +146,7 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ uint32_t lds32(uint32_t a) { uint32_t r; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r) : "r"(a) : "memory"); return r; }
@@ -122,14 +169,11 @@ template <int N> __device__ __forceinline__ void lds_words(uint32_t a, uint32_t 
 __device__ __forceinline__ float scale_of(uint32_t par) { return __uint_as_float(par << 16); }
 __device__ __forceinline__ float minimum_of(uint32_t par) { return __uint_as_float(par & 0xffff0000u); }
 __device__ __forceinline__ uint32_t f16_pair(float lo, float hi) { return pack_pair<f16_t>(lo, hi); }
-__device__ __forceinline__ float quad_max(float x) {
-    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-    return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-}
 __device__ __forceinline__ float quad_sum(float x) {
     x += __shfl_xor_sync(0xffffffffu, x, 1);
     return x + __shfl_xor_sync(0xffffffffu, x, 2);
 }
+__device__ __forceinline__ float rcp_approx(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float across_max(float x) {      // over the eight lanes with the same column
     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
@@ -161,363 +205,424 @@ __device__ __forceinline__ long long ka_out_row(const KaParams& p, int b, int h,
     const int i = row / p.group, g = row - i * p.group;
     return ((long long)b * p.seqs.Q + i) * ((long long)p.cache.heads * p.group) + (long long)h * p.group + g;
 }
-__device__ __forceinline__ float ka_lse(float m, float l) { return l == 0.f ? -INFINITY : fmaf(m, 0.69314718055994531f, logf(l)); }
+__device__ __forceinline__ float ka_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f; }
 
 // ---- the kernel ------------------------------------------------------------------------------------------------
 // E: the queries' type.  SPLIT: weights enter the second product in two halves (22 bits): one half-precision weight is off by
 // 2^-12 on average, which is nothing beside a bfloat16 result's 2^-9 but would be as much as a half-precision result's own rounding.
 template <typename E, int D, int NT>
-__global__ void __launch_bounds__(kKaThreads) ears_kv_attention_kernel(const KaParams p) {
+__global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT == 2 && D <= 128 ? KA_OCC2 : 2) ears_kv_attention_kernel(const KaParams p) {
     using S = KaShape<D>;
     constexpr int NG = S::NG, RB = S::RB, ROWS = NT * 8;
     constexpr bool SPLIT = std::is_same<E, f16_t>::value;
-    constexpr uint32_t M0 = 0x000f000fu, M1 = 0x00f000f0u;
-    constexpr int PIECES = RB / 32;               // 16-byte pieces of a tile's codes per lane
+    constexpr int PL = SPLIT ? 3 : 2;                     // parts of a query element, four bits each
+    constexpr int SUB = NT == 1 ? KA_SUB : 1;             // tiles taken together
+    constexpr bool QREG = NT * NG <= 4;                   // queries' operands stay in registers
+    constexpr uint32_t M0 = 0x000f000fu, M1 = 0x00f000f0u, M8 = 0x0f0f0f0fu;
 
     extern __shared__ __align__(128) unsigned char ring_mem[];
-    __shared__ float s_m[kKaWarps][ROWS], s_l[kKaWarps][ROWS];
-    __shared__ long long s_sum[kKaWarps], s_base;
-    __shared__ int s_b;
+    // queries' operands; with NT = 1 in the stage of warp 1's ring that is filled last, until they are in registers
+    constexpr bool QRING = NT == 1;
+    static_assert(!QRING || (QREG && NG * PL * 512 <= S::kStage), "queries in a stage");
+    static_assert(8 * D * 2 <= S::kStage, "eight rows as they come");
+    static_assert(kKaWarps * ROWS * D * 4 <= S::kSmem, "the warps' results meet in the ring's memory");
+    __shared__ uint4 s_q_own[QRING ? 1 : NT * NG * PL * 32];
+    uint4* const s_q = QRING ? reinterpret_cast<uint4*>(ring_mem + (2 * S::kStages - 1) * S::kStage) : s_q_own;
+    __shared__ float s_fr[ROWS], s_qs[NG][ROWS], s_m[kKaWarps][ROWS], s_l[kKaWarps][ROWS];
+    __shared__ int s_pos[ROWS], s_out[ROWS], s_ask[ROWS], s_sum[kKaWarps], s_b, s_off;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, j = lane & 3;
     wait_for_stream();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // ---- this CTA's share of all chunks
+    // ---- this CTA's share of all chunks (their number fits 31 bits: the host's check)
     const int per_seq = p.cache.heads * p.blocks;
     const int each = (p.seqs.B + kKaThreads - 1) / kKaThreads;
     const int b0 = min(p.seqs.B, tid * each), b1 = min(p.seqs.B, b0 + each);
-    long long own = 0;
-    for (int b = b0; b < b1; ++b) own += (long long)ka_span(p, b).chunks() * per_seq;
-    long long before = own;
+    int own = 0;
+#pragma unroll 1
+    for (int b = b0; b < b1; ++b) own += ka_span(p, b).cost() * per_seq;
+    int before = own;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const long long up = __shfl_up_sync(0xffffffffu, before, d);
+        const int up = __shfl_up_sync(0xffffffffu, before, d);
         if (lane >= d) before += up;
     }
     if (lane == 31) s_sum[warp] = before;
     __syncthreads();
-    long long total = 0;
+    int total = 0;
 #pragma unroll
     for (int w = 0; w < kKaWarps; ++w) {
         if (w < warp) before += s_sum[w];
         total += s_sum[w];
     }
     before -= own;
-    const long long ctas = min((long long)gridDim.x, total);
+    const int ctas = min((int)gridDim.x, total), share = total / ctas, longer = total - share * ctas;   // the first `longer` have one more
     if (tid == 0) p.cut[blockIdx.x] = make_int4(-1, 0, 0, 0);
     if (blockIdx.x >= ctas) return;
-    const long long x0 = total * blockIdx.x / ctas, x1 = total * (blockIdx.x + 1) / ctas;
-    if (own && before <= x0 && x0 < before + own) {
-        long long base = before;
-        int b = b0;
+    const int begin = (int)blockIdx.x * share + min((int)blockIdx.x, longer);
+    if (own && before <= begin && begin < before + own) {
+        int base = before, b = b0;
+#pragma unroll 1
         for (;; ++b) {
-            const long long n = (long long)ka_span(p, b).chunks() * per_seq;
-            if (x0 < base + n) break;
+            const int n = ka_span(p, b).cost() * per_seq;
+            if (begin < base + n) break;
             base += n;
         }
         s_b = b;
-        s_base = base;
+        s_off = begin - base;
     }
     __syncthreads();
+    int left = share + (blockIdx.x < longer), b = s_b, off = s_off;        // cost still to do; the sequence it starts in, and where there
 
     // ---- addresses that do not change
     const uint32_t ring = smem_u32(ring_mem) + warp * (S::kStages * S::kStage);
-    uint32_t put_k[PIECES], put_v[PIECES];
-#pragma unroll
-    for (int n = 0; n < PIECES; ++n) {
-        const int piece = lane + 32 * n, t = piece / (RB / 16), c = piece % (RB / 16);
-        // keys: product row i holds token (i >> 1) | (i & 1) << 2 of each eight, so that the values' token pairs lie in different banks
-        const int i = (t & 8) | ((t & 3) << 1) | ((t >> 2) & 1);
-        put_k[n] = i * RB + ((c ^ S::swizzle(i)) << 4);
-        put_v[n] = S::kCodes + t * RB + ((c ^ S::swizzle(t)) << 4);
-    }
     const int my_token = (r >> 1) | ((r & 1) << 2);
     const uint32_t get_k = r * RB + ((S::swizzle(r) + (j >> 1)) << 4) + (j & 1) * 8;
     const uint32_t get_v = S::kCodes + j * RB + ((S::swizzle(j) + (r >> 2)) << 4) + (r & 3) * 4;
     const uint32_t get_p = 2 * S::kCodes + my_token * NG * 4;
+    // copies: half a warp per tile; a lane has every 16th piece of 16 bytes, its tokens t0, t0 + 256 / RB, ...
+    const int l16 = lane & 15, t0 = l16 / (RB / 16), c16 = l16 % (RB / 16);
+    const uint32_t put_tile = ring + (lane >> 4) * S::kTileBytes;
+    const uint32_t put_k = (uint32_t)(c16 ^ S::swizzle(ka_row_of(t0))) << 4, put_v = (uint32_t)(c16 ^ S::swizzle(t0)) << 4;
+    const long long v_rows = (long long)p.cache.heads * p.cache.page;
 
-    long long x = x0, base = s_base;
-    int b = s_b;
     KaSpan span = ka_span(p, b);
-    while (x < x1) {
-        const int chunks = span.chunks();
-        const long long seq_total = (long long)chunks * per_seq;
-        if (x >= base + seq_total) {
-            base += seq_total;
+    while (left > 0) {
+        const int chunks = span.chunks(), cost = span.cost(), unit = off / cost, at0 = off - unit * cost;
+        if (unit >= per_seq) {
             span = ka_span(p, ++b);
+            off = 0;
             continue;
         }
-        const int unit = (int)((x - base) / chunks), c0 = (int)((x - base) - (long long)unit * chunks);
-        const int take = (int)min((long long)(chunks - c0), x1 - x);
+        const int taken = min(cost - at0, left), c0 = max(0, at0 - kKaAhead), c1 = max(0, at0 + taken - kKaAhead);
+        off += taken;
+        left -= taken;
+        if (c0 == c1) continue;
         const int h = unit / p.blocks, row0 = (unit - h * p.blocks) * ROWS;
+        const int last_pos = span.start + max(span.count - 1, 0);
 
-        // ---- queries: normalised to 2^14 at most per row, halves; odd dimensions / 16
-        uint32_t qf[NT][NG][4][2];
-        float fr[NT][2], qs[NT][2][NG], mb[NT][2], l[NT][2], om[NT][2][NG], o[NT][NG * 4][4];
+        // ---- this warp's tiles, first + 4 k; a stage of its ring holds two
+        const int first = c0 * kKaWarps + warp;
+        const int n_tiles = max(0, (min(c1 * kKaWarps, span.tiles) - first + kKaWarps - 1) / kKaWarps);
+        const int n_pairs = (n_tiles + 1) / 2;
+        long long at = 0;                                   // row of the tile of `lane` in the current 32, -1: no page
+        const unsigned char* from_k = p.cache.codes + (long long)h * p.cache.page * RB + l16 * 16;
+        const unsigned char* from_p = reinterpret_cast<const unsigned char*>(p.cache.params) + (long long)h * p.cache.page * (NG * 4);
+        auto issue = [&](int i, int slot) {
+            if ((i & 15) == 0) {
+                at = -1;
+                if (2 * i + lane < n_tiles) at = kv_row(p.cache, p.seqs, b, (long long)span.tile(first + (2 * i + lane) * kKaWarps) * kKaTile);
+            }
+            const long long row = __shfl_sync(0xffffffffu, at, ((2 * i) & 31) + (lane >> 4));
+            const uint32_t to = put_tile + slot * S::kStage;
+            if (row >= 0) {
+                const unsigned char *k = from_k + row * RB, *v = k + v_rows * RB, *q = from_p + row * (NG * 4);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int row = row0 + nt * 8 + r, i = row / p.group, qh = h * p.group + (row - i * p.group);
-            float v[NG][16], big = 0.f;
-            const bool real = row < p.M;
-            const E* src = reinterpret_cast<const E*>(p.q) + (real ? b * p.sb + i * p.sq + qh * p.sh : 0) + j * 16;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    float e[8];
-                    if (real) KvEight<E>::load(src + g * kKvGroup + half * 8, p.vec, e);
-#pragma unroll
-                    for (int n = 0; n < 8; ++n) {
-                        v[g][half * 8 + n] = real ? e[n] : 0.f;
-                        big = max_nan(big, fabsf(v[g][half * 8 + n]));
-                    }
+                for (int n = 0; n < RB / 16; ++n) {
+                    // token t0 + tn: which bits of the row's number and of its swizzle tn adds is known
+                    const int tn = n * (256 / RB), in = ka_row_of(tn);
+                    copy16(to + ka_row_of(t0) * RB + (put_k ^ (S::swizzle(in) << 4)) + in * RB, k + n * 256);
+                    copy16(to + S::kCodes + t0 * RB + (put_v ^ (S::swizzle(tn) << 4)) + tn * RB, v + n * 256);
                 }
+                if constexpr (NG == 1) {
+                    if (l16 < 8) copy16(to + 2 * S::kCodes + l16 * 16, q + (l16 & 4 ? v_rows * (NG * 4) : 0) + (l16 & 3) * 16);
+                } else if constexpr (NG == 2) {
+                    copy16(to + 2 * S::kCodes + l16 * 16, q + (l16 & 8 ? v_rows * (NG * 4) : 0) + (l16 & 7) * 16);
+                } else {
+                    copy16(to + 2 * S::kCodes + l16 * 16, q + l16 * 16);
+                    copy16(to + 2 * S::kCodes + S::kPars + l16 * 16, q + v_rows * (NG * 4) + l16 * 16);
+                }
+            } else if (2 * i + (lane >> 4) < n_tiles) {
+                // no page: its tokens' scales and minima are NaN, and so are the rows that see them
+#pragma unroll
+                for (int n = 0; n < 2 * NG; ++n) sts32(to + 2 * S::kCodes + (l16 + 16 * n) * 4, 0x7fc07fc0u);
+                if (l16 == 0 && p.status) atomicOr(p.status, kDevInvalid);
+            }
+        };
+#pragma unroll 1
+        for (int i = 0; i < S::kStages - 1; ++i) {
+            if (i < n_pairs) issue(i, i);
+            copies_commit();
+        }
+
+        // ---- queries, eight rows per warp, which its ring's last stage takes as they come: normalised to below 2^8 per row
+        // and taken apart into PL numbers of four bits
+#pragma unroll 1
+        for (int nt = warp; nt < NT; nt += kKaWarps) {
+            E* raw = reinterpret_cast<E*>(ring_mem + ((warp + 1) * S::kStages - 1) * S::kStage);
+            const int row = row0 + nt * 8 + r;
+            const bool real = row < p.M;
+            const int i = row / p.group, qh = h * p.group + (row - i * p.group);
+            const E* src = reinterpret_cast<const E*>(p.q) + (real ? b * p.sb + i * p.sq + qh * p.sh : 0);
+            __syncwarp();
+            if (!real || p.vec) {
+#pragma unroll
+                for (int n = 0; n < D / 32; ++n)            // 16 bytes of the row per lane
+                    reinterpret_cast<uint4*>(raw + r * D)[4 * n + j] = real ? __ldg(reinterpret_cast<const uint4*>(src) + 4 * n + j) : make_uint4(0, 0, 0, 0);
+            } else {
+#pragma unroll 1
+                for (int n = j; n < D; n += 4) raw[r * D + n] = ld_elem(src + n);
+            }
+            __syncwarp();
+            const uint4* mine = reinterpret_cast<const uint4*>(raw + r * D + j * 16);
+            float big = 0.f, v[16];
+            auto sixteen = [&](int g) {
+                const uint4 lo = mine[8 * g], hi = mine[8 * g + 1];
+                const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    const float2 f = unpack_pair<E>(w[n]);
+                    v[2 * n] = f.x; v[2 * n + 1] = f.y;
+                }
+            };
+#pragma unroll 1
+            for (int g = 0; g < NG; ++g) {
+                sixteen(g);
+                float sum = 0.f;
+#pragma unroll
+                for (int n = 0; n < 16; ++n) { sum += v[n]; big = max_nan(big, fabsf(v[n])); }
+                sum = quad_sum(sum) * p.scale2;
+                if (j == 0) s_qs[g][nt * 8 + r] = sum;
             }
             big = max_nan(big, __shfl_xor_sync(0xffffffffu, big, 1));
             big = max_nan(big, __shfl_xor_sync(0xffffffffu, big, 2));
             const int ex = max((int)(__float_as_uint(big) >> 23) - 127, -100);
-            const float up = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
-            // scores: codes stand for c 2^-24, the row for q 2^(14 - ex)
-            float f = p.scale2 * 1024.f * __uint_as_float((uint32_t)(127 + ex) << 23);
-            if (!(big <= FLT_MAX)) f = NAN;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                float sum = 0.f;
-#pragma unroll
-                for (int n = 0; n < 16; ++n) sum += v[g][n];
-                sum = quad_sum(sum) * p.scale2;
-#pragma unroll
-                for (int col = 0; col < 2; ++col) qs[nt][col][g] = __shfl_sync(0xffffffffu, sum, (2 * j + col) * 4);
-#pragma unroll
-                for (int w = 0; w < 2; ++w)
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        const float u = (n & 1) ? up * 0.0625f : up;
-                        qf[nt][g][2 * w + (n >> 1)][n & 1] = f16_pair(v[g][8 * w + n] * u, v[g][8 * w + n + 4] * u);
-                    }
+            const float up = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
+            if (j == 0) {
+                // a code stands for c 2^-9, the row for q 2^(7 - ex)
+                s_fr[nt * 8 + r] = big <= FLT_MAX ? p.scale2 * 4.f * __uint_as_float((uint32_t)(127 + ex) << 23) : NAN;
+                s_pos[nt * 8 + r] = min(last_pos, span.start + (real ? i : (p.M - 1) / p.group));
+                s_out[nt * 8 + r] = real ? i * p.cache.heads * p.group + qh : -1;
+                s_ask[nt * 8 + r] = i < span.count;
             }
+#pragma unroll 1
+            for (int g = 0; g < NG; ++g) {
+                sixteen(g);
+                float part[4][4];                            // (word, parity) of the element: the order in which codes come out
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) part[n][e] = v[(n >> 1) * 8 + 2 * e + (n & 1)] * up;
+#pragma unroll
+                for (int pl = 0; pl < PL; ++pl)
+                    s_q[((nt * NG + g) * PL + pl) * 32 + lane] = make_uint4(take_e4m3(part[0]), take_e4m3(part[1]), take_e4m3(part[2]), take_e4m3(part[3]));
+            }
+        }
+        __syncthreads();
+        uint4 qf[QREG ? NT : 1][QREG ? NG : 1][QREG ? PL : 1];
+        float fr[NT][2], qs[NT][2][NG], mb[NT][2], l[NT][2], om[NT][2][NG], o[NT][NG * 4][4];    // mb: minus the running maximum
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int col = 0; col < 2; ++col) {
-                fr[nt][col] = __shfl_sync(0xffffffffu, f, (2 * j + col) * 4);
+                fr[nt][col] = s_fr[nt * 8 + 2 * j + col];
                 mb[nt][col] = 0.f;
                 l[nt][col] = 0.f;
 #pragma unroll
-                for (int g = 0; g < NG; ++g) om[nt][col][g] = 0.f;
+                for (int g = 0; g < NG; ++g) { om[nt][col][g] = 0.f; qs[nt][col][g] = s_qs[g][nt * 8 + 2 * j + col]; }
             }
 #pragma unroll
             for (int n = 0; n < NG * 4; ++n)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) o[nt][n][k] = 0.f;
-        }
-        uint32_t unset = (1u << (2 * NT)) - 1;              // rows that have seen no token yet, a bit per (nt, column)
-        float cs = 0x1p120f;                                // the values' scales enter times this power of two
-        const int last_pos = span.start + max(span.count - 1, 0);
-        const int pmin = min(last_pos, span.start + row0 / p.group), pmax = min(last_pos, span.start + (min(row0 + ROWS, p.M) - 1) / p.group);
-
-        // ---- this warp's tiles: first + 4 k
-        const int first = c0 * kKaWarps + warp;
-        const int n_tiles = max(0, (min((c0 + take) * kKaWarps, span.tiles) - first + kKaWarps - 1) / kKaWarps);
-        long long at = 0;                                   // row of the tile of `lane` in the current 32, -1: no page
-        uint32_t unusable = 0;
-        auto issue = [&](int k) {
-            if ((k & 31) == 0) {
-                at = -1;
-                if (k + lane < n_tiles) at = kv_row(p.cache, p.seqs, b, (long long)span.tile(first + (k + lane) * kKaWarps) * kKaTile);
-            }
-            const long long row = __shfl_sync(0xffffffffu, at, k & 31);
-            unusable = (unusable & ~(1u << (k & 31))) | ((uint32_t)(row < 0) << (k & 31));
-            if (row >= 0) {
-                const uint32_t to = ring + (k % S::kStages) * S::kStage;
-                const long long kr = row + (long long)h * p.cache.page, vr = kr + (long long)p.cache.heads * p.cache.page;
+            if constexpr (QREG) {
 #pragma unroll
-                for (int n = 0; n < PIECES; ++n) {
-                    copy16(to + put_k[n], p.cache.codes + kr * RB + (lane + 32 * n) * 16);
-                    copy16(to + put_v[n], p.cache.codes + vr * RB + (lane + 32 * n) * 16);
-                }
-                if (lane < 8 * NG) {
-                    const long long pr = lane < 4 * NG ? kr : vr;
-                    copy16(to + 2 * S::kCodes + lane * 16, reinterpret_cast<const unsigned char*>(p.cache.params + pr * NG) + (lane & (4 * NG - 1)) * 16);
-                }
-            } else if (lane == 0 && p.status) {
-                atomicOr(p.status, kDevInvalid);
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int pl = 0; pl < PL; ++pl) qf[nt][g][pl] = s_q[((nt * NG + g) * PL + pl) * 32 + lane];
             }
-        };
-#pragma unroll 1
-        for (int k = 0; k < S::kStages - 1; ++k) {
-            if (k < n_tiles) issue(k);
-            copies_commit();
         }
+        const int pmin = s_pos[0], pmax = s_pos[ROWS - 1];
+        if constexpr (QRING) __syncthreads();
+        uint32_t unset = (1u << (2 * NT)) - 1;              // rows that have seen no token yet, a bit per (nt, column)
+        float cs = 0x1p120f, ics = 0x1p-120f;               // the values' scales enter times this power of two; 1 / cs
+
+        int slot = 0;
 #pragma unroll 1
-        for (int k = 0; k < n_tiles; ++k) {
-            const bool broken = (unusable >> (k & 31)) & 1;
+        for (int i = 0; i < n_pairs; ++i) {
             copies_wait<S::kStages - 2>();
             __syncwarp();
-            if (k + S::kStages - 1 < n_tiles) issue(k + S::kStages - 1);
+            if (i + S::kStages - 1 < n_pairs) issue(i + S::kStages - 1, slot ? slot - 1 : S::kStages - 1);
             copies_commit();
-            const uint32_t stage = ring + (k % S::kStages) * S::kStage;
+#pragma unroll 1
+            for (int s2 = 0; s2 < 2; s2 += SUB) {
+                if (SUB == 1 && 2 * i + s2 >= n_tiles) break;
+                const uint32_t stage = ring + slot * S::kStage + s2 * S::kTileBytes;
 
-            uint32_t kp[2][NG], vp[2][NG];
+                uint32_t kp[2 * SUB][NG], vp[2 * SUB][NG];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                lds_words<NG>(stage + get_p + e * 8 * NG * 4, kp[e]);
-                lds_words<NG>(stage + get_p + S::kParams + e * 8 * NG * 4, vp[e]);
-            }
+                for (int e = 0; e < 2 * SUB; ++e) {
+                    lds_words<NG>(stage + (e >> 1) * S::kTileBytes + get_p + (e & 1) * 8 * NG * 4, kp[e]);
+                    lds_words<NG>(stage + (e >> 1) * S::kTileBytes + get_p + S::kPars + (e & 1) * 8 * NG * 4, vp[e]);
+                }
 
-            // scores relative to the running maximum, base 2: [nt][2 e + col], token e of this thread's two
-            float sc[NT][4], dot[NT][4];
+                // scores relative to the running maximum, base 2: [nt][2 e + col], token e of this thread's
+                float sc[NT][4 * SUB], dot[NT][4 * SUB];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+                for (int g = 0; g < NG; ++g) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) { sc[nt][c] = -mb[nt][c & 1]; dot[nt][c] = 0.f; }
+                    for (int u = 0; u < SUB; ++u) {
+                        const uint32_t from = stage + u * S::kTileBytes + (get_k ^ (g << 5));
+                        const uint2 w0 = lds64(from), w1 = lds64(from + 8 * RB);
+                        const uint32_t a[2][4] = {{w0.x & M8, w1.x & M8, (w0.x >> 4) & M8, (w1.x >> 4) & M8},
+                                                  {w0.y & M8, w1.y & M8, (w0.y >> 4) & M8, (w1.y >> 4) & M8}};
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                uint2 w0 = lds64(stage + (get_k ^ (g << 5))), w1 = lds64(stage + (get_k ^ (g << 5)) + 8 * RB);
-                float acc[NT][4];
+                        for (int nt = 0; nt < NT; ++nt) {
+                            float acc[4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                            for (int pl = 0; pl < PL; ++pl) {
+                                uint4 q;
+                                if constexpr (QREG) q = qf[nt][g][pl];
+                                else q = s_q[((nt * NG + g) * PL + pl) * 32 + lane];
+                                if (pl == 0) mma_e4m3<true>(acc, a[0], q.x, q.y);
+                                else mma_e4m3<false>(acc, a[0], q.x, q.y);
+                                mma_e4m3<false>(acc, a[1], q.z, q.w);
+                            }
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) acc[nt][c] = 0.f;
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    const uint32_t x0w = w ? w0.y : w0.x, x1w = w ? w1.y : w1.x, y0 = x0w >> 8, y1 = x1w >> 8;
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        mma_f16(acc[nt], x0w & M0, x1w & M0, x0w & M1, x1w & M1, qf[nt][g][2 * w][0], qf[nt][g][2 * w][1]);
-                        mma_f16(acc[nt], y0 & M0, y1 & M0, y0 & M1, y1 & M1, qf[nt][g][2 * w + 1][0], qf[nt][g][2 * w + 1][1]);
+                            for (int c = 0; c < 4; ++c) {
+                                const int e = 2 * u + (c >> 1);
+                                float &d = dot[nt][4 * u + c], &t = sc[nt][4 * u + c];
+                                d = g ? fmaf(acc[c], scale_of(kp[e][g]), d) : acc[c] * scale_of(kp[e][g]);
+                                t = fmaf(minimum_of(kp[e][g]), qs[nt][c & 1][g], g ? t : mb[nt][c & 1]);
+                            }
+                        }
                     }
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        dot[nt][c] = fmaf(acc[nt][c], scale_of(kp[c >> 1][g]), dot[nt][c]);
-                        sc[nt][c] = fmaf(minimum_of(kp[c >> 1][g]), qs[nt][c & 1][g], sc[nt][c]);
-                    }
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) sc[nt][c] = fmaf(dot[nt][c], fr[nt][c & 1], sc[nt][c]);
+                    for (int c = 0; c < 4 * SUB; ++c) sc[nt][c] = fmaf(dot[nt][c], fr[nt][c & 1], sc[nt][c]);
 
-            // masks, where the tile needs them
-            const int t0 = span.tile(first + k * kKaWarps) * kKaTile;
-            if (broken || t0 + kKaTile - 1 > pmin || (p.window && t0 + kKaTile - 1 >= p.sinks && t0 <= pmax - p.window)) {
+                // masks, where a tile needs them
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int t = t0 + e * 8 + my_token;
-                    bool lost = broken;                        // values of no use: rows that see the token become NaN by their score
+                for (int u = 0; u < SUB; ++u) {
+                    const int k = 2 * i + s2 + u;
+                    const int tt = k < n_tiles ? span.tile(first + k * kKaWarps) * kKaTile : INT_MAX - kKaTile;
+                    if (tt + kKaTile - 1 > pmin || (p.window && tt + kKaTile - 1 >= p.sinks && tt <= pmax - p.window)) {
 #pragma unroll
-                    for (int g = 0; g < NG; ++g) {
-                        lost = lost || !(scale_of(vp[e][g]) <= FLT_MAX) || !(fabsf(minimum_of(vp[e][g])) <= FLT_MAX);
+                        for (int e = 2 * u; e < 2 * u + 2; ++e) {
+                            const int t = tt + (e & 1) * 8 + my_token;
+                            bool lost = false;                     // values of no use: rows that see the token become NaN by their score
+#pragma unroll
+                            for (int g = 0; g < NG; ++g)
+                                lost = lost || !(scale_of(vp[e][g]) <= FLT_MAX) || !(fabsf(minimum_of(vp[e][g])) <= FLT_MAX);
+                            if (lost || t > pmax || (p.window && t >= p.sinks && t <= pmin - p.window)) {
+#pragma unroll
+                                for (int g = 0; g < NG; ++g) vp[e][g] = 0;
+                            }
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int col = 0; col < 2; ++col) {
+                                    const int pos = s_pos[nt * 8 + 2 * j + col];
+                                    float& v = sc[nt][2 * e + col];
+                                    if (lost) v = NAN;
+                                    if (t > pos || (p.window && t >= p.sinks && t <= pos - p.window)) v = -INFINITY;
+                                }
+                        }
                     }
-                    if (lost || t > pmax || (p.window && t >= p.sinks && t <= pmin - p.window)) {
+                }
+
+                const float cap = ics * kKaScaleCap;
+                bool raise = unset != 0;
 #pragma unroll
-                        for (int g = 0; g < NG; ++g) vp[e][g] = 0;
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 4 * SUB; ++c) raise = raise || sc[nt][c] > kKaSlack;
+#pragma unroll
+                for (int e = 0; e < 2 * SUB; ++e)
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) raise = raise || scale_of(vp[e][g]) > cap;
+                if (__any_sync(0xffffffffu, raise)) {
+                    float sv = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 2 * SUB; ++e)
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) sv = fmaxf(sv, scale_of(vp[e][g]));
+                    sv = across_max(sv);
+                    float ratio = 1.f;
+                    if (sv > cap) {                                    // >= 2^-117, a finite normal number: to between 2 and 4
+                        const int ex = (int)(__float_as_uint(sv) >> 23) - 127;
+                        ratio = __uint_as_float((uint32_t)(127 + 1 - ex) << 23) * ics;
+                        cs = __uint_as_float((uint32_t)(127 + 1 - ex) << 23);
+                        ics = __uint_as_float((uint32_t)(127 - 1 + ex) << 23);
                     }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int col = 0; col < 2; ++col) {
-                            const int row = min(row0 + nt * 8 + 2 * j + col, p.M - 1);
-                            const int pos = min(last_pos, span.start + row / p.group);
-                            float& v = sc[nt][2 * e + col];
-                            if (lost) v = NAN;
-                            if (t > pos || (p.window && t >= p.sinks && t <= pos - p.window)) v = -INFINITY;
+                            float top = sc[nt][col];
+#pragma unroll
+                            for (int e = 1; e < 2 * SUB; ++e) top = fmaxf(top, sc[nt][2 * e + col]);
+                            top = across_max(top);
+                            const uint32_t bit = 1u << (2 * nt + col);
+                            float alpha = 1.f;
+                            if (top > kKaSlack || ((unset & bit) && top > -INFINITY)) {
+                                alpha = (unset & bit) ? 0.f : ex2_approx(-top);
+                                mb[nt][col] -= top;
+#pragma unroll
+                                for (int e = 0; e < 2 * SUB; ++e) sc[nt][2 * e + col] -= top;
+                                unset &= ~bit;
+                            }
+                            l[nt][col] *= alpha;
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) om[nt][col][g] *= alpha;
+                            alpha *= ratio;
+#pragma unroll
+                            for (int n = 0; n < NG * 4; ++n) { o[nt][n][col] *= alpha; o[nt][n][2 + col] *= alpha; }
                         }
                 }
-            }
 
-            bool raise = unset != 0;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) raise = raise || sc[nt][c] > kKaSlack;
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int g = 0; g < NG; ++g) raise = raise || scale_of(vp[e][g]) * cs > 128.f;
-            if (__any_sync(0xffffffffu, raise)) {
-                float sv = 0.f;
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-#pragma unroll
-                    for (int g = 0; g < NG; ++g) sv = fmaxf(sv, scale_of(vp[e][g]));
-                sv = across_max(sv);
-                float ratio = 1.f;
-                if (sv * cs > 128.f) {
-                    const int ex = (int)(__float_as_uint(sv) >> 23) - 127;           // sv >= 2^-120: a finite normal number
-                    const float now = __uint_as_float((uint32_t)(127 + 6 - ex) << 23);
-                    ratio = now / cs;
-                    cs = now;
-                }
+                // weights
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int col = 0; col < 2; ++col) {
-                        const float top = across_max(fmaxf(sc[nt][col], sc[nt][2 + col]));
-                        const uint32_t bit = 1u << (2 * nt + col);
-                        float alpha = 1.f;
-                        if (top > kKaSlack || ((unset & bit) && top > -INFINITY)) {
-                            alpha = (unset & bit) ? 0.f : ex2_approx(-top);
-                            mb[nt][col] += top;
-                            sc[nt][col] -= top;
-                            sc[nt][2 + col] -= top;
-                            unset &= ~bit;
-                        }
-                        l[nt][col] *= alpha;
+                    for (int c = 0; c < 4 * SUB; ++c) {
+                        const float w = ex2_approx(sc[nt][c]);
+                        sc[nt][c] = w;
+                        l[nt][c & 1] += w;
 #pragma unroll
-                        for (int g = 0; g < NG; ++g) om[nt][col][g] *= alpha;
-                        alpha *= ratio;
-#pragma unroll
-                        for (int n = 0; n < NG * 4; ++n) { o[nt][n][col] *= alpha; o[nt][n][2 + col] *= alpha; }
+                        for (int g = 0; g < NG; ++g) om[nt][c & 1][g] = fmaf(w, minimum_of(vp[c >> 1][g]), om[nt][c & 1][g]);
                     }
-            }
-
-            // weights
+                // values
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+                for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const float w = ex2_approx(sc[nt][c]);
-                    sc[nt][c] = w;
-                    l[nt][c & 1] += w;
-#pragma unroll
-                    for (int g = 0; g < NG; ++g) om[nt][c & 1][g] = fmaf(w, minimum_of(vp[c >> 1][g]), om[nt][c & 1][g]);
-                }
-            // values
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                const float s0 = scale_of(vp[0][g]) * cs, s1 = scale_of(vp[1][g]) * cs;
-                uint32_t wf[NT][2], wl[SPLIT ? NT : 1][2];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const float a = sc[nt][0] * s0, bq = sc[nt][1] * s0, c = sc[nt][2] * s1, d = sc[nt][3] * s1;
-                    const uint32_t u = f16_pair(a, bq), v = f16_pair(c, d);
-                    if constexpr (SPLIT) {
-                        const float2 fu = f16x2_to_float2(u), fv = f16x2_to_float2(v);
-                        wl[nt][0] = transpose_8x8(f16_pair(a - fu.x, bq - fu.y));
-                        wl[nt][1] = transpose_8x8(f16_pair(c - fv.x, d - fv.y));
-                    }
-                    wf[nt][0] = transpose_8x8(u);
-                    wf[nt][1] = transpose_8x8(v);
-                }
-                const uint32_t from = stage + (get_v ^ (g << 5));
-                const uint32_t wa = lds32(from), wb = lds32(from + 4 * RB), wc = lds32(from + 8 * RB), wd = lds32(from + 12 * RB);
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint32_t ab = __byte_perm(wa, wb, half ? 0x7632 : 0x5410), cd = __byte_perm(wc, wd, half ? 0x7632 : 0x5410);
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        const uint32_t xa = n ? ab >> 8 : ab, xc = n ? cd >> 8 : cd;
+                    for (int g = 0; g < NG; ++g) {
+                        const float s0 = scale_of(vp[2 * u][g]) * cs, s1 = scale_of(vp[2 * u + 1][g]) * cs;
+                        uint32_t wf[NT][2], wl[SPLIT ? NT : 1][2];
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            mma_f16(o[nt][g * 4 + half * 2 + n], xa & M0, xa & M1, xc & M0, xc & M1, wf[nt][0], wf[nt][1]);
-                            if constexpr (SPLIT) mma_f16(o[nt][g * 4 + half * 2 + n], xa & M0, xa & M1, xc & M0, xc & M1, wl[nt][0], wl[nt][1]);
+                            const float* w = &sc[nt][4 * u];
+                            const float a = w[0] * s0, bq = w[1] * s0, c = w[2] * s1, d = w[3] * s1;
+                            const uint32_t x = f16_pair(a, bq), y = f16_pair(c, d);
+                            if constexpr (SPLIT) {
+                                const float2 fx = f16x2_to_float2(x), fy = f16x2_to_float2(y);
+                                wl[nt][0] = transpose_8x8(f16_pair(a - fx.x, bq - fx.y));
+                                wl[nt][1] = transpose_8x8(f16_pair(c - fy.x, d - fy.y));
+                            }
+                            wf[nt][0] = transpose_8x8(x);
+                            wf[nt][1] = transpose_8x8(y);
+                        }
+                        const uint32_t from = stage + u * S::kTileBytes + (get_v ^ (g << 5));
+                        const uint32_t wa = lds32(from), wb = lds32(from + 4 * RB), wc = lds32(from + 8 * RB), wd = lds32(from + 12 * RB);
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            const uint32_t ab = __byte_perm(wa, wb, half ? 0x7632 : 0x5410), cd = __byte_perm(wc, wd, half ? 0x7632 : 0x5410);
+#pragma unroll
+                            for (int n = 0; n < 2; ++n) {
+                                const uint32_t xa = n ? ab >> 8 : ab, xc = n ? cd >> 8 : cd;
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    mma_f16(o[nt][g * 4 + half * 2 + n], xa & M0, xa & M1, xc & M0, xc & M1, wf[nt][0], wf[nt][1]);
+                                    if constexpr (SPLIT) mma_f16(o[nt][g * 4 + half * 2 + n], xa & M0, xa & M1, xc & M0, xc & M1, wl[nt][0], wl[nt][1]);
+                                }
+                            }
                         }
                     }
-                }
             }
+            slot = slot == S::kStages - 1 ? 0 : slot + 1;
         }
 
         // ---- the warps' results together
@@ -530,16 +635,15 @@ __global__ void __launch_bounds__(kKaThreads) ears_kv_attention_kernel(const KaP
 #pragma unroll
                 for (int g = 0; g < NG; ++g) om[nt][col][g] = across_sum(om[nt][col][g]);
                 if (r == 0) {
-                    s_m[warp][nt * 8 + 2 * j + col] = (unset >> (2 * nt + col)) & 1 ? -INFINITY : mb[nt][col];
+                    s_m[warp][nt * 8 + 2 * j + col] = (unset >> (2 * nt + col)) & 1 ? -INFINITY : -mb[nt][col];
                     s_l[warp][nt * 8 + 2 * j + col] = l[nt][col];
                 }
             }
         __syncthreads();
-        const bool whole = take == chunks;
-        const long long slot = (long long)blockIdx.x * 2 + (c0 == 0);
-        float* red = reinterpret_cast<float*>(ring_mem);      // [warp][8][D]
+        // [warp][row][D], pairs of a row in an order that goes by the row: what a warp stores at once lies in different banks
+        float2* const red = reinterpret_cast<float2*>(ring_mem);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int col = 0; col < 2; ++col) {
                 const int row = nt * 8 + 2 * j + col;
@@ -547,65 +651,71 @@ __global__ void __launch_bounds__(kKaThreads) ears_kv_attention_kernel(const KaP
 #pragma unroll
                 for (int w = 0; w < kKaWarps; ++w) top = fmaxf(top, s_m[w][row]);
                 const float mine = s_m[warp][row], f = mine == -INFINITY ? 0.f : ex2_approx(mine - top);
-                const float even = f / cs;                     // cs a power of two
-                float* to = red + ((warp * 8 + 2 * j + col) * D) + r * 8;
+                const float even = f * ics;
+                float2* to = red + (warp * ROWS + row) * (D / 2) + r * 4;
 #pragma unroll
-                for (int g = 0; g < NG; ++g)
+                for (int g = 0; g < NG; ++g) {
+                    const float shift = f * om[nt][col][g];
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        const float a = o[nt][g * 4 + n][col] * 0x1p24f, c = o[nt][g * 4 + n][2 + col] * 0x1p20f;
-                        const float shift = f * om[nt][col][g];
-                        *reinterpret_cast<float2*>(to + g * kKvGroup + 2 * n) = make_float2(fmaf(a, even, shift), fmaf(c, even, shift));
-                    }
-            }
-            __syncthreads();
-            {
-                constexpr int PER = D / 16;
-                const int row = tid >> 4, d0 = (tid & 15) * PER, in_block = nt * 8 + row, rr = row0 + in_block;
-                float top = -INFINITY, sum = 0.f, v[PER];
-#pragma unroll
-                for (int w = 0; w < kKaWarps; ++w) top = fmaxf(top, s_m[w][in_block]);
-#pragma unroll
-                for (int w = 0; w < kKaWarps; ++w) {
-                    const float m = s_m[w][in_block];
-                    sum = fmaf(s_l[w][in_block], m == -INFINITY ? 0.f : ex2_approx(m - top), sum);
-                }
-#pragma unroll
-                for (int n = 0; n < PER; ++n) v[n] = 0.f;
-#pragma unroll
-                for (int w = 0; w < kKaWarps; ++w)
-#pragma unroll
-                    for (int n = 0; n < PER; ++n) v[n] += red[(w * 8 + row) * D + d0 + n];
-                if (rr < p.M) {
-                    if (whole) {
-                        const bool asked = rr / p.group < span.count;
-                        const long long orow = ka_out_row(p, b, h, rr);
-                        float f = asked && sum != 0.f ? 1.f / sum : 0.f;
-                        if (asked && span.bad) f = NAN;
-                        if (!asked) {
-#pragma unroll
-                            for (int n = 0; n < PER; ++n) v[n] = 0.f;
-                        }
-                        ka_store<E, PER>(reinterpret_cast<E*>(p.out) + orow * D + d0, v, f);
-                        if (p.lse && (tid & 15) == 0) p.lse[orow] = !asked ? -INFINITY : span.bad ? NAN : ka_lse(top, sum);
-                    } else {
-                        float* to = p.part_o + (slot * ROWS + in_block) * D + d0;
-#pragma unroll
-                        for (int n = 0; n < PER; n += 4) *reinterpret_cast<float4*>(to + n) = make_float4(v[n], v[n + 1], v[n + 2], v[n + 3]);
-                        if ((tid & 15) == 0) p.part_ml[slot * ROWS + in_block] = make_float2(top, sum);
-                    }
+                    for (int n = 0; n < 4; ++n)
+                        to[g * (kKvGroup / 2) + (n ^ j)] = make_float2(fmaf(o[nt][g * 4 + n][col] * 0x1p24f, even, shift),
+                                                                      fmaf(o[nt][g * 4 + n][2 + col] * 0x1p20f, even, shift));
                 }
             }
-            __syncthreads();
+        __syncthreads();
+        const bool whole = c1 - c0 == chunks;
+        const long long part = (long long)blockIdx.x * 2 + (c0 == 0);
+#pragma unroll 1
+        for (int nt = 0; nt < NT; ++nt) {
+            constexpr int PER = D / 16;
+            const int in_block = nt * 8 + (tid >> 4), d0 = (tid & 15) * PER, place = s_out[in_block];
+            if (place < 0) continue;
+            float top = -INFINITY, sum = 0.f, v[PER];
+#pragma unroll
+            for (int w = 0; w < kKaWarps; ++w) top = fmaxf(top, s_m[w][in_block]);
+#pragma unroll
+            for (int n = 0; n < PER; ++n) v[n] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kKaWarps; ++w) {
+                const float m = s_m[w][in_block];
+                sum = fmaf(s_l[w][in_block], m == -INFINITY ? 0.f : ex2_approx(m - top), sum);
+                const float2* from = red + (w * ROWS + in_block) * (D / 2) + d0 / 2;
+#pragma unroll
+                for (int n = 0; n < PER / 2; ++n) {
+                    // d0 / 2 + n with the two low bits turned by the row's
+                    const float2 x = PER >= 8 ? from[n ^ ((in_block >> 1) & 3)] : red[(w * ROWS + in_block) * (D / 2) + ((d0 / 2 + n) ^ ((in_block >> 1) & 3))];
+                    v[2 * n] += x.x;
+                    v[2 * n + 1] += x.y;
+                }
+            }
+            if (whole) {
+                const bool asked = s_ask[in_block];
+                const long long orow = (long long)b * p.seqs.Q * (p.cache.heads * p.group) + place;
+                float f = asked && sum != 0.f ? rcp_approx(sum) : 0.f;
+                if (asked && span.bad) f = NAN;
+                if (!asked) {
+#pragma unroll
+                    for (int n = 0; n < PER; ++n) v[n] = 0.f;
+                }
+                ka_store<E, PER>(reinterpret_cast<E*>(p.out) + orow * D + d0, v, f);
+                if (p.lse && (tid & 15) == 0) p.lse[orow] = !asked ? -INFINITY : span.bad ? NAN : ka_lse(top, sum);
+            } else {
+                float* to = p.part_o + (part * ROWS + in_block) * D + d0;
+#pragma unroll
+                for (int n = 0; n < PER; n += 4) *reinterpret_cast<float4*>(to + n) = make_float4(v[n], v[n + 1], v[n + 2], v[n + 3]);
+                if ((tid & 15) == 0) p.part_ml[part * ROWS + in_block] = make_float2(top, sum);
+            }
         }
         if (tid == 0) {
             if (span.bad && p.status) atomicOr(p.status, kDevInvalid);
             if (!whole && c0 == 0) {
-                const long long end = base + (long long)(unit + 1) * chunks - 1;       // the unit's last chunk, and whose it is
-                p.cut[blockIdx.x] = make_int4(b, unit, (int)(((end + 1) * ctas - 1) / total), 0);
+                // who has the unit's last chunk
+                const int end = begin + (share + (blockIdx.x < longer) - left) - taken - at0 + cost - 1, few = longer * (share + 1);
+                const bool early = end < few;
+                p.cut[blockIdx.x] = make_int4(b, unit, (early ? 0 : longer) + (early ? end : end - few) / (early ? share + 1 : share), 0);
             }
         }
-        x += take;
+        __syncthreads();
     }
 }
 
