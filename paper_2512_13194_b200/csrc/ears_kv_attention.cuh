@@ -5,12 +5,12 @@
 //     q . k_t = sum_g s_tg (q_g . c_tg) + m_tg sum(q_g),      out_g = sum_t (P_t s_tg) c_tg + sum_t P_t m_tg
 // so that the products run on the codes themselves, and scales and minima touch a value per token and row only.
 //
-// What bounds it: 4.5 bits per value have to be read, and each code turned into an operand of the tensor cores.  A code c in a byte IS
-// the 8-bit floating-point number (e4m3) c 2^-9, and one in the lowest bits of a half-precision number the subnormal c 2^-24, or
-// c 2^-20 four bits further up; tensor cores take them all at full speed.  For the keys two masks and a shift make eight
-// operands, against queries taken apart into two e4m3 numbers (bfloat16: 8 bits, exact) or three (half precision: 11 bits), whose
-// products and sums are exact or rounded once to 32 bits; the 8-bit product runs at four times the rate of the 16-bit one.
-// For the values, whose weights need half precision's range, 12 operations on a pair of tokens make sixteen operands.
+// What bounds it: 4.5 bits per value have to be read, and each code turned into a 16-bit operand.  A code c placed in the lowest
+// bits of a half-precision number IS the subnormal c 2^-24, and one in bits 4..7 is c 2^-20, which tensor cores take at full
+// speed: two masks and one shift make eight operands of a 32-bit word, with nothing to subtract; the powers of two go into q
+// (odd dimensions of keys / 16) and into the result (odd dimensions of values).  (8-bit floating-point operands would take fewer
+// operations still, c 2^-9 being one as it stands, but m16n8k32 with them is made of conversions and 16-bit products here:
+// 68 conversions per tile of 16 tokens counted, and 437 instructions against 386.)
 //
 // The products have 16 tokens (or, for the values, dimensions) as rows and eight of the head group's
 // queries as columns: M = Q x heads per key head is seldom more than a few eights, and no work goes into padding a tile of
@@ -108,35 +108,18 @@ __device__ __forceinline__ KaSpan ka_span(const KaParams& p, int b) {
 }
 
 // ---- instructions -----------------------------------------------------------------------------------------
+// c = a b + c (ZERO: a b)
+template <bool ZERO = false>
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-// c = a b + c (ZERO: a b), a and b of four 8-bit floating-point numbers (e4m3) per register
-template <bool ZERO>
-__device__ __forceinline__ void mma_e4m3(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     if constexpr (ZERO) {
-        asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
                      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
     } else {
-        asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     }
-}
-// four numbers as e4m3, the first in the lowest byte; x keeps what is left of them
-__device__ __forceinline__ uint32_t take_e4m3(float (&x)[4]) {
-    uint16_t lo, hi;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x[1]), "f"(x[0]));
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x[3]), "f"(x[2]));
-    uint32_t a, b;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(a) : "h"(lo));
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(b) : "h"(hi));
-    const float2 fa = f16x2_to_float2(a), fb = f16x2_to_float2(b);
-    x[0] -= fa.x; x[1] -= fa.y; x[2] -= fb.x; x[3] -= fb.y;
-    return (uint32_t)lo | (uint32_t)hi << 16;
 }
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
     uint32_t r;
@@ -215,20 +198,20 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
     using S = KaShape<D>;
     constexpr int NG = S::NG, RB = S::RB, ROWS = NT * 8;
     constexpr bool SPLIT = std::is_same<E, f16_t>::value;
-    constexpr int PL = SPLIT ? 3 : 2;                     // parts of a query element, four bits each
     constexpr int SUB = NT == 1 ? KA_SUB : 1;             // tiles taken together
     constexpr bool QREG = NT * NG <= 4;                   // queries' operands stay in registers
-    constexpr uint32_t M0 = 0x000f000fu, M1 = 0x00f000f0u, M8 = 0x0f0f0f0fu;
+    constexpr uint32_t M0 = 0x000f000fu, M1 = 0x00f000f0u;
 
     extern __shared__ __align__(128) unsigned char ring_mem[];
     // queries' operands; with NT = 1 in the stage of warp 1's ring that is filled last, until they are in registers
     constexpr bool QRING = NT == 1;
-    static_assert(!QRING || (QREG && NG * PL * 512 <= S::kStage), "queries in a stage");
+    static_assert(!QRING || (QREG && NG * 1024 <= S::kStage), "queries in a stage");
     static_assert(8 * D * 2 <= S::kStage, "eight rows as they come");
     static_assert(kKaWarps * ROWS * D * 4 <= S::kSmem, "the warps' results meet in the ring's memory");
-    __shared__ uint4 s_q_own[QRING ? 1 : NT * NG * PL * 32];
+    __shared__ uint4 s_q_own[QRING ? 1 : NT * NG * 64];
     uint4* const s_q = QRING ? reinterpret_cast<uint4*>(ring_mem + (2 * S::kStages - 1) * S::kStage) : s_q_own;
     __shared__ float s_fr[ROWS], s_qs[NG][ROWS], s_m[kKaWarps][ROWS], s_l[kKaWarps][ROWS];
+    __shared__ float2 s_ml[ROWS];
     __shared__ int s_pos[ROWS], s_out[ROWS], s_ask[ROWS], s_sum[kKaWarps], s_b, s_off;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, j = lane & 3;
@@ -285,7 +268,7 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
     const int l16 = lane & 15, t0 = l16 / (RB / 16), c16 = l16 % (RB / 16);
     const uint32_t put_tile = ring + (lane >> 4) * S::kTileBytes;
     const uint32_t put_k = (uint32_t)(c16 ^ S::swizzle(ka_row_of(t0))) << 4, put_v = (uint32_t)(c16 ^ S::swizzle(t0)) << 4;
-    const long long v_rows = (long long)p.cache.heads * p.cache.page;
+    const long long v_bytes = (long long)p.cache.heads * p.cache.page * RB;              // from a page's keys to its values
 
     KaSpan span = ka_span(p, b);
     while (left > 0) {
@@ -306,18 +289,20 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
         const int first = c0 * kKaWarps + warp;
         const int n_tiles = max(0, (min(c1 * kKaWarps, span.tiles) - first + kKaWarps - 1) / kKaWarps);
         const int n_pairs = (n_tiles + 1) / 2;
-        long long at = 0;                                   // row of the tile of `lane` in the current 32, -1: no page
+        int at = 0;                                         // a sixteenth of the row of tile `lane` of the current 32, -1: no page
         const unsigned char* from_k = p.cache.codes + (long long)h * p.cache.page * RB + l16 * 16;
-        const unsigned char* from_p = reinterpret_cast<const unsigned char*>(p.cache.params) + (long long)h * p.cache.page * (NG * 4);
+        const unsigned char* from_p = reinterpret_cast<const unsigned char*>(p.cache.params) + (long long)h * p.cache.page * (NG * 4) +
+                                      (NG == 4 ? l16 * 16 : (l16 & (4 * NG - 1)) * 16 + (l16 & (4 * NG) ? v_bytes / 8 : 0));
         auto issue = [&](int i, int slot) {
             if ((i & 15) == 0) {
                 at = -1;
-                if (2 * i + lane < n_tiles) at = kv_row(p.cache, p.seqs, b, (long long)span.tile(first + (2 * i + lane) * kKaWarps) * kKaTile);
+                if (2 * i + lane < n_tiles) at = (int)(kv_row(p.cache, p.seqs, b, (long long)span.tile(first + (2 * i + lane) * kKaWarps) * kKaTile) >> 4);
             }
-            const long long row = __shfl_sync(0xffffffffu, at, ((2 * i) & 31) + (lane >> 4));
+            const int row = __shfl_sync(0xffffffffu, at, ((2 * i) & 31) + (lane >> 4));
             const uint32_t to = put_tile + slot * S::kStage;
             if (row >= 0) {
-                const unsigned char *k = from_k + row * RB, *v = k + v_rows * RB, *q = from_p + row * (NG * 4);
+                const unsigned char *k = from_k + (unsigned long long)(unsigned)row * (16 * RB), *v = k + v_bytes;
+                const unsigned char* q = from_p + (unsigned long long)(unsigned)row * (64 * NG);
 #pragma unroll
                 for (int n = 0; n < RB / 16; ++n) {
                     // token t0 + tn: which bits of the row's number and of its swizzle tn adds is known
@@ -326,12 +311,12 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
                     copy16(to + S::kCodes + t0 * RB + (put_v ^ (S::swizzle(tn) << 4)) + tn * RB, v + n * 256);
                 }
                 if constexpr (NG == 1) {
-                    if (l16 < 8) copy16(to + 2 * S::kCodes + l16 * 16, q + (l16 & 4 ? v_rows * (NG * 4) : 0) + (l16 & 3) * 16);
+                    if (l16 < 8) copy16(to + 2 * S::kCodes + l16 * 16, q);
                 } else if constexpr (NG == 2) {
-                    copy16(to + 2 * S::kCodes + l16 * 16, q + (l16 & 8 ? v_rows * (NG * 4) : 0) + (l16 & 7) * 16);
+                    copy16(to + 2 * S::kCodes + l16 * 16, q);
                 } else {
-                    copy16(to + 2 * S::kCodes + l16 * 16, q + l16 * 16);
-                    copy16(to + 2 * S::kCodes + S::kPars + l16 * 16, q + v_rows * (NG * 4) + l16 * 16);
+                    copy16(to + 2 * S::kCodes + l16 * 16, q);
+                    copy16(to + 2 * S::kCodes + S::kPars + l16 * 16, q + v_bytes / 8);     // 4 NG bytes a token beside RB = 32 NG
                 }
             } else if (2 * i + (lane >> 4) < n_tiles) {
                 // no page: its tokens' scales and minima are NaN, and so are the rows that see them
@@ -340,31 +325,33 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
                 if (l16 == 0 && p.status) atomicOr(p.status, kDevInvalid);
             }
         };
+        // ---- queries, eight rows per warp: on their way while the page table is looked up, into its ring's last stage
+        static_assert(NT <= kKaWarps, "a block of rows per warp");
+        E* const raw = reinterpret_cast<E*>(ring_mem + ((warp + 1) * S::kStages - 1) * S::kStage);
+        const int q_row = row0 + warp * 8 + r, q_pos = q_row / p.group, q_head = h * p.group + (q_row - q_pos * p.group);
+        const bool q_real = q_row < p.M;
+        if (warp < NT) {
+            const E* src = reinterpret_cast<const E*>(p.q) + (q_real ? b * p.sb + q_pos * p.sq + q_head * p.sh : 0);
+            if (q_real && p.vec) {
+#pragma unroll
+                for (int n = 0; n < D / 32; ++n) copy16(smem_u32(raw + r * D) + (4 * n + j) * 16, src + (4 * n + j) * 8);
+            } else {
+#pragma unroll 1
+                for (int n = j; n < D; n += 4) raw[r * D + n] = q_real ? ld_elem(src + n) : E();
+            }
+        }
+        copies_commit();
 #pragma unroll 1
         for (int i = 0; i < S::kStages - 1; ++i) {
             if (i < n_pairs) issue(i, i);
             copies_commit();
         }
 
-        // ---- queries, eight rows per warp, which its ring's last stage takes as they come: normalised to below 2^8 per row
-        // and taken apart into PL numbers of four bits
-#pragma unroll 1
-        for (int nt = warp; nt < NT; nt += kKaWarps) {
-            E* raw = reinterpret_cast<E*>(ring_mem + ((warp + 1) * S::kStages - 1) * S::kStage);
-            const int row = row0 + nt * 8 + r;
-            const bool real = row < p.M;
-            const int i = row / p.group, qh = h * p.group + (row - i * p.group);
-            const E* src = reinterpret_cast<const E*>(p.q) + (real ? b * p.sb + i * p.sq + qh * p.sh : 0);
-            __syncwarp();
-            if (!real || p.vec) {
-#pragma unroll
-                for (int n = 0; n < D / 32; ++n)            // 16 bytes of the row per lane
-                    reinterpret_cast<uint4*>(raw + r * D)[4 * n + j] = real ? __ldg(reinterpret_cast<const uint4*>(src) + 4 * n + j) : make_uint4(0, 0, 0, 0);
-            } else {
-#pragma unroll 1
-                for (int n = j; n < D; n += 4) raw[r * D + n] = ld_elem(src + n);
-            }
-            __syncwarp();
+        // normalised to below 2^15 per row, in half precision, odd dimensions / 16
+        copies_wait<S::kStages - 1>();
+        __syncwarp();
+        if (warp < NT) {
+            const int nt = warp;
             const uint4* mine = reinterpret_cast<const uint4*>(raw + r * D + j * 16);
             float big = 0.f, v[16];
             auto sixteen = [&](int g) {
@@ -388,29 +375,31 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
             big = max_nan(big, __shfl_xor_sync(0xffffffffu, big, 1));
             big = max_nan(big, __shfl_xor_sync(0xffffffffu, big, 2));
             const int ex = max((int)(__float_as_uint(big) >> 23) - 127, -100);
-            const float up = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
+            const float up = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
             if (j == 0) {
-                // a code stands for c 2^-9, the row for q 2^(7 - ex)
-                s_fr[nt * 8 + r] = big <= FLT_MAX ? p.scale2 * 4.f * __uint_as_float((uint32_t)(127 + ex) << 23) : NAN;
-                s_pos[nt * 8 + r] = min(last_pos, span.start + (real ? i : (p.M - 1) / p.group));
-                s_out[nt * 8 + r] = real ? i * p.cache.heads * p.group + qh : -1;
-                s_ask[nt * 8 + r] = i < span.count;
+                // a code stands for c 2^-24, the row for q 2^(14 - ex)
+                s_fr[nt * 8 + r] = big <= FLT_MAX ? p.scale2 * 1024.f * __uint_as_float((uint32_t)(127 + ex) << 23) : NAN;
+                s_pos[nt * 8 + r] = min(last_pos, span.start + (q_real ? q_pos : (p.M - 1) / p.group));
+                s_out[nt * 8 + r] = q_real ? q_pos * p.cache.heads * p.group + q_head : -1;
+                s_ask[nt * 8 + r] = q_pos < span.count;
             }
 #pragma unroll 1
             for (int g = 0; g < NG; ++g) {
                 sixteen(g);
-                float part[4][4];                            // (word, parity) of the element: the order in which codes come out
 #pragma unroll
-                for (int n = 0; n < 4; ++n)
+                for (int w = 0; w < 2; ++w) {              // the order in which codes come out of a word
+                    uint32_t f[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) part[n][e] = v[(n >> 1) * 8 + 2 * e + (n & 1)] * up;
-#pragma unroll
-                for (int pl = 0; pl < PL; ++pl)
-                    s_q[((nt * NG + g) * PL + pl) * 32 + lane] = make_uint4(take_e4m3(part[0]), take_e4m3(part[1]), take_e4m3(part[2]), take_e4m3(part[3]));
+                    for (int n = 0; n < 4; ++n) {
+                        const float u = (n & 1) ? up * 0.0625f : up;
+                        f[n] = f16_pair(v[8 * w + n] * u, v[8 * w + n + 4] * u);
+                    }
+                    s_q[((nt * NG + g) * 2 + w) * 32 + lane] = make_uint4(f[0], f[1], f[2], f[3]);
+                }
             }
         }
         __syncthreads();
-        uint4 qf[QREG ? NT : 1][QREG ? NG : 1][QREG ? PL : 1];
+        uint4 qf[QREG ? NT : 1][QREG ? NG : 1][2];
         float fr[NT][2], qs[NT][2][NG], mb[NT][2], l[NT][2], om[NT][2][NG], o[NT][NG * 4][4];    // mb: minus the running maximum
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -430,7 +419,7 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
 #pragma unroll
                 for (int g = 0; g < NG; ++g)
 #pragma unroll
-                    for (int pl = 0; pl < PL; ++pl) qf[nt][g][pl] = s_q[((nt * NG + g) * PL + pl) * 32 + lane];
+                    for (int w = 0; w < 2; ++w) qf[nt][g][w] = s_q[((nt * NG + g) * 2 + w) * 32 + lane];
             }
         }
         const int pmin = s_pos[0], pmax = s_pos[ROWS - 1];
@@ -438,9 +427,13 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
         uint32_t unset = (1u << (2 * NT)) - 1;              // rows that have seen no token yet, a bit per (nt, column)
         float cs = 0x1p120f, ics = 0x1p-120f;               // the values' scales enter times this power of two; 1 / cs
 
+        // tiles [lo, hi) of the unit's list are seen whole by all rows; two of this warp's at once if the first is in [lo, hi - 4)
+        const int lo = p.window ? span.sinks + max(0, pmax - p.window + kKaTile) / kKaTile - span.first : 0;
+        const int hi = min(span.sinks + (pmin + 1) / kKaTile - span.first, c1 * kKaWarps);
         int slot = 0;
 #pragma unroll 1
         for (int i = 0; i < n_pairs; ++i) {
+            const int place = first + 2 * kKaWarps * i;
             copies_wait<S::kStages - 2>();
             __syncwarp();
             if (i + S::kStages - 1 < n_pairs) issue(i + S::kStages - 1, slot ? slot - 1 : S::kStages - 1);
@@ -465,25 +458,27 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
                     for (int u = 0; u < SUB; ++u) {
                         const uint32_t from = stage + u * S::kTileBytes + (get_k ^ (g << 5));
                         const uint2 w0 = lds64(from), w1 = lds64(from + 8 * RB);
-                        const uint32_t a[2][4] = {{w0.x & M8, w1.x & M8, (w0.x >> 4) & M8, (w1.x >> 4) & M8},
-                                                  {w0.y & M8, w1.y & M8, (w0.y >> 4) & M8, (w1.y >> 4) & M8}};
+                        float acc[NT][4];
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) {
+                            const uint32_t x0 = w ? w0.y : w0.x, x1 = w ? w1.y : w1.x, y0 = x0 >> 8, y1 = x1 >> 8;
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                uint4 q;
+                                if constexpr (QREG) q = qf[nt][g][w];
+                                else q = s_q[((nt * NG + g) * 2 + w) * 32 + lane];
+                                if (w == 0) mma_f16<true>(acc[nt], x0 & M0, x1 & M0, x0 & M1, x1 & M1, q.x, q.y);
+                                else mma_f16(acc[nt], x0 & M0, x1 & M0, x0 & M1, x1 & M1, q.x, q.y);
+                                mma_f16(acc[nt], y0 & M0, y1 & M0, y0 & M1, y1 & M1, q.z, q.w);
+                            }
+                        }
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            float acc[4];
-#pragma unroll
-                            for (int pl = 0; pl < PL; ++pl) {
-                                uint4 q;
-                                if constexpr (QREG) q = qf[nt][g][pl];
-                                else q = s_q[((nt * NG + g) * PL + pl) * 32 + lane];
-                                if (pl == 0) mma_e4m3<true>(acc, a[0], q.x, q.y);
-                                else mma_e4m3<false>(acc, a[0], q.x, q.y);
-                                mma_e4m3<false>(acc, a[1], q.z, q.w);
-                            }
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
                                 const int e = 2 * u + (c >> 1);
                                 float &d = dot[nt][4 * u + c], &t = sc[nt][4 * u + c];
-                                d = g ? fmaf(acc[c], scale_of(kp[e][g]), d) : acc[c] * scale_of(kp[e][g]);
+                                d = g ? fmaf(acc[nt][c], scale_of(kp[e][g]), d) : acc[nt][c] * scale_of(kp[e][g]);
                                 t = fmaf(minimum_of(kp[e][g]), qs[nt][c & 1][g], g ? t : mb[nt][c & 1]);
                             }
                         }
@@ -495,11 +490,11 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
                     for (int c = 0; c < 4 * SUB; ++c) sc[nt][c] = fmaf(dot[nt][c], fr[nt][c & 1], sc[nt][c]);
 
                 // masks, where a tile needs them
+                if (place + s2 * kKaWarps < lo || place + (s2 + SUB - 1) * kKaWarps >= hi) {
 #pragma unroll
-                for (int u = 0; u < SUB; ++u) {
-                    const int k = 2 * i + s2 + u;
-                    const int tt = k < n_tiles ? span.tile(first + k * kKaWarps) * kKaTile : INT_MAX - kKaTile;
-                    if (tt + kKaTile - 1 > pmin || (p.window && tt + kKaTile - 1 >= p.sinks && tt <= pmax - p.window)) {
+                    for (int u = 0; u < SUB; ++u) {
+                        const int k = 2 * i + s2 + u;
+                        const int tt = k < n_tiles ? span.tile(first + k * kKaWarps) * kKaTile : INT_MAX - kKaTile;
 #pragma unroll
                         for (int e = 2 * u; e < 2 * u + 2; ++e) {
                             const int t = tt + (e & 1) * 8 + my_token;
@@ -525,21 +520,16 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
                 }
 
                 const float cap = ics * kKaScaleCap;
-                bool raise = unset != 0;
+                float most = sc[0][0], sv = 0.f;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int c = 0; c < 4 * SUB; ++c) raise = raise || sc[nt][c] > kKaSlack;
+                    for (int c = 0; c < 4 * SUB; ++c) most = fmaxf(most, sc[nt][c]);
 #pragma unroll
                 for (int e = 0; e < 2 * SUB; ++e)
 #pragma unroll
-                    for (int g = 0; g < NG; ++g) raise = raise || scale_of(vp[e][g]) > cap;
-                if (__any_sync(0xffffffffu, raise)) {
-                    float sv = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 2 * SUB; ++e)
-#pragma unroll
-                        for (int g = 0; g < NG; ++g) sv = fmaxf(sv, scale_of(vp[e][g]));
+                    for (int g = 0; g < NG; ++g) sv = fmaxf(sv, scale_of(vp[e][g]));
+                if (__any_sync(0xffffffffu, unset != 0 || most > kKaSlack || sv > cap)) {
                     sv = across_max(sv);
                     float ratio = 1.f;
                     if (sv > cap) {                                    // >= 2^-117, a finite normal number: to between 2 and 4
@@ -640,6 +630,14 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
                 }
             }
         __syncthreads();
+        if (tid < ROWS) {
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < kKaWarps; ++w) top = fmaxf(top, s_m[w][tid]);
+#pragma unroll
+            for (int w = 0; w < kKaWarps; ++w) sum = fmaf(s_l[w][tid], s_m[w][tid] == -INFINITY ? 0.f : ex2_approx(s_m[w][tid] - top), sum);
+            s_ml[tid] = make_float2(top, sum);
+        }
         // [warp][row][D], pairs of a row in an order that goes by the row: what a warp stores at once lies in different banks
         float2* const red = reinterpret_cast<float2*>(ring_mem);
 #pragma unroll
@@ -670,15 +668,12 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
             constexpr int PER = D / 16;
             const int in_block = nt * 8 + (tid >> 4), d0 = (tid & 15) * PER, place = s_out[in_block];
             if (place < 0) continue;
-            float top = -INFINITY, sum = 0.f, v[PER];
-#pragma unroll
-            for (int w = 0; w < kKaWarps; ++w) top = fmaxf(top, s_m[w][in_block]);
+            const float2 ml = s_ml[in_block];
+            float v[PER];
 #pragma unroll
             for (int n = 0; n < PER; ++n) v[n] = 0.f;
 #pragma unroll
             for (int w = 0; w < kKaWarps; ++w) {
-                const float m = s_m[w][in_block];
-                sum = fmaf(s_l[w][in_block], m == -INFINITY ? 0.f : ex2_approx(m - top), sum);
                 const float2* from = red + (w * ROWS + in_block) * (D / 2) + d0 / 2;
 #pragma unroll
                 for (int n = 0; n < PER / 2; ++n) {
@@ -691,19 +686,19 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
             if (whole) {
                 const bool asked = s_ask[in_block];
                 const long long orow = (long long)b * p.seqs.Q * (p.cache.heads * p.group) + place;
-                float f = asked && sum != 0.f ? rcp_approx(sum) : 0.f;
+                float f = asked && ml.y != 0.f ? rcp_approx(ml.y) : 0.f;
                 if (asked && span.bad) f = NAN;
                 if (!asked) {
 #pragma unroll
                     for (int n = 0; n < PER; ++n) v[n] = 0.f;
                 }
                 ka_store<E, PER>(reinterpret_cast<E*>(p.out) + orow * D + d0, v, f);
-                if (p.lse && (tid & 15) == 0) p.lse[orow] = !asked ? -INFINITY : span.bad ? NAN : ka_lse(top, sum);
+                if (p.lse && (tid & 15) == 0) p.lse[orow] = !asked ? -INFINITY : span.bad ? NAN : ka_lse(ml.x, ml.y);
             } else {
                 float* to = p.part_o + (part * ROWS + in_block) * D + d0;
 #pragma unroll
                 for (int n = 0; n < PER; n += 4) *reinterpret_cast<float4*>(to + n) = make_float4(v[n], v[n + 1], v[n + 2], v[n + 3]);
-                if ((tid & 15) == 0) p.part_ml[part * ROWS + in_block] = make_float2(top, sum);
+                if ((tid & 15) == 0) p.part_ml[part * ROWS + in_block] = ml;
             }
         }
         if (tid == 0) {
@@ -732,24 +727,41 @@ __global__ void __launch_bounds__(kKaJoinRows * 32) ears_kv_join_kernel(const Ka
     if (row >= p.M) return;
     const int c0 = blockIdx.x, parts = cut.z - c0 + 1;
     auto place = [&](int n) { return ((long long)(c0 + n) * 2 + (n == 0)) * ROWS + in_block; };
-    float top = -INFINITY;
-    for (int n = lane; n < parts; n += 32) top = fmaxf(top, p.part_ml[place(n)].x);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    float v[PER], sum = 0.f;
+    // one look at the maxima and sums, a lane per part; results of up to eight parts on their way at once
+    float top = -INFINITY, sum = 0.f, v[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) v[i] = 0.f;
-#pragma unroll 4
-    for (int n = 0; n < parts; ++n) {
-        const float2 ml = p.part_ml[place(n)];
-        const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
-        const float* from = p.part_o + place(n) * D + lane * PER;
-        sum = fmaf(ml.y, f, sum);
+    for (int n0 = 0; n0 < parts; n0 += 32) {
+        const int count = min(32, parts - n0);
+        const float2 ml = lane < count ? p.part_ml[place(n0 + lane)] : make_float2(-INFINITY, 0.f);
+        float most = fmaxf(top, ml.x);
 #pragma unroll
-        for (int i = 0; i < PER; i += 2) {
-            const float2 w = *reinterpret_cast<const float2*>(from + i);
-            v[i] = fmaf(w.x, f, v[i]);
-            v[i + 1] = fmaf(w.y, f, v[i + 1]);
+        for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        const float before = top == -INFINITY ? 0.f : ex2_approx(top - most), f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - most);
+        top = most;
+        sum *= before;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] *= before;
+        float mine = ml.y * f;
+#pragma unroll
+        for (int d = 16; d; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+        sum += mine;
+        for (int m0 = 0; m0 < count; m0 += 8) {
+            float2 w[8][PER / 2];
+#pragma unroll
+            for (int m = 0; m < 8; ++m)
+#pragma unroll
+                for (int i = 0; i < PER / 2; ++i)
+                    w[m][i] = m0 + m < count ? __ldcg(reinterpret_cast<const float2*>(p.part_o + place(n0 + m0 + m) * D + lane * PER) + i) : make_float2(0.f, 0.f);
+#pragma unroll
+            for (int m = 0; m < 8; ++m) {
+                const float g = __shfl_sync(0xffffffffu, f, (m0 + m) & 31);
+#pragma unroll
+                for (int i = 0; i < PER / 2; ++i) {
+                    v[2 * i] = fmaf(w[m][i].x, g, v[2 * i]);
+                    v[2 * i + 1] = fmaf(w[m][i].y, g, v[2 * i + 1]);
+                }
+            }
         }
     }
     const bool asked = row / p.group < kv_count(p.seqs, b);
@@ -758,7 +770,7 @@ __global__ void __launch_bounds__(kKaJoinRows * 32) ears_kv_join_kernel(const Ka
         for (int i = 0; i < PER; ++i) v[i] = 0.f;
     }
     const long long orow = ka_out_row(p, b, h, row);
-    ka_store<E, PER>(reinterpret_cast<E*>(p.out) + orow * D + lane * PER, v, asked && sum != 0.f ? 1.f / sum : 0.f);
+    ka_store<E, PER>(reinterpret_cast<E*>(p.out) + orow * D + lane * PER, v, asked && sum != 0.f ? rcp_approx(sum) : 0.f);
     if (p.lse && lane == 0) p.lse[orow] = asked ? ka_lse(top, sum) : -INFINITY;
 }
 
