@@ -100,7 +100,7 @@ typedef void (*AttentionKernel)(const KaParams);
 struct Variant { AttentionKernel attention, join; size_t smem; int nt; };
 
 template <typename E, int D, int NT>
-Variant variant_of() { return Variant{ears_kv_attention_kernel<E, D, NT>, ears_kv_join_kernel<E, D, NT>, KaShape<D>::kSmem, NT}; }
+Variant variant_of() { return Variant{ears_kv_attention_kernel<E, D, NT>, ears_kv_join_kernel<E, D, NT>, KaShape<D, NT>::kSmem, NT}; }
 
 template <typename E, int D>
 Variant choose_tiles(int nt) {

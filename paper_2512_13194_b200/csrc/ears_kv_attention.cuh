@@ -29,33 +29,26 @@
 
 namespace ears {
 
-#ifndef KA_SUB
-#define KA_SUB 1
-#endif
-#ifndef KA_OCC2
-#define KA_OCC2 3
-#endif
-#ifndef KA_AHEAD
-#define KA_AHEAD 2
-#endif
-#ifndef KA_OCC
-#define KA_OCC 4
-#endif
 constexpr int kKaWarps = 4, kKaThreads = kKaWarps * 32;
 constexpr int kKaTile = 16;                         // tokens of a warp's tile
 constexpr int kKaChunk = kKaWarps * kKaTile;
+#ifndef KA_AHEAD
+#define KA_AHEAD 4
+#endif
 constexpr int kKaAhead = KA_AHEAD;                  // what starting and ending a unit costs, in chunks
 // The running maximum is raised when a score passes it by 2^12, and the values' scales enter times a power of two that keeps
 // them below 8: their product, a weight, stays below half precision's 2^16.
 constexpr float kKaSlack = 12.f, kKaScaleCap = 8.f;
 
-template <int D> struct KaShape {
+template <int D, int NT> struct KaShape {
     static constexpr int NG = D / kKvGroup;
     static constexpr int RB = D / 2;                // bytes of a token's codes
     static constexpr int kCodes = kKaTile * RB, kPars = kKaTile * NG * 4;
     static constexpr int kTileBytes = 2 * (kCodes + kPars);        // keys' codes, values' codes, keys' parameters, values' parameters
     static constexpr int kStage = 2 * kTileBytes;   // two tiles
-    static constexpr int kStages = D == 64 ? 5 : 3;
+    // CTAs per SM that registers allow, and as many stages as their shared memory does
+    static constexpr int kCtas = NT == 1 && D <= 128 ? 3 : 2;
+    static constexpr int kStages = D == 64 ? (kCtas == 3 ? 8 : 10) : D == 128 ? (kCtas == 3 ? 4 : 5) : 3;
     static constexpr int kSmem = kKaWarps * kStages * kStage;
     // 16-byte pieces of row i are kept in another order, so that what a warp loads at once lies in different banks
     __device__ static __forceinline__ int swizzle(int i) { return RB == 128 ? ((i & 1) << 2) | (i & 2) : RB == 64 ? (i & 2) : 0; }
@@ -149,6 +142,7 @@ template <int N> __device__ __forceinline__ void lds_words(uint32_t a, uint32_t 
         asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
     }
 }
+__device__ __forceinline__ float2 apart(f32x2 p) { float2 r; unpack2(p, r.x, r.y); return r; }
 __device__ __forceinline__ float scale_of(uint32_t par) { return __uint_as_float(par << 16); }
 __device__ __forceinline__ float minimum_of(uint32_t par) { return __uint_as_float(par & 0xffff0000u); }
 __device__ __forceinline__ uint32_t f16_pair(float lo, float hi) { return pack_pair<f16_t>(lo, hi); }
@@ -166,6 +160,16 @@ __device__ __forceinline__ float across_sum(float x) {
     x += __shfl_xor_sync(0xffffffffu, x, 4);
     x += __shfl_xor_sync(0xffffffffu, x, 8);
     return x + __shfl_xor_sync(0xffffffffu, x, 16);
+}
+
+__device__ __forceinline__ uint32_t raw_half(const uint16_t* p) { return __ldg(p); }
+__device__ __forceinline__ uint32_t raw_half(const f16_t* p) { return __ldg(&p->bits); }
+template <typename E>
+__device__ __noinline__ uint4 ka_unaligned(const E* p) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = raw_half(p + 2 * i) | raw_half(p + 2 * i + 1) << 16;
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // ---- a row's result ------------------------------------------------------------------------------------------
@@ -194,11 +198,11 @@ __device__ __forceinline__ float ka_lse(float m, float l) { return l == 0.f ? -I
 // E: the queries' type.  SPLIT: weights enter the second product in two halves (22 bits): one half-precision weight is off by
 // 2^-12 on average, which is nothing beside a bfloat16 result's 2^-9 but would be as much as a half-precision result's own rounding.
 template <typename E, int D, int NT>
-__global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT == 2 && D <= 128 ? KA_OCC2 : 2) ears_kv_attention_kernel(const KaParams p) {
-    using S = KaShape<D>;
+__global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_attention_kernel(const KaParams p) {
+    using S = KaShape<D, NT>;
     constexpr int NG = S::NG, RB = S::RB, ROWS = NT * 8;
     constexpr bool SPLIT = std::is_same<E, f16_t>::value;
-    constexpr int SUB = NT == 1 ? KA_SUB : 1;             // tiles taken together
+    constexpr int SUB = NT <= 2 ? 2 : 1;                             // tiles taken together
     constexpr bool QREG = NT * NG <= 4;                   // queries' operands stay in registers
     constexpr uint32_t M0 = 0x000f000fu, M1 = 0x00f000f0u;
 
@@ -206,11 +210,11 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
     // queries' operands; with NT = 1 in the stage of warp 1's ring that is filled last, until they are in registers
     constexpr bool QRING = NT == 1;
     static_assert(!QRING || (QREG && NG * 1024 <= S::kStage), "queries in a stage");
-    static_assert(8 * D * 2 <= S::kStage, "eight rows as they come");
     static_assert(kKaWarps * ROWS * D * 4 <= S::kSmem, "the warps' results meet in the ring's memory");
     __shared__ uint4 s_q_own[QRING ? 1 : NT * NG * 64];
     uint4* const s_q = QRING ? reinterpret_cast<uint4*>(ring_mem + (2 * S::kStages - 1) * S::kStage) : s_q_own;
-    __shared__ float s_fr[ROWS], s_qs[NG][ROWS], s_m[kKaWarps][ROWS], s_l[kKaWarps][ROWS];
+    __shared__ __align__(8) float s_fr[ROWS], s_qs[NG][ROWS];
+    __shared__ float s_m[kKaWarps][ROWS], s_l[kKaWarps][ROWS];
     __shared__ float2 s_ml[ROWS];
     __shared__ int s_pos[ROWS], s_out[ROWS], s_ask[ROWS], s_sum[kKaWarps], s_b, s_off;
 
@@ -325,22 +329,24 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
                 if (l16 == 0 && p.status) atomicOr(p.status, kDevInvalid);
             }
         };
-        // ---- queries, eight rows per warp: on their way while the page table is looked up, into its ring's last stage
-        static_assert(NT <= kKaWarps, "a block of rows per warp");
-        E* const raw = reinterpret_cast<E*>(ring_mem + ((warp + 1) * S::kStages - 1) * S::kStage);
-        const int q_row = row0 + warp * 8 + r, q_pos = q_row / p.group, q_head = h * p.group + (q_row - q_pos * p.group);
-        const bool q_real = q_row < p.M;
-        if (warp < NT) {
-            const E* src = reinterpret_cast<const E*>(p.q) + (q_real ? b * p.sb + q_pos * p.sq + q_head * p.sh : 0);
-            if (q_real && p.vec) {
+        // ---- queries, eight elements of a row per thread: on their way while the page table is looked up
+        constexpr int TPR = D / 8, RPP = kKaThreads / TPR, PASSES = (ROWS + RPP - 1) / RPP;
+        const int q_c = tid % TPR;
+        uint4 raw[PASSES];
+        int q_at[PASSES], q_pos[PASSES];                   // where the row's result goes, -1: no row; its position in the call
 #pragma unroll
-                for (int n = 0; n < D / 32; ++n) copy16(smem_u32(raw + r * D) + (4 * n + j) * 16, src + (4 * n + j) * 8);
-            } else {
-#pragma unroll 1
-                for (int n = j; n < D; n += 4) raw[r * D + n] = q_real ? ld_elem(src + n) : E();
+        for (int n = 0; n < PASSES; ++n) {
+            const int in_block = tid / TPR + n * RPP, row = row0 + in_block, i = row / p.group, head = h * p.group + (row - i * p.group);
+            const bool real = in_block < ROWS && row < p.M;
+            q_at[n] = real ? i * (p.cache.heads * p.group) + head : -1;
+            q_pos[n] = real ? i : (p.M - 1) / p.group;
+            raw[n] = make_uint4(0, 0, 0, 0);
+            if (real) {
+                const E* src = reinterpret_cast<const E*>(p.q) + b * p.sb + i * p.sq + head * p.sh + q_c * 8;
+                if (p.vec) raw[n] = __ldg(reinterpret_cast<const uint4*>(src));
+                else raw[n] = ka_unaligned(src);
             }
         }
-        copies_commit();
 #pragma unroll 1
         for (int i = 0; i < S::kStages - 1; ++i) {
             if (i < n_pairs) issue(i, i);
@@ -348,68 +354,55 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
         }
 
         // normalised to below 2^15 per row, in half precision, odd dimensions / 16
-        copies_wait<S::kStages - 1>();
-        __syncwarp();
-        if (warp < NT) {
-            const int nt = warp;
-            const uint4* mine = reinterpret_cast<const uint4*>(raw + r * D + j * 16);
-            float big = 0.f, v[16];
-            auto sixteen = [&](int g) {
-                const uint4 lo = mine[8 * g], hi = mine[8 * g + 1];
-                const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-                for (int n = 0; n < 8; ++n) {
-                    const float2 f = unpack_pair<E>(w[n]);
-                    v[2 * n] = f.x; v[2 * n + 1] = f.y;
-                }
-            };
-#pragma unroll 1
-            for (int g = 0; g < NG; ++g) {
-                sixteen(g);
-                float sum = 0.f;
+        for (int n = 0; n < PASSES; ++n) {
+            const int row = tid / TPR + n * RPP;
+            const uint32_t w[4] = {raw[n].x, raw[n].y, raw[n].z, raw[n].w};
+            float v[8], big = 0.f, sum = 0.f;
 #pragma unroll
-                for (int n = 0; n < 16; ++n) { sum += v[n]; big = max_nan(big, fabsf(v[n])); }
-                sum = quad_sum(sum) * p.scale2;
-                if (j == 0) s_qs[g][nt * 8 + r] = sum;
+            for (int e = 0; e < 4; ++e) {
+                const float2 f = unpack_pair<E>(w[e]);
+                v[2 * e] = f.x; v[2 * e + 1] = f.y;
+                sum += f.x + f.y;
+                big = max_nan(big, max_nan(fabsf(f.x), fabsf(f.y)));
             }
-            big = max_nan(big, __shfl_xor_sync(0xffffffffu, big, 1));
-            big = max_nan(big, __shfl_xor_sync(0xffffffffu, big, 2));
+#pragma unroll
+            for (int d = 1; d < TPR; d <<= 1) {
+                big = max_nan(big, __shfl_xor_sync(0xffffffffu, big, d));
+                if (d < 8) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            }
             const int ex = max((int)(__float_as_uint(big) >> 23) - 127, -100);
-            const float up = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
-            if (j == 0) {
-                // a code stands for c 2^-24, the row for q 2^(14 - ex)
-                s_fr[nt * 8 + r] = big <= FLT_MAX ? p.scale2 * 1024.f * __uint_as_float((uint32_t)(127 + ex) << 23) : NAN;
-                s_pos[nt * 8 + r] = min(last_pos, span.start + (q_real ? q_pos : (p.M - 1) / p.group));
-                s_out[nt * 8 + r] = q_real ? q_pos * p.cache.heads * p.group + q_head : -1;
-                s_ask[nt * 8 + r] = q_pos < span.count;
-            }
-#pragma unroll 1
-            for (int g = 0; g < NG; ++g) {
-                sixteen(g);
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {              // the order in which codes come out of a word
-                    uint32_t f[4];
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        const float u = (n & 1) ? up * 0.0625f : up;
-                        f[n] = f16_pair(v[8 * w + n] * u, v[8 * w + n + 4] * u);
-                    }
-                    s_q[((nt * NG + g) * 2 + w) * 32 + lane] = make_uint4(f[0], f[1], f[2], f[3]);
+            const float up = __uint_as_float((uint32_t)(127 + 14 - ex) << 23), odd = up * 0.0625f;
+            if (row < ROWS) {
+                if (q_c % 8 == 0) s_qs[q_c / 8][row] = sum * p.scale2;
+                if (q_c == 0) {
+                    // a code stands for c 2^-24, the row for q 2^(14 - ex)
+                    s_fr[row] = big <= FLT_MAX ? p.scale2 * 1024.f * __uint_as_float((uint32_t)(127 + ex) << 23) : NAN;
+                    s_pos[row] = min(last_pos, span.start + q_pos[n]);
+                    s_out[row] = q_at[n];
+                    s_ask[row] = q_pos[n] < span.count;
                 }
+                // the order in which codes come out of a word
+                s_q[(((row >> 3) * NG + q_c / 8) * 2 + (q_c & 1)) * 32 + (row & 7) * 4 + (q_c % 8) / 2] =
+                    make_uint4(f16_pair(v[0] * up, v[4] * up), f16_pair(v[1] * odd, v[5] * odd), f16_pair(v[2] * up, v[6] * up), f16_pair(v[3] * odd, v[7] * odd));
             }
         }
         __syncthreads();
         uint4 qf[QREG ? NT : 1][QREG ? NG : 1][2];
-        float fr[NT][2], qs[NT][2][NG], mb[NT][2], l[NT][2], om[NT][2][NG], o[NT][NG * 4][4];    // mb: minus the running maximum
+        float fr[QREG ? NT : 1][2], qs[QREG ? NT : 1][2][NG], mb[NT][2], l[NT][2], om[NT][2][NG], o[NT][NG * 4][4];    // mb: minus the running maximum
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int col = 0; col < 2; ++col) {
-                fr[nt][col] = s_fr[nt * 8 + 2 * j + col];
                 mb[nt][col] = 0.f;
                 l[nt][col] = 0.f;
 #pragma unroll
-                for (int g = 0; g < NG; ++g) { om[nt][col][g] = 0.f; qs[nt][col][g] = s_qs[g][nt * 8 + 2 * j + col]; }
+                for (int g = 0; g < NG; ++g) om[nt][col][g] = 0.f;
+                if constexpr (QREG) {
+                    fr[nt][col] = s_fr[nt * 8 + 2 * j + col];
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) qs[nt][col][g] = s_qs[g][nt * 8 + 2 * j + col];
+                }
             }
 #pragma unroll
             for (int n = 0; n < NG * 4; ++n)
@@ -430,71 +423,93 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
         // tiles [lo, hi) of the unit's list are seen whole by all rows; two of this warp's at once if the first is in [lo, hi - 4)
         const int lo = p.window ? span.sinks + max(0, pmax - p.window + kKaTile) / kKaTile - span.first : 0;
         const int hi = min(span.sinks + (pmin + 1) / kKaTile - span.first, c1 * kKaWarps);
-        int slot = 0;
-#pragma unroll 1
-        for (int i = 0; i < n_pairs; ++i) {
-            const int place = first + 2 * kKaWarps * i;
-            copies_wait<S::kStages - 2>();
-            __syncwarp();
-            if (i + S::kStages - 1 < n_pairs) issue(i + S::kStages - 1, slot ? slot - 1 : S::kStages - 1);
-            copies_commit();
-#pragma unroll 1
-            for (int s2 = 0; s2 < 2; s2 += SUB) {
-                if (SUB == 1 && 2 * i + s2 >= n_tiles) break;
-                const uint32_t stage = ring + slot * S::kStage + s2 * S::kTileBytes;
-
-                uint32_t kp[2 * SUB][NG], vp[2 * SUB][NG];
+        // Scores of the SUB tiles at `stage` relative to the running maximum, base 2, [nt][2 e + col] for token e of this thread's,
+        // and the tokens' parameters for the values.
+        auto scores = [&](uint32_t stage, float (&sc)[NT][4 * SUB], uint32_t (&vp)[2 * SUB][NG]) {
+            uint32_t kp[2 * SUB][NG];
+            f32x2 dot[NT][2 * SUB], part[NT][2 * SUB];
 #pragma unroll
-                for (int e = 0; e < 2 * SUB; ++e) {
-                    lds_words<NG>(stage + (e >> 1) * S::kTileBytes + get_p + (e & 1) * 8 * NG * 4, kp[e]);
-                    lds_words<NG>(stage + (e >> 1) * S::kTileBytes + get_p + S::kPars + (e & 1) * 8 * NG * 4, vp[e]);
+            for (int e = 0; e < 2 * SUB; ++e) {
+                lds_words<NG>(stage + (e >> 1) * S::kTileBytes + get_p + (e & 1) * 8 * NG * 4, kp[e]);
+                lds_words<NG>(stage + (e >> 1) * S::kTileBytes + get_p + S::kPars + (e & 1) * 8 * NG * 4, vp[e]);
+            }
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                uint2 kw[SUB][2];
+                float acc[SUB][NT][4];
+#pragma unroll
+                for (int u = 0; u < SUB; ++u) {
+                    const uint32_t from = stage + u * S::kTileBytes + (get_k ^ (g << 5));
+                    kw[u][0] = lds64(from);
+                    kw[u][1] = lds64(from + 8 * RB);
                 }
-
-                // scores relative to the running maximum, base 2: [nt][2 e + col], token e of this thread's
-                float sc[NT][4 * SUB], dot[NT][4 * SUB];
 #pragma unroll
-                for (int g = 0; g < NG; ++g) {
+                for (int w = 0; w < 2; ++w) {
+                    uint4 q[NT];
 #pragma unroll
-                    for (int u = 0; u < SUB; ++u) {
-                        const uint32_t from = stage + u * S::kTileBytes + (get_k ^ (g << 5));
-                        const uint2 w0 = lds64(from), w1 = lds64(from + 8 * RB);
-                        float acc[NT][4];
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if constexpr (QREG) q[nt] = qf[nt][g][w];
+                        else q[nt] = s_q[((nt * NG + g) * 2 + w) * 32 + lane];
+                    }
 #pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            const uint32_t x0 = w ? w0.y : w0.x, x1 = w ? w1.y : w1.x, y0 = x0 >> 8, y1 = x1 >> 8;
+                    for (int half = 0; half < 2; ++half)
+#pragma unroll
+                        for (int u = 0; u < SUB; ++u) {
+                            const uint32_t x0 = (w ? kw[u][0].y : kw[u][0].x) >> (8 * half), x1 = (w ? kw[u][1].y : kw[u][1].x) >> (8 * half);
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
-                                uint4 q;
-                                if constexpr (QREG) q = qf[nt][g][w];
-                                else q = s_q[((nt * NG + g) * 2 + w) * 32 + lane];
-                                if (w == 0) mma_f16<true>(acc[nt], x0 & M0, x1 & M0, x0 & M1, x1 & M1, q.x, q.y);
-                                else mma_f16(acc[nt], x0 & M0, x1 & M0, x0 & M1, x1 & M1, q.x, q.y);
-                                mma_f16(acc[nt], y0 & M0, y1 & M0, y0 & M1, y1 & M1, q.z, q.w);
+                                const uint32_t b0 = half ? q[nt].z : q[nt].x, b1 = half ? q[nt].w : q[nt].y;
+                                if (w == 0 && half == 0) mma_f16<true>(acc[u][nt], x0 & M0, x1 & M0, x0 & M1, x1 & M1, b0, b1);
+                                else mma_f16(acc[u][nt], x0 & M0, x1 & M0, x0 & M1, x1 & M1, b0, b1);
                             }
                         }
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                const int e = 2 * u + (c >> 1);
-                                float &d = dot[nt][4 * u + c], &t = sc[nt][4 * u + c];
-                                d = g ? fmaf(acc[nt][c], scale_of(kp[e][g]), d) : acc[nt][c] * scale_of(kp[e][g]);
-                                t = fmaf(minimum_of(kp[e][g]), qs[nt][c & 1][g], g ? t : mb[nt][c & 1]);
-                            }
-                        }
-                    }
                 }
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int nt = 0; nt < NT; ++nt) {
+                    f32x2 sums;
+                    if constexpr (QREG) sums = pack2(qs[nt][0][g], qs[nt][1][g]);
+                    else sums = *reinterpret_cast<const f32x2*>(&s_qs[g][nt * 8 + 2 * j]);
 #pragma unroll
-                    for (int c = 0; c < 4 * SUB; ++c) sc[nt][c] = fmaf(dot[nt][c], fr[nt][c & 1], sc[nt][c]);
-
+                    for (int e = 0; e < 2 * SUB; ++e) {
+                        const float sk = scale_of(kp[e][g]), mk = minimum_of(kp[e][g]);
+                        const f32x2 x = pack2(acc[e >> 1][nt][2 * (e & 1)], acc[e >> 1][nt][2 * (e & 1) + 1]);
+                        dot[nt][e] = g ? fma2(x, pack2(sk, sk), dot[nt][e]) : mul2(x, pack2(sk, sk));
+                        part[nt][e] = fma2(pack2(mk, mk), sums, g ? part[nt][e] : pack2(mb[nt][0], mb[nt][1]));
+                    }
+                }
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                f32x2 f;
+                if constexpr (QREG) f = pack2(fr[nt][0], fr[nt][1]);
+                else f = *reinterpret_cast<const f32x2*>(&s_fr[nt * 8 + 2 * j]);
+#pragma unroll
+                for (int e = 0; e < 2 * SUB; ++e) {
+                    const float2 x = apart(fma2(dot[nt][e], f, part[nt][e]));
+                    sc[nt][2 * e] = x.x;
+                    sc[nt][2 * e + 1] = x.y;
+                }
+            }
+        };
+        if (S::kStages - 1 < n_pairs) issue(S::kStages - 1, S::kStages - 1);
+        copies_commit();
+        float sc[NT][4 * SUB];
+        uint32_t vp[2 * SUB][NG], stage = ring;
+        int slot = 0;
+#pragma unroll 1
+        for (int k = 0; k < n_tiles; k += SUB) {
+            const int place = first + kKaWarps * k;
+            {
+                if (SUB == 2 || !(k & 1)) {
+                    copies_wait<S::kStages - 1>();
+                    __syncwarp();
+                }
+                scores(stage, sc, vp);
                 // masks, where a tile needs them
-                if (place + s2 * kKaWarps < lo || place + (s2 + SUB - 1) * kKaWarps >= hi) {
+                if (place < lo || place + (SUB - 1) * kKaWarps >= hi) {
 #pragma unroll
                     for (int u = 0; u < SUB; ++u) {
-                        const int k = 2 * i + s2 + u;
-                        const int tt = k < n_tiles ? span.tile(first + k * kKaWarps) * kKaTile : INT_MAX - kKaTile;
+                        const int tt = k + u < n_tiles ? span.tile(place + u * kKaWarps) * kKaTile : INT_MAX - kKaTile;
 #pragma unroll
                         for (int e = 2 * u; e < 2 * u + 2; ++e) {
                             const int t = tt + (e & 1) * 8 + my_token;
@@ -564,16 +579,22 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
                         }
                 }
 
+                f32x2 wt[NT][2 * SUB];
                 // weights
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int c = 0; c < 4 * SUB; ++c) {
-                        const float w = ex2_approx(sc[nt][c]);
-                        sc[nt][c] = w;
-                        l[nt][c & 1] += w;
+                    for (int e = 0; e < 2 * SUB; ++e) {
+                        const f32x2 w = pack2(ex2_approx(sc[nt][2 * e]), ex2_approx(sc[nt][2 * e + 1]));
+                        wt[nt][e] = w;
+                        const float2 sum = apart(add2(pack2(l[nt][0], l[nt][1]), w));
+                        l[nt][0] = sum.x; l[nt][1] = sum.y;
 #pragma unroll
-                        for (int g = 0; g < NG; ++g) om[nt][c & 1][g] = fmaf(w, minimum_of(vp[c >> 1][g]), om[nt][c & 1][g]);
+                        for (int g = 0; g < NG; ++g) {
+                            const float m = minimum_of(vp[e][g]);
+                            const float2 x = apart(fma2(w, pack2(m, m), pack2(om[nt][0][g], om[nt][1][g])));
+                            om[nt][0][g] = x.x; om[nt][1][g] = x.y;
+                        }
                     }
                 // values
 #pragma unroll
@@ -584,13 +605,12 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
                         uint32_t wf[NT][2], wl[SPLIT ? NT : 1][2];
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            const float* w = &sc[nt][4 * u];
-                            const float a = w[0] * s0, bq = w[1] * s0, c = w[2] * s1, d = w[3] * s1;
-                            const uint32_t x = f16_pair(a, bq), y = f16_pair(c, d);
+                            const float2 a = apart(mul2(wt[nt][2 * u], pack2(s0, s0))), c = apart(mul2(wt[nt][2 * u + 1], pack2(s1, s1)));
+                            const uint32_t x = f16_pair(a.x, a.y), y = f16_pair(c.x, c.y);
                             if constexpr (SPLIT) {
                                 const float2 fx = f16x2_to_float2(x), fy = f16x2_to_float2(y);
-                                wl[nt][0] = transpose_8x8(f16_pair(a - fx.x, bq - fx.y));
-                                wl[nt][1] = transpose_8x8(f16_pair(c - fy.x, d - fy.y));
+                                wl[nt][0] = transpose_8x8(f16_pair(a.x - fx.x, a.y - fx.y));
+                                wl[nt][1] = transpose_8x8(f16_pair(c.x - fy.x, c.y - fy.y));
                             }
                             wf[nt][0] = transpose_8x8(x);
                             wf[nt][1] = transpose_8x8(y);
@@ -611,8 +631,15 @@ __global__ void __launch_bounds__(kKaThreads, NT == 1 && D <= 128 ? KA_OCC : NT 
                             }
                         }
                     }
+                if (SUB == 2 || (k & 1)) {               // the stage is done with
+                    __syncwarp();
+                    const int i = k / 2 + S::kStages;
+                    if (i < n_pairs) issue(i, slot);
+                    copies_commit();
+                    slot = slot == S::kStages - 1 ? 0 : slot + 1;
+                }
+                stage = stage + SUB * S::kTileBytes == ring + S::kStages * S::kStage ? ring : stage + SUB * S::kTileBytes;
             }
-            slot = slot == S::kStages - 1 ? 0 : slot + 1;
         }
 
         // ---- the warps' results together
