@@ -51,23 +51,6 @@ __device__ __forceinline__ long long kv_row(const KvCache& c, const KvSeqs& s, i
 
 __device__ __forceinline__ float min_nan(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 
-// eight consecutive elements; `vec`: 16-byte aligned
-template <typename E> struct KvEight;
-template <> struct KvEight<float> {
-    __device__ static __forceinline__ void load(const float* p, bool vec, float (&x)[8]) {
-        if (vec) {
-            const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = __ldg(p + i);
-        }
-    }
-    __device__ static __forceinline__ void store(float* p, const float (&x)[8]) {
-        reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
-    }
-};
 template <typename E> __device__ __forceinline__ uint32_t pack_pair(float lo, float hi);
 template <> __device__ __forceinline__ uint32_t pack_pair<uint16_t>(float lo, float hi) {
     uint32_t r; asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo)); return r;
@@ -80,25 +63,77 @@ template <> __device__ __forceinline__ float2 unpack_pair<uint16_t>(uint32_t w) 
     return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
 template <> __device__ __forceinline__ float2 unpack_pair<f16_t>(uint32_t w) { return f16x2_to_float2(w); }
+template <typename E> __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b);
+template <> __device__ __forceinline__ uint32_t min2<uint16_t>(uint32_t a, uint32_t b) {
+    uint32_t r; asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r;
+}
+template <> __device__ __forceinline__ uint32_t min2<f16_t>(uint32_t a, uint32_t b) {
+    uint32_t r; asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r;
+}
+__device__ __forceinline__ uint32_t half_bits(const uint16_t* p) { return __ldg(p); }
+__device__ __forceinline__ uint32_t half_bits(const f16_t* p) { return __ldg(&p->bits); }
+// Eight consecutive elements as they lie (`vec`: 16-byte aligned), their values, and their smallest and largest, NaN if there is one.
 template <typename E> struct KvEight {
-    __device__ static __forceinline__ void load(const E* p, bool vec, float (&x)[8]) {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const E* p, bool vec) {
         if (vec) {
-            const uint4 w = __ldg(reinterpret_cast<const uint4*>(p));
-            const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = unpack_pair<E>(v[i]);
-                x[2 * i] = f.x; x[2 * i + 1] = f.y;
-            }
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = load_logit(p + i);
+            for (int i = 0; i < 4; ++i) w[i] = half_bits(p + 2 * i) | half_bits(p + 2 * i + 1) << 16;
         }
     }
-    __device__ static __forceinline__ void store(E* p, const float (&x)[8]) {
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack_pair<E>(x[0], x[1]), pack_pair<E>(x[2], x[3]), pack_pair<E>(x[4], x[5]), pack_pair<E>(x[6], x[7]));
+    __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = 0; }
+    __device__ __forceinline__ float2 pair(int i) const { return unpack_pair<E>(w[i]); }
+    // over the eight lanes of a group: (smallest, minus the largest) travel together, exact in the elements' type
+    __device__ __forceinline__ float2 range() const {
+        const uint32_t lo = min2<E>(min2<E>(w[0], w[1]), min2<E>(w[2], w[3]));
+        const uint32_t hi = min2<E>(min2<E>(w[0] ^ 0x80008000u, w[1] ^ 0x80008000u), min2<E>(w[2] ^ 0x80008000u, w[3] ^ 0x80008000u));
+        uint32_t r = min2<E>(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
+#pragma unroll
+        for (int e = 4; e; e >>= 1) r = min2<E>(r, __shfl_xor_sync(0xffffffffu, r, e));
+        const float2 f = unpack_pair<E>(r);
+        return make_float2(f.x, -f.y);
     }
 };
+template <> struct KvEight<float> {
+    float x[8];
+    __device__ __forceinline__ void load(const float* p, bool vec) {
+        if (vec) {
+            const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __ldg(p + i);
+        }
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 0.f;
+    }
+    __device__ __forceinline__ float2 pair(int i) const { return make_float2(x[2 * i], x[2 * i + 1]); }
+    __device__ __forceinline__ float2 range() const {
+        float lo = x[0], hi = x[0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) { lo = min_nan(lo, x[j]); hi = max_nan(hi, x[j]); }
+#pragma unroll
+        for (int e = 4; e; e >>= 1) {
+            lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, e));
+            hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, e));
+        }
+        return make_float2(lo, hi);
+    }
+};
+// 16 bytes; the results are not read again here
+__device__ __forceinline__ void kv_store(float* p, const float (&x)[4]) { __stcs(reinterpret_cast<float4*>(p), make_float4(x[0], x[1], x[2], x[3])); }
+template <typename E>
+__device__ __forceinline__ void kv_store(E* p, const float (&x)[8]) {
+    __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack_pair<E>(x[0], x[1]), pack_pair<E>(x[2], x[3]), pack_pair<E>(x[4], x[5]), pack_pair<E>(x[6], x[7])));
+}
+
+__device__ __forceinline__ uint2 halves_of(f32x2 v) { uint2 r; asm("mov.b64 {%0, %1}, %2;" : "=r"(r.x), "=r"(r.y) : "l"(v)); return r; }
+__device__ __forceinline__ f32x2 add2_down(f32x2 a, f32x2 b) { f32x2 r; asm("add.rm.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 
 // ---- write ------------------------------------------------------------------------------------------
 struct KvWriteParams {
@@ -110,72 +145,91 @@ struct KvWriteParams {
     int32_t* status;
 };
 
-constexpr int kKvThreads = 256;
-constexpr int kKvTeams = kKvThreads / 8;  // eight threads have a group of 64, eight values each
+// Warps have a position's keys and values of all heads, eight consecutive values per lane and step: a group is eight lanes, a
+// position's place is looked up once, and what a warp loads or stores at once is contiguous.  `parts` warps share a position
+// where there are few of them.
+constexpr int kKvThreads = 128;
+constexpr int kKvUnroll = 4;              // steps whose loads are on their way together
+
+struct KvPlace {
+    long long row;                        // of the position's keys in head 0; -1: no place
+    int b, i, part;
+    bool mine;                            // the position is asked for
+};
+__device__ __forceinline__ KvPlace kv_place(const KvCache& c, const KvSeqs& s, int parts, int32_t* status) {
+    const unsigned warp = (blockIdx.x * kKvThreads + threadIdx.x) / 32, at = warp / (unsigned)parts;
+    KvPlace p;
+    p.part = (int)(warp - at * parts);
+    p.b = (int)(at / (unsigned)s.Q);
+    p.i = (int)(at - (unsigned)p.b * s.Q);
+    p.row = -1;
+    p.mine = p.b < s.B && p.i < kv_count(s, p.b);
+    if (p.mine) {
+        p.row = kv_row(c, s, p.b, (long long)__ldg(s.start + p.b) + p.i);
+        if (p.row < 0 && p.part == 0 && threadIdx.x % 32 == 0 && status) atomicOr(status, kDevInvalid);
+    }
+    return p;
+}
 
 template <typename E, int D>
-__global__ void __launch_bounds__(kKvThreads) ears_kv_write_kernel(const KvWriteParams p) {
-    constexpr int NG = D / kKvGroup;
+__global__ void __launch_bounds__(kKvThreads) ears_kv_write_kernel(const KvWriteParams p, int parts) {
+    constexpr int NG = D / kKvGroup, PER = D / 8, HEADS = 32 / PER;      // lanes per head, heads per step
     wait_for_stream();
-    const int lane = threadIdx.x & 7;
-    const unsigned per_kind = (unsigned)p.cache.heads * NG, per_row = 2 * per_kind;
-    const unsigned items = (unsigned)p.seqs.B * p.seqs.Q * per_row;
-    const unsigned item = blockIdx.x * kKvTeams + threadIdx.x / 8;
-    const unsigned row = min(item, items - 1) / per_row, in_row = min(item, items - 1) - row * per_row;
-    const int b = (int)(row / (unsigned)p.seqs.Q), i = (int)(row - (unsigned)b * p.seqs.Q);
-    const int kind = in_row >= per_kind;
-    const unsigned hg = in_row - kind * per_kind;
-    const int h = (int)(hg / NG), g = (int)(hg % NG);
-    const bool mine = item < items && i < kv_count(p.seqs, b);
-
-    float x[8];
-    long long at = -1;
-    if (mine) {
-        KvEight<E>::load(reinterpret_cast<const E*>(kind ? p.x[1] : p.x[0]) + b * (kind ? p.sb[1] : p.sb[0]) + i * (kind ? p.sq[1] : p.sq[0]) +
-                             h * (kind ? p.sh[1] : p.sh[0]) + g * kKvGroup + lane * 8,
-                         kind ? p.vec[1] : p.vec[0], x);
-        at = kv_row(p.cache, p.seqs, b, (long long)__ldg(p.seqs.start + b) + i);
-        if (at < 0 && lane == 0 && p.status) atomicOr(p.status, kDevInvalid);
-    } else {
+    const int lane = threadIdx.x & 31, d = lane % PER;
+    const KvPlace at = kv_place(p.cache, p.seqs, parts, p.status);
+    if (!at.mine) return;                                  // the whole warp; the place is waited for behind the first loads
+    const int per_kind = (p.cache.heads + HEADS - 1) / HEADS, steps = 2 * per_kind;
+    const E* const keys = reinterpret_cast<const E*>(p.x[0]) + at.b * p.sb[0] + at.i * p.sq[0] + d * 8;
+    const E* const values = reinterpret_cast<const E*>(p.x[1]) + at.b * p.sb[1] + at.i * p.sq[1] + d * 8;
+#pragma unroll 1
+    for (int s0 = at.part; s0 < steps; s0 += parts * kKvUnroll) {
+        KvEight<E> x[kKvUnroll];
+        int rows[kKvUnroll];                               // kind x heads + head, -1: none
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = 0.f;
-    }
-    float lo = x[0], hi = x[0];
+        for (int u = 0; u < kKvUnroll; ++u) {
+            const int st = s0 + u * parts, kind = st >= per_kind, h = (st - kind * per_kind) * HEADS + lane / PER;
+            rows[u] = st < steps && h < p.cache.heads ? kind * p.cache.heads + h : -1;
+            if (rows[u] >= 0) x[u].load(kind ? values + h * p.sh[1] : keys + h * p.sh[0], kind ? p.vec[1] : p.vec[0]);
+            else x[u].clear();
+        }
 #pragma unroll
-    for (int j = 1; j < 8; ++j) { lo = min_nan(lo, x[j]); hi = max_nan(hi, x[j]); }
+        for (int u = 0; u < kKvUnroll; ++u) {
+            if (s0 + u * parts >= steps) break;            // the whole warp
+            const float2 ends = x[u].range();
+            const float lo = ends.x, hi = ends.y;
+            const uint32_t mb = __float_as_uint(lo);
+            uint32_t cut = mb & 0xffff0000u;
+            if ((int)mb < 0 && mb != cut) cut += 0x10000u;
+            const float m = __uint_as_float(cut);
+            const float range = __fmul_rn(__fsub_rn(hi, m), 1.f / 15.f);
+            const bool fine = range <= FLT_MAX;            // false for NaN too
+            uint32_t sbits = __float_as_uint(range);
+            if (sbits & 0xffffu) sbits = (sbits & 0xffff0000u) + 0x10000u;
+            const float s = fmaxf(__uint_as_float(sbits), 0x1p-126f);
+            // k: floor of an approximate quotient, in the low bits of 2^23 + q rounded down.  The border s (k + 1/2) has 13 bits and
+            // is exact, so that the comparison decides as the exact quotient would, also where the floor is one off beside a whole
+            // number; a tie goes to the even code.  t >= 0 and the border are compared as integers.  The 2^23s add up to kOffset.
+            constexpr uint32_t kOffset = 0x4b000000u * 0x11111111u;
+            const float r = __frcp_rn(s), half = 0.5f * s;
+            const f32x2 m2 = pack2(-m, -m), r2 = pack2(r, r), s2 = pack2(s, s), h2 = pack2(half, half), big = pack2(8388608.f, 8388608.f),
+                        less = pack2(-8388608.f, -8388608.f);
+            uint32_t word = 0;
 #pragma unroll
-    for (int d = 4; d; d >>= 1) {
-        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, d));
-    }
-    uint32_t mb = __float_as_uint(lo), cut = mb & 0xffff0000u;
-    if ((int)mb < 0 && mb != cut) cut += 0x10000u;
-    const float m = __uint_as_float(cut);
-    const float range = __fmul_rn(__fsub_rn(hi, m), 1.f / 15.f);
-    const bool fine = range <= FLT_MAX;               // false for NaN too
-    uint32_t sbits = __float_as_uint(range);
-    if (sbits & 0xffffu) sbits = (sbits & 0xffff0000u) + 0x10000u;
-    float s = __uint_as_float(sbits);
-    s = fmaxf(s, 0x1p-126f);
-    uint32_t word = 0, par = 0x7fc07fc0u;
-    if (fine) {
-        par = (__float_as_uint(s) >> 16) | (__float_as_uint(m) & 0xffff0000u);
-        const float r = 1.f / s;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            // floor of an approximate quotient; the border s (k + 1/2) has 13 bits and is exact, so that the comparison
-            // decides as the exact quotient would, also where the floor is one off beside a whole number
-            const float t = __fsub_rn(x[j], m);
-            const float k = floorf(t * r), border = s * (k + 0.5f);
-            int c = (int)k;
-            c += t > border || (t == border && (c & 1));
-            word |= (uint32_t)min(max(c, 0), 15) << (4 * j);
+            for (int j = 0; j < 4; ++j) {
+                const float2 v = x[u].pair(j);
+                const f32x2 t = add2(pack2(v.x, v.y), m2), q = add2_down(mul2(t, r2), big), border = fma2(s2, add2(q, less), h2);
+                const uint2 tb = halves_of(t), qb = halves_of(q), bb = halves_of(border);
+                word += (qb.x + ((bb.x - tb.x - (qb.x & 1u)) >> 31)) << (8 * j);
+                word += (qb.y + ((bb.y - tb.y - (qb.y & 1u)) >> 31)) << (8 * j + 4);
+            }
+            word -= kOffset;
+            if (rows[u] >= 0 && at.row >= 0) {
+                const long long to = at.row + (long long)rows[u] * p.cache.page;
+                *reinterpret_cast<uint32_t*>(p.cache.codes + to * (D / 2) + d * 4) = fine ? word : 0u;
+                if (lane % 8 == 0) p.cache.params[to * NG + d / 8] = fine ? (__float_as_uint(s) >> 16) | (__float_as_uint(m) & 0xffff0000u) : 0x7fc07fc0u;
+            }
         }
     }
-    if (at < 0) return;
-    const long long to = at + ((long long)kind * p.cache.heads + h) * p.cache.page;
-    *reinterpret_cast<uint32_t*>(p.cache.codes + to * (D / 2) + g * (kKvGroup / 2) + lane * 4) = word;
-    if (lane == 0) p.cache.params[to * NG + g] = par;
 }
 
 // ---- read -------------------------------------------------------------------------------------------
@@ -187,38 +241,51 @@ struct KvReadParams {
 };
 
 template <typename E, int D>
-__global__ void __launch_bounds__(kKvThreads) ears_kv_read_kernel(const KvReadParams p) {
-    constexpr int NG = D / kKvGroup;
+__global__ void __launch_bounds__(kKvThreads) ears_kv_read_kernel(const KvReadParams p, int parts) {
+    constexpr int N = sizeof(E) == 4 ? 4 : 8;              // values per lane and step: 16 bytes of the result
+    constexpr int NG = D / kKvGroup, PER = D / N, WARPS = PER > 32 ? PER / 32 : 1, HEADS = PER > 32 ? 1 : 32 / PER;   // steps per head, or heads per step
     wait_for_stream();
-    const int lane = threadIdx.x & 7;
-    const unsigned per_kind = (unsigned)p.cache.heads * NG, per_row = 2 * per_kind;
-    const unsigned items = (unsigned)p.seqs.B * p.seqs.Q * per_row;
-    const unsigned item = blockIdx.x * kKvTeams + threadIdx.x / 8;
-    if (item >= items) return;
-    const unsigned row = item / per_row, in_row = item - row * per_row;
-    const int b = (int)(row / (unsigned)p.seqs.Q), i = (int)(row - (unsigned)b * p.seqs.Q);
-    const int kind = in_row >= per_kind;
-    const unsigned hg = in_row - kind * per_kind;
-    const int h = (int)(hg / NG), g = (int)(hg % NG);
-    float x[8];
-    if (i < kv_count(p.seqs, b)) {
-        const long long at = kv_row(p.cache, p.seqs, b, (long long)__ldg(p.seqs.start + b) + i);
-        uint32_t word = 0, par = 0x7fc07fc0u;
-        if (at >= 0) {
-            const long long from = at + ((long long)kind * p.cache.heads + h) * p.cache.page;
-            word = *reinterpret_cast<const uint32_t*>(p.cache.codes + from * (D / 2) + g * (kKvGroup / 2) + lane * 4);
-            par = p.cache.params[from * NG + g];
-        } else if (lane == 0 && p.status) {
-            atomicOr(p.status, kDevInvalid);
+    const int lane = threadIdx.x & 31;
+    const KvPlace at = kv_place(p.cache, p.seqs, parts, p.status);
+    if (at.b >= p.seqs.B) return;
+    const int per_kind = (p.cache.heads + HEADS - 1) / HEADS * WARPS, steps = 2 * per_kind;
+    const long long out = ((long long)at.b * p.seqs.Q + at.i) * p.cache.heads * D;
+    const uint32_t none = at.mine ? 0x7fc07fc0u : 0u;      // without a place: NaN where asked for, zeros where not
+#pragma unroll 1
+    for (int s0 = at.part; s0 < steps; s0 += parts * kKvUnroll) {
+        uint32_t word[kKvUnroll], par[kKvUnroll];
+        int place[kKvUnroll];                              // of the first value in the position's result, -1: none
+#pragma unroll
+        for (int u = 0; u < kKvUnroll; ++u) {
+            const int st = s0 + u * parts, kind = st >= per_kind, in = st - kind * per_kind;
+            const int h = in / WARPS * HEADS + (HEADS > 1 ? lane / PER : 0), d = (in % WARPS * 32 + lane) % PER * N;
+            place[u] = st < steps && h < p.cache.heads ? h * D + d : -1;
+            word[u] = 0;
+            par[u] = none;
+            if (place[u] >= 0 && at.row >= 0) {
+                const long long from = at.row + (long long)(kind * p.cache.heads + h) * p.cache.page;
+                const uint8_t* codes = p.cache.codes + from * (D / 2) + d / 2;
+                word[u] = N == 8 ? *reinterpret_cast<const uint32_t*>(codes) : *reinterpret_cast<const uint16_t*>(codes);
+                par[u] = p.cache.params[from * NG + d / kKvGroup];
+            }
         }
-        const float s = __uint_as_float(par << 16), m = __uint_as_float(par & 0xffff0000u);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = __fmaf_rn(s, (float)((word >> (4 * j)) & 15u), m);
-    } else {
+        for (int u = 0; u < kKvUnroll; ++u) {
+            if (place[u] < 0) continue;
+            const int kind = s0 + u * parts >= per_kind;
+            const float s = __uint_as_float(par[u] << 16), m = __uint_as_float(par[u] & 0xffff0000u);
+            const f32x2 s2 = pack2(s, s), m2 = pack2(m, m), less = pack2(-8388608.f, -8388608.f);
+            const uint32_t even = word[u] & 0x0f0f0f0fu, odd = (word[u] >> 4) & 0x0f0f0f0fu;
+            float x[N];
+            // a code in the low byte of 2^23's bits is 2^23 + c
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = 0.f;
+            for (int j = 0; j < N / 2; ++j) {
+                const f32x2 c2 = add2(pack2(__uint_as_float(__byte_perm(even, 0x4b000000u, 0x7440 + j)), __uint_as_float(__byte_perm(odd, 0x4b000000u, 0x7440 + j))), less);
+                unpack2(fma2(s2, c2, m2), x[2 * j], x[2 * j + 1]);
+            }
+            kv_store(reinterpret_cast<E*>(kind ? p.out[1] : p.out[0]) + out + place[u], x);
+        }
     }
-    KvEight<E>::store(reinterpret_cast<E*>(kind ? p.out[1] : p.out[0]) + ((long long)row * per_kind + hg) * kKvGroup + lane * 8, x);
 }
 
 }  // namespace ears

@@ -38,8 +38,8 @@ int check_seqs(const ears_kv_cache* c, const KvSeqs& s) {
     if (s.B < 1 || s.Q < 1 || s.width < 1 || s.stride < 0) return EARS_ERR_SHAPE;
     if ((long long)s.width * c->page_size > INT_MAX) return EARS_ERR_SHAPE;
     if ((long double)(s.B - 1) * s.stride + s.width > 1.0e18L) return EARS_ERR_SHAPE;
-    // a thread team per group of a call
-    if ((long double)s.B * s.Q * 2 * c->heads * (c->head_dim / kKvGroup) > (long double)INT_MAX) return EARS_ERR_SHAPE;
+    // eights of a call's elements, counted in 31 bits
+    if ((long double)s.B * s.Q * 2 * c->heads * (c->head_dim / 8) > (long double)INT_MAX) return EARS_ERR_SHAPE;
     if (misaligned(s.table, 4) || misaligned(s.start, 4) || misaligned(s.counts, 4)) return EARS_ERR_ALIGN;
     return EARS_OK;
 }
@@ -69,8 +69,8 @@ int with_type(int dtype, F&& f) {
     return f((uint16_t*)nullptr);
 }
 
-template <typename P>
-int launch(void (*kernel)(P), const P& p, dim3 grid, int threads, size_t smem, void* stream, const char* what) {
+template <typename P, typename... Extra>
+int launch(void (*kernel)(P, Extra...), const std::decay_t<P>& p, dim3 grid, int threads, size_t smem, void* stream, const char* what, Extra... extra) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads, 1, 1);
@@ -81,15 +81,24 @@ int launch(void (*kernel)(P), const P& p, dim3 grid, int threads, size_t smem, v
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p, extra...);
     if (e == cudaSuccess) return EARS_OK;
     (void)cudaGetLastError();
     return host_cuda_fail(e, what);
 }
 
-unsigned teams(const KvSeqs& s, const ears_kv_cache* c) {
-    const long long items = (long long)s.B * s.Q * 2 * c->heads * (c->head_dim / kKvGroup);
-    return (unsigned)((items + kKvTeams - 1) / kKvTeams);
+// Warps per position of a write or a read, and the grid: fewer positions than a few per SM are shared by up to a warp per step.
+int share_positions(const KvSeqs& s, const ears_kv_cache* c, int values, int* parts, unsigned* grid) {
+    int sms = 0;
+    const int rc = host_device_sms(&sms);
+    if (rc) return rc;
+    const long long positions = (long long)s.B * s.Q;
+    const int lanes = c->head_dim / values, steps = 2 * (lanes > 32 ? c->heads * (lanes / 32) : (c->heads + 32 / lanes - 1) / (32 / lanes));
+    int n = 1;
+    while (n * 2 <= steps && positions * n < 16ll * sms) n *= 2;
+    *parts = n;
+    *grid = (unsigned)((positions * n + kKvThreads / 32 - 1) / (kKvThreads / 32));
+    return EARS_OK;
 }
 
 // ---- attention: variant and grid
@@ -207,10 +216,13 @@ int ears_kv_write(int dtype, const ears_kv_cache* cache, const void* k, const vo
     p.vec[0] = vectors(k, es, B, Q, cache->heads, k_stride_b, k_stride_q, k_stride_h);
     p.vec[1] = vectors(v, es, B, Q, cache->heads, v_stride_b, v_stride_q, v_stride_h);
     p.status = status;
+    int parts = 1;
+    unsigned grid = 1;
+    EARS_TRY(share_positions(p.seqs, cache, 8, &parts, &grid));
     return with_dim(cache->head_dim, [&](auto d) {
         return with_type(dtype, [&](auto* e) {
-            return launch(ears_kv_write_kernel<std::remove_pointer_t<decltype(e)>, decltype(d)::value>, p, dim3(teams(p.seqs, cache)),
-                          kKvThreads, 0, stream, "ears_kv_write_kernel launch");
+            return launch(ears_kv_write_kernel<std::remove_pointer_t<decltype(e)>, decltype(d)::value>, p, dim3(grid), kKvThreads, 0, stream,
+                          "ears_kv_write_kernel launch", parts);
         });
     });
 }
@@ -227,10 +239,13 @@ int ears_kv_read(int dtype, const ears_kv_cache* cache, int B, int Q, const int3
     if (misaligned(out_k, 16) || misaligned(out_v, 16) || misaligned(status, 4)) return EARS_ERR_ALIGN;
     p.out[0] = out_k; p.out[1] = out_v;
     p.status = status;
+    int parts = 1;
+    unsigned grid = 1;
+    EARS_TRY(share_positions(p.seqs, cache, dtype == EARS_DTYPE_F32 ? 4 : 8, &parts, &grid));
     return with_dim(cache->head_dim, [&](auto d) {
         return with_type(dtype, [&](auto* e) {
-            return launch(ears_kv_read_kernel<std::remove_pointer_t<decltype(e)>, decltype(d)::value>, p, dim3(teams(p.seqs, cache)),
-                          kKvThreads, 0, stream, "ears_kv_read_kernel launch");
+            return launch(ears_kv_read_kernel<std::remove_pointer_t<decltype(e)>, decltype(d)::value>, p, dim3(grid), kKvThreads, 0, stream,
+                          "ears_kv_read_kernel launch", parts);
         });
     });
 }

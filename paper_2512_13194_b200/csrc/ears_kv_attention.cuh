@@ -32,10 +32,7 @@ namespace ears {
 constexpr int kKaWarps = 4, kKaThreads = kKaWarps * 32;
 constexpr int kKaTile = 16;                         // tokens of a warp's tile
 constexpr int kKaChunk = kKaWarps * kKaTile;
-#ifndef KA_AHEAD
-#define KA_AHEAD 4
-#endif
-constexpr int kKaAhead = KA_AHEAD;                  // what starting and ending a unit costs, in chunks
+constexpr int kKaAhead = 8;                  // what starting and ending a unit costs, in chunks
 // The running maximum is raised when a score passes it by 2^12, and the values' scales enter times a power of two that keeps
 // them below 8: their product, a weight, stays below half precision's 2^16.
 constexpr float kKaSlack = 12.f, kKaScaleCap = 8.f;
@@ -162,13 +159,11 @@ __device__ __forceinline__ float across_sum(float x) {
     return x + __shfl_xor_sync(0xffffffffu, x, 16);
 }
 
-__device__ __forceinline__ uint32_t raw_half(const uint16_t* p) { return __ldg(p); }
-__device__ __forceinline__ uint32_t raw_half(const f16_t* p) { return __ldg(&p->bits); }
 template <typename E>
 __device__ __noinline__ uint4 ka_unaligned(const E* p) {
     uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = raw_half(p + 2 * i) | raw_half(p + 2 * i + 1) << 16;
+    for (int i = 0; i < 4; ++i) w[i] = half_bits(p + 2 * i) | half_bits(p + 2 * i + 1) << 16;
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
