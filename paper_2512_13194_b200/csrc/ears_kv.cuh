@@ -24,7 +24,7 @@ constexpr int kDevInvalid = 1;            // EARS_DEV_INVALID_INPUT
 struct KvCache {
     uint8_t* codes;
     uint32_t* params;
-    int pages, heads, page;               // pages in the pool, heads, tokens per page
+    int pages, heads, page;               // pages in the pool, heads, tokens per page; a page has less than 2^31 bytes (the host's check)
 };
 
 // Where the sequences of a call stand: position i of sequence b is its token start[b] + i, for i < counts[b].
@@ -132,6 +132,7 @@ __device__ __forceinline__ void kv_store(E* p, const float (&x)[8]) {
     __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack_pair<E>(x[0], x[1]), pack_pair<E>(x[2], x[3]), pack_pair<E>(x[4], x[5]), pack_pair<E>(x[6], x[7])));
 }
 
+__device__ __forceinline__ float rcp_approx(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ uint2 halves_of(f32x2 v) { uint2 r; asm("mov.b64 {%0, %1}, %2;" : "=r"(r.x), "=r"(r.y) : "l"(v)); return r; }
 __device__ __forceinline__ f32x2 add2_down(f32x2 a, f32x2 b) { f32x2 r; asm("add.rm.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 
@@ -181,14 +182,16 @@ __global__ void __launch_bounds__(kKvThreads) ears_kv_write_kernel(const KvWrite
     const int per_kind = (p.cache.heads + HEADS - 1) / HEADS, steps = 2 * per_kind;
     const E* const keys = reinterpret_cast<const E*>(p.x[0]) + at.b * p.sb[0] + at.i * p.sq[0] + d * 8;
     const E* const values = reinterpret_cast<const E*>(p.x[1]) + at.b * p.sb[1] + at.i * p.sq[1] + d * 8;
+    uint8_t* const codes = p.cache.codes + at.row * (D / 2) + d * 4;
+    uint32_t* const params = p.cache.params + at.row * NG + d / 8;
 #pragma unroll 1
     for (int s0 = at.part; s0 < steps; s0 += parts * kKvUnroll) {
         KvEight<E> x[kKvUnroll];
-        int rows[kKvUnroll];                               // kind x heads + head, -1: none
+        int rows[kKvUnroll];                               // first token of (kind, head) in a page, -1: none
 #pragma unroll
         for (int u = 0; u < kKvUnroll; ++u) {
             const int st = s0 + u * parts, kind = st >= per_kind, h = (st - kind * per_kind) * HEADS + lane / PER;
-            rows[u] = st < steps && h < p.cache.heads ? kind * p.cache.heads + h : -1;
+            rows[u] = st < steps && h < p.cache.heads ? (kind * p.cache.heads + h) * p.cache.page : -1;
             if (rows[u] >= 0) x[u].load(kind ? values + h * p.sh[1] : keys + h * p.sh[0], kind ? p.vec[1] : p.vec[0]);
             else x[u].clear();
         }
@@ -210,7 +213,7 @@ __global__ void __launch_bounds__(kKvThreads) ears_kv_write_kernel(const KvWrite
             // is exact, so that the comparison decides as the exact quotient would, also where the floor is one off beside a whole
             // number; a tie goes to the even code.  t >= 0 and the border are compared as integers.  The 2^23s add up to kOffset.
             constexpr uint32_t kOffset = 0x4b000000u * 0x11111111u;
-            const float r = __frcp_rn(s), half = 0.5f * s;
+            const float r = rcp_approx(s), half = 0.5f * s;      // s in [2^-126, 2^126): so is 1 / s
             const f32x2 m2 = pack2(-m, -m), r2 = pack2(r, r), s2 = pack2(s, s), h2 = pack2(half, half), big = pack2(8388608.f, 8388608.f),
                         less = pack2(-8388608.f, -8388608.f);
             uint32_t word = 0;
@@ -224,9 +227,8 @@ __global__ void __launch_bounds__(kKvThreads) ears_kv_write_kernel(const KvWrite
             }
             word -= kOffset;
             if (rows[u] >= 0 && at.row >= 0) {
-                const long long to = at.row + (long long)rows[u] * p.cache.page;
-                *reinterpret_cast<uint32_t*>(p.cache.codes + to * (D / 2) + d * 4) = fine ? word : 0u;
-                if (lane % 8 == 0) p.cache.params[to * NG + d / 8] = fine ? (__float_as_uint(s) >> 16) | (__float_as_uint(m) & 0xffff0000u) : 0x7fc07fc0u;
+                *reinterpret_cast<uint32_t*>(codes + (unsigned)rows[u] * (D / 2)) = fine ? word : 0u;
+                if (lane % 8 == 0) params[(unsigned)rows[u] * NG] = fine ? (__float_as_uint(s) >> 16) | (__float_as_uint(m) & 0xffff0000u) : 0x7fc07fc0u;
             }
         }
     }
@@ -250,6 +252,8 @@ __global__ void __launch_bounds__(kKvThreads) ears_kv_read_kernel(const KvReadPa
     if (at.b >= p.seqs.B) return;
     const int per_kind = (p.cache.heads + HEADS - 1) / HEADS * WARPS, steps = 2 * per_kind;
     const long long out = ((long long)at.b * p.seqs.Q + at.i) * p.cache.heads * D;
+    const uint8_t* const codes = p.cache.codes + at.row * (D / 2);
+    const uint32_t* const params = p.cache.params + at.row * NG;
     const uint32_t none = at.mine ? 0x7fc07fc0u : 0u;      // without a place: NaN where asked for, zeros where not
 #pragma unroll 1
     for (int s0 = at.part; s0 < steps; s0 += parts * kKvUnroll) {
@@ -263,10 +267,10 @@ __global__ void __launch_bounds__(kKvThreads) ears_kv_read_kernel(const KvReadPa
             word[u] = 0;
             par[u] = none;
             if (place[u] >= 0 && at.row >= 0) {
-                const long long from = at.row + (long long)(kind * p.cache.heads + h) * p.cache.page;
-                const uint8_t* codes = p.cache.codes + from * (D / 2) + d / 2;
-                word[u] = N == 8 ? *reinterpret_cast<const uint32_t*>(codes) : *reinterpret_cast<const uint16_t*>(codes);
-                par[u] = p.cache.params[from * NG + d / kKvGroup];
+                const unsigned from = (unsigned)((kind * p.cache.heads + h) * p.cache.page);
+                const uint8_t* at_code = codes + from * (D / 2) + d / 2;
+                word[u] = N == 8 ? *reinterpret_cast<const uint32_t*>(at_code) : *reinterpret_cast<const uint16_t*>(at_code);
+                par[u] = params[from * NG + d / kKvGroup];
             }
         }
 #pragma unroll

@@ -27,7 +27,7 @@ int check_cache(const ears_kv_cache* c) {
     if (!c || !c->codes || !c->params) return EARS_ERR_NULL;
     if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return EARS_ERR_SHAPE;
     if (c->pages < 1 || c->heads < 1 || c->heads > (1 << 16) || c->page_size < 16 || c->page_size % 16 || c->page_size > (1 << 20)) return EARS_ERR_SHAPE;
-    if ((long double)c->pages * 2 * c->heads * c->page_size * (c->head_dim / 2) > 4.0e18L) return EARS_ERR_SHAPE;
+    if ((long long)c->heads * c->page_size * c->head_dim > INT_MAX) return EARS_ERR_SHAPE;       // bytes of a page
     if ((long double)c->pages * 2 * c->heads * c->page_size > 3.0e10L) return EARS_ERR_SHAPE;    // sixteenths of rows in 31 bits
     if (misaligned(c->codes, 16) || misaligned(c->params, 16)) return EARS_ERR_ALIGN;
     return EARS_OK;
