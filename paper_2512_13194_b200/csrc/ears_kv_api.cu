@@ -33,10 +33,12 @@ int check_cache(const ears_kv_cache* c) {
     return EARS_OK;
 }
 
+constexpr long long kMaxTokens = INT_MAX - 1024;      // of a table: positions and what is added to them stay in 31 bits
+
 int check_seqs(const ears_kv_cache* c, const KvSeqs& s) {
     if (!s.table || !s.start) return EARS_ERR_NULL;
     if (s.B < 1 || s.Q < 1 || s.width < 1 || s.stride < 0) return EARS_ERR_SHAPE;
-    if ((long long)s.width * c->page_size > INT_MAX) return EARS_ERR_SHAPE;
+    if ((long long)s.width * c->page_size > kMaxTokens) return EARS_ERR_SHAPE;
     if ((long double)(s.B - 1) * s.stride + s.width > 1.0e18L) return EARS_ERR_SHAPE;
     // eights of a call's elements, counted in 31 bits
     if ((long double)s.B * s.Q * 2 * c->heads * (c->head_dim / 8) > (long double)INT_MAX) return EARS_ERR_SHAPE;
@@ -251,7 +253,7 @@ int ears_kv_read(int dtype, const ears_kv_cache* cache, int B, int Q, const int3
 }
 
 size_t ears_kv_attention_workspace_bytes(int dtype, const ears_kv_cache* cache, int B, int Q, int heads_q, int table_width, int window, int sinks) {
-    if (check_cache(cache) || B < 1 || Q < 1 || table_width < 1 || (long long)table_width * cache->page_size > INT_MAX) return 0;
+    if (check_cache(cache) || B < 1 || Q < 1 || table_width < 1 || (long long)table_width * cache->page_size > kMaxTokens) return 0;
     if (check_attention(dtype, cache, B, Q, heads_q, table_width, window, sinks)) return 0;
     KaPlan plan;
     if (make_plan(dtype, cache, B, Q, heads_q, table_width, window, sinks, &plan)) return 0;
@@ -285,7 +287,10 @@ int ears_kv_attention(int dtype, const ears_kv_cache* cache, const void* q, int 
     p.window = window; p.sinks = sinks;
     p.out = out; p.lse = out_lse; p.status = status;
     EARS_TRY(launch(plan.v.attention, p, dim3((unsigned)plan.grid), kKaThreads, plan.v.smem, stream, "ears_kv_attention_kernel launch"));
-    return launch(plan.v.join, p, dim3((unsigned)plan.grid, (unsigned)(plan.v.nt * 8 / kKaJoinRows)), kKaJoinRows * 32, 0, stream,
+    // few units have many parts each: as many warps per row as leave a warp a dozen of them
+    const long long units = (long long)B * cache->heads * plan.blocks;
+    const int warps = plan.grid > 24 * units ? 4 : plan.grid > 12 * units ? 2 : 1;
+    return launch(plan.v.join, p, dim3((unsigned)plan.grid, (unsigned)(plan.v.nt * 8 / kKaJoinRows)), kKaJoinRows * 32 * warps, 0, stream,
                   "ears_kv_join_kernel launch");
 }
 

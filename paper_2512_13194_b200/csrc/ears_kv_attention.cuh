@@ -86,11 +86,12 @@ __device__ __forceinline__ KaSpan ka_span(const KaParams& p, int b) {
     s.count = kv_count(p.seqs, b);
     s.bad = s.count > 0 && (s.start < 0 || (long long)s.start + s.count > (long long)p.seqs.width * p.cache.page);
     s.sinks = s.first = s.tiles = 0;
+    if (s.bad) s.start = 0;               // no tile is looked at, and no position that passes 31 bits formed
     if (s.count > 0 && !s.bad) {
         const int last = (s.start + s.count - 1) / kKaTile;
         if (p.window) {
             s.first = max(0, s.start - p.window + 1) / kKaTile;
-            s.sinks = min((p.sinks + kKaTile - 1) / kKaTile, s.first);
+            s.sinks = min(p.sinks / kKaTile + (p.sinks % kKaTile != 0), s.first);
         }
         s.tiles = s.sinks + last - s.first + 1;
     }
@@ -735,38 +736,41 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
     }
 }
 
-// ---- units that several CTAs had parts of: the first CTA's second slot, the others' first, in that order
-constexpr int kKaJoinRows = 4;             // a warp each
+// ---- units that several CTAs had parts of: the first CTA's second slot, the others' first, in a fixed order
+constexpr int kKaJoinRows = 4;             // per block; each has blockDim / 128 warps, which take every so-manieth part
+constexpr int kKaJoinWarps = 4;            // of a row at most
 template <typename E, int D, int NT>
-__global__ void __launch_bounds__(kKaJoinRows * 32) ears_kv_join_kernel(const KaParams p) {
+__global__ void __launch_bounds__(kKaJoinRows * kKaJoinWarps * 32) ears_kv_join_kernel(const KaParams p) {
     constexpr int ROWS = NT * 8, PER = D / 32;
+    __shared__ float2 s_ml[kKaJoinWarps][kKaJoinRows];
+    __shared__ float s_v[kKaJoinWarps - 1][kKaJoinRows][D];
     wait_for_stream();
     const int4 cut = p.cut[blockIdx.x];
     if (cut.x < 0) return;
-    const int lane = threadIdx.x & 31, in_block = blockIdx.y * kKaJoinRows + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = warp / kKaJoinRows, warps = blockDim.x / (32 * kKaJoinRows);
+    const int in_block = blockIdx.y * kKaJoinRows + warp % kKaJoinRows;
     const int b = cut.x, h = cut.y / p.blocks, row = (cut.y - h * p.blocks) * ROWS + in_block;
-    if (row >= p.M) return;
     const int c0 = blockIdx.x, parts = cut.z - c0 + 1;
-    auto place = [&](int n) { return ((long long)(c0 + n) * 2 + (n == 0)) * ROWS + in_block; };
-    // one look at the maxima and sums, a lane per part; results of up to eight parts on their way at once
+    const int own = row < p.M ? (parts - mine + warps - 1) / warps : 0;        // parts mine, mine + warps, ...
+    auto place = [&](int k) { const int n = mine + k * warps; return ((long long)(c0 + n) * 2 + (n == 0)) * ROWS + in_block; };
+    // one look at the maxima and sums, a lane per part; results of eight parts on their way at once
     float top = -INFINITY, sum = 0.f, v[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) v[i] = 0.f;
-    for (int n0 = 0; n0 < parts; n0 += 32) {
-        const int count = min(32, parts - n0);
+    for (int n0 = 0; n0 < own; n0 += 32) {
+        const int count = min(32, own - n0);
         const float2 ml = lane < count ? p.part_ml[place(n0 + lane)] : make_float2(-INFINITY, 0.f);
         float most = fmaxf(top, ml.x);
 #pragma unroll
         for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
         const float before = top == -INFINITY ? 0.f : ex2_approx(top - most), f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - most);
         top = most;
-        sum *= before;
+        float part = ml.y * f;
+#pragma unroll
+        for (int d = 16; d; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
+        sum = fmaf(sum, before, part);
 #pragma unroll
         for (int i = 0; i < PER; ++i) v[i] *= before;
-        float mine = ml.y * f;
-#pragma unroll
-        for (int d = 16; d; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
-        sum += mine;
         for (int m0 = 0; m0 < count; m0 += 8) {
             float2 w[8][PER / 2];
 #pragma unroll
@@ -785,6 +789,30 @@ __global__ void __launch_bounds__(kKaJoinRows * 32) ears_kv_join_kernel(const Ka
             }
         }
     }
+    if (warps > 1) {
+        if (lane == 0) s_ml[mine][warp % kKaJoinRows] = make_float2(top, sum);
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) s_v[mine - 1][warp % kKaJoinRows][i * 32 + lane] = v[i];
+        }
+        __syncthreads();
+        if (mine) return;
+        float most = top;
+        for (int w = 1; w < warps; ++w) most = fmaxf(most, s_ml[w][warp].x);
+        const float f0 = top == -INFINITY ? 0.f : ex2_approx(top - most);
+        sum *= f0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] *= f0;
+        for (int w = 1; w < warps; ++w) {
+            const float2 ml = s_ml[w][warp];
+            const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - most);
+            sum = fmaf(ml.y, f, sum);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) v[i] = fmaf(s_v[w - 1][warp][i * 32 + lane], f, v[i]);
+        }
+        top = most;
+    }
+    if (row >= p.M) return;
     const bool asked = row / p.group < kv_count(p.seqs, b);
     if (!asked) {
 #pragma unroll

@@ -211,7 +211,7 @@ def test_attention(ears, dtype, D, Q, group):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
-@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (7, 3), (16, 16), (50, 4), (64, 33), (100, 500), (1000, 4), (5000, 0)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (7, 3), (16, 16), (50, 4), (64, 33), (100, 500), (1000, 4), (5000, 0), (2**31 - 1, 0), (9, 2**31 - 1)])
 def test_attention_with_a_window_and_sinks(ears, dtype, window, sinks):
     attend(ears, dtype, [3, 40, 100, 333, 900], 5, 4, 2, 64, 32, window=window, sinks=sinks, seed=window)
     attend(ears, dtype, [700, 20], 3, 2, 1, 128, 16, window=window, sinks=sinks, seed=window + 1)

@@ -46,6 +46,8 @@ def test_every_entry_point_checks_cache_and_positions(name):
     assert call(s=seqs(width=0)) == -2 and call(s=seqs(stride=-1)) == -2 and call(s=seqs(width=2**28)) == -2
     assert call(B=0) == -2 and call(Q=0) == -2 and call(B=2**20, Q=2**20) == -2
     assert call(s=seqs(table=P + 2)) == -4 and call(s=seqs(start=P + 1)) == -4 and call(s=seqs(counts=P + 2)) == -4
+    assert call(s=seqs(width=(2**31 - 1) // 16)) == -2        # positions and what is added to them stay in 31 bits
+    assert call(c=cache(heads=2**15, page_size=2**11)) == -2   # a page of 2^32 bytes
     assert call(dtype=3) == -3 and call(dtype=-1) == -3
     assert call(st=P + 2) == -4
 
@@ -56,6 +58,13 @@ def test_write_and_read_check_their_tensors():
     assert w(k=P + 1) == -4 and w(dtype=0, v=P + 2) == -4 and r(k=P + 8) == -4 and r(v=P + 2) == -4
     for bad in ((-1, 128, 64), (256, -128, 64), (256, 128, -1), (2**62, 128, 64)):
         assert w(B=3, ks=bad) == -2 and w(B=3, vs=bad) == -2
+
+
+def test_a_missing_cache_is_refused():
+    assert lib().ears_kv_write(1, None, P, P, 1, 2, 256, 128, 64, 256, 128, 64, P, 3, 3, P, None, None, None) == -1
+    assert lib().ears_kv_read(1, None, 1, 2, P, 3, 3, P, None, P, P, None, None) == -1
+    assert lib().ears_kv_attention(1, None, P, 1, 2, 4, 512, 256, 64, P, 3, 3, P, None, 0.125, 0, 0, P, None, P, 1 << 30, None, None) == -1
+    assert lib().ears_kv_attention_workspace_bytes(1, None, 1, 1, 4, 3, 0, 0) == 0
 
 
 def test_attention_checks_its_arguments():
