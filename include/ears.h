@@ -615,7 +615,8 @@ int ears_kv_read(int dtype, const ears_kv_cache* cache, int B, int Q, const int3
  * Positions that are left out get zeros and -inf.  A NaN or infinity in a row of q, or a NaN read from a token that it sees, makes
  * that row NaN and no other.
  * Scores, their sums and the results are kept in 32 bits; q is taken as it is, or, where its row spans more than 2^25, to within
- * 2^-26 of the row's largest element; weights enter the second product in half precision (bfloat16 q) or in two halves.
+ * 2^-26 of the row's largest element; weights enter the second product in half precision; for half-precision q what
+ * that loses is added back times the middle code, so that 2^-11 times at most 7.5 scales is left of it.
  * workspace: ears_kv_attention_workspace_bytes for the same arguments on the same device (0: they would be refused), 256-byte
  * aligned; its contents before and after mean nothing.  It does not grow with the lengths.  The same call on the same kind of
  * device gives the same bits; a row's may differ with what else is in the batch (the order of its sums).

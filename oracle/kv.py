@@ -51,6 +51,7 @@ class Attention(NamedTuple):
     out: torch.Tensor       # [B, Q, HQ, D]
     lse: torch.Tensor       # [B, Q, HQ]
     weighted: torch.Tensor  # sum_t p_t s_t c_t: what a relative error of the weights enters times
+    spread: torch.Tensor    # 7.5 sum_t p_t s_t: the same for codes less their middle, at the most
     reach: torch.Tensor     # max_t |v_t - out| over the tokens seen: what an error of the weights can move a result by
     size: torch.Tensor      # [B, Q, HQ] max_t of sum_d |q| (|m| + s c) scale log2(e): the size of what the scores sum
     tiny: torch.Tensor      # [B, Q, HQ] tokens seen times the largest scale among them
@@ -60,8 +61,7 @@ def attention(q, codes, params, pages, start, counts=None, scale=None, window=0,
     B, Q, HQ, D = q.shape
     H = codes.shape[2]
     scale = D ** -0.5 if scale is None else scale
-    rows = [torch.zeros(B, Q, HQ, D, dtype=torch.float64) for _ in range(3)]
-    out, weighted, reach = rows
+    out, weighted, spread, reach = (torch.zeros(B, Q, HQ, D, dtype=torch.float64) for _ in range(4))
     lse = torch.full((B, Q, HQ), -math.inf, dtype=torch.float64)
     size, tiny = torch.zeros(B, Q, HQ, dtype=torch.float64), torch.zeros(B, Q, HQ, dtype=torch.float64)
     for b in range(B):
@@ -87,7 +87,8 @@ def attention(q, codes, params, pages, start, counts=None, scale=None, window=0,
             r = w @ v
             out[b, i], lse[b, i] = r.reshape(HQ, D), s.logsumexp(-1).reshape(HQ)
             weighted[b, i] = (w @ (v - lo[1])).reshape(HQ, D)
+            spread[b, i] = 7.5 * (w @ m[1][:, see][..., 0].double().repeat_interleave(GROUP, -1)).reshape(HQ, D)
             reach[b, i] = torch.maximum(v.amax(1, keepdim=True) - r, r - v.amin(1, keepdim=True)).reshape(HQ, D)
             size[b, i] = (x.abs() @ (lo[0].abs() + (k - lo[0])).transpose(1, 2)).amax(-1).reshape(HQ) * abs(scale) / math.log(2)
             tiny[b, i] = (len(v[0]) * m[1][:, see][..., 0].double().amax((1, 2))).repeat_interleave(HQ // H)
-    return Attention(out, lse, weighted, reach, size, tiny)
+    return Attention(out, lse, weighted, spread, reach, size, tiny)

@@ -7,8 +7,8 @@ Attention, tolerances from the arithmetic.  In units of log2 a score is a sum of
 most `size` (oracle): the query's 2^-26 of its largest element (2^-26 * 64 terms of that size at worst, 2^-20 size), at most
 D / 64 * 8 accumulations on tensor cores (truncating: 2^-23 each) and about ten 32-bit roundings: 2^-17.9 size at D = 256;
 S_TOL = 2^-17 (size + 1), the 1 for the exponential's own 2^-22.  A relative error e in every weight moves a result by at most 2 e reach, e = ln 2
-S_TOL.  A weight's rounding to half precision is 2^-11 of `weighted` for bfloat16 queries and 2^-22 for half-precision ones (two
-halves); weights that are subnormal there are off by at most 2^-25 of 2^-6 of the largest scale, 15 codes each: 2^-27 tiny.  The sums
+S_TOL.  A weight's rounding to half precision is 2^-11 of `weighted` for bfloat16 queries; for half-precision ones, where what it
+lost is added back times the middle code, 2^-11 of `spread`, 7.5 codes either way; weights that are subnormal there are off by at most 2^-25 of 2^-6 of the largest scale, 15 codes each: 2^-27 tiny.  The sums
 over up to some ten thousand tokens are in 32 bits, split over at least four warps: below 2^-14 relative of what is summed at the
 worst, sqrt of that in truth; 2^-18 (weighted + |out| + reach).  Then one rounding to the type, half a step.
 """
@@ -171,8 +171,8 @@ def close(got, want, dtype, lse=None):
     eps = torch.finfo(DT[dtype]).eps / 2
     got = got.cpu().double()
     e = 2.0 ** -17 * math.log(2) * (want.size + 1)
-    weight = 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22
-    limit = (2 * e.unsqueeze(-1) * want.reach + (weight + 2.0 ** -18) * want.weighted + 2.0 ** -18 * (want.out.abs() + want.reach)
+    rounded = want.weighted if dtype == "bf16" else want.spread
+    limit = (2 * e.unsqueeze(-1) * want.reach + 2.0 ** -11 * rounded + 2.0 ** -18 * want.weighted + 2.0 ** -18 * (want.out.abs() + want.reach)
              + 2.0 ** -27 * want.tiny.unsqueeze(-1))
     limit = limit * (1 + eps) + eps * want.out.abs() + (2.0 ** -25 if dtype == "fp16" else 0.0)
     err = (got - want.out).abs()
