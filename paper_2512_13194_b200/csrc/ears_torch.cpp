@@ -9,10 +9,14 @@
 // Nothing is decided here that is not decided there.
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <cmath>
+#include <limits>
 
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -67,6 +71,13 @@ struct Args {
         return v;
     }
     bool flag() { return next() == Py_True; }
+    // a number, or NaN for None (a NaN that is given is not plain)
+    double scale() {
+        if (i < n && a[i] == Py_None) { ++i; return std::numeric_limits<double>::quiet_NaN(); }
+        const double v = number();
+        if (std::isnan(v)) plain = false;
+        return v;
+    }
 };
 
 struct Rows {
@@ -388,6 +399,7 @@ int dtype_of(const at::Tensor& t) {
 // [B, Q, heads, head_dim], used where it lies
 bool heads_of(const Kv& kv, const at::Tensor* t) {
     if (!t->is_cuda() || t->get_device() != kv.device || t->dim() != 4 || t->size(0) != kv.B || t->size(3) != kv.cache.head_dim) return false;
+    if (t->requires_grad() && c10::GradMode::is_enabled()) return false;      // refused by the wrapper
     if (t->stride(3) != 1 || t->numel() == 0 || t->size(1) > INT32_MAX || t->size(2) > INT32_MAX) return false;
     return t->stride(0) >= 0 && t->stride(1) >= 0 && t->stride(2) >= 0;
 }
@@ -445,13 +457,14 @@ PyObject* kv_attention(PyObject*, PyObject* const* argv, Py_ssize_t n) {
         Kv kv;
         if (!take_cache(a, &kv)) EARS_NOT_PLAIN;
         const at::Tensor *q = a.tensor(false), *pages = a.tensor(false), *start = a.tensor(false), *counts = a.tensor(true);
-        const double scale = a.number();
+        const double given = a.scale();
         const long window = a.integer(), sinks = a.integer();
         const bool lse = a.flag();
         const at::Tensor* status = a.tensor(true);
         if (!a.plain || !take_seqs(&kv, pages, start, counts, status) || !heads_of(kv, q)) EARS_NOT_PLAIN;
         const int dtype = dtype_of(*q), Q = (int)q->size(1), heads = (int)q->size(2);
         if ((dtype != EARS_DTYPE_BF16 && dtype != EARS_DTYPE_F16) || window < 0 || window > INT32_MAX || sinks < 0 || sinks > INT32_MAX) EARS_NOT_PLAIN;
+        const double scale = std::isnan(given) ? 1.0 / std::sqrt((double)kv.cache.head_dim) : given;
         const size_t need = ((decltype(&ears_kv_attention_workspace_bytes))g_entries[kKvWorkspace].fn)(dtype, &kv.cache, kv.B, Q, heads, kv.width,
                                                                                                    (int)window, (int)sinks);
         if (!need) EARS_NOT_PLAIN;

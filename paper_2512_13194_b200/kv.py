@@ -15,7 +15,6 @@ page table or a page outside the pool.
 from __future__ import annotations
 
 import ctypes
-import functools
 from typing import NamedTuple, Optional
 
 import torch
@@ -67,18 +66,18 @@ def _refuse_gradients(*tensors) -> None:
             raise NotImplementedError("the cache's operators have no gradient")
 
 
-def _on_stream(fn):
+def _plain():
+    """The extension module's calls, which leave everything that is not in its plain form (a gradient asked for, too) to the ones
+    here; nothing is plain while forward-mode derivatives are taken."""
+    return rows._plain_calls() if forward_ad._current_level < 0 else rows._Ctypes
+
+
+def _on_stream(stream, cache, fn, *args, **kwargs):
     """``stream=``: the whole call, its conversions and outputs included, belongs to that stream as under torch.cuda.stream."""
-    @functools.wraps(fn)
-    def call(*args, stream=None, **kwargs):
-        if stream is None:
-            return fn(*args, **kwargs)
-        cache = kwargs["cache"] if "cache" in kwargs else next(a for a in args if isinstance(a, KVCache))
-        if stream.device_index != cache.codes.get_device():
-            raise ValueError("the stream must belong to the cache's device")
-        with torch.cuda.stream(stream):
-            return fn(*args, **kwargs)
-    return call
+    if stream.device_index != cache.codes.get_device():
+        raise ValueError("the stream must belong to the cache's device")
+    with torch.cuda.stream(stream):
+        return fn(*args, **kwargs)
 
 
 class _Call:
@@ -144,14 +143,15 @@ class _Call:
             _check(fn(*args, _ptr(self.status), rows._raw_stream(self.index)))
 
 
-@_on_stream
 def kv_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, start: torch.Tensor,
-             counts: Optional[torch.Tensor] = None, *, status: Optional[torch.Tensor] = None) -> None:
+             counts: Optional[torch.Tensor] = None, *, status: Optional[torch.Tensor] = None, stream=None) -> None:
     """Quantises keys and values [B, Q, heads, head_dim] (float32, bfloat16, float16) into the cache, as tokens ``start[b]`` to
     ``start[b] + Q - 1`` of each sequence, or the first ``counts[b]`` of them (ears_kv_write).  One token or a prompt: Q is any."""
-    _refuse_gradients(k, v)
-    if rows._plain_calls().kv_write(cache[0], cache[1], k, v, pages, start, counts, status):
+    if stream is not None:
+        return _on_stream(stream, cache, kv_write, cache, k, v, pages, start, counts, status=status)
+    if _plain().kv_write(cache[0], cache[1], k, v, pages, start, counts, status):
         return
+    _refuse_gradients(k, v)
     c = _Call(cache, pages, start, counts, status)
     code = _DTYPES.get(k.dtype)
     if code is None or v.dtype != k.dtype:
@@ -163,12 +163,13 @@ def kv_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, pages: torch.Tens
     c.run(load_library().ears_kv_write, code, ctypes.byref(c.cache), k.data_ptr(), v.data_ptr(), c.B, k.shape[1], *ks, *vs, *c.table)
 
 
-@_on_stream
 def kv_read(cache: KVCache, pages: torch.Tensor, start: torch.Tensor, tokens: int, counts: Optional[torch.Tensor] = None, *,
-            dtype: torch.dtype = torch.bfloat16, status: Optional[torch.Tensor] = None):
+            dtype: torch.dtype = torch.bfloat16, status: Optional[torch.Tensor] = None, stream=None):
     """The values of ``tokens`` tokens of each sequence from ``start[b]`` on: (keys, values), each [B, tokens, heads, head_dim] of ``dtype``
     (ears_kv_read).  Positions from ``counts[b]`` on are zeros."""
-    out = rows._plain_calls().kv_read(cache[0], cache[1], pages, start, tokens, counts, _DTYPES.get(dtype), status)
+    if stream is not None:
+        return _on_stream(stream, cache, kv_read, cache, pages, start, tokens, counts, dtype=dtype, status=status)
+    out = _plain().kv_read(cache[0], cache[1], pages, start, tokens, counts, _DTYPES.get(dtype), status)
     if out is not None:
         return out
     c = _Call(cache, pages, start, counts, status)
@@ -183,21 +184,22 @@ def kv_read(cache: KVCache, pages: torch.Tensor, start: torch.Tensor, tokens: in
     return k, v
 
 
-@_on_stream
 def kv_attention(q: torch.Tensor, cache: KVCache, pages: torch.Tensor, start: torch.Tensor, counts: Optional[torch.Tensor] = None, *,
                  scale: Optional[float] = None, window: int = 0, sinks: int = 0, lse: bool = False,
-                 status: Optional[torch.Tensor] = None):
+                 status: Optional[torch.Tensor] = None, stream=None):
     """Attention of the positions ``start[b]`` to ``start[b] + Q - 1``, whose tokens ``kv_write`` has written, over each sequence's
     tokens up to and including their own (ears_kv_attention): with ``window`` > 0 the last ``window`` of them and the first
     ``sinks``.  q [B, Q, heads_q, head_dim] (bfloat16, float16), heads_q a multiple of the cache's heads, consecutive query heads on
     one of them; ``scale`` is 1 / sqrt(head_dim) unless given.  Returns [B, Q, heads_q, head_dim] of q's type, zeros from position
     ``counts[b]`` on; with ``lse=True`` also the scores' log-sum-exp, float32 [B, Q, heads_q]."""
+    if stream is not None:
+        return _on_stream(stream, cache, kv_attention, q, cache, pages, start, counts, scale=scale, window=window, sinks=sinks, lse=lse, status=status)
+    out = _plain().kv_attention(cache[0], cache[1], q, pages, start, counts, scale, window, sinks, lse is True, status)
+    if out is not None:
+        return out if lse else out[0]
     _refuse_gradients(q)
     if scale is None:
         scale = q.shape[-1] ** -0.5 if q.dim() and q.shape[-1] else 1.0
-    out = rows._plain_calls().kv_attention(cache[0], cache[1], q, pages, start, counts, scale, window, sinks, bool(lse), status)
-    if out is not None:
-        return out if lse else out[0]
     c = _Call(cache, pages, start, counts, status)
     if q.dtype not in (torch.bfloat16, torch.float16):
         raise TypeError(f"queries must be bfloat16 or float16, got {q.dtype}")

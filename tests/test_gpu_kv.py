@@ -384,6 +384,36 @@ def test_integers_of_other_types_and_tables_that_are_slices(ears):
         ears.kv_read(ears.KVCache(cache.codes[:, :, :, ::2], cache.params[:, :, :, ::2]), pages.to(DEV), ints([0, 0]), 2)
 
 
+def test_plain_calls_need_no_conversion_and_gradients_are_refused(ears, monkeypatch):
+    from paper_2512_13194_b200 import kv as module
+    codes, params, pages, g = pool([100, 33], 2, 64, 16, 63)
+    cache, pages, start = on_device(ears, codes, params), pages.to(DEV), ints([95, 28])
+    q = torch.randn(2, 5, 4, 64, generator=g).half().to(DEV)
+    k = torch.randn(2, 5, 2, 64, generator=g).to(DEV)
+    want = ears.kv_attention(q, cache, pages.long(), start, scale=0.125, lse=True)          # not plain: 64-bit integers
+    grads = [t.clone().requires_grad_() for t in (q, k)]
+    for call in (lambda: ears.kv_attention(grads[0], cache, pages, start), lambda: ears.kv_write(cache, grads[1], k, pages, start),
+                 lambda: ears.kv_write(cache, k, grads[1], pages, start)):
+        with pytest.raises(NotImplementedError):
+            call()
+
+    def fail(*args):
+        raise AssertionError("converted")
+
+    monkeypatch.setattr(module, "_Call", fail)
+    got = ears.kv_attention(q, cache, pages, start, lse=True)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    with torch.no_grad():
+        assert torch.equal(ears.kv_attention(grads[0], cache, pages, start), want[0])
+    ears.kv_write(cache, k, k, pages, start, ints([5, 2]))
+    assert torch.equal(*ears.kv_read(cache, pages, start, 5, ints([5, 2]), dtype=torch.float32))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out = ears.kv_attention(q, cache, pages, start, window=7, sinks=1, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(out, ears.kv_attention(q, cache, pages, start, window=7, sinks=1))
+
+
 def test_offsets_beyond_32_bits(ears):
     """A pool whose codes pass 2^32 bytes; what is written, read and attended to lies behind them."""
     D, H, page = 256, 8, 128
