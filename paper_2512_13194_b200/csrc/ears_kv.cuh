@@ -148,7 +148,9 @@ struct KvWriteParams {
 
 // Warps have a position's keys and values of all heads, eight consecutive values per lane and step: a group is eight lanes, a
 // position's place is looked up once, and what a warp loads or stores at once is contiguous.  `parts` warps share a position
-// where there are few of them.
+// where there are few of them.  Measured, 8 heads of 128: 13100 positions of bf16 written in 24 us (11 at the copy rate; issue 75 %:
+// some 190 instructions per step of a warp), 65003 read as bf16 in 60 us (52), as fp32 in 98 (93).  A thread team per group, which looks the
+// place up for each, took 55, 129 and more.
 constexpr int kKvThreads = 128;
 constexpr int kKvUnroll = 4;              // steps whose loads are on their way together
 
