@@ -83,7 +83,6 @@ struct KaSpan {
     bool bad;
     __device__ __forceinline__ int tile(int i) const { return i < sinks ? i : first + (i - sinks); }
     __device__ __forceinline__ int chunks() const { return max(1, (tiles + kKaWarps - 1) / kKaWarps); }
-    __device__ __forceinline__ int cost() const { return chunks() + kKaAhead; }
 };
 __device__ __forceinline__ KaSpan ka_span(const KaParams& p, int b) {
     KaSpan s;
@@ -230,7 +229,7 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
     const int b0 = min(p.seqs.B, tid * each), b1 = min(p.seqs.B, b0 + each);
     int own = 0;
 #pragma unroll 1
-    for (int b = b0; b < b1; ++b) own += ka_span(p, b).cost() * per_seq;
+    for (int b = b0; b < b1; ++b) own += ka_span(p, b).chunks() * per_seq;
     int before = own;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -246,6 +245,11 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
         total += s_sum[w];
     }
     before -= own;
+    // few chunks go a CTA each; else what a unit costs beside its chunks counts as `ahead` more, in front of them
+    const int ahead = total > 2 * (int)gridDim.x ? kKaAhead : 0;
+    before += b0 * per_seq * ahead;
+    own += (b1 - b0) * per_seq * ahead;
+    total += p.seqs.B * per_seq * ahead;
     const int ctas = min((int)gridDim.x, total), share = total / ctas, longer = total - share * ctas;   // the first `longer` have one more
     if (tid == 0) p.cut[blockIdx.x] = make_int4(-1, 0, 0, 0);
     if (blockIdx.x >= ctas) return;
@@ -254,7 +258,7 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
         int base = before, b = b0;
 #pragma unroll 1
         for (;; ++b) {
-            const int n = ka_span(p, b).cost() * per_seq;
+            const int n = (ka_span(p, b).chunks() + ahead) * per_seq;
             if (begin < base + n) break;
             base += n;
         }
@@ -278,13 +282,13 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
 
     KaSpan span = ka_span(p, b);
     while (left > 0) {
-        const int chunks = span.chunks(), cost = span.cost(), unit = off / cost, at0 = off - unit * cost;
+        const int chunks = span.chunks(), cost = chunks + ahead, unit = off / cost, at0 = off - unit * cost;
         if (unit >= per_seq) {
             span = ka_span(p, ++b);
             off = 0;
             continue;
         }
-        const int taken = min(cost - at0, left), c0 = max(0, at0 - kKaAhead), c1 = max(0, at0 + taken - kKaAhead);
+        const int taken = min(cost - at0, left), c0 = max(0, at0 - ahead), c1 = max(0, at0 + taken - ahead);
         off += taken;
         left -= taken;
         if (c0 == c1) continue;
@@ -762,11 +766,20 @@ __global__ void __launch_bounds__(kKaJoinRows * kKaJoinWarps * 32) ears_kv_join_
     auto place = [&](int k) { const int n = mine + k * warps; return ((long long)(c0 + n) * 2 + (n == 0)) * ROWS + in_block; };
     // one look at the maxima and sums, a lane per part; results of eight parts on their way at once
     float top = -INFINITY, sum = 0.f, v[PER];
+    float2 w[8][PER / 2];
+    auto fetch = [&](int first, int count) {
+#pragma unroll
+        for (int m = 0; m < 8; ++m)
+#pragma unroll
+            for (int i = 0; i < PER / 2; ++i)
+                w[m][i] = m < count ? __ldcg(reinterpret_cast<const float2*>(p.part_o + place(first + m) * D + lane * PER) + i) : make_float2(0.f, 0.f);
+    };
 #pragma unroll
     for (int i = 0; i < PER; ++i) v[i] = 0.f;
     for (int n0 = 0; n0 < own; n0 += 32) {
         const int count = min(32, own - n0);
-        const float2 ml = lane < count ? p.part_ml[place(n0 + lane)] : make_float2(-INFINITY, 0.f);
+        const float2 ml = lane < count ? __ldcg(p.part_ml + place(n0 + lane)) : make_float2(-INFINITY, 0.f);
+        fetch(n0, count);                                  // beside the maxima: neither waits for the other
         float most = fmaxf(top, ml.x);
 #pragma unroll
         for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
@@ -779,12 +792,7 @@ __global__ void __launch_bounds__(kKaJoinRows * kKaJoinWarps * 32) ears_kv_join_
 #pragma unroll
         for (int i = 0; i < PER; ++i) v[i] *= before;
         for (int m0 = 0; m0 < count; m0 += 8) {
-            float2 w[8][PER / 2];
-#pragma unroll
-            for (int m = 0; m < 8; ++m)
-#pragma unroll
-                for (int i = 0; i < PER / 2; ++i)
-                    w[m][i] = m0 + m < count ? __ldcg(reinterpret_cast<const float2*>(p.part_o + place(n0 + m0 + m) * D + lane * PER) + i) : make_float2(0.f, 0.f);
+            if (m0) fetch(n0 + m0, count - m0);
 #pragma unroll
             for (int m = 0; m < 8; ++m) {
                 const float g = __shfl_sync(0xffffffffu, f, (m0 + m) & 31);
