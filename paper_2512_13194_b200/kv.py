@@ -194,7 +194,7 @@ def kv_attention(q: torch.Tensor, cache: KVCache, pages: torch.Tensor, start: to
     ``counts[b]`` on; with ``lse=True`` also the scores' log-sum-exp, float32 [B, Q, heads_q]."""
     if stream is not None:
         return _on_stream(stream, cache, kv_attention, q, cache, pages, start, counts, scale=scale, window=window, sinks=sinks, lse=lse, status=status)
-    out = _plain().kv_attention(cache[0], cache[1], q, pages, start, counts, scale, window, sinks, lse is True, status)
+    out = _plain().kv_attention(cache[0], cache[1], q, pages, start, counts, scale, window, sinks, bool(lse), status)
     if out is not None:
         return out if lse else out[0]
     _refuse_gradients(q)

@@ -403,6 +403,7 @@ def test_plain_calls_need_no_conversion_and_gradients_are_refused(ears, monkeypa
     monkeypatch.setattr(module, "_Call", fail)
     got = ears.kv_attention(q, cache, pages, start, lse=True)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert torch.equal(ears.kv_attention(q, cache, pages, start, lse=1)[1], want[1])
     with torch.no_grad():
         assert torch.equal(ears.kv_attention(grads[0], cache, pages, start), want[0])
     ears.kv_write(cache, k, k, pages, start, ints([5, 2]))
