@@ -12,7 +12,7 @@
 // operations still, c 2^-9 being one as it stands, but m16n8k32 with them is made of conversions and 16-bit products here:
 // 68 conversions per tile of 16 tokens counted, and 437 instructions against 386.)
 // Measured: 64 single tokens, 64 / 8 heads of 128, 6000 to 8192 tokens (527 MB): 110 us, 73 % of the copy rate, 261 instructions per tile of
-// 16 tokens; 128 x 5 positions, 32 / 8 heads, 680 MB: 260 us, 411 instructions, of them 48 matrix products, which other
+// 16 tokens; 128 x 5 positions, 32 / 8 heads, 680 MB: 238 us, 390 instructions, of them 48 matrix products, which other
 // instructions overlap in part only.
 //
 // The products have 16 tokens (or, for the values, dimensions) as rows and eight of the head group's
@@ -197,13 +197,14 @@ __device__ __forceinline__ float ka_lse(float m, float l) { return l == 0.f ? -I
 // E: the queries' type.  FINE: a half-precision weight is off by up to 2^-11 (2^-12.3 in the mean), times codes that lie between 0 and 15:
 // nothing beside a bfloat16 result's own 2^-9, but twice a half-precision result's rounding.  For those what a weight lost is
 // added back times the middle code, 7.5, with the minima, so that its error meets codes less their middle.  (Weights in two halves
-// would be exact and double the second product: 72000 tokens x 8 x 8 heads of 128, 20 rows: 305 us against 236 without either.)
+// would be exact and double the second product: 72000 tokens x 8 x 8 heads of 128, 20 rows: 305 us against 253.)
 template <typename E, int D, int NT>
 __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_attention_kernel(const KaParams p) {
     using S = KaShape<D, NT>;
     constexpr int NG = S::NG, RB = S::RB, ROWS = NT * 8;
     constexpr bool FINE = std::is_same<E, f16_t>::value;
-    constexpr int SUB = NT * NG <= 4 ? 2 : 1;                            // tiles taken together
+    // tiles taken together, as registers allow: 128 x 5 positions take 259 us by one, 242 by two
+    constexpr int SUB = NT * NG <= 6 ? 2 : 1;
     constexpr bool QREG = NT * NG <= 4;                   // queries' operands stay in registers
     constexpr uint32_t M0 = 0x000f000fu, M1 = 0x00f000f0u;
 
