@@ -160,19 +160,26 @@ int resident(const Variant& v, int* ctas) {
 
 int make_plan(int dtype, const ears_kv_cache* c, int B, int Q, int heads_q, int width, int window, int sinks, KaPlan* plan) {
     const int M = Q * (heads_q / c->heads), tiles = (M + 7) / 8;
+    int sms = 0;
+    const int rc_sms = host_device_sms(&sms);
+    if (rc_sms) return rc_sms;
+    // chunks of a sequence at the most, whatever its length
+    long long tokens = (long long)width * c->page_size;
+    if (window && (long long)window + sinks + Q + 3 * kKaTile < tokens) tokens = (long long)window + sinks + Q + 3 * kKaTile;
+    const long long chunks = (tokens + kKaChunk - 1) / kKaChunk;
+    // Up to 16 chunks per SM, latency counts, and blocks of one eight are done soonest, although each reads the cache (5 positions of one
+    // sequence, 32 / 8 heads of 128: 1000 tokens 13.2 us with one block of three eights, 11.8 with three of one; 3500 tokens 20.3,
+    // 13.9; 9 positions 16.2, 11.6; 4 sequences of up to 3000: 17.9, 16.3; 8 of up to 4096, 28 per SM: 22.2, 23.7).
+    const bool few = (long double)B * c->heads * chunks <= 16.0L * sms;
     with_dim(c->head_dim, [&](auto d) {
         constexpr int D = decltype(d)::value;
-        const int nt = choose_rows<D>(tiles);
+        const int nt = few ? 1 : choose_rows<D>(tiles);
         plan->v = dtype == EARS_DTYPE_F16 ? choose_tiles<f16_t, D>(nt) : choose_tiles<uint16_t, D>(nt);
         return 0;
     });
     plan->blocks = (tiles + plan->v.nt - 1) / plan->v.nt;
     const int rc = resident(plan->v, &plan->grid);
     if (rc) return rc;
-    // no more CTAs than chunks can be, whatever the lengths
-    long long tokens = (long long)width * c->page_size;
-    if (window && (long long)window + sinks + Q + 3 * kKaTile < tokens) tokens = (long long)window + sinks + Q + 3 * kKaTile;
-    const long long chunks = (tokens + kKaChunk - 1) / kKaChunk;
     const long double units = (long double)B * c->heads * plan->blocks;
     if (units * (chunks + kKaAhead) > (long double)INT_MAX) return EARS_ERR_SHAPE;    // the device counts in 31 bits
     if (units * chunks < plan->grid) plan->grid = (int)(units * chunks);

@@ -246,8 +246,8 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
         total += s_sum[w];
     }
     before -= own;
-    // few chunks go a CTA each; else what a unit costs beside its chunks counts as `ahead` more, in front of them
-    const int ahead = total > 2 * (int)gridDim.x ? kKaAhead : 0;
+    // no more chunks than CTAs go one each; else what a unit costs beside its chunks counts as `ahead` more, in front of them
+    const int ahead = total > (int)gridDim.x ? kKaAhead : 0;
     before += b0 * per_seq * ahead;
     own += (b1 - b0) * per_seq * ahead;
     total += p.seqs.B * per_seq * ahead;

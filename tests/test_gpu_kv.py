@@ -203,11 +203,22 @@ def attend(ears, dtype, lengths, Q, group, H, D, page, counts=None, window=0, si
     return got
 
 
-@pytest.mark.parametrize("Q,group", [(1, 1), (1, 8), (5, 4), (3, 3), (6, 1), (2, 16), (9, 5), (1, 71)])
+# a table as wide as 12800 tokens and more has rows in blocks of several eights, a narrow one a block per eight
+@pytest.mark.parametrize("table_extra", [0, 800])
+@pytest.mark.parametrize("Q,group", [(1, 1), (1, 8), (5, 4), (3, 3), (6, 1), (2, 16), (9, 5), (1, 71), (4, 4), (7, 8)])
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
-def test_attention(ears, dtype, D, Q, group):
-    attend(ears, dtype, [1, 2, 17, 64, 65, 300, 1000, 0], Q, group, 2, D, 16 if D == 64 else 48, seed=D + Q)
+def test_attention(ears, dtype, D, Q, group, table_extra):
+    attend(ears, dtype, [1, 2, 17, 64, 65, 300, 1000, 0], Q, group, 2, D, 16 if D == 64 else 48, seed=D + Q, table_extra=table_extra)
+
+
+@pytest.mark.parametrize("Q,group", [(2, 8), (5, 4), (8, 4), (5, 8)])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_windows_over_many_units_of_several_eights(ears, dtype, D, Q, group):
+    g = torch.Generator().manual_seed(D + Q)
+    lengths = torch.randint(0, 700, (40,), generator=g).tolist()
+    attend(ears, dtype, lengths, Q, group, 8, D, 64, window=401, sinks=5, seed=D)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
