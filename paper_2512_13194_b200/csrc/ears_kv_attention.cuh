@@ -38,9 +38,18 @@ constexpr int kKaTile = 16;                         // tokens of a warp's tile
 constexpr int kKaChunk = kKaWarps * kKaTile;
 constexpr int kKaAhead = 8;                         // what starting and ending a unit costs, in chunks (128 x 5 positions as above: 279 us with 4,
                                                     // 264 with 6, 260 with 8, 270 with 16)
-// The running maximum is raised when a score passes it by 2^12, and the values' scales enter times a power of two that keeps
-// them below 8: their product, a weight, stays below half precision's 2^16.
-constexpr float kKaSlack = 12.f, kKaScaleCap = 8.f;
+// A row's weights are P = 2^(score - reference).  The reference, a whole number, is raised when a P passes 2^-18, to where the largest is
+// between 2^-31 and 2^-30: their sums with minima up to the type's largest number stay finite, and minima down to 2^-100 keep their bits.
+// The second product's half-precision operands are P s cs, with a power of two cs for each group that goes by the largest P s of a warp's tiles: it
+// brings that to between 2^4 and 2^5 when one may pass 2^15.  Not by the largest s, which may be that of a token of no weight (131072 tokens, one of them
+// with values 4096 times the others' and a weight of e^-60: an error of 0.08 of the result that way, 0.0015 this way, its own rounding).  What falls below half precision's normal numbers
+// is off by 2^-25 at most, so that a warp's n tokens are right to 2^-12 of a row's sum of P s cs as long as the largest of its
+// sums of P s cs c is 15 n 2^-13 or more.  That is looked at when the unit's tiles are through; where a row has less, as one that does not see a token whose
+// large values another row's result is made of, the warp takes its tiles once more with a cs of each row's own (a batch where every last draft is such a token, 128 x 5 positions: 615 us beside 248).
+// A lower goal than 2^4 leaves no room for rows that differ, a higher one has the powers set again more often: 2^6 250 us, 2^8 254, where 2^4 takes 246.
+constexpr int kKaLow = 30;
+constexpr float kKaTop = -18.f, kKaMost = 0x1p15f;
+constexpr int kKaGoal = 4, kKaRowGoal = 10, kKaFar = 1000;
 
 template <int D, int NT> struct KaShape {
     static constexpr int NG = D / kKvGroup;
@@ -173,10 +182,10 @@ __device__ __noinline__ uint4 ka_unaligned(const E* p) {
 
 // ---- a row's result ------------------------------------------------------------------------------------------
 template <typename E, int N>
-__device__ __forceinline__ void ka_store(E* out, const float (&x)[N], float factor) {
+__device__ __forceinline__ void ka_store(E* out, const float (&x)[N]) {
     uint32_t w[N / 2];
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) w[i] = pack_pair<E>(x[2 * i] * factor, x[2 * i + 1] * factor);
+    for (int i = 0; i < N / 2; ++i) w[i] = pack_pair<E>(x[2 * i], x[2 * i + 1]);
     if constexpr (N % 8 == 0) {
 #pragma unroll
         for (int i = 0; i < N / 8; ++i) reinterpret_cast<uint4*>(out)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
@@ -191,7 +200,14 @@ __device__ __forceinline__ long long ka_out_row(const KaParams& p, int b, int h,
     const int i = row / p.group, g = row - i * p.group;
     return ((long long)b * p.seqs.Q + i) * ((long long)p.cache.heads * p.group) + (long long)h * p.group + g;
 }
-__device__ __forceinline__ float ka_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f; }
+__device__ __forceinline__ float ka_lse(float ref, float l) { return l == 0.f ? -INFINITY : ((ref - kKaLow) + __log2f(l * 0x1p30f)) * 0.69314718055994531f; }
+// the inverse of a sum of weights; 0 where there are none, NaN where one is
+__device__ __forceinline__ float ka_inverse(float sum) { return sum != 0.f ? rcp_approx(sum) : 0.f; }
+__device__ __forceinline__ float pow2_of(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }      // -126 <= e <= 127
+__device__ __forceinline__ float inverse_pow2(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
+__device__ __forceinline__ int exponent_of(float x) { return (int)(__float_as_uint(x) >> 23) - 127; }       // x >= 0
+__device__ __forceinline__ uint32_t upper_halves(float x, float y) { return __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632); }
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) { uint32_t r; asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }
 
 // ---- the kernel ------------------------------------------------------------------------------------------------
 // E: the queries' type.  FINE: a half-precision weight is off by up to 2^-11 (2^-12.3 in the mean), times codes that lie between 0 and 15:
@@ -217,8 +233,10 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
     uint4* const s_q = QRING ? reinterpret_cast<uint4*>(ring_mem + (2 * S::kStages - 1) * S::kStage) : s_q_own;
     __shared__ __align__(8) float s_fr[ROWS], s_qs[NG][ROWS];
     __shared__ float s_m[kKaWarps][ROWS], s_l[kKaWarps][ROWS];
+    __shared__ __align__(8) float s_cs[kKaWarps][NG][ROWS];
     __shared__ float2 s_ml[ROWS];
-    __shared__ int s_pos[ROWS], s_out[ROWS], s_ask[ROWS], s_sum[kKaWarps], s_b, s_off;
+    __shared__ __align__(8) int s_ask[ROWS];
+    __shared__ int s_pos[ROWS], s_out[ROWS], s_sum[kKaWarps], s_b, s_off;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, j = lane & 3;
     wait_for_stream();
@@ -387,7 +405,7 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
                     s_fr[row] = big <= FLT_MAX ? p.scale2 * 1024.f * __uint_as_float((uint32_t)(127 + ex) << 23) : NAN;
                     s_pos[row] = min(last_pos, span.start + q_pos[n]);
                     s_out[row] = q_at[n];
-                    s_ask[row] = q_pos[n] < span.count;
+                    s_ask[row] = q_at[n] >= 0 && q_pos[n] < span.count;
                 }
                 // the order in which codes come out of a word
                 s_q[(((row >> 3) * NG + q_c / 8) * 2 + (q_c & 1)) * 32 + (row & 7) * 4 + (q_c % 8) / 2] =
@@ -396,26 +414,16 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
         }
         __syncthreads();
         uint4 qf[QREG ? NT : 1][QREG ? NG : 1][2];
-        float fr[QREG ? NT : 1][2], qs[QREG ? NT : 1][2][NG], mb[NT][2], l[NT][2], om[NT][2][NG], o[NT][NG * 4][4];    // mb: minus the running maximum
+        float fr[QREG ? NT : 1][2], qs[QREG ? NT : 1][2][NG];
+        if constexpr (QREG) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+            for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-            for (int col = 0; col < 2; ++col) {
-                mb[nt][col] = 0.f;
-                l[nt][col] = 0.f;
-#pragma unroll
-                for (int g = 0; g < NG; ++g) om[nt][col][g] = 0.f;
-                if constexpr (QREG) {
+                for (int col = 0; col < 2; ++col) {
                     fr[nt][col] = s_fr[nt * 8 + 2 * j + col];
 #pragma unroll
                     for (int g = 0; g < NG; ++g) qs[nt][col][g] = s_qs[g][nt * 8 + 2 * j + col];
                 }
-            }
-#pragma unroll
-            for (int n = 0; n < NG * 4; ++n)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) o[nt][n][k] = 0.f;
-            if constexpr (QREG) {
 #pragma unroll
                 for (int g = 0; g < NG; ++g)
 #pragma unroll
@@ -424,8 +432,10 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
         }
         const int pmin = s_pos[0], pmax = s_pos[ROWS - 1];
         if constexpr (QRING) __syncthreads();
-        uint32_t unset = (1u << (2 * NT)) - 1;              // rows that have seen no token yet, a bit per (nt, column)
-        float cs = 0x1p120f, ics = 0x1p-120f;               // the values' scales enter times this power of two; 1 / cs
+        float mb[NT][2], l[NT][2], om[NT][2][NG], o[NT][NG * 4][4];        // mb: minus the reference
+        uint32_t unset;                                     // rows that have seen no token yet, a bit per (nt, column)
+        float cs[NG];                                       // powers of two; with a row's own s_cs instead
+        auto cs_of = [&](int nt, int g) { return *reinterpret_cast<const f32x2*>(&s_cs[warp][g][nt * 8 + 2 * j]); };
 
         // tiles [lo, hi) of the unit's list are seen whole by all rows; two of this warp's at once if the first is in [lo, hi - 4)
         const int lo = p.window ? span.sinks + max(0, pmax - p.window + kKaTile) / kKaTile - span.first : 0;
@@ -498,159 +508,313 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
                 }
             }
         };
-        if (S::kStages - 1 < n_pairs) issue(S::kStages - 1, S::kStages - 1);
-        copies_commit();
-        float sc[NT][4 * SUB];
-        uint32_t vp[2 * SUB][NG], stage = ring;
-        int slot = 0;
-#pragma unroll 1
-        for (int k = 0; k < n_tiles; k += SUB) {
-            const int place = first + kKaWarps * k;
-            {
-                if (SUB == 2 || !(k & 1)) {
-                    copies_wait<S::kStages - 1>();
-                    __syncwarp();
+        // ---- all tiles; ROWWISE: with a cs of each row's own
+        auto sweep = [&](auto rowwise) {
+            constexpr bool ROWWISE = decltype(rowwise)::value;
+            unset = (1u << (2 * NT)) - 1;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) cs[g] = 1.f;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int col = 0; col < 2; ++col) {
+                    mb[nt][col] = 0.f;
+                    l[nt][col] = 0.f;
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) om[nt][col][g] = 0.f;
                 }
-                scores(stage, sc, vp);
-                // masks, where a tile needs them
-                if (place < lo || place + (SUB - 1) * kKaWarps >= hi) {
 #pragma unroll
-                    for (int u = 0; u < SUB; ++u) {
-                        const int tt = k + u < n_tiles ? span.tile(place + u * kKaWarps) * kKaTile : INT_MAX - kKaTile;
+                for (int n = 0; n < NG * 4; ++n)
 #pragma unroll
-                        for (int e = 2 * u; e < 2 * u + 2; ++e) {
-                            const int t = tt + (e & 1) * 8 + my_token;
-                            bool lost = false;                     // values of no use: rows that see the token become NaN by their score
+                    for (int k = 0; k < 4; ++k) o[nt][n][k] = 0.f;
+            }
+            float sc[NT][4 * SUB];
+            uint32_t vp[2 * SUB][NG], stage = ring;
+            int slot = 0;
+#pragma unroll 1
+            for (int k = 0; k < n_tiles; k += SUB) {
+                const int place = first + kKaWarps * k;
+                {
+                    if (SUB == 2 || !(k & 1)) {
+                        copies_wait<S::kStages - 1>();
+                        __syncwarp();
+                    }
+                    scores(stage, sc, vp);
+                    // masks, where a tile needs them
+                    if (place < lo || place + (SUB - 1) * kKaWarps >= hi) {
 #pragma unroll
-                            for (int g = 0; g < NG; ++g)
-                                lost = lost || !(scale_of(vp[e][g]) <= FLT_MAX) || !(fabsf(minimum_of(vp[e][g])) <= FLT_MAX);
-                            if (lost || t > pmax || (p.window && t >= p.sinks && t <= pmin - p.window)) {
+                        for (int u = 0; u < SUB; ++u) {
+                            const int tt = k + u < n_tiles ? span.tile(place + u * kKaWarps) * kKaTile : INT_MAX - kKaTile;
 #pragma unroll
-                                for (int g = 0; g < NG; ++g) vp[e][g] = 0;
-                            }
+                            for (int e = 2 * u; e < 2 * u + 2; ++e) {
+                                const int t = tt + (e & 1) * 8 + my_token;
+                                bool lost = false;                     // values of no use: rows that see the token become NaN by their score
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
+                                for (int g = 0; g < NG; ++g)
+                                    lost = lost || !(scale_of(vp[e][g]) <= FLT_MAX) || !(fabsf(minimum_of(vp[e][g])) <= FLT_MAX);
+                                if (lost || t > pmax || (p.window && t >= p.sinks && t <= pmin - p.window)) {
 #pragma unroll
-                                for (int col = 0; col < 2; ++col) {
-                                    const int pos = s_pos[nt * 8 + 2 * j + col];
-                                    float& v = sc[nt][2 * e + col];
-                                    if (lost) v = NAN;
-                                    if (t > pos || (p.window && t >= p.sinks && t <= pos - p.window)) v = -INFINITY;
+                                    for (int g = 0; g < NG; ++g) vp[e][g] = 0;
                                 }
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int col = 0; col < 2; ++col) {
+                                        const int pos = s_pos[nt * 8 + 2 * j + col];
+                                        float& v = sc[nt][2 * e + col];
+                                        if (lost) v = NAN;
+                                        if (t > pos || (p.window && t >= p.sinks && t <= pos - p.window)) v = -INFINITY;
+                                    }
+                            }
                         }
                     }
-                }
 
-                const float cap = ics * kKaScaleCap;
-                float most = sc[0][0], sv = 0.f;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int c = 0; c < 4 * SUB; ++c) most = fmaxf(most, sc[nt][c]);
-#pragma unroll
-                for (int e = 0; e < 2 * SUB; ++e)
-#pragma unroll
-                    for (int g = 0; g < NG; ++g) sv = fmaxf(sv, scale_of(vp[e][g]));
-                if (__any_sync(0xffffffffu, unset != 0 || most > kKaSlack || sv > cap)) {
-                    sv = across_max(sv);
-                    float ratio = 1.f;
-                    if (sv > cap) {                                    // >= 2^-117, a finite normal number: to between 2 and 4
-                        const int ex = (int)(__float_as_uint(sv) >> 23) - 127;
-                        ratio = __uint_as_float((uint32_t)(127 + 1 - ex) << 23) * ics;
-                        cs = __uint_as_float((uint32_t)(127 + 1 - ex) << 23);
-                        ics = __uint_as_float((uint32_t)(127 - 1 + ex) << 23);
-                    }
+                    float most = sc[0][0], bound = 0.f;
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int col = 0; col < 2; ++col) {
-                            float top = sc[nt][col];
-#pragma unroll
-                            for (int e = 1; e < 2 * SUB; ++e) top = fmaxf(top, sc[nt][2 * e + col]);
-                            top = across_max(top);
-                            const uint32_t bit = 1u << (2 * nt + col);
-                            float alpha = 1.f;
-                            if (top > kKaSlack || ((unset & bit) && top > -INFINITY)) {
-                                alpha = (unset & bit) ? 0.f : ex2_approx(-top);
-                                mb[nt][col] -= top;
-#pragma unroll
-                                for (int e = 0; e < 2 * SUB; ++e) sc[nt][2 * e + col] -= top;
-                                unset &= ~bit;
-                            }
-                            l[nt][col] *= alpha;
-#pragma unroll
-                            for (int g = 0; g < NG; ++g) om[nt][col][g] *= alpha;
-                            alpha *= ratio;
-#pragma unroll
-                            for (int n = 0; n < NG * 4; ++n) { o[nt][n][col] *= alpha; o[nt][n][2 + col] *= alpha; }
-                        }
-                }
-
-                f32x2 wt[NT][2 * SUB];
-                // weights
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2 * SUB; ++e) {
-                        const f32x2 w = pack2(ex2_approx(sc[nt][2 * e]), ex2_approx(sc[nt][2 * e + 1]));
-                        wt[nt][e] = w;
-                        const float2 sum = apart(add2(pack2(l[nt][0], l[nt][1]), w));
-                        l[nt][0] = sum.x; l[nt][1] = sum.y;
-#pragma unroll
-                        for (int g = 0; g < NG; ++g) {
-                            const float m = minimum_of(vp[e][g]);
-                            const float2 x = apart(fma2(w, pack2(m, m), pack2(om[nt][0][g], om[nt][1][g])));
-                            om[nt][0][g] = x.x; om[nt][1][g] = x.y;
-                        }
-                    }
-                // values
-#pragma unroll
-                for (int u = 0; u < SUB; ++u)
+                        for (int c = 0; c < 4 * SUB; ++c) most = fmaxf(most, sc[nt][c]);
+                    const float heaviest = ex2_approx(most);
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
-                        const float s0 = scale_of(vp[2 * u][g]) * cs, s1 = scale_of(vp[2 * u + 1][g]) * cs;
-                        uint32_t wf[NT][2];
+                        float sv = scale_of(vp[0][g]);
+#pragma unroll
+                        for (int e = 1; e < 2 * SUB; ++e) sv = fmaxf(sv, scale_of(vp[e][g]));
+                        if constexpr (!ROWWISE) bound = fmaxf(bound, sv * cs[g] * heaviest);
+                    }
+                    if (ROWWISE || __any_sync(0xffffffffu, unset != 0 || most > kKaTop || bound > kKaMost)) {
+                        const uint32_t fresh = unset;                  // rows without weights so far
+                        float top[NT][2];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int col = 0; col < 2; ++col) {
+                                top[nt][col] = sc[nt][col];
+#pragma unroll
+                                for (int e = 1; e < 2 * SUB; ++e) top[nt][col] = fmaxf(top[nt][col], sc[nt][2 * e + col]);
+                            }
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1)               // all rows' at once: their latencies overlap
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int col = 0; col < 2; ++col) top[nt][col] = fmaxf(top[nt][col], __shfl_xor_sync(0xffffffffu, top[nt][col], d));
+                        int raised[NT][2], lift = kKaFar;              // log2 of what weights shrink by; the least of it among rows that have weights
+                        float2 big[ROWWISE ? NT : 1][NG];              // the largest P s 2^18 here, of each row or of all
+#pragma unroll
+                        for (int nt = 0; nt < (ROWWISE ? NT : 1); ++nt)
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) big[nt][g] = make_float2(0.f, 0.f);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            const float2 a = apart(mul2(wt[nt][2 * u], pack2(s0, s0))), c = apart(mul2(wt[nt][2 * u + 1], pack2(s1, s1)));
-                            const uint32_t x = f16_pair(a.x, a.y), y = f16_pair(c.x, c.y);
-                            if constexpr (FINE) {
-                                const float2 fx = f16x2_to_float2(x), fy = f16x2_to_float2(y);
-                                const f32x2 less = pack2(-1.f, -1.f), middle = pack2(7.5f * ics, 7.5f * ics);
-                                const f32x2 lost = add2(fma2(pack2(fx.x, fx.y), less, pack2(a.x, a.y)), fma2(pack2(fy.x, fy.y), less, pack2(c.x, c.y)));
-                                unpack2(fma2(lost, middle, pack2(om[nt][0][g], om[nt][1][g])), om[nt][0][g], om[nt][1][g]);
+#pragma unroll
+                            for (int col = 0; col < 2; ++col) {
+                                const uint32_t bit = 1u << (2 * nt + col);
+                                const bool raise = top[nt][col] > -kKaLow || ((fresh & bit) && top[nt][col] > -INFINITY);
+                                const float d = raise ? ceilf(top[nt][col] + kKaLow) : 0.f;
+                                if (raise) unset &= ~bit;
+                                mb[nt][col] -= d;
+#pragma unroll
+                                for (int e = 0; e < 2 * SUB; ++e) sc[nt][2 * e + col] -= d;
+                                raised[nt][col] = (int)fminf(fmaxf(d, 0.f), (float)kKaFar);
+                                if (!(fresh & bit)) lift = min(lift, raised[nt][col]);
+                                const float alpha = (fresh & bit) || raised[nt][col] > 126 ? 0.f : pow2_of(-raised[nt][col]);
+                                l[nt][col] *= alpha;
+#pragma unroll
+                                for (int g = 0; g < NG; ++g) om[nt][col][g] *= alpha;
                             }
-                            wf[nt][0] = transpose_8x8(x);
-                            wf[nt][1] = transpose_8x8(y);
-                        }
-                        const uint32_t from = stage + u * S::kTileBytes + (get_v ^ (g << 5));
-                        const uint32_t wa = lds32(from), wb = lds32(from + 4 * RB), wc = lds32(from + 8 * RB), wd = lds32(from + 12 * RB);
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const uint32_t ab = __byte_perm(wa, wb, half ? 0x7632 : 0x5410), cd = __byte_perm(wc, wd, half ? 0x7632 : 0x5410);
+                            for (int e = 0; e < 2 * SUB; ++e) {
+                                const float wx = ex2_approx(sc[nt][2 * e] + 18.f), wy = ex2_approx(sc[nt][2 * e + 1] + 18.f);
 #pragma unroll
-                            for (int n = 0; n < 2; ++n) {
-                                const uint32_t xa = n ? ab >> 8 : ab, xc = n ? cd >> 8 : cd;
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) {
-                                    mma_f16(o[nt][g * 4 + half * 2 + n], xa & M0, xa & M1, xc & M0, xc & M1, wf[nt][0], wf[nt][1]);
+                                for (int g = 0; g < NG; ++g) {
+                                    float2& b = big[ROWWISE ? nt : 0][g];
+                                    b.x = fmaxf(b.x, wx * scale_of(vp[e][g]));
+                                    b.y = fmaxf(b.y, wy * scale_of(vp[e][g]));
                                 }
                             }
                         }
+                        auto scale_o = [&](int nt, int g, int col, int by) {        // times 2^by
+                            const float ratio = (fresh >> (2 * nt + col)) & 1 || by < -126 ? 0.f : pow2_of(min(by, 127));
+#pragma unroll
+                            for (int n = 0; n < 4; ++n) { o[nt][g * 4 + n][col] *= ratio; o[nt][g * 4 + n][2 + col] *= ratio; }
+                        };
+                        if constexpr (!ROWWISE) {
+                            float all[NG];
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) all[g] = fmaxf(big[0][g].x, big[0][g].y);
+                            lift = __reduce_min_sync(0xffffffffu, lift);
+#pragma unroll
+                            for (int g = 0; g < NG; ++g)           // not negative: ordered as whole numbers are
+                                all[g] = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(all[g])));
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) {
+                                const int before = exponent_of(cs[g]), size = exponent_of(all[g]) - 18;
+                                int power = before;
+                                // all weights so far have shrunk by 2^lift, from 2^15 at the most
+                                if (size + before >= 15) power = kKaGoal - size;
+                                else if (lift > 15 - kKaGoal) power = max(before, min(before + lift - (15 - kKaGoal), min(kKaGoal - size, 126)));
+                                cs[g] = pow2_of(power);
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int col = 0; col < 2; ++col) scale_o(nt, g, col, power - before - raised[nt][col]);
+                            }
+                        } else {
+                            uint32_t both[NT][NG];                     // the upper 16 bits of two rows' values
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int g = 0; g < NG; ++g) both[nt][g] = upper_halves(big[nt][g].x, big[nt][g].y);
+#pragma unroll
+                            for (int d = 4; d < 32; d <<= 1)
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int g = 0; g < NG; ++g) both[nt][g] = max_halves(both[nt][g], __shfl_xor_sync(0xffffffffu, both[nt][g], d));
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int g = 0; g < NG; ++g) {
+                                    float2* const own = reinterpret_cast<float2*>(&s_cs[warp][g][nt * 8 + 2 * j]);
+                                    const float2 was = *own;
+                                    float is[2];
+#pragma unroll
+                                    for (int col = 0; col < 2; ++col) {
+                                        const bool first = (fresh >> (2 * nt + col)) & 1;
+                                        const int before = exponent_of(col ? was.y : was.x), size = (int)((both[nt][g] >> (16 * col + 7)) & 255) - 127 - 18;
+                                        int power = first ? 126 : min(before + raised[nt][col], 126);
+                                        if (first || size + power >= 15) power = min(kKaRowGoal - size, 126);
+                                        scale_o(nt, g, col, power - before - raised[nt][col]);
+                                        is[col] = pow2_of(power);
+                                    }
+                                    __syncwarp();
+                                    if (r == 0) *own = make_float2(is[0], is[1]);
+                                }
+                            __syncwarp();
+                        }
                     }
-                if (SUB == 2 || (k & 1)) {               // the stage is done with
-                    __syncwarp();
-                    const int i = k / 2 + S::kStages;
-                    if (i < n_pairs) issue(i, slot);
-                    copies_commit();
-                    slot = slot == S::kStages - 1 ? 0 : slot + 1;
+
+                    // weights
+                    f32x2 wt[NT][2 * SUB];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2 * SUB; ++e) {
+                            const f32x2 w = pack2(ex2_approx(sc[nt][2 * e]), ex2_approx(sc[nt][2 * e + 1]));
+                            wt[nt][e] = w;
+                            const float2 sum = apart(add2(pack2(l[nt][0], l[nt][1]), w));
+                            l[nt][0] = sum.x; l[nt][1] = sum.y;
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) {
+                                const float m = minimum_of(vp[e][g]);
+                                const float2 x = apart(fma2(w, pack2(m, m), pack2(om[nt][0][g], om[nt][1][g])));
+                                om[nt][0][g] = x.x; om[nt][1][g] = x.y;
+                            }
+                        }
+                    // values
+#pragma unroll
+                    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) {
+                            const float up = ROWWISE ? 1.f : cs[g], s0 = scale_of(vp[2 * u][g]) * up, s1 = scale_of(vp[2 * u + 1][g]) * up;
+                            uint32_t wf[NT][2];
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                f32x2 w0 = wt[nt][2 * u], w1 = wt[nt][2 * u + 1];
+                                if constexpr (ROWWISE) { w0 = mul2(w0, cs_of(nt, g)); w1 = mul2(w1, cs_of(nt, g)); }
+                                const float2 a = apart(mul2(w0, pack2(s0, s0))), c = apart(mul2(w1, pack2(s1, s1)));
+                                const uint32_t x = f16_pair(a.x, a.y), y = f16_pair(c.x, c.y);
+                                if constexpr (FINE) {
+                                    const float2 fx = f16x2_to_float2(x), fy = f16x2_to_float2(y);
+                                    const float2 cu = ROWWISE ? apart(cs_of(nt, g)) : make_float2(cs[g], cs[g]);
+                                    const f32x2 less = pack2(-1.f, -1.f), middle = pack2(7.5f * inverse_pow2(cu.x), 7.5f * inverse_pow2(cu.y));
+                                    const f32x2 lost = add2(fma2(pack2(fx.x, fx.y), less, pack2(a.x, a.y)), fma2(pack2(fy.x, fy.y), less, pack2(c.x, c.y)));
+                                    unpack2(fma2(lost, middle, pack2(om[nt][0][g], om[nt][1][g])), om[nt][0][g], om[nt][1][g]);
+                                }
+                                wf[nt][0] = transpose_8x8(x);
+                                wf[nt][1] = transpose_8x8(y);
+                            }
+                            const uint32_t from = stage + u * S::kTileBytes + (get_v ^ (g << 5));
+                            const uint32_t wa = lds32(from), wb = lds32(from + 4 * RB), wc = lds32(from + 8 * RB), wd = lds32(from + 12 * RB);
+#pragma unroll
+                            for (int half = 0; half < 2; ++half) {
+                                const uint32_t ab = __byte_perm(wa, wb, half ? 0x7632 : 0x5410), cd = __byte_perm(wc, wd, half ? 0x7632 : 0x5410);
+#pragma unroll
+                                for (int n = 0; n < 2; ++n) {
+                                    const uint32_t xa = n ? ab >> 8 : ab, xc = n ? cd >> 8 : cd;
+#pragma unroll
+                                    for (int nt = 0; nt < NT; ++nt) {
+                                        mma_f16(o[nt][g * 4 + half * 2 + n], xa & M0, xa & M1, xc & M0, xc & M1, wf[nt][0], wf[nt][1]);
+                                    }
+                                }
+                            }
+                        }
+                    if (SUB == 2 || (k & 1)) {               // the stage is done with
+                        __syncwarp();
+                        const int i = k / 2 + S::kStages;
+                        if (i < n_pairs) issue(i, slot);
+                        copies_commit();
+                        slot = slot == S::kStages - 1 ? 0 : slot + 1;
+                    }
+                    stage = stage + SUB * S::kTileBytes == ring + S::kStages * S::kStage ? ring : stage + SUB * S::kTileBytes;
                 }
-                stage = stage + SUB * S::kTileBytes == ring + S::kStages * S::kStage ? ring : stage + SUB * S::kTileBytes;
             }
+            copies_wait<0>();
+        };
+        if (S::kStages - 1 < n_pairs) issue(S::kStages - 1, S::kStages - 1);
+        copies_commit();
+        sweep(std::false_type());
+
+        // ---- rows whose products were too small for the others' cs
+        constexpr int BITS = 2 * NT * NG, WORDS = BITS > 8 ? 2 : 1;        // a bit per row of this lane's and group; four lanes' side by side
+        const float least = (float)n_tiles * (kKaTile * 15 * 0x1p-33f);
+        uint32_t poor = 0;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const float limit = cs[g] < 0x1p126f ? least : 0.f;
+#pragma unroll
+                for (int col = 0; col < 2; ++col) {
+                    float even = o[nt][g * 4][col], odd = o[nt][g * 4][2 + col];          // c 2^-24, c 2^-20
+#pragma unroll
+                    for (int n = 1; n < 4; ++n) {
+                        even = fmaxf(even, o[nt][g * 4 + n][col]);
+                        odd = fmaxf(odd, o[nt][g * 4 + n][2 + col]);
+                    }
+                    poor |= (uint32_t)(fmaxf(even * 16.f, odd) < limit) << ((nt * NG + g) * 2 + col);
+                }
+            }
+        const int shift = BITS * (WORDS == 2 ? j & 1 : j);
+        uint32_t all = 0;
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {                   // in none of the eight lanes' dimensions
+            const uint32_t seen = __reduce_and_sync(0xffffffffu, WORDS == 2 && (j >> 1) != w ? ~0u : ~(((1u << BITS) - 1) << shift) | poor << shift);
+            if (WORDS == 1 || (j >> 1) == w) all = seen >> shift;
+        }
+        uint32_t asked = 0;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int2 ask = *reinterpret_cast<const int2*>(&s_ask[nt * 8 + 2 * j]);
+            const uint32_t rows = (uint32_t)(ask.x | ask.y << 1) & ~(unset >> (2 * nt)) & 3u;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) asked |= rows << ((nt * NG + g) * 2);
+        }
+        const bool rowwise = __any_sync(0xffffffffu, (all & asked) != 0);
+        if (rowwise) {
+            __syncwarp();
+#pragma unroll 1
+            for (int i = 0; i < S::kStages; ++i) {
+                if (i < n_pairs) issue(i, i);
+                copies_commit();
+            }
+            sweep(std::true_type());
         }
 
-        // ---- the warps' results together
-        copies_wait<0>();
+        // ---- the warps' results together: means by their own sums of weights, so that nothing is larger than a value
+        // [warp][row][D], pairs of a row in an order that goes by the row: what a warp stores at once lies in different banks
+        float2* const red = reinterpret_cast<float2*>(ring_mem);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -665,35 +829,37 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
             }
         __syncthreads();
         if (tid < ROWS) {
-            float top = -INFINITY, sum = 0.f;
+            float top = -INFINITY, sum = 0.f, f[kKaWarps];
 #pragma unroll
             for (int w = 0; w < kKaWarps; ++w) top = fmaxf(top, s_m[w][tid]);
 #pragma unroll
-            for (int w = 0; w < kKaWarps; ++w) sum = fmaf(s_l[w][tid], s_m[w][tid] == -INFINITY ? 0.f : ex2_approx(s_m[w][tid] - top), sum);
+            for (int w = 0; w < kKaWarps; ++w) {
+                f[w] = s_l[w][tid] * (s_m[w][tid] == -INFINITY ? 0.f : ex2_approx(s_m[w][tid] - top));
+                sum += f[w];
+            }
+            const float inv = ka_inverse(sum);
+#pragma unroll
+            for (int w = 0; w < kKaWarps; ++w) s_l[w][tid] = f[w] * inv;       // a warp's share of the row
             s_ml[tid] = make_float2(top, sum);
         }
-        // [warp][row][D], pairs of a row in an order that goes by the row: what a warp stores at once lies in different banks
-        float2* const red = reinterpret_cast<float2*>(ring_mem);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+            const float inv[2] = {ka_inverse(l[nt][0]), ka_inverse(l[nt][1])};
 #pragma unroll
-            for (int col = 0; col < 2; ++col) {
-                const int row = nt * 8 + 2 * j + col;
-                float top = -INFINITY;
+            for (int g = 0; g < NG; ++g) {
+                const float2 up = rowwise ? apart(cs_of(nt, g)) : make_float2(cs[g], cs[g]);
 #pragma unroll
-                for (int w = 0; w < kKaWarps; ++w) top = fmaxf(top, s_m[w][row]);
-                const float mine = s_m[warp][row], f = mine == -INFINITY ? 0.f : ex2_approx(mine - top);
-                const float even = f * ics;
-                float2* to = red + (warp * ROWS + row) * (D / 2) + r * 4;
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    const float shift = f * om[nt][col][g];
+                for (int col = 0; col < 2; ++col) {
+                    const int row = nt * 8 + 2 * j + col;
+                    const float down = inverse_pow2(col ? up.y : up.x), shift = om[nt][col][g] * inv[col];
+                    float2* to = red + (warp * ROWS + row) * (D / 2) + r * 4 + g * (kKvGroup / 2);
 #pragma unroll
                     for (int n = 0; n < 4; ++n)
-                        to[g * (kKvGroup / 2) + (n ^ j)] = make_float2(fmaf(o[nt][g * 4 + n][col] * 0x1p24f, even, shift),
-                                                                      fmaf(o[nt][g * 4 + n][2 + col] * 0x1p20f, even, shift));
+                        to[n ^ j] = make_float2(fmaf(o[nt][g * 4 + n][col] * (inv[col] * 0x1p24f), down, shift),
+                                                fmaf(o[nt][g * 4 + n][2 + col] * (inv[col] * 0x1p20f), down, shift));
                 }
             }
+        }
         __syncthreads();
         const bool whole = c1 - c0 == chunks;
         const long long part = (long long)blockIdx.x * 2 + (c0 == 0);
@@ -709,24 +875,23 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
 #pragma unroll
             for (int w = 0; w < kKaWarps; ++w) {
                 const float2* from = red + (w * ROWS + in_block) * (D / 2) + d0 / 2;
+                const float f = s_l[w][in_block];
 #pragma unroll
                 for (int n = 0; n < PER / 2; ++n) {
                     // d0 / 2 + n with the two low bits turned by the row's
                     const float2 x = PER >= 8 ? from[n ^ ((in_block >> 1) & 3)] : red[(w * ROWS + in_block) * (D / 2) + ((d0 / 2 + n) ^ ((in_block >> 1) & 3))];
-                    v[2 * n] += x.x;
-                    v[2 * n + 1] += x.y;
+                    v[2 * n] = fmaf(x.x, f, v[2 * n]);
+                    v[2 * n + 1] = fmaf(x.y, f, v[2 * n + 1]);
                 }
             }
             if (whole) {
                 const bool asked = s_ask[in_block];
                 const long long orow = (long long)b * p.seqs.Q * (p.cache.heads * p.group) + place;
-                float f = asked && ml.y != 0.f ? rcp_approx(ml.y) : 0.f;
-                if (asked && span.bad) f = NAN;
-                if (!asked) {
+                if (!asked || span.bad) {
 #pragma unroll
-                    for (int n = 0; n < PER; ++n) v[n] = 0.f;
+                    for (int n = 0; n < PER; ++n) v[n] = asked ? NAN : 0.f;
                 }
-                ka_store<E, PER>(reinterpret_cast<E*>(p.out) + orow * D + d0, v, f);
+                ka_store<E, PER>(reinterpret_cast<E*>(p.out) + orow * D + d0, v);
                 if (p.lse && (tid & 15) == 0) p.lse[orow] = !asked ? -INFINITY : span.bad ? NAN : ka_lse(ml.x, ml.y);
             } else {
                 float* to = p.part_o + (part * ROWS + in_block) * D + d0;
@@ -784,14 +949,16 @@ __global__ void __launch_bounds__(kKaJoinRows * kKaJoinWarps * 32) ears_kv_join_
         float most = fmaxf(top, ml.x);
 #pragma unroll
         for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-        const float before = top == -INFINITY ? 0.f : ex2_approx(top - most), f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - most);
+        const float had = sum * (top == -INFINITY ? 0.f : ex2_approx(top - most));
+        float f = ml.y * (ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - most)), part = f;
         top = most;
-        float part = ml.y * f;
 #pragma unroll
         for (int d = 16; d; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
-        sum = fmaf(sum, before, part);
+        sum = had + part;
+        const float inv = ka_inverse(sum);                 // v stays a mean
+        f *= inv;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) v[i] *= before;
+        for (int i = 0; i < PER; ++i) v[i] *= had * inv;
         for (int m0 = 0; m0 < count; m0 += 8) {
             if (m0) fetch(n0 + m0, count - m0);
 #pragma unroll
@@ -815,14 +982,15 @@ __global__ void __launch_bounds__(kKaJoinRows * kKaJoinWarps * 32) ears_kv_join_
         if (mine) return;
         float most = top;
         for (int w = 1; w < warps; ++w) most = fmaxf(most, s_ml[w][warp].x);
-        const float f0 = top == -INFINITY ? 0.f : ex2_approx(top - most);
-        sum *= f0;
+        auto share = [&](float2 ml) { return ml.y * (ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - most)); };
+        const float f0 = share(make_float2(top, sum));
+        sum = f0;
+        for (int w = 1; w < warps; ++w) sum += share(s_ml[w][warp]);
+        const float inv = ka_inverse(sum);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) v[i] *= f0;
+        for (int i = 0; i < PER; ++i) v[i] *= f0 * inv;
         for (int w = 1; w < warps; ++w) {
-            const float2 ml = s_ml[w][warp];
-            const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - most);
-            sum = fmaf(ml.y, f, sum);
+            const float f = share(s_ml[w][warp]) * inv;
 #pragma unroll
             for (int i = 0; i < PER; ++i) v[i] = fmaf(s_v[w - 1][warp][i * 32 + lane], f, v[i]);
         }
@@ -835,7 +1003,7 @@ __global__ void __launch_bounds__(kKaJoinRows * kKaJoinWarps * 32) ears_kv_join_
         for (int i = 0; i < PER; ++i) v[i] = 0.f;
     }
     const long long orow = ka_out_row(p, b, h, row);
-    ka_store<E, PER>(reinterpret_cast<E*>(p.out) + orow * D + lane * PER, v, asked && sum != 0.f ? rcp_approx(sum) : 0.f);
+    ka_store<E, PER>(reinterpret_cast<E*>(p.out) + orow * D + lane * PER, v);
     if (p.lse && lane == 0) p.lse[orow] = asked ? ka_lse(top, sum) : -INFINITY;
 }
 
