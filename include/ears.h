@@ -612,8 +612,8 @@ int ears_kv_read(int dtype, const ears_kv_cache* cache, int B, int Q, const int3
  *   out = sum_t softmax_t(scale q . k_t) v_t,    out_lse = ln sum_t exp(scale q . k_t)   (optional)
  * q [B, Q, heads_q, head_dim] bfloat16 or half precision; query head n reads head n / (heads_q / cache->heads).  out, of q's type,
  * [B, Q, heads_q, head_dim] contiguous, 16-byte aligned; out_lse [B, Q, heads_q].  They must not overlap the inputs.
- * Positions that are left out get zeros and -inf.  A NaN or infinity in a row of q, or a NaN read from a token that it sees, makes
- * that row NaN and no other.
+ * Positions that are left out get zeros and -inf.  A NaN or infinity in a row of q, or a NaN (of values, an infinity too) read from a token
+ * that it sees, makes that row and its out_lse NaN, in all dimensions, and no other.
  * Scores, their sums (n / 32 weights one after the other, for n tokens) and the results are kept in 32 bits; q is taken as it is, or, where its
  * row spans more than 2^25, to within 2^-26 of the row's largest element.  Weights times scales, p s, enter the second product in half precision,
  * whose range follows the row's and group's own products: what that loses of sum_t p_t s_t c_t is at most 2^-11 of it and 2^-11 of 7.5 sum_t p_t s_t,

@@ -822,6 +822,10 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
                 l[nt][col] = across_sum(l[nt][col]);
 #pragma unroll
                 for (int g = 0; g < NG; ++g) om[nt][col][g] = across_sum(om[nt][col][g]);
+                // a token seen that is not finite in one group makes the row NaN in all, as where masks are looked at
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+                    if (!(fabsf(om[nt][col][g]) <= FLT_MAX) || !(fabsf(o[nt][g * 4][col]) <= FLT_MAX)) l[nt][col] = NAN;
                 if (r == 0) {
                     s_m[warp][nt * 8 + 2 * j + col] = (unset >> (2 * nt + col)) & 1 ? -INFINITY : -mb[nt][col];
                     s_l[warp][nt * 8 + 2 * j + col] = l[nt][col];

@@ -1,4 +1,4 @@
-"""Attention over the 4-bit cache where values' scales, minima and weights differ by powers of two.
+"""Attention over the 4-bit cache where values' scales, minima and weights differ by powers of two, and where parameters are not finite.
 
 Tolerances as in test_gpu_kv.py, but for two terms.  A relative error e in every weight moves a result by at most 2 e drift with drift =
 sum_t p_t |v_t - out| (not the farthest token's distance).  Where a block has a row's tokens to itself, its 32 lanes of a row add n / 32
@@ -196,3 +196,24 @@ def test_constant_groups(ears, D):
     params[:, 1, 0, :, 0][flat] = torch.tensor([2.0 ** -126, -3.25], dtype=torch.bfloat16)
     codes[:, 1, 0, :, :32][flat] = 0
     check(ears, ask(2, 2, D, "bf16"), codes, params, pages, n - 2, "bf16")
+
+
+# ---- parameters that are not finite ----------------------------------------------------------------------
+
+@pytest.mark.parametrize("table_extra", [0, 3000])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("token", [10, 200, 296, 298])
+@pytest.mark.parametrize("what", ["scale", "minimum", "both", "infinite scale", "infinite minimum"])
+def test_a_nan_in_one_group_of_values_takes_the_whole_row(ears, D, token, what, table_extra):
+    """Wherever the token stands, in a part that all rows see or in one that only some do."""
+    n, Q, page = 300, 5, 16
+    codes, params, pages, g = pool(n, D, page, 12, torch.randn(n, generator=torch.Generator().manual_seed(1)))
+    at = place(pages, token, page)
+    bad = {"scale": (math.nan, 0.5), "minimum": (0.5, math.nan), "both": (math.nan, math.nan), "infinite scale": (math.inf, 0.5),
+           "infinite minimum": (0.5, -math.inf)}[what]
+    params[at[0], 1, 0, at[1], D // 64 - 1] = torch.tensor(bad, dtype=torch.bfloat16)
+    for heads, copies in ((1, 1), (6, 1), (1, 450), (6, 450)):
+        got, lse = call(ears, ask(Q, heads, D, "bf16"), codes, params, pages, n - Q, copies, table_extra)
+        first = max(0, token - (n - Q))                     # rows from here on see it
+        assert got[:, first:].isnan().all() and lse[:, first:].isnan().all()
+        assert got[:, :first].isfinite().all() and lse[:, :first].isfinite().all()
