@@ -167,10 +167,12 @@ int make_plan(int dtype, const ears_kv_cache* c, int B, int Q, int heads_q, int 
     long long tokens = (long long)width * c->page_size;
     if (window && (long long)window + sinks + Q + 3 * kKaTile < tokens) tokens = (long long)window + sinks + Q + 3 * kKaTile;
     const long long chunks = (tokens + kKaChunk - 1) / kKaChunk;
-    // Up to 16 chunks per SM, latency counts, and blocks of one eight are done soonest, although each reads the cache (5 positions of one
-    // sequence, 32 / 8 heads of 128: 1000 tokens 13.2 us with one block of three eights, 11.8 with three of one; 3500 tokens 20.3,
-    // 13.9; 9 positions 16.2, 11.6; 4 sequences of up to 3000: 17.9, 16.3; 8 of up to 4096, 28 per SM: 22.2, 23.7).
-    const bool few = (long double)B * c->heads * chunks <= 16.0L * sms;
+    // Few chunks are bound by latency, and blocks of one eight are done soonest, although each reads the cache: up to 16 chunks per SM, 64
+    // counting every block's.  Blocks of one eight and those of choose_rows, us, 8 heads of 128: 3 eights of rows, 1000 tokens (2.6 counting
+    // every block's) 12.3 and 13.8, 4000 (10) 14.9 and 20.6; 9 eights, 8000 tokens (61) 25.9 and 28.2; 33 eights, 2000 tokens (57) 26.7 and 25.7,
+    // 4000 (112) 39.5 and 34.5, 16000 (446) 112 and 82; 2 eights, 4 sequences of 8000 (54, but 27 chunks) 25.1 and 23.1.
+    const long double work = (long double)B * c->heads * chunks;
+    const bool few = work <= 16.0L * sms && work * tiles <= 64.0L * sms;
     with_dim(c->head_dim, [&](auto d) {
         constexpr int D = decltype(d)::value;
         const int nt = few ? 1 : choose_rows<D>(tiles);

@@ -217,3 +217,31 @@ def test_a_nan_in_one_group_of_values_takes_the_whole_row(ears, D, token, what, 
         first = max(0, token - (n - Q))                     # rows from here on see it
         assert got[:, first:].isnan().all() and lse[:, first:].isnan().all()
         assert got[:, :first].isfinite().all() and lse[:, :first].isfinite().all()
+
+
+# ---- rows per block ---------------------------------------------------------------------------------------
+
+def eights_per_block(ears, D, H, B, Q, group, tokens, window=0, sinks=0):
+    """As the workspace shows: two parts of a block's rows for every resident CTA, three per SM with one eight of up to 128 dimensions, else two."""
+    import ctypes
+    from paper_2512_13194_b200.binding import KvCacheStruct
+    cache = KvCacheStruct(256, 256, 10, H, 64, D)          # nothing is read
+    need = ears.load_library().ears_kv_attention_workspace_bytes(1, ctypes.byref(cache), B, Q, H * group, -(-tokens // 64), window, sinks)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    for nt in (1, 2, 3, 4):
+        grid = sms * (3 if nt == 1 and D <= 128 else 2)
+        if 0 <= need - grid * (16 + 2 * nt * 8 * (8 + 4 * D)) < 3 * 256:
+            return nt
+    return need
+
+
+def test_rows_per_block_go_by_all_blocks_chunks(ears):
+    for D in (64, 128, 256):
+        assert eights_per_block(ears, D, 8, 1, 5, 4, 16000) == 1                # 3 eights, 13.5 chunks per SM
+        assert eights_per_block(ears, D, 8, 1, 33, 8, 2000) == 1                # 33 eights of 1.7
+        for B, Q, tokens in ((1, 33, 4000), (1, 33, 18900), (12, 33, 1000), (4, 66, 2000)):
+            assert eights_per_block(ears, D, 8, B, Q, 8, tokens) in (2, 3, 4)
+    assert eights_per_block(ears, 128, 8, 128, 5, 4, 9001) == 3
+    assert eights_per_block(ears, 64, 8, 32, 8, 8, 20000, 1024, 4) == 4
+    assert eights_per_block(ears, 64, 8, 1, 5, 4, 131072) == 3                  # the table's width counts
+    assert eights_per_block(ears, 64, 8, 1, 5, 4, 131072, 1000, 4) == 1         # but no more of it than a window shows
