@@ -222,7 +222,8 @@ def test_a_nan_in_one_group_of_values_takes_the_whole_row(ears, D, token, what, 
 # ---- rows per block ---------------------------------------------------------------------------------------
 
 def eights_per_block(ears, D, H, B, Q, group, tokens, window=0, sinks=0):
-    """As the workspace shows: two parts of a block's rows for every resident CTA, three per SM with one eight of up to 128 dimensions, else two."""
+    """As the workspace shows: two parts of a block's rows for every resident CTA, three per SM with one eight of up to 128 dimensions, else two (for calls
+    that fill them)."""
     import ctypes
     from paper_2512_13194_b200.binding import KvCacheStruct
     cache = KvCacheStruct(256, 256, 10, H, 64, D)          # nothing is read
@@ -244,4 +245,4 @@ def test_rows_per_block_go_by_all_blocks_chunks(ears):
     assert eights_per_block(ears, 128, 8, 128, 5, 4, 9001) == 3
     assert eights_per_block(ears, 64, 8, 32, 8, 8, 20000, 1024, 4) == 4
     assert eights_per_block(ears, 64, 8, 1, 5, 4, 131072) == 3                  # the table's width counts
-    assert eights_per_block(ears, 64, 8, 1, 5, 4, 131072, 1000, 4) == 1         # but no more of it than a window shows
+    assert eights_per_block(ears, 64, 8, 1, 5, 4, 131072, 4000, 4) == 1         # but no more of it than a window shows
