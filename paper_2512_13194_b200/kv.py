@@ -221,11 +221,22 @@ def kv_attention(q: torch.Tensor, cache: KVCache, pages: torch.Tensor, start: to
     return (out, sums) if lse else out
 
 
+def _check_start(start, shape, index) -> None:
+    """What kv_advance can move in place."""
+    if start.dtype not in (torch.int32, torch.int64) or tuple(start.shape) != tuple(shape) or start.get_device() != index:
+        raise ValueError("start must be an integer tensor of accept_len's shape and device")
+    if any(n > 1 and s == 0 for n, s in zip(start.shape, start.stride())):
+        raise ValueError("start must have an element of its own for every sequence")
+    if start.is_inference() and not torch.is_inference_mode_enabled():
+        raise ValueError("start was made in inference mode and cannot be moved outside of it")
+
+
 def kv_advance(start: torch.Tensor, accept_len: torch.Tensor, *, stream=None) -> torch.Tensor:
     """``start`` [B], in place, behind the tokens that a verification step keeps: the one before the drafts and ``accept_len`` drafts; the
     token it emits last has not been through the model yet.  An unusable sequence (-1) stays where it is."""
-    if start.dtype not in (torch.int32, torch.int64) or start.shape != accept_len.shape or start.get_device() != accept_len.get_device():
-        raise ValueError("start must be an integer tensor of accept_len's shape and device")
+    _check_start(start, accept_len.shape, accept_len.get_device())
+    if accept_len.dtype not in (torch.int32, torch.int64):
+        raise TypeError("accept_len must hold integers")
     if stream is None:
         return start.add_(accept_len).add_(1)
     with torch.cuda.stream(stream):

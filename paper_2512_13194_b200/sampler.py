@@ -78,6 +78,8 @@ class EarsSampler:
         (CUDA tensors).  Asynchronous on ``stream``; the returned tensors are ready once it is.
         kv_start: [B] where the pass that made these logits began in the key/value cache (``kv_write``'s ``start``); it is
         moved, in place, behind the tokens that the step keeps."""
+        if kv_start is not None:         # before anything is launched: a step that is refused has used no random numbers
+            kv._check_start(kv_start, draft_tokens.shape[:1], target_logits.get_device())
         T, seq_T = self._split(self.temperature)
         beta, seq_beta = self._split(self.beta)
         out = binding.verify(target_logits, draft_logits, draft_tokens, T, beta if seq_beta is None else 0.0,
