@@ -235,7 +235,7 @@ def kv_advance(start: torch.Tensor, accept_len: torch.Tensor, *, stream=None) ->
     """``start`` [B], in place, behind the tokens that a verification step keeps: the one before the drafts and ``accept_len`` drafts; the
     token it emits last has not been through the model yet.  An unusable sequence (-1) stays where it is."""
     _check_start(start, accept_len.shape, accept_len.get_device())
-    if accept_len.dtype not in (torch.int32, torch.int64):
+    if accept_len.dtype.is_floating_point or accept_len.dtype.is_complex or accept_len.dtype is torch.bool:
         raise TypeError("accept_len must hold integers")
     if stream is None:
         return start.add_(accept_len).add_(1)

@@ -33,4 +33,4 @@ def test_advance_refuses_lengths_that_are_no_integers():
             ears.kv_advance(start, bad)
     with pytest.raises(ValueError):
         ears.kv_advance(start[:1].expand(3), torch.zeros(3, dtype=torch.int32))
-    assert start.tolist() == [0, 0, 0]
+    assert ears.kv_advance(start, torch.tensor([1, 0, -1], dtype=torch.int16)).tolist() == [2, 1, 0]
