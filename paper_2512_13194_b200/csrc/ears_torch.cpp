@@ -359,6 +359,7 @@ bool on(const at::Tensor* t, int device, at::ScalarType type) { return t->is_cud
 bool take_cache(Args& a, Kv* kv) {
     const at::Tensor *codes = a.tensor(false), *params = a.tensor(false);
     if (!a.plain || !codes->is_cuda() || codes->dim() != 5 || params->dim() != 6) return false;
+    if (params->requires_grad() && c10::GradMode::is_enabled()) return false;        // refused by the wrapper
     kv->device = codes->get_device();
     if (c10::cuda::current_device() != kv->device) return false;
     if (codes->scalar_type() != at::kByte || !on(params, kv->device, at::kBFloat16) || !codes->is_contiguous() || !params->is_contiguous()) return false;

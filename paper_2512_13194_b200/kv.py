@@ -8,7 +8,7 @@ moves ``start`` there without a word to the host.  What was written behind is ov
 
 ``pages`` [B, W], ``start`` [B] and ``counts`` [B] (optional) are integer CUDA tensors, int32 where nothing is to be converted (integers
 that 32 bits cannot hold stay unusable); keys, values and queries are used where they lie as long as the elements of a head
-are contiguous.  Serving only: inputs that require a gradient are refused.
+are contiguous.  Serving only: inputs that require a gradient, a cache's ``params`` among them, are refused.
 ``status``: optional int32 CUDA tensor of one element that gets EARS_DEV_INVALID_INPUT OR-ed in where a position lies outside the
 page table or a page outside the pool.
 """
@@ -151,7 +151,7 @@ def kv_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, pages: torch.Tens
         return _on_stream(stream, cache, kv_write, cache, k, v, pages, start, counts, status=status)
     if _plain().kv_write(cache[0], cache[1], k, v, pages, start, counts, status):
         return
-    _refuse_gradients(k, v)
+    _refuse_gradients(k, v, *cache)
     c = _Call(cache, pages, start, counts, status)
     code = _DTYPES.get(k.dtype)
     if code is None or v.dtype != k.dtype:
@@ -172,6 +172,7 @@ def kv_read(cache: KVCache, pages: torch.Tensor, start: torch.Tensor, tokens: in
     out = _plain().kv_read(cache[0], cache[1], pages, start, tokens, counts, _DTYPES.get(dtype), status)
     if out is not None:
         return out
+    _refuse_gradients(*cache)
     c = _Call(cache, pages, start, counts, status)
     if dtype not in _DTYPES:
         raise TypeError(f"values can be read as float32, bfloat16 or float16, not {dtype}")
@@ -197,7 +198,7 @@ def kv_attention(q: torch.Tensor, cache: KVCache, pages: torch.Tensor, start: to
     out = _plain().kv_attention(cache[0], cache[1], q, pages, start, counts, scale, window, sinks, bool(lse), status)
     if out is not None:
         return out if lse else out[0]
-    _refuse_gradients(q)
+    _refuse_gradients(q, *cache)
     if scale is None:
         scale = q.shape[-1] ** -0.5 if q.dim() and q.shape[-1] else 1.0
     c = _Call(cache, pages, start, counts, status)

@@ -246,3 +246,31 @@ def test_rows_per_block_go_by_all_blocks_chunks(ears):
     assert eights_per_block(ears, 64, 8, 32, 8, 8, 20000, 1024, 4) == 4
     assert eights_per_block(ears, 64, 8, 1, 5, 4, 131072) == 3                  # the table's width counts
     assert eights_per_block(ears, 64, 8, 1, 5, 4, 131072, 4000, 4) == 1         # but no more of it than a window shows
+
+
+# ---- gradients ---------------------------------------------------------------------------------------------
+
+def test_a_cache_that_requires_a_gradient_is_refused(ears):
+    from torch.autograd import forward_ad
+    codes, params, pages, g = pool(40, 64, 16, 13)
+    plain = ears.KVCache(codes.to(DEV), params.to(DEV))
+    k, q = torch.randn(1, 3, 1, 64, generator=g).to(DEV), ask(3, 2, 64, "bf16").to(DEV)
+    at = (pages.to(DEV), ints([20]))
+    want = ears.kv_attention(q, plain, *at)
+
+    def calls(cache):
+        return (lambda: ears.kv_attention(q, cache, *at), lambda: ears.kv_read(cache, *at, 3), lambda: ears.kv_write(cache, k, k, *at),
+                lambda: ears.kv_attention(q, cache, at[0].long(), at[1]))
+
+    cache = ears.KVCache(plain.codes, plain.params.clone().requires_grad_())
+    for call in calls(cache):
+        with pytest.raises(NotImplementedError):
+            call()
+    with torch.no_grad():
+        assert torch.equal(ears.kv_attention(q, cache, *at), want)
+        ears.kv_write(cache, k, k, *at)
+        assert torch.equal(*ears.kv_read(cache, *at, 3))
+    with forward_ad.dual_level():
+        for call in calls(ears.KVCache(plain.codes, forward_ad.make_dual(plain.params, torch.ones_like(plain.params)))):
+            with pytest.raises(NotImplementedError):
+                call()
