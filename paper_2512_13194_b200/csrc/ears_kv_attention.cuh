@@ -99,7 +99,7 @@ __device__ __forceinline__ KaSpan ka_span(const KaParams& p, int b) {
     s.count = kv_count(p.seqs, b);
     s.bad = s.count > 0 && (s.start < 0 || (long long)s.start + s.count > (long long)p.seqs.width * p.cache.page);
     s.sinks = s.first = s.tiles = 0;
-    if (s.bad) s.start = 0;               // no tile is looked at, and no position that passes 31 bits formed
+    if (s.bad || s.count == 0) s.start = 0;      // no tile is looked at, and no position that passes 31 bits formed
     if (s.count > 0 && !s.bad) {
         const int last = (s.start + s.count - 1) / kKaTile;
         if (p.window) {
