@@ -139,23 +139,33 @@ struct KaPlan { Variant v; int blocks, grid; };
 int resident(const Variant& v, int* ctas) {
     static std::mutex mutex;
     static std::map<std::pair<const void*, int>, int> known;
-    int dev = 0, sms = 0;
+    int dev = 0, sms = 0, per_sm = 0;
+    const char* what = "cudaGetDevice";
     cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return host_cuda_fail(e, "cudaGetDevice");
-    const int rc = host_device_sms(&sms);
-    if (rc) return rc;
-    std::lock_guard<std::mutex> lock(mutex);
-    int& n = known[{(const void*)v.attention, dev}];
-    if (!n) {
-        e = cudaFuncSetAttribute((const void*)v.attention, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)v.smem);
-        if (e != cudaSuccess) return host_cuda_fail(e, "cudaFuncSetAttribute");
-        int per_sm = 0;
-        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, v.attention, kKaThreads, v.smem);
-        if (e != cudaSuccess) return host_cuda_fail(e, "cudaOccupancyMaxActiveBlocksPerMultiprocessor");
-        n = sms * (per_sm < 1 ? 1 : per_sm);
+    if (e == cudaSuccess) {
+        const int rc = host_device_sms(&sms);
+        if (rc) return rc;
+        try {
+            std::lock_guard<std::mutex> lock(mutex);
+            int& n = known[{(const void*)v.attention, dev}];
+            if (!n) {
+                what = "cudaFuncSetAttribute";
+                e = cudaFuncSetAttribute((const void*)v.attention, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)v.smem);
+                if (e == cudaSuccess) {
+                    what = "cudaOccupancyMaxActiveBlocksPerMultiprocessor";
+                    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, v.attention, kKaThreads, v.smem);
+                }
+                if (e == cudaSuccess) n = sms * (per_sm < 1 ? 1 : per_sm);
+            }
+            *ctas = n;
+        } catch (...) {                   // the host is out of memory, or its lock failed: no exception passes the C entry
+            what = "the table of resident CTAs";
+            e = cudaErrorMemoryAllocation;
+        }
     }
-    *ctas = n;
-    return EARS_OK;
+    if (e == cudaSuccess) return EARS_OK;
+    (void)cudaGetLastError();
+    return host_cuda_fail(e, what);
 }
 
 int make_plan(int dtype, const ears_kv_cache* c, int B, int Q, int heads_q, int width, int window, int sinks, KaPlan* plan) {
