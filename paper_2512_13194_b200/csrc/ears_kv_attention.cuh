@@ -574,13 +574,14 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int c = 0; c < 4 * SUB; ++c) most = fmaxf(most, sc[nt][c]);
-                    const float heaviest = ex2_approx(most);
+                    const float heaviest = fmaxf(ex2_approx(most), kKaMost * 0x1p-126f);       // so that s cs alone stays below 2^126, too
+                    float sv[NG];
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
-                        float sv = scale_of(vp[0][g]);
+                        sv[g] = 0.f;
 #pragma unroll
-                        for (int e = 1; e < 2 * SUB; ++e) sv = fmaxf(sv, scale_of(vp[e][g]));
-                        if constexpr (!ROWWISE) bound = fmaxf(bound, sv * cs[g] * heaviest);
+                        for (int e = 0; e < 2 * SUB; ++e) sv[g] = fmaxf(sv[g], scale_of(vp[e][g]));
+                        bound = fmaxf(bound, sv[g] * cs[g] * heaviest);
                     }
                     if (ROWWISE || __any_sync(0xffffffffu, unset != 0 || most > kKaTop || bound > kKaMost)) {
                         const uint32_t fresh = unset;                  // rows without weights so far
@@ -650,10 +651,12 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
 #pragma unroll
                             for (int g = 0; g < NG; ++g) {
                                 const int before = exponent_of(cs[g]), size = exponent_of(all[g]) - 18;
+                                const int limit = 124 - exponent_of(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sv[g]))));
+                                const int goal = min(kKaGoal - size, min(limit, 126));
                                 int power = before;
                                 // all weights so far have shrunk by 2^lift, from 2^15 at the most
-                                if (size + before >= 15) power = kKaGoal - size;
-                                else if (lift > 15 - kKaGoal) power = max(before, min(before + lift - (15 - kKaGoal), min(kKaGoal - size, 126)));
+                                if (size + before >= 15 || before > limit) power = goal;
+                                else if (lift > 15 - kKaGoal) power = max(before, min(before + lift - (15 - kKaGoal), goal));
                                 cs[g] = pow2_of(power);
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt)

@@ -187,6 +187,20 @@ def test_large_and_small_values(ears, D, heads, table_extra, size, n):
     check(ears, ask(1, heads, D, "bf16"), codes, params, pages, n - 1, "bf16", table_extra=table_extra)
 
 
+@pytest.mark.parametrize("D,heads", [(64, 2), (128, 5), (256, 8)])
+@pytest.mark.parametrize("at", [0, 5, 1000])
+def test_a_token_without_any_weight_beside_tiny_values(ears, D, heads, at):
+    """Its scale times the power of two that the others' take would pass 2^127."""
+    n = 2000
+    keys = torch.zeros(n)
+    keys[at] = -1000.0
+    codes, params, pages, g = pool(n, D, 16, 14, keys)
+    params[:, 1] = (params[:, 1].float() * 2.0 ** -80).bfloat16()
+    slot = place(pages, at, 16)
+    params[slot[0], 1, 0, slot[1]] = torch.tensor([2.0 ** 100, 1.0], dtype=torch.bfloat16)
+    check(ears, ask(1, heads, D, "bf16"), codes, params, pages, n - 1, "bf16")
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_constant_groups(ears, D):
     """Scales of 2^-126, all that counts is in the minima, beside tokens of ordinary groups."""
