@@ -41,15 +41,16 @@ constexpr int kKaAhead = 8;                         // what starting and ending 
 // A row's weights are P = 2^(score - reference).  The reference, a whole number, is raised when a P passes 2^-18, to where the largest is
 // between 2^-31 and 2^-30: their sums with minima up to the type's largest number stay finite, and minima down to 2^-100 keep their bits.
 // The second product's half-precision operands are P s cs, with a power of two cs for each group that goes by the largest P s of a warp's tiles: it
-// brings that to between 2^4 and 2^5 when one may pass 2^15.  Not by the largest s, which may be that of a token of no weight (131072 tokens, one of them
-// with values 4096 times the others' and a weight of e^-60: an error of 0.08 of the result that way, 0.0015 this way, its own rounding).  What falls below half precision's normal numbers
-// is off by 2^-25 at most, so that a warp's n tokens are right to 2^-12 of a row's sum of P s cs as long as the largest of its
-// sums of P s cs c is 15 n 2^-13 or more.  That is looked at when the unit's tiles are through; where a row has less, as one that does not see a token whose
-// large values another row's result is made of, the warp takes its tiles once more with a cs of each row's own (a batch where every last draft is such a token, 128 x 5 positions: 615 us beside 248).
-// A lower goal than 2^4 leaves no room for rows that differ, a higher one has the powers set again more often: 2^6 250 us, 2^8 254, where 2^4 takes 246.
+// brings that to 2^4 (2^6 to 2^10 for 8192 to 131072 tokens of a warp) when one may pass 2^15.  Not by the largest s, which may be that of a token of no
+// weight (131072 tokens, one of them with values 4096 times the others' and a weight of e^-60: an error of 0.08 of the result that way, 0.0015 this
+// way, its own rounding).  What falls below half precision's normal numbers is off by 2^-25 at most, so that a warp's n tokens are right to 2^-12 of a
+// row's sum of P s cs as long as the largest of its sums of P s cs c is 15 n 2^-13 or more.  That is looked at when the unit's tiles are through; where a
+// row has less, as one that does not see a token whose large values another row's result is made of, the warp takes its tiles once more with a cs of
+// each row's own (a batch where every last draft is such a token, 128 x 5 positions: 615 us beside 248).  A lower goal than 2^4 leaves no room
+// for rows that differ, a higher one has the powers set again more often: 2^6 250 us, 2^8 254, where 2^4 takes 246.
 constexpr int kKaLow = 30;
 constexpr float kKaTop = -18.f, kKaMost = 0x1p15f;
-constexpr int kKaGoal = 4, kKaRowGoal = 10, kKaFar = 1000;
+constexpr int kKaMinGoal = 4, kKaMaxGoal = 10, kKaFar = 1000;
 
 template <int D, int NT> struct KaShape {
     static constexpr int NG = D / kKvGroup;
@@ -508,6 +509,8 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
                 }
             }
         };
+        // 2^6 above where a row's products are too small for the warp's tokens
+        const int aim = min(kKaMaxGoal, max(kKaMinGoal, 24 - __clz(max(n_tiles, 1) * kKaTile)));
         // ---- all tiles; ROWWISE: with a cs of each row's own
         auto sweep = [&](auto rowwise) {
             constexpr bool ROWWISE = decltype(rowwise)::value;
@@ -652,11 +655,11 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
                             for (int g = 0; g < NG; ++g) {
                                 const int before = exponent_of(cs[g]), size = exponent_of(all[g]) - 18;
                                 const int limit = 124 - exponent_of(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sv[g]))));
-                                const int goal = min(kKaGoal - size, min(limit, 126));
+                                const int goal = min(aim - size, min(limit, 126));
                                 int power = before;
                                 // all weights so far have shrunk by 2^lift, from 2^15 at the most
                                 if (size + before >= 15 || before > limit) power = goal;
-                                else if (lift > 15 - kKaGoal) power = max(before, min(before + lift - (15 - kKaGoal), goal));
+                                else if (lift > 15 - aim) power = max(before, min(before + lift - (15 - aim), goal));
                                 cs[g] = pow2_of(power);
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt)
@@ -687,7 +690,7 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
                                         const bool first = (fresh >> (2 * nt + col)) & 1;
                                         const int before = exponent_of(col ? was.y : was.x), size = (int)((both[nt][g] >> (16 * col + 7)) & 255) - 127 - 18;
                                         int power = first ? 126 : min(before + raised[nt][col], 126);
-                                        if (first || size + power >= 15) power = min(kKaRowGoal - size, 126);
+                                        if (first || size + power >= 15) power = min(kKaMaxGoal - size, 126);
                                         scale_o(nt, g, col, power - before - raised[nt][col]);
                                         is[col] = pow2_of(power);
                                     }
