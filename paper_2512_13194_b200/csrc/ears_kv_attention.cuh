@@ -11,9 +11,10 @@
 // (odd dimensions of keys / 16) and into the result (odd dimensions of values).  (8-bit floating-point operands would take fewer
 // operations still, c 2^-9 being one as it stands, but m16n8k32 with them is made of conversions and 16-bit products here:
 // 68 conversions per tile of 16 tokens counted, and 437 instructions against 386.)
-// Measured: 64 single tokens, 64 / 8 heads of 128, 6000 to 8192 tokens (527 MB): 110 us, 73 % of the copy rate, 261 instructions per tile of
-// 16 tokens; 128 x 5 positions, 32 / 8 heads, 680 MB: 238 us, 390 instructions, of them 48 matrix products, which other
-// instructions overlap in part only.
+// Measured: 64 single tokens, 64 / 8 heads of 128, 6000 to 8192 tokens (527 MB): 115 us, 70 % of the copy rate, 266 instructions per tile of
+// 16 tokens; 128 x 5 positions, 32 / 8 heads, 680 MB: 246 to 260 us by the lengths drawn, 403 instructions, of them 48 matrix products.
+// No unit is full (issue 53 and 44 %, ALU 55 and 35 %, matrix products 27 and 41 %): each scheduler has two or three warps, whose
+// matrix products and logic overlap in part only.
 //
 // The products have 16 tokens (or, for the values, dimensions) as rows and eight of the head group's
 // queries as columns: M = Q x heads per key head is seldom more than a few eights, and no work goes into padding a tile of
@@ -36,8 +37,8 @@ namespace ears {
 constexpr int kKaWarps = 4, kKaThreads = kKaWarps * 32;
 constexpr int kKaTile = 16;                         // tokens of a warp's tile
 constexpr int kKaChunk = kKaWarps * kKaTile;
-constexpr int kKaAhead = 8;                         // what starting and ending a unit costs, in chunks (128 x 5 positions as above: 279 us with 4,
-                                                    // 264 with 6, 260 with 8, 270 with 16)
+constexpr int kKaAhead = 8;                         // what starting and ending a unit costs, in chunks: with 4, 8, 12, 16 of them 277, 247, 246, 251 us
+                                                    // for 128 x 5 positions as above, 25.2, 22.9, 23.7, 23.3 for 8 x 6, 49.6, 48.6, 47.1, 47.3 for a window
 // A row's weights are P = 2^(score - reference).  The reference, a whole number, is raised when a P passes 2^-18, to where the largest is
 // between 2^-31 and 2^-30: their sums with minima up to the type's largest number stay finite, and minima down to 2^-100 keep their bits.
 // The second product's half-precision operands are P s cs, with a power of two cs for each group that goes by the largest P s of a warp's tiles: it
@@ -220,7 +221,7 @@ __global__ void __launch_bounds__(kKaThreads, KaShape<D, NT>::kCtas) ears_kv_att
     using S = KaShape<D, NT>;
     constexpr int NG = S::NG, RB = S::RB, ROWS = NT * 8;
     constexpr bool FINE = std::is_same<E, f16_t>::value;
-    // tiles taken together, as registers allow: 128 x 5 positions take 259 us by one, 242 by two
+    // tiles taken together, as registers allow: 128 x 5 positions take 269 us by one, 246 by two
     constexpr int SUB = NT * NG <= 6 ? 2 : 1;
     constexpr bool QREG = NT * NG <= 4;                   // queries' operands stay in registers
     constexpr uint32_t M0 = 0x000f000fu, M1 = 0x00f000f0u;

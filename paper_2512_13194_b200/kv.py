@@ -191,7 +191,8 @@ def kv_attention(q: torch.Tensor, cache: KVCache, pages: torch.Tensor, start: to
     """Attention of the positions ``start[b]`` to ``start[b] + Q - 1``, whose tokens ``kv_write`` has written, over each sequence's
     tokens up to and including their own (ears_kv_attention): with ``window`` > 0 the last ``window`` of them and the first
     ``sinks``.  q [B, Q, heads_q, head_dim] (bfloat16, float16), heads_q a multiple of the cache's heads, consecutive query heads on
-    one of them; ``scale`` is 1 / sqrt(head_dim) unless given.  Returns [B, Q, heads_q, head_dim] of q's type, zeros from position
+    one of them; ``scale`` is 1 / sqrt(head_dim) unless given.  A sequence with a position outside its table is NaN in all its rows
+    (``counts`` leaves positions out).  Small calls are faster with a table no wider than they need.  Returns [B, Q, heads_q, head_dim] of q's type, zeros from position
     ``counts[b]`` on; with ``lse=True`` also the scores' log-sum-exp, float32 [B, Q, heads_q]."""
     if stream is not None:
         return _on_stream(stream, cache, kv_attention, q, cache, pages, start, counts, scale=scale, window=window, sinks=sinks, lse=lse, status=status)
