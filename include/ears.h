@@ -604,7 +604,8 @@ int ears_kv_write(int dtype, const ears_kv_cache* cache, const void* k, const vo
                   int table_width, int64_t table_stride, const int32_t* start, const int32_t* counts, int32_t* status, void* stream);
 
 /* The values m + s c of Q tokens per sequence, in 32 bits and rounded once to `dtype`: out_k, out_v [B, Q, heads, head_dim],
-   contiguous, 16-byte aligned.  Positions that are left out are zeros. */
+   contiguous, 16-byte aligned.  Positions that are left out are zeros.  A value that rounds past the type's largest is infinite: within s / 2
+   of it, what is read can lie beyond where what was written did not (-65504 in half precision, stored as a minimum of -65536). */
 int ears_kv_read(int dtype, const ears_kv_cache* cache, int B, int Q, const int32_t* page_table, int table_width, int64_t table_stride,
                  const int32_t* start, const int32_t* counts, void* out_k, void* out_v, int32_t* status, void* stream);
 
