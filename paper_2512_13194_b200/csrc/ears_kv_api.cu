@@ -107,7 +107,7 @@ int share_positions(const KvSeqs& s, const ears_kv_cache* c, int values, int* pa
 // Eights of rows per block.  A unit's blocks each read its part of the cache (from L2 all but the first time), which blocks of few rows
 // do faster: the time of a block of 1, 2, .. eights, in us for 576000 tokens x 8 heads of 64 or 128, 240000 x 4 of 256.
 template <int D> constexpr int kMaxTiles = D == 64 ? 4 : D == 128 ? 4 : 2;
-constexpr int kBlockTime[3][4] = {{76, 104, 130, 162}, {119, 164, 214, 300}, {46, 76, 0, 0}};
+constexpr int kBlockTime[3][4] = {{83, 114, 144, 177}, {127, 169, 228, 322}, {65, 98, 0, 0}};
 template <int D>
 int choose_rows(int tiles) {
     int best = 1;
