@@ -619,10 +619,10 @@ int ears_kv_read(int dtype, const ears_kv_cache* cache, int B, int Q, const int3
  * that it sees, makes that row and its out_lse NaN, in all dimensions, and no other.
  * Scores, their sums (n / 32 weights one after the other, for n tokens) and the results are kept in 32 bits; q is taken as it is, or, where its
  * row spans more than 2^25, to within 2^-26 of the row's largest element.  Weights times scales, p s, enter the second product in half precision,
- * whose range follows the row's and group's own products: what that loses of sum_t p_t s_t c_t is at most 2^-11 of it and 2^-11 of 7.5 sum_t p_t s_t,
- * whatever scales there are in other groups or in tokens that weigh nothing or are not seen.  For half-precision q what rounding loses is
- * added back times the middle code: 2^-11 + 2^-12 of 7.5 sum_t p_t s_t are left.  Values between 2^-86 and the type's largest; weights below
- * 2^-95 of a row's largest are none.
+ * whose range follows the row's and group's own products: of sum_t p_t s_t c_t that and the product lose at most 2^-11 of it and 2^-10 of
+ * 7.5 sum_t p_t s_t, whatever scales there are in other groups or in tokens that weigh nothing or are not seen.  For half-precision q what
+ * rounding loses is added back times the middle code: 2^-10 of 7.5 sum_t p_t s_t are left.  Values between 2^-86 and the type's largest; weights
+ * below 2^-95 of a row's largest are none.
  * workspace: ears_kv_attention_workspace_bytes for the same arguments on the same device (0: they would be refused), 256-byte
  * aligned; its contents before and after mean nothing.  It does not grow with the lengths.  The same call on the same kind of
  * device gives the same bits; a row's may differ with what else is in the batch (the order of its sums).
